@@ -410,6 +410,126 @@ parason_status parason_lse_merge(const void *o_a, const float *lse_a, const void
                                  int64_t rows, int32_t head_dim, int32_t mode,
                                  parason_stream_t stream);
 
+/* ------------------------------------------------------------------------
+ * Filling and reading the paged cache
+ *
+ * What a model does around parason_attn_decode: keys and values of new tokens
+ * are rotated to their positions, rounded to the cache's type and written into
+ * the slots the caller's page table gives them; finished tokens are taken out
+ * again, for example to move them.  The paper leaves positions and the cache
+ * to its engine (Sec. 3.4); these calls are what that engine has to do.
+ *
+ * A slot is page * 16 + offset in the page: token t of a node sits in slot
+ * 16 * page_ids[node_page_ptr[node] + t / 16] + t % 16.  `cfg` gives the head
+ * counts, head_dim, page size and mode of the cache (sm_scale is not used),
+ * validated as by parason_attn_plan.  Rows of tokens are bf16 (PARASON_BF16
+ * and PARASON_FP8_E4M3_KV) or fp32 (PARASON_FP32).
+ * ------------------------------------------------------------------------ */
+
+/* Rows of num_tokens tokens by some heads of head_dim elements: element i of
+ * head h of token t is data[t * token_stride + h * head_stride + i].  Strides
+ * count elements; data and every stride that is used are multiples of 16
+ * bytes (a stride over a dimension of 1 is not used).  Device memory. */
+typedef struct {
+    void *data;
+    int64_t token_stride;
+    int64_t head_stride;
+} parason_rows;
+
+/* Rotary positions.  Frequency i (0 <= i < rotary_dim / 2) of token t turns
+ * its pair of elements (x0, x1) of a head by the angle
+ *   a = positions[axis * position_stride + t] * inv_freq[i],
+ *   axis = freq_axis ? freq_axis[i] : 0
+ * to (x0 cos a - x1 sin a, x0 sin a + x1 cos a).  The product is taken
+ * exactly and reduced in 64 bits, so far positions lose nothing.  Elements
+ * from rotary_dim on stay as they are. */
+enum { PARASON_ROTARY_HALVES = 0,       /* pair i is elements i, i + rotary_dim / 2 */
+       PARASON_ROTARY_INTERLEAVED = 1 };/* pair i is elements 2 i, 2 i + 1          */
+typedef struct {
+    int32_t rotary_dim;        /* multiple of 16, at most head_dim                  */
+    int32_t pairs;             /* PARASON_ROTARY_HALVES or _INTERLEAVED             */
+    int32_t num_axes;          /* 1..4: e.g. text 1; time, height, width 3          */
+    const uint8_t *freq_axis;  /* host [rotary_dim / 2], each < num_axes; NULL: 0   */
+    const float *inv_freq;     /* device [rotary_dim / 2], finite                   */
+    const int32_t *positions;  /* device [num_axes][num_tokens], negative ones too  */
+    int64_t position_stride;   /* elements between the axes' rows                   */
+} parason_rotary;
+
+/*
+ * Write the keys and values of num_tokens tokens into their slots, and rotate
+ * their queries on the way:
+ *   K[slot] = round(rot(k) / k_scale[h]),  V[slot] = round(v / v_scale[h]),
+ *   q_out   = round(rot(q))
+ * with the scales in PARASON_FP8_E4M3_KV mode only (ignored, may be NULL,
+ * otherwise; positive and finite).  Arithmetic is fp32, rounded once (to
+ * nearest even); e4m3 saturates at +-448, infinities too, and keeps NaN.
+ *
+ *   q       rows [num_tokens, H_q, head_dim], or NULL (no queries; q_out unused)
+ *   k, v    rows [num_tokens, H_kv, head_dim]
+ *   rotary  NULL: nothing turns (q_out is then a copy of q)
+ *   slots   device int32 [num_tokens].  A token whose slot is outside the
+ *           pool (negative, or 16 * num_physical_pages and up) is not written;
+ *           its query is rotated all the same.  Every other slot of the pool
+ *           keeps what it holds.  Slots are distinct: of two tokens with one
+ *           slot, it is unspecified which one's elements it holds.
+ *   q_out   device [num_tokens, H_q, head_dim], contiguous, 16-byte aligned,
+ *           the layout parason_attn_decode takes; may be q's own memory if q
+ *           has that layout, and overlaps nothing else here
+ *   k_pages, v_pages  the pools of parason_attn_decode
+ *
+ * One kernel on `stream`, no allocation, capturable.  It reads positions,
+ * slots and scales on the device, so a captured step can be replayed with new
+ * ones.  PARASON_EINVAL for a bad config, a NULL or misaligned pointer, a
+ * negative count, a rotary description outside the above;
+ * PARASON_EUNSUPPORTED if num_physical_pages * H_kv * 16 passes int32 (as in
+ * parason_attn_plan); PARASON_ECUDA if the launch fails.
+ */
+parason_status parason_kv_write(const parason_attn_config *cfg, int64_t num_tokens,
+                                const parason_rows *q, const parason_rows *k,
+                                const parason_rows *v, const parason_rotary *rotary,
+                                const int32_t *slots, const float *k_scale, const float *v_scale,
+                                void *q_out, void *k_pages, void *v_pages,
+                                int64_t num_physical_pages, parason_stream_t stream);
+
+/*
+ * Take num_tokens tokens out of the cache: k_out[t] = round(K[slots[t]] *
+ * k_scale[h]), v_out likewise, in the type of the mode's rows (an exact copy
+ * in PARASON_BF16 and PARASON_FP32 modes).  A slot outside the pool gives a
+ * row of zeros; a slot may be read any number of times.  k_out and v_out are
+ * rows [num_tokens, H_kv, head_dim] whose strides keep them apart (at least
+ * head_dim elements between heads and between tokens).  Keys come out as they
+ * were written: parason_kv_write with the difference of positions moves them
+ * to others.  Launch, capture and errors as parason_kv_write.
+ */
+parason_status parason_kv_read(const parason_attn_config *cfg, int64_t num_tokens,
+                               const int32_t *slots, const void *k_pages, const void *v_pages,
+                               int64_t num_physical_pages, const float *k_scale,
+                               const float *v_scale, const parason_rows *k_out,
+                               const parason_rows *v_out, parason_stream_t stream);
+
+/*
+ * e4m3 scales per kv head that hold the given tokens:
+ *   v_scale[h] = max |v| / 448 over the tokens,
+ *   k_scale[h] = max over the pairs that `rotary` turns of sqrt(x0^2 + x1^2),
+ *                and of |x| of the other elements, / 448.
+ * No rotation takes an element of a pair past its sqrt, so the K scale holds
+ * at every position, after a join has moved the keys too.  Of `rotary` only
+ * rotary_dim and pairs are used (NULL: no pairs).  slots may be NULL; tokens
+ * with a negative slot do not count.  NaN does not count, and a magnitude
+ * above 2^63 (infinities too) counts as 2^63.
+ *
+ * accumulate 0: the scales are set, at least to 2^-126.  accumulate 1: a
+ * scale that is larger already stays (they hold positive finite values on
+ * entry), so that the scales of several batches come out the same in any
+ * order.  PARASON_FP8_E4M3_KV mode only (PARASON_EINVAL otherwise).  One or
+ * two kernels on `stream`; capture and errors as parason_kv_write.
+ */
+parason_status parason_kv_scales(const parason_attn_config *cfg, int64_t num_tokens,
+                                 const parason_rows *k, const parason_rows *v,
+                                 const parason_rotary *rotary, const int32_t *slots,
+                                 int32_t accumulate, float *k_scale, float *v_scale,
+                                 parason_stream_t stream);
+
 /* Synchronise `stream`, then read and clear the plan's device error word:
  * PARASON_ETIMEOUT if a kernel gave up a bounded wait since the last check,
  * PARASON_ERANGE if an e4m3-KV decode met a q element of magnitude 65520 or

@@ -46,6 +46,18 @@ class PlanInfo(ctypes.Structure):
                 ("tile_pairs", ctypes.c_int32)]
 
 
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("pairs", ctypes.c_int32),
+                ("num_axes", ctypes.c_int32), ("freq_axis", ctypes.c_void_p),
+                ("inv_freq", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("position_stride", ctypes.c_int64)]
+
+
 class TraceStats(ctypes.Structure):
     _fields_ = [("total_tokens", ctypes.c_int64), ("latency_tokens", ctypes.c_int64),
                 ("subtask_tokens", ctypes.c_int64), ("trial_tokens", ctypes.c_int64),
@@ -53,6 +65,10 @@ class TraceStats(ctypes.Structure):
                 ("max_depth", ctypes.c_int32), ("top_level_blocks", ctypes.c_int32),
                 ("acceleration", ctypes.c_double), ("eta", ctypes.c_double)]
 
+
+_cfg = ctypes.POINTER(AttnConfig)
+_rows = ctypes.POINTER(Rows)
+_rot = ctypes.POINTER(RotaryDesc)
 
 SIGNATURES = {
     "parason_attn_plan": (ctypes.c_int, [ctypes.POINTER(AttnConfig), _i32, _p, _p, _p, _p, _i32,
@@ -79,6 +95,10 @@ SIGNATURES = {
                                                ctypes.POINTER(ctypes.c_int32),
                                                ctypes.POINTER(ctypes.c_int32)]),
     "parason_lse_merge": (ctypes.c_int, [_p, _p, _p, _p, _p, _p, _i64, _i32, _i32, _p]),
+    "parason_kv_write": (ctypes.c_int, [_cfg, _i64, _rows, _rows, _rows, _rot, _p, _p, _p, _p, _p,
+                                        _p, _i64, _p]),
+    "parason_kv_read": (ctypes.c_int, [_cfg, _i64, _p, _p, _p, _i64, _p, _p, _rows, _rows, _p]),
+    "parason_kv_scales": (ctypes.c_int, [_cfg, _i64, _rows, _rows, _rot, _p, _i32, _p, _p, _p]),
     "parason_plan_check": (ctypes.c_int, [_p, _p]),
     "parason_plan_destroy": (None, [_p]),
     "parason_status_string": (ctypes.c_char_p, [ctypes.c_int]),

@@ -362,11 +362,240 @@ def lse_merge(o_a: torch.Tensor, lse_a: torch.Tensor, o_b: torch.Tensor, lse_b: 
     return o_out, lse_out
 
 
+# ---------------------------------------------------------------------------
+# the paged cache: filling it, reading it, its e4m3 scales
+# ---------------------------------------------------------------------------
+
+_POOL_MODES = {dtype: mode for mode, dtype in _KV_DTYPES.items()}
+
+
+class Rotary:
+    """Rotary positions (C type ``parason_rotary``): ``inv_freq`` (cuda fp32
+    [rotary_dim / 2]) turns the first rotary_dim elements of each head, as pairs
+    (i, i + rotary_dim / 2) or, ``interleaved``, (2 i, 2 i + 1).  ``axes`` gives
+    each frequency's position axis (0..3; one axis if None): positions are then
+    [number of axes, tokens], e.g. time, height and width of image tokens."""
+
+    def __init__(self, inv_freq: torch.Tensor, axes=None, interleaved: bool = False):
+        if (inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_cuda
+                or not inv_freq.is_contiguous()):
+            raise ValueError("inv_freq must be a contiguous 1-D cuda float32 tensor")
+        half = inv_freq.shape[0]
+        if half % 8 or not 0 < half <= 64:
+            raise ValueError("inv_freq must have a multiple of 8 elements, 64 at most")
+        self.inv_freq, self.interleaved = inv_freq, bool(interleaved)
+        self.num_axes, self._axes = 1, None
+        if axes is not None:
+            a = np.asarray(axes)
+            if (a.shape != (half,) or a.dtype.kind not in "iu" or a.min() < 0 or a.max() > 3):
+                raise ValueError(f"axes must be {half} integers in 0..3")
+            self._axes = np.ascontiguousarray(a, dtype=np.uint8)
+            self.num_axes = int(self._axes.max()) + 1
+
+    @property
+    def rotary_dim(self) -> int:
+        return 2 * self.inv_freq.shape[0]
+
+    def _desc(self, positions):
+        d = _lib.RotaryDesc(self.rotary_dim, int(self.interleaved), self.num_axes,
+                            None if self._axes is None else self._axes.ctypes.data,
+                            self.inv_freq.data_ptr(), None, 0)
+        if positions is not None:
+            d.positions = positions.data_ptr()
+            d.position_stride = positions.stride(0) if positions.dim() == 2 else 0
+        return d
+
+
+def _token_rows(name, t, tokens, heads, dim, dtype, dev, out=False):
+    """The C view of rows [tokens, heads, dim] with any strides of 16 bytes."""
+    if t.dtype != dtype or t.shape != (tokens, heads, dim) or t.device != dev:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {(tokens, heads, dim)} on {dev}")
+    ts, hs, es = t.stride()
+    elem = t.element_size()
+    if tokens == 0:
+        return _lib.Rows(None, 0, 0)
+    if (es != 1 or t.data_ptr() % 16 or (tokens > 1 and ts * elem % 16)
+            or (heads > 1 and hs * elem % 16)):
+        raise ValueError(f"{name} must have contiguous elements and start and strides of 16 bytes")
+    if out and ((tokens > 1 and ts < dim) or (heads > 1 and hs < dim)):
+        raise ValueError(f"{name} must not overlap itself")
+    return _lib.Rows(t.data_ptr(), ts, hs)
+
+
+def _token_ints(name, t, shape, dev):
+    if t.dtype != torch.int32 or tuple(t.shape) != shape or t.device != dev or (
+            t.numel() > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name} must be an int32 tensor of shape {shape} on {dev}, contiguous "
+                         "along the tokens")
+    return t
+
+
+def _pool_config(k_pages, v_pages, num_q_heads):
+    """(mode, config, device) of a pair of pools."""
+    mode = _POOL_MODES.get(k_pages.dtype)
+    if (mode is None or k_pages.dim() != 4 or k_pages.shape[2] != 16 or not k_pages.is_cuda
+            or not k_pages.is_contiguous()):
+        raise ValueError("k_pages must be a contiguous cuda tensor [pages, kv heads, 16, head_dim] "
+                         "in bf16, fp32 or float8_e4m3fn")
+    if (v_pages.dtype != k_pages.dtype or v_pages.shape != k_pages.shape
+            or v_pages.device != k_pages.device or not v_pages.is_contiguous()):
+        raise ValueError("v_pages must be like k_pages")
+    heads, d = k_pages.shape[1], k_pages.shape[3]
+    _on_current(k_pages.device)
+    return mode, _lib.AttnConfig(num_q_heads or heads, heads, d, 16, _lib.MODES[mode], 0.0), k_pages.device
+
+
+def _on_current(dev):
+    if dev.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {dev}, which is not the current device")
+
+
+def _head_scales(scales, heads, dev):
+    for s in scales:
+        if (s is None or s.dtype != torch.float32 or tuple(s.shape) != (heads,) or s.device != dev
+                or not s.is_contiguous()):
+            raise ValueError(f"an e4m3 cache needs k_scale and v_scale: contiguous float32 [{heads}] "
+                             f"on {dev}")
+    return tuple(s.data_ptr() for s in scales)
+
+
+def _new(stream, shape, dtype, dev):
+    """A new tensor whose memory belongs to the stream that will write it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=dev)
+
+
+def kv_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+             slots: torch.Tensor, q: Optional[torch.Tensor] = None,
+             q_out: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None,
+             positions: Optional[torch.Tensor] = None, k_scale=None, v_scale=None, stream=None):
+    """Keys and values of new tokens into their slots of the paged cache
+    (``parason_kv_write``): k is rotated to ``positions``, both are rounded to
+    the cache's type (e4m3: divided by the scales first).  Returns the rotated
+    queries [T, H_q, d] if ``q`` is given, else None.  Asynchronous.
+
+    k, v, q: [T, heads, d] in bf16 (fp32 for an fp32 cache), views with strides
+    of 16 bytes allowed.  slots: cuda int32 [T], page * 16 + offset; a token
+    whose slot is outside the pool (-1, say) is not written.  positions: cuda
+    int32 [T], or [axes, T] as ``rotary`` has axes.  ``q_out`` may be ``q``
+    itself where that is contiguous."""
+    mode, cfg, dev = _pool_config(k_pages, v_pages, None if q is None else q.shape[1])
+    dtype, heads, d = _Q_DTYPES[mode], cfg.num_kv_heads, cfg.head_dim
+    tokens = k.shape[0]
+    ck = _token_rows("k", k, tokens, heads, d, dtype, dev)
+    cv = _token_rows("v", v, tokens, heads, d, dtype, dev)
+    _token_ints("slots", slots, (tokens,), dev)
+    ks = vs = None
+    if mode == "fp8":
+        ks, vs = _head_scales((k_scale, v_scale), heads, dev)
+    rot = None
+    if rotary is not None:
+        if positions is None:
+            raise ValueError("rotary needs positions")
+        if rotary.inv_freq.device != dev or rotary.rotary_dim > d:
+            raise ValueError(f"rotary must be on {dev} and turn at most {d} elements")
+        _token_ints("positions", positions, (tokens,) if positions.dim() == 1 and rotary.num_axes == 1
+                    else (rotary.num_axes, tokens), dev)
+        rot = ctypes.byref(rotary._desc(positions))
+    elif positions is not None:
+        raise ValueError("positions need a rotary")
+    cq = None
+    if q is not None:
+        if q.dim() != 3 or q.shape[1] == 0 or q.shape[1] % heads:
+            raise ValueError(f"q must be [T, a multiple of {heads} heads, {d}]")
+        cq = ctypes.byref(_token_rows("q", q, tokens, cfg.num_q_heads, d, dtype, dev))
+        if q_out is None:
+            q_out = _new(stream, q.shape, dtype, dev)
+        elif (q_out.dtype != dtype or q_out.shape != q.shape or q_out.device != dev
+              or not q_out.is_contiguous() or q_out.data_ptr() % 16):
+            raise ValueError(f"q_out must be a contiguous {dtype} tensor of q's shape on {dev}, "
+                             "16-byte aligned")
+        elif q_out.data_ptr() == q.data_ptr() and not q.is_contiguous():
+            raise ValueError("q_out may be q itself only where q is contiguous")
+    elif q_out is not None:
+        raise ValueError("q_out needs q")
+    st = _lib.load().parason_kv_write(
+        ctypes.byref(cfg), tokens, cq, ctypes.byref(ck), ctypes.byref(cv), rot, slots.data_ptr(),
+        ks, vs, None if q is None else q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+        k_pages.shape[0], _stream_int(stream))
+    if st:
+        check(st, "parason_kv_write")
+    return q_out
+
+
+def kv_read(k_pages: torch.Tensor, v_pages: torch.Tensor, slots: torch.Tensor,
+            k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None, k_scale=None,
+            v_scale=None, stream=None):
+    """The tokens of ``slots`` (cuda int32 [T]) out of the cache: (k, v), each
+    [T, H_kv, d] in bf16 (fp32 from an fp32 cache), e4m3 times its scale
+    (``parason_kv_read``).  A slot outside the pool gives zeros.  Given ``k`` and
+    ``v`` may be views with strides of 16 bytes.  Asynchronous."""
+    mode, cfg, dev = _pool_config(k_pages, v_pages, None)
+    dtype, heads, d = _Q_DTYPES[mode], cfg.num_kv_heads, cfg.head_dim
+    tokens = slots.shape[0] if slots.dim() == 1 else -1
+    _token_ints("slots", slots, (tokens,), dev)
+    ks = vs = None
+    if mode == "fp8":
+        ks, vs = _head_scales((k_scale, v_scale), heads, dev)
+    k = _new(stream, (tokens, heads, d), dtype, dev) if k is None else k
+    v = _new(stream, (tokens, heads, d), dtype, dev) if v is None else v
+    ck = _token_rows("k", k, tokens, heads, d, dtype, dev, out=True)
+    cv = _token_rows("v", v, tokens, heads, d, dtype, dev, out=True)
+    st = _lib.load().parason_kv_read(
+        ctypes.byref(cfg), tokens, slots.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+        k_pages.shape[0], ks, vs, ctypes.byref(ck), ctypes.byref(cv), _stream_int(stream))
+    if st:
+        check(st, "parason_kv_read")
+    return k, v
+
+
+def kv_scales(k: torch.Tensor, v: torch.Tensor, rotary: Optional[Rotary] = None,
+              slots: Optional[torch.Tensor] = None, k_scale: Optional[torch.Tensor] = None,
+              v_scale: Optional[torch.Tensor] = None, accumulate: bool = False, stream=None):
+    """(k_scale, v_scale), float32 [H_kv]: e4m3 scales that hold the tokens k, v
+    [T, H_kv, 128] (bf16) at any positions ``rotary`` may turn them to
+    (``parason_kv_scales``).  Tokens with a negative slot do not count.  With
+    ``accumulate``, given scales are raised where the tokens need it.
+    Asynchronous."""
+    if k.dim() != 3 or not k.is_cuda:
+        raise ValueError("k must be a cuda tensor [T, kv heads, 128]")
+    tokens, heads, d = k.shape
+    dev = k.device
+    _on_current(dev)
+    ck = _token_rows("k", k, tokens, heads, d, torch.bfloat16, dev)
+    cv = _token_rows("v", v, tokens, heads, d, torch.bfloat16, dev)
+    if slots is not None:
+        _token_ints("slots", slots, (tokens,), dev)
+    if accumulate and (k_scale is None or v_scale is None):
+        raise ValueError("accumulate needs the scales to raise")
+    k_scale = _new(stream, (heads,), torch.float32, dev) if k_scale is None else k_scale
+    v_scale = _new(stream, (heads,), torch.float32, dev) if v_scale is None else v_scale
+    ks, vs = _head_scales((k_scale, v_scale), heads, dev)
+    rot = None
+    if rotary is not None:
+        if rotary.rotary_dim > d:
+            raise ValueError(f"rotary must turn at most {d} elements")
+        rot = ctypes.byref(rotary._desc(None))
+    cfg = _lib.AttnConfig(heads, heads, d, 16, _lib.MODES["fp8"], 0.0)
+    st = _lib.load().parason_kv_scales(
+        ctypes.byref(cfg), tokens, ctypes.byref(ck), ctypes.byref(cv), rot,
+        None if slots is None else slots.data_ptr(), int(bool(accumulate)), ks, vs,
+        _stream_int(stream))
+    if st:
+        check(st, "parason_kv_scales")
+    return k_scale, v_scale
+
+
 def version() -> str:
     return _lib.load().parason_version().decode()
 
 
-__all__ = ["Plan", "lse_merge", "version", "ParasonError"]
+__all__ = ["Plan", "Rotary", "kv_read", "kv_scales", "kv_write", "lse_merge", "version",
+           "ParasonError"]
 
 
 # ---------------------------------------------------------------------------

@@ -118,6 +118,9 @@ struct MergeArgs {
     int32_t queue_start[2];
 };
 
+// The checks of a parason_attn_config that every entry point makes.
+parason_status check_config(const parason_attn_config *cfg);
+
 // Device a plan's metadata lives on (-1 for a host-only plan or NULL).
 int plan_device(parason_plan plan);
 

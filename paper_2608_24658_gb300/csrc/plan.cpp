@@ -471,18 +471,14 @@ struct parason_plan_s {
     std::vector<cudaEvent_t> events;   // 3 per recorded call
 };
 
-namespace {
+namespace parason {
 
-// ---------------------------------------------------------------------------
-// validation and work decomposition (no CUDA calls)
-// ---------------------------------------------------------------------------
-
-parason_status validate_config(const parason_attn_config *cfg) {
+parason_status check_config(const parason_attn_config *cfg) {
     if (!cfg) return PARASON_EINVAL;
     if (cfg->num_q_heads <= 0 || cfg->num_kv_heads <= 0) return PARASON_EINVAL;
     if (cfg->num_q_heads % cfg->num_kv_heads != 0) return PARASON_EINVAL;
     if (cfg->head_dim != 64 && cfg->head_dim != 128) return PARASON_EINVAL;
-    if (cfg->page_size != parason::kPageSize) return PARASON_EINVAL;
+    if (cfg->page_size != kPageSize) return PARASON_EINVAL;
     if (cfg->mode != PARASON_BF16 && cfg->mode != PARASON_FP32 &&
         cfg->mode != PARASON_FP8_E4M3_KV)
         return PARASON_EINVAL;
@@ -490,6 +486,14 @@ parason_status validate_config(const parason_attn_config *cfg) {
     if (cfg->mode == PARASON_FP8_E4M3_KV && cfg->head_dim != 128) return PARASON_EUNSUPPORTED;
     return PARASON_OK;
 }
+
+}  // namespace parason
+
+namespace {
+
+// ---------------------------------------------------------------------------
+// validation and work decomposition (no CUDA calls)
+// ---------------------------------------------------------------------------
 
 // The tree and its page table: parents before children, page counts that
 // match the lengths, page ids in range and owned once, branches distinct,
@@ -549,7 +553,7 @@ parason_status build_host(parason_plan_s *p, const parason_attn_config *cfg, int
                           const int32_t *node_page_ptr, const int32_t *page_ids,
                           int32_t num_leaves, const int32_t *leaf_node,
                           int64_t num_phys, int32_t num_sms, bool prefill = false) {
-    parason_status st = validate_config(cfg);
+    parason_status st = parason::check_config(cfg);
     if (st != PARASON_OK) return st;
     // the prefill's causal mask is in the tcgen05 tile: bf16 or e4m3 KV at head_dim 128
     if (prefill && (cfg->mode == PARASON_FP32 || cfg->head_dim != 128)) return PARASON_EUNSUPPORTED;
@@ -1514,7 +1518,7 @@ parason_status plan_device(const parason_attn_config *cfg, int32_t num_nodes, co
     if (!out) return PARASON_EINVAL;
     *out = nullptr;
     // validate before touching CUDA, so malformed input is EINVAL everywhere
-    parason_status st = validate_config(cfg);
+    parason_status st = parason::check_config(cfg);
     if (st != PARASON_OK) return st;
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess ||
@@ -1627,7 +1631,7 @@ parason_status plan_shard(const parason_attn_config *cfg, int32_t num_nodes, con
                           parason_plan *out) {
     if (!out) return PARASON_EINVAL;
     *out = nullptr;
-    parason_status st = validate_config(cfg);
+    parason_status st = parason::check_config(cfg);
     if (st != PARASON_OK) return st;
     if (world < 1 || rank < 0 || rank >= world) return PARASON_EINVAL;
     st = validate_tree(num_nodes, parent, node_len, node_page_ptr, page_ids, num_leaves, leaf_node,
