@@ -31,7 +31,8 @@
  *   out       [num_leaves, H_q, head_dim]   same dtype as q
  *   lse       [num_leaves, H_q] fp32, natural log of sum_t exp(s_t)
  *   q head h reads kv head h / (H_q / H_kv)  (grouped-query attention)
- *   s_t = sm_scale * <q, k_t>, sm_scale = 1/sqrt(head_dim) unless given.
+ *   s_t = sm_scale * <q, k_t>, sm_scale = 1/sqrt(head_dim) unless given
+ *   (capped by a tanh after parason_plan_set_logit_cap).
  */
 #ifndef PARASON_H
 #define PARASON_H
@@ -409,6 +410,22 @@ parason_status parason_lse_merge(const void *o_a, const float *lse_a, const void
                                  const float *lse_b, void *o_out, float *lse_out,
                                  int64_t rows, int32_t head_dim, int32_t mode,
                                  parason_stream_t stream);
+
+/*
+ * Cap the logits of a plan's attention, decode and prefill alike: from the
+ * next parason_attn_decode on,
+ *   s_t = cap * tanh(sm_scale * <q, k_t> / cap)
+ * instead of s_t = sm_scale * <q, k_t>; softmax, out and lse as before.  The
+ * paper has no counterpart: it is the attention of models that bound their
+ * logits.  cap is 0 (none; what a new plan has) or in [2^-10, 2^20];
+ * PARASON_EINVAL otherwise (NaN included), for NULL, and for a
+ * current device that is not the plan's.  Nothing is launched: a decode takes
+ * the cap that is set when it is called, and a captured decode keeps the one it
+ * was captured with.  Plans of every mode and kind take a cap, and it
+ * stays through appends and forks.  lse_merge of two capped results over
+ * disjoint keys is their capped result over both.
+ */
+parason_status parason_plan_set_logit_cap(parason_plan plan, float cap);
 
 /* ------------------------------------------------------------------------
  * Filling and reading the paged cache

@@ -105,6 +105,7 @@ SIGNATURES = {
     "parason_plan_get_info": (ctypes.c_int, [_p, ctypes.POINTER(PlanInfo)]),
     "parason_plan_export": (ctypes.c_int, [_p, _i32, _p, _sz]),
     "parason_plan_set_debug": (ctypes.c_int, [_p, ctypes.c_uint32, _i64]),
+    "parason_plan_set_logit_cap": (ctypes.c_int, [_p, ctypes.c_float]),
     "parason_plan_enable_timing": (ctypes.c_int, [_p, _i32]),
     "parason_plan_read_timing": (ctypes.c_int, [_p, _p, _p, _i32, ctypes.POINTER(ctypes.c_int32)]),
     "parason_plan_launches_per_decode": (_i32, [_p]),

@@ -60,14 +60,14 @@ class Plan:
     CUDA (for inspection on machines without a GPU).  ``prefill=True`` plans a
     tree-masked prefill instead (parason_prefill_plan): ``leaf_node`` then
     lists the chunk nodes, and every token of every chunk is a query row of
-    ``q`` (chunk by chunk) in ``decode``.
+    ``q`` (chunk by chunk) in ``decode``.  ``logit_cap``: see set_logit_cap.
     """
 
     def __init__(self, *, num_q_heads: int, num_kv_heads: int, head_dim: int, mode: str,
                  parent, node_len, node_page_ptr, page_ids, leaf_node,
                  num_physical_pages: int, sm_scale: float = 0.0, page_size: int = 16,
                  stream=None, host_only: bool = False, num_sms: int = 152,
-                 prefill: bool = False, shard=None):
+                 prefill: bool = False, shard=None, logit_cap: float = 0.0):
         lib = _lib.load()
         self.mode = mode
         self.num_q_heads, self.num_kv_heads, self.head_dim = num_q_heads, num_kv_heads, head_dim
@@ -102,6 +102,8 @@ class Plan:
             if skind == _lib.SHARD_KV_HEADS:
                 self.num_q_heads //= world
                 self.num_kv_heads //= world
+            if logit_cap:
+                self.set_logit_cap(logit_cap)
             return
         if host_only:
             fn = getattr(lib, f"parason_{kind}_plan_host")
@@ -120,6 +122,8 @@ class Plan:
         self.prefill = prefill
         if prefill:
             self.num_leaves = int(self.info()["num_leaves"])     # queries
+        if logit_cap:
+            self.set_logit_cap(logit_cap)
 
     @classmethod
     def for_tree(cls, tree, **kw) -> "Plan":
@@ -319,6 +323,12 @@ class Plan:
     def check(self, stream=None) -> None:
         """Synchronise ``stream`` and raise if a kernel reported a failure."""
         check(_lib.load().parason_plan_check(self.handle, _stream_handle(stream)), "plan_check")
+
+    def set_logit_cap(self, cap: float) -> None:
+        """Cap the logits of later decodes: cap * tanh(scale <q, k> / cap); 0
+        takes the cap off (parason_plan_set_logit_cap)."""
+        check(_lib.load().parason_plan_set_logit_cap(self.handle, float(cap)),
+              "parason_plan_set_logit_cap")
 
     def set_debug(self, flags: int = 0, wait_limit_ns: int = 0) -> None:
         check(_lib.load().parason_plan_set_debug(self.handle, flags, wait_limit_ns), "set_debug")

@@ -73,7 +73,8 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
         : "memory");
 }
 
-template <int D>
+// CAP: x = cap_log2 tanh(to_cap <q, k>) in place of scale_log2 <q, k>.
+template <int D, bool CAP>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     attn_fp32_kernel(const AttnArgs a, const float *__restrict__ kp, const float *__restrict__ vp) {
     using S = F32<D>;
@@ -209,7 +210,8 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
         }
         const bool seen = 4 * (2 * b2 + b1) + tg < valid;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) x[h] = seen ? x[h] * a.scale_log2 : -INFINITY;
+        for (int h = 0; h < 2; ++h)
+            x[h] = seen ? (CAP ? a.cap_log2 * tanhf(x[h] * a.to_cap) : x[h] * a.scale_log2) : -INFINITY;
         // the reference max moves (and o, l with it) only when a score passes
         // it by 2^8: always at the warp's first page, seldom later
         if (__any_sync(0xffffffffu, x[0] > m[0] + kGrowLog2 || x[1] > m[1] + kGrowLog2)) {
@@ -361,13 +363,13 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     }
 }
 
-template <int D>
+template <int D, bool CAP>
 cudaError_t launch(const AttnArgs &a, const float *k_pages, const float *v_pages, cudaStream_t stream) {
     // per device and idempotent: set before each launch, as the device may change
-    const cudaError_t e = cudaFuncSetAttribute(attn_fp32_kernel<D>,
+    const cudaError_t e = cudaFuncSetAttribute(attn_fp32_kernel<D, CAP>,
                                                cudaFuncAttributeMaxDynamicSharedMemorySize, kRing);
     if (e != cudaSuccess) return e;
-    return launch_dependent(a.early != 0, attn_fp32_kernel<D>, dim3(a.num_items), dim3(kThreads), kRing, stream, a,
+    return launch_dependent(a.early != 0, attn_fp32_kernel<D, CAP>, dim3(a.num_items), dim3(kThreads), kRing, stream, a,
                             k_pages, v_pages);
 }
 
@@ -376,8 +378,11 @@ cudaError_t launch(const AttnArgs &a, const float *k_pages, const float *v_pages
 cudaError_t launch_attn_fp32(const AttnArgs &a, const float *k_pages, const float *v_pages,
                              int head_dim, cudaStream_t stream) {
     if (a.num_items <= 0) return cudaSuccess;
-    if (head_dim == 128) return launch<128>(a, k_pages, v_pages, stream);
-    if (head_dim == 64) return launch<64>(a, k_pages, v_pages, stream);
+    const bool cap = a.cap_log2 > 0.f;
+    if (head_dim == 128)
+        return cap ? launch<128, true>(a, k_pages, v_pages, stream) : launch<128, false>(a, k_pages, v_pages, stream);
+    if (head_dim == 64)
+        return cap ? launch<64, true>(a, k_pages, v_pages, stream) : launch<64, false>(a, k_pages, v_pages, stream);
     return cudaErrorNotSupported;
 }
 

@@ -56,6 +56,7 @@
 #include <mutex>
 
 #include "device_common.cuh"
+#include "logit_cap.cuh"
 #include "tcgen05.cuh"
 #include "tile_common.cuh"
 
@@ -84,16 +85,26 @@ struct KvBf16 {
     static constexpr int kElemBytes = 2;
     static constexpr int kSuffixWarps = 8;
     static constexpr int kStepPages = 1;
+    static constexpr bool kCap = false;
 };
 struct KvBf16Deep {
     static constexpr int kElemBytes = 2;
     static constexpr int kSuffixWarps = 6;
     static constexpr int kStepPages = 1;
+    static constexpr bool kCap = false;
 };
 struct KvE4m3 {
     static constexpr int kElemBytes = 1;
     static constexpr int kSuffixWarps = 12;
     static constexpr int kStepPages = 2;
+    static constexpr bool kCap = false;
+};
+
+// The same formats under a logit cap (instantiations of their own: the others
+// keep their registers and code).
+template <class KV>
+struct Capped : KV {
+    static constexpr bool kCap = true;
 };
 
 template <int D, class KV>
@@ -174,15 +185,18 @@ __device__ __forceinline__ int out_col(int nt, int e, int tig) {
 // Online softmax over one page's scores s (two n-tiles of 8 tokens), then
 // rescale o; returns P packed as the A operand of the PV MMA.
 template <int D, class KV>
-__device__ __forceinline__ void softmax_page(const float (&sc)[2][4], int valid, float scale_log2,
-                                             WarpState<D> &st, int tig, uint32_t (&pa)[4]) {
+__device__ __forceinline__ void softmax_page(float (&sc)[2][4], int valid, float scale_log2,
+                                             float cap_log2, WarpState<D> &st, int tig,
+                                             uint32_t (&pa)[4]) {
+    // (under a cap scale_log2 is the factor into the tanh)
+    if constexpr (KV::kCap) cap_scores<2, 4>(sc, scale_log2, cap_log2);
     float x[2][4];
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int tok = nt * 8 + 2 * tig + (e & 1);
-            x[nt][e] = tok < valid ? sc[nt][e] * scale_log2 : -INFINITY;
+            x[nt][e] = tok < valid ? (KV::kCap ? sc[nt][e] : sc[nt][e] * scale_log2) : -INFINITY;
         }
     float mx0 = fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1]));
     float mx1 = fmaxf(fmaxf(x[0][2], x[0][3]), fmaxf(x[1][2], x[1][3]));
@@ -239,7 +253,7 @@ __device__ __forceinline__ void softmax_page(const float (&sc)[2][4], int valid,
 template <int D, class KV>
 __device__ __forceinline__ void page_step(uint32_t kbase, uint32_t vbase, int valid,
                                           const uint32_t (&qa)[D / 16][4], WarpState<D> &st,
-                                          float scale_log2, int lane) {
+                                          float scale_log2, float cap_log2, int lane) {
     using S = Shape<D, KV>;
     const int gid = lane >> 2, tig = lane & 3;
     const int mi = lane >> 3, r8 = lane & 7;
@@ -279,7 +293,7 @@ __device__ __forceinline__ void page_step(uint32_t kbase, uint32_t vbase, int va
         for (int e = 0; e < 4; ++e) sc[nt][e] += sd[nt][e];
 
     uint32_t pa[4];
-    softmax_page<D, KV>(sc, valid, scale_log2, st, tig, pa);
+    softmax_page<D, KV>(sc, valid, scale_log2, cap_log2, st, tig, pa);
 
     if constexpr (KV::kElemBytes == 2) {
         // slots past the node's length may hold anything (NaN included): their
@@ -514,18 +528,27 @@ __device__ __forceinline__ void pv_t(uint32_t vbase, int valid, uint32_t pb0, ui
 template <int D, class KV, int NP>
 __device__ __forceinline__ void pages_step_t(const uint32_t *kbase, const uint32_t *vbase,
                                              int valid_last, const uint32_t (&qb)[D / 16][2],
-                                             WarpStateT<D> &st, float scale_log2, int lane) {
+                                             WarpStateT<D> &st, float scale_log2, float cap_log2,
+                                             int lane) {
     const int gid = lane >> 2;
     float x[NP][4];
+    if constexpr (KV::kCap) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) scores_t<D, KV>(kbase[p], qb, lane, x[p]);
+        cap_scores<NP, 4>(x, scale_log2, cap_log2);
+    }
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
         float sp[4];
-        scores_t<D, KV>(kbase[p], qb, lane, sp);
+        if constexpr (!KV::kCap) scores_t<D, KV>(kbase[p], qb, lane, sp);
         const int valid = p == NP - 1 ? valid_last : kPageSize;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int tok = gid + ((e >> 1) << 3);
-            x[p][e] = tok < valid ? sp[e] * scale_log2 : -INFINITY;
+            if constexpr (KV::kCap)
+                x[p][e] = tok < valid ? x[p][e] : -INFINITY;
+            else
+                x[p][e] = tok < valid ? sp[e] * scale_log2 : -INFINITY;
         }
     }
     // row maxima over the pages' tokens: the 8 lanes of a tig
@@ -613,14 +636,15 @@ __device__ __forceinline__ void load_q_fragments(const AttnArgs &a, const WorkIt
     if constexpr (KV::kElemBytes == 1) report_q_range(a, big, lane);
 }
 
-// Softmax scale of an item and the factor of its partial o (the kv head's
-// e4m3 scales for K and V; 1 for bf16).
+// Softmax scale of an item (under a cap the factor into the tanh) and the
+// factor of its partial o (the kv head's e4m3 scales for K and V; 1 for bf16).
 template <class KV>
 __device__ __forceinline__ float2 item_scales(const AttnArgs &a, const WorkItem &it) {
+    const float scale = KV::kCap ? a.to_cap : a.scale_log2;
     if constexpr (KV::kElemBytes == 2)
-        return make_float2(a.scale_log2, 1.f);
+        return make_float2(scale, 1.f);
     else
-        return make_float2(a.scale_log2 * a.k_scale[it.kv_head], a.v_scale[it.kv_head]);
+        return make_float2(scale * a.k_scale[it.kv_head], a.v_scale[it.kv_head]);
 }
 
 // A warp writes the partials of its item's up to 16 rows straight from registers.
@@ -822,9 +846,9 @@ __device__ void suffix_warp(const KvMaps &maps, const AttnArgs &a, uint32_t ring
                 if (!ok) break;
                 const int valid = pg + np == it.num_pages ? it.last_valid : kPageSize;
                 if (kStepPages > 1 && np == kStepPages)
-                    pages_step_t<D, KV, kStepPages>(kb, vb, valid, qb, st, scl.x, lane);
+                    pages_step_t<D, KV, kStepPages>(kb, vb, valid, qb, st, scl.x, a.cap_log2, lane);
                 else
-                    pages_step_t<D, KV, 1>(kb, vb, valid, qb, st, scl.x, lane);
+                    pages_step_t<D, KV, 1>(kb, vb, valid, qb, st, scl.x, a.cap_log2, lane);
                 __syncwarp();
                 for (int p = 0; p < np; ++p) issue_next();
                 pg += np;
@@ -848,7 +872,7 @@ __device__ void suffix_warp(const KvMaps &maps, const AttnArgs &a, uint32_t ring
             const int valid = (pg == it.num_pages - 1) ? it.last_valid : kPageSize;
             page_step<D, KV>(my_ring + s * S::kStageBytes,
                              my_ring + s * S::kStageBytes + S::kPageBytes, valid, qa, st, scl.x,
-                             lane);
+                             a.cap_log2, lane);
             // refill this slot: its shared-memory reads are complete, since
             // every MMA that consumed them has issued (in order) before this point
             __syncwarp();
@@ -1326,7 +1350,10 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
             const int tokens = (it.num_pages - 1) * kPageSize + it.last_valid;
             const uint32_t tO = lane_base + kTmemO + 128u * (k & 1);
             // e4m3 K: the kv head's scale goes into the logits
-            const float sl = kF8 ? a.scale_log2 * a.k_scale[it.kv_head] : a.scale_log2;
+            // (under a cap the scores become logits as they are read, sl is 1)
+            const float scale = KV::kCap ? a.to_cap : a.scale_log2;
+            const float item_scale = kF8 ? scale * a.k_scale[it.kv_head] : scale;
+            const float sl = KV::kCap ? 1.f : item_scale;
             float m_use = -INFINITY, l = 0.f;
             bool ok = true;
             for (int i = 0; i < nb; ++i) {
@@ -1346,6 +1373,7 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
                 float x[64];
 #pragma unroll
                 for (int j = 0; j < 64; ++j) x[j] = __uint_as_float(sr[j >> 5][j & 31]);
+                if constexpr (KV::kCap) cap_scores<64>(x, item_scale, a.cap_log2);
                 if (valid < kTcBlockTokens) {
 #pragma unroll
                     for (int j = 0; j < 64; ++j) hide_from(x[j], j, valid);
@@ -1670,7 +1698,7 @@ __device__ __forceinline__ int pair_item(const AttnArgs &a, int k) {
     return 2 * k + 1 < a.num_wide_items ? 2 * k : -1;
 }
 
-template <int D>
+template <int D, class KV>
 __device__ void prefix_cta_tc_pair(const KvMaps *maps, const AttnArgs &a, uint8_t *smem, uint32_t bars,
                                    uint32_t tmem, int warp, int lane, volatile int *abort_flag,
                                    TcMeta *meta) {
@@ -1993,6 +2021,7 @@ __device__ void prefix_cta_tc_pair(const KvMaps *maps, const AttnArgs &a, uint8_
                     float x[64];
 #pragma unroll
                     for (int q = 0; q < 64; ++q) x[q] = __uint_as_float(sr[q >> 5][q & 31]);
+                    if constexpr (KV::kCap) cap_scores<64>(x, a.to_cap, a.cap_log2);
                     if (valid < kTcBlockTokens) {
 #pragma unroll
                         for (int q = 0; q < 64; ++q) hide_from(x[q], q, valid);
@@ -2001,7 +2030,7 @@ __device__ void prefix_cta_tc_pair(const KvMaps *maps, const AttnArgs &a, uint8_
 #pragma unroll
                     for (int q = 1; q + 1 < 64; q += 2) mr = dev::max3(mr, x[q], x[q + 1]);
                     mr = fmaxf(mr, x[63]);
-                    const float sl = a.scale_log2;
+                    const float sl = KV::kCap ? 1.f : a.scale_log2;
                     const float mb = mr * sl;
                     if (i == 0) {
                         m_use = mb;
@@ -2162,7 +2191,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc::fence_after_sync();
         if constexpr (kPairs) {
             if (tc_pairs)
-                prefix_cta_tc_pair<D>(&maps, a, smem, bars, tmem_base, warp, lane, &abort_flag, tc_meta);
+                prefix_cta_tc_pair<D, KV>(&maps, a, smem, bars, tmem_base, warp, lane, &abort_flag, tc_meta);
             else
                 prefix_cta_tc<D, KV>(&maps, a, smem, bars, tmem_base, warp, lane, &abort_flag, tc_meta);
         } else {
@@ -2240,6 +2269,20 @@ cudaError_t launch(const AttnArgs &a, const KvMaps &maps, cudaStream_t stream) {
 
 }  // namespace
 
+// The kernel of a shape, as the launch below picks it.
+template <template <class> class Kind>
+static cudaError_t launch_bf16(const AttnArgs &a, const KvMaps &maps, int head_dim, cudaStream_t stream) {
+    if (head_dim == 128)
+        return a.suffix_warps == KvBf16Deep::kSuffixWarps
+                   ? launch<128, Kind<KvBf16Deep>>(a, maps, stream)
+                   : launch<128, Kind<KvBf16>>(a, maps, stream);
+    if (head_dim == 64) return launch<64, Kind<KvBf16>>(a, maps, stream);
+    return cudaErrorNotSupported;
+}
+
+template <class KV>
+using Plain = KV;
+
 cudaError_t attn_mma_ctas_per_sm(int head_dim, int mode, int *ctas_per_sm) {
     if (mode == PARASON_FP8_E4M3_KV)
         return head_dim == 128 ? configure<128, KvE4m3>(ctas_per_sm) : cudaErrorNotSupported;
@@ -2255,18 +2298,25 @@ cudaError_t attn_mma_ctas_per_sm(int head_dim, int mode, int *ctas_per_sm) {
 cudaError_t launch_attn_bf16(const AttnArgs &a, const KvMaps &maps, int head_dim,
                              cudaStream_t stream) {
     if (a.num_items <= 0 || a.num_ctas <= 0) return cudaSuccess;
-    if (head_dim == 128)
-        return a.suffix_warps == KvBf16Deep::kSuffixWarps ? launch<128, KvBf16Deep>(a, maps, stream)
-                                                          : launch<128, KvBf16>(a, maps, stream);
-    if (head_dim == 64) return launch<64, KvBf16>(a, maps, stream);
-    return cudaErrorNotSupported;
+    return a.cap_log2 > 0.f ? launch_bf16<Capped>(a, maps, head_dim, stream)
+                            : launch_bf16<Plain>(a, maps, head_dim, stream);
 }
 
 cudaError_t launch_attn_fp8(const AttnArgs &a, const KvMaps &maps, int head_dim,
                             cudaStream_t stream) {
     if (a.num_items <= 0 || a.num_ctas <= 0) return cudaSuccess;
-    if (head_dim == 128) return launch<128, KvE4m3>(a, maps, stream);
-    return cudaErrorNotSupported;
+    if (head_dim != 128) return cudaErrorNotSupported;
+    return a.cap_log2 > 0.f ? launch<128, Capped<KvE4m3>>(a, maps, stream)
+                            : launch<128, KvE4m3>(a, maps, stream);
+}
+
+cudaError_t attn_mma_prepare_cap(int head_dim, int mode) {
+    if (mode == PARASON_FP8_E4M3_KV)
+        return head_dim == 128 ? configure<128, Capped<KvE4m3>>(nullptr) : cudaErrorNotSupported;
+    if (head_dim == 64) return configure<64, Capped<KvBf16>>(nullptr);
+    if (head_dim != 128) return cudaErrorNotSupported;
+    const cudaError_t e = configure<128, Capped<KvBf16Deep>>(nullptr);
+    return e != cudaSuccess ? e : configure<128, Capped<KvBf16>>(nullptr);
 }
 
 }  // namespace parason

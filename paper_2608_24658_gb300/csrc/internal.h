@@ -65,6 +65,8 @@ struct AttnArgs {
     int32_t num_kv_heads;
     int32_t group;
     float scale_log2;       // sm_scale * log2(e): x_t = scale_log2 * <q, k_t>
+    float cap_log2;         // 0, or the logit cap * log2(e): x_t = cap_log2 *
+    float to_cap;           // tanh(to_cap * <q, k_t>), to_cap = sm_scale / cap
 
     // dynamic schedule: items are numbered in pull order, prefix-pass items
     // [0, num_wide_items) then suffix-pass items.  CTAs [0, num_wide_ctas)
@@ -167,6 +169,11 @@ inline cudaError_t launch_dependent(bool early, void (*kernel)(Params...), dim3 
     cfg.numAttrs = early ? 1 : 0;
     return cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
 }
+
+// Set the attributes of the capped kernels of a mode on the current device, so
+// that a first capped decode may be captured.
+cudaError_t attn_mma_prepare_cap(int head_dim, int mode);
+cudaError_t prefill_prepare_cap(int mode);
 
 // Kernel launchers; each returns the launch's cudaError_t.
 cudaError_t launch_attn_bf16(const AttnArgs &a, const KvMaps &maps, int head_dim,

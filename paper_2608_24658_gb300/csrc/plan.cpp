@@ -458,6 +458,7 @@ struct parason_plan_s {
     int32_t *d_err = nullptr;
     uint32_t debug_flags = 0;
     int64_t wait_limit_ns = kDefaultWaitNs;
+    float logit_cap = 0.0f;            // 0: none
 
     // tensor maps of the last KV pools seen
     std::mutex tm_mutex;
@@ -1800,6 +1801,10 @@ parason_status parason_attn_decode(parason_plan p, const void *q, const void *k_
         a.num_kv_heads = p->cfg.num_kv_heads;
         a.group = p->group;
         a.scale_log2 = sm_scale * 1.4426950408889634f;
+        if (p->logit_cap > 0.0f) {
+            a.cap_log2 = p->logit_cap * 1.4426950408889634f;
+            a.to_cap = sm_scale / p->logit_cap;
+        }
         a.item_rec = p->d_item_rec;
         a.num_wide_items = static_cast<int32_t>(p->wide_queue.size());
         a.num_narrow_items = static_cast<int32_t>(p->narrow_queue.size());
@@ -2365,6 +2370,21 @@ parason_status parason_plan_set_debug(parason_plan p, uint32_t flags, int64_t wa
     if (!p || wait_limit_ns < 0) return PARASON_EINVAL;
     p->debug_flags = flags;
     if (wait_limit_ns > 0) p->wait_limit_ns = wait_limit_ns;
+    return PARASON_OK;
+}
+
+parason_status parason_plan_set_logit_cap(parason_plan p, float cap) {
+    // (a NaN fails every comparison)
+    if (!p || !(cap == 0.0f || (cap >= 0x1p-10f && cap <= 0x1p20f))) return PARASON_EINVAL;
+    if (cap > 0.0f && p->on_device && p->cfg.mode != PARASON_FP32) {
+        int dev = -1;
+        if (cudaGetDevice(&dev) != cudaSuccess) return PARASON_ECUDA;
+        if (dev != p->device) return PARASON_EINVAL;
+        const cudaError_t e = p->prefill ? parason::prefill_prepare_cap(p->cfg.mode)
+                                         : parason::attn_mma_prepare_cap(p->cfg.head_dim, p->cfg.mode);
+        if (e != cudaSuccess) return PARASON_ECUDA;
+    }
+    p->logit_cap = cap;
     return PARASON_OK;
 }
 

@@ -63,6 +63,7 @@
 #include <mutex>
 
 #include "device_common.cuh"
+#include "logit_cap.cuh"
 #include "tcgen05.cuh"
 #include "tile_common.cuh"
 
@@ -203,10 +204,11 @@ __device__ __forceinline__ void widen_block(uint32_t src, uint32_t dst, int v0, 
     }
 }
 
+// CAP: the logits are capped (logit_cap.cuh).
 // DIRECT: every pair holds its rows' whole paths, and the kernel writes the
 // result itself (an instantiation of its own: a run-time test cost the join
 // 3%).
-template <bool F8, bool DIRECT>
+template <bool F8, bool DIRECT, bool CAP>
 __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
     prefill_kernel(const __grid_constant__ KvMaps maps, const AttnArgs a) {
     using C = Cfg<F8>;
@@ -329,7 +331,10 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                 const int key0 = t == 0 ? m.key0 : m.key0B;
                 // the row's last visible key, relative to the item's first
                 const int t_rel = key0 == kNoKey0 ? (1 << 30) : (it.row0 + r) / a.group - key0;
-                const float sl = F8 ? a.scale_log2 * a.k_scale[it.kv_head] : a.scale_log2;
+                // (under a cap the scores become logits as they are read, sl is 1)
+                const float scale = CAP ? a.to_cap : a.scale_log2;
+                const float item_scale = F8 ? scale * a.k_scale[it.kv_head] : scale;
+                const float sl = CAP ? 1.f : item_scale;
                 const unsigned long long slp = dev::f32x2(sl, sl);
                 float m_use = -INFINITY, l = 0.f;
                 for (int i = 0; i < nb; ++i, ++u) {
@@ -347,6 +352,12 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                     auto read_half = [&](int h, uint32_t(&x0)[32], uint32_t(&x1)[32]) {
                         tc::ld32(tS + 64 * h, x0);
                         tc::ld32(tS + 64 * h + 32, x1);
+                    };
+                    auto cap_half = [&](uint32_t(&x0)[32], uint32_t(&x1)[32]) {
+                        if constexpr (CAP) {
+                            cap_scores<32>(x0, item_scale, a.cap_log2);
+                            cap_scores<32>(x1, item_scale, a.cap_log2);
+                        }
                     };
                     // keys the row does not see (past the last token of a
                     // half, or past the row's own token): -inf
@@ -374,10 +385,12 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                     if constexpr (F8) {
                         read_half(0, x[0], x[1]);
                         tc::wait_ld();
+                        cap_half(x[0], x[1]);
                         hide_half(0, x[0], x[1]);
                         mx = max_half(x[0], x[1]);
                         read_half(1, x[0], x[1]);
                         tc::wait_ld();
+                        cap_half(x[0], x[1]);
                         hide_half(1, x[0], x[1]);
                         mx = fmaxf(mx, max_half(x[0], x[1]));
                     } else {
@@ -396,6 +409,8 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                         }
                     }
                     if constexpr (!F8) {
+                        cap_half(x[0], x[1]);
+                        cap_half(x[2], x[3]);
                         hide_half(0, x[0], x[1]);
                         hide_half(1, x[2], x[3]);
                         mx = fmaxf(max_half(x[0], x[1]), max_half(x[2], x[3]));
@@ -449,6 +464,7 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                         if constexpr (F8) {
                             read_half(h, x[0], x[1]);
                             tc::wait_ld();
+                            cap_half(x[0], x[1]);
                             hide_half(h, x[0], x[1]);
                         }
                         lsum = exponentiate(h, pw, lsum);
@@ -904,7 +920,7 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
 // Shared memory is configured once per device; the launch needs one CTA per SM.
 constexpr int kMaxConfigDevices = 64;
 
-template <bool F8, bool DIRECT>
+template <bool F8, bool DIRECT, bool CAP>
 cudaError_t configure() {
     static std::mutex mu;
     static bool done[kMaxConfigDevices] = {};
@@ -914,22 +930,33 @@ cudaError_t configure() {
     if (dev < 0 || dev >= kMaxConfigDevices) return cudaErrorNotSupported;
     std::lock_guard<std::mutex> lock(mu);
     if (done[dev]) return cudaSuccess;
-    e = cudaFuncSetAttribute(prefill_kernel<F8, DIRECT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    e = cudaFuncSetAttribute(prefill_kernel<F8, DIRECT, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                              smem_bytes<F8>());
     if (e != cudaSuccess) return e;
-    e = cudaFuncSetAttribute(prefill_kernel<F8, DIRECT>, cudaFuncAttributePreferredSharedMemoryCarveout,
+    e = cudaFuncSetAttribute(prefill_kernel<F8, DIRECT, CAP>, cudaFuncAttributePreferredSharedMemoryCarveout,
                              cudaSharedmemCarveoutMaxShared);
     if (e != cudaSuccess) return e;
     done[dev] = true;
     return cudaSuccess;
 }
 
-template <bool F8, bool DIRECT>
+template <bool F8, bool DIRECT, bool CAP>
 cudaError_t launch(const AttnArgs &a, const KvMaps &maps, cudaStream_t stream) {
-    const cudaError_t e = configure<F8, DIRECT>();
+    const cudaError_t e = configure<F8, DIRECT, CAP>();
     if (e != cudaSuccess) return e;
-    return launch_dependent(a.early != 0, prefill_kernel<F8, DIRECT>, dim3(a.num_ctas),
+    return launch_dependent(a.early != 0, prefill_kernel<F8, DIRECT, CAP>, dim3(a.num_ctas),
                             dim3(Cfg<F8>::kThreads), smem_bytes<F8>(), stream, maps, a);
+}
+
+template <bool F8, bool CAP>
+cudaError_t launch_form(const AttnArgs &a, const KvMaps &maps, cudaStream_t stream) {
+    return a.out ? launch<F8, true, CAP>(a, maps, stream) : launch<F8, false, CAP>(a, maps, stream);
+}
+
+template <bool F8>
+cudaError_t prepare_cap() {
+    const cudaError_t e = configure<F8, true, true>();
+    return e != cudaSuccess ? e : configure<F8, false, true>();
 }
 
 }  // namespace
@@ -937,8 +964,14 @@ cudaError_t launch(const AttnArgs &a, const KvMaps &maps, cudaStream_t stream) {
 cudaError_t launch_prefill(const AttnArgs &a, const KvMaps &maps, int mode, cudaStream_t stream) {
     if (a.num_items <= 0 || a.num_ctas <= 0) return cudaSuccess;
     if (mode == PARASON_FP8_E4M3_KV)
-        return a.out ? launch<true, true>(a, maps, stream) : launch<true, false>(a, maps, stream);
-    return a.out ? launch<false, true>(a, maps, stream) : launch<false, false>(a, maps, stream);
+        return a.cap_log2 > 0.f ? launch_form<true, true>(a, maps, stream)
+                                : launch_form<true, false>(a, maps, stream);
+    return a.cap_log2 > 0.f ? launch_form<false, true>(a, maps, stream)
+                            : launch_form<false, false>(a, maps, stream);
+}
+
+cudaError_t prefill_prepare_cap(int mode) {
+    return mode == PARASON_FP8_E4M3_KV ? prepare_cap<true>() : prepare_cap<false>();
 }
 
 }  // namespace parason
