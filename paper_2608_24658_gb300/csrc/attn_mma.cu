@@ -189,7 +189,7 @@ __device__ __forceinline__ void softmax_page(float (&sc)[2][4], int valid, float
                                              float cap_log2, WarpState<D> &st, int tig,
                                              uint32_t (&pa)[4]) {
     // (under a cap scale_log2 is the factor into the tanh)
-    if constexpr (KV::kCap) cap_scores<2, 4>(sc, scale_log2, cap_log2);
+    if constexpr (KV::kCap) cap_scores<2, 4, float>(sc, scale_log2, cap_log2);
     float x[2][4];
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt)
@@ -535,7 +535,7 @@ __device__ __forceinline__ void pages_step_t(const uint32_t *kbase, const uint32
     if constexpr (KV::kCap) {
 #pragma unroll
         for (int p = 0; p < NP; ++p) scores_t<D, KV>(kbase[p], qb, lane, x[p]);
-        cap_scores<NP, 4>(x, scale_log2, cap_log2);
+        cap_scores<NP, 4, float>(x, scale_log2, cap_log2);
     }
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
@@ -1373,7 +1373,7 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
                 float x[64];
 #pragma unroll
                 for (int j = 0; j < 64; ++j) x[j] = __uint_as_float(sr[j >> 5][j & 31]);
-                if constexpr (KV::kCap) cap_scores<64>(x, item_scale, a.cap_log2);
+                if constexpr (KV::kCap) cap_scores<64, float>(x, item_scale, a.cap_log2);
                 if (valid < kTcBlockTokens) {
 #pragma unroll
                     for (int j = 0; j < 64; ++j) hide_from(x[j], j, valid);
@@ -2021,7 +2021,7 @@ __device__ void prefix_cta_tc_pair(const KvMaps *maps, const AttnArgs &a, uint8_
                     float x[64];
 #pragma unroll
                     for (int q = 0; q < 64; ++q) x[q] = __uint_as_float(sr[q >> 5][q & 31]);
-                    if constexpr (KV::kCap) cap_scores<64>(x, a.to_cap, a.cap_log2);
+                    if constexpr (KV::kCap) cap_scores<64, float>(x, a.to_cap, a.cap_log2);
                     if (valid < kTcBlockTokens) {
 #pragma unroll
                         for (int q = 0; q < 64; ++q) hide_from(x[q], q, valid);

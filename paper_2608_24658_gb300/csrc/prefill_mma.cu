@@ -355,8 +355,8 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                     };
                     auto cap_half = [&](uint32_t(&x0)[32], uint32_t(&x1)[32]) {
                         if constexpr (CAP) {
-                            cap_scores<32>(x0, item_scale, a.cap_log2);
-                            cap_scores<32>(x1, item_scale, a.cap_log2);
+                            cap_scores<32, uint32_t>(x0, item_scale, a.cap_log2);
+                            cap_scores<32, uint32_t>(x1, item_scale, a.cap_log2);
                         }
                     };
                     // keys the row does not see (past the last token of a
