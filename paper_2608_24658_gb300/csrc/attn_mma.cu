@@ -85,26 +85,30 @@ struct KvBf16 {
     static constexpr int kElemBytes = 2;
     static constexpr int kSuffixWarps = 8;
     static constexpr int kStepPages = 1;
-    static constexpr bool kCap = false;
+    static constexpr int kCap = kCapNone;
 };
 struct KvBf16Deep {
     static constexpr int kElemBytes = 2;
     static constexpr int kSuffixWarps = 6;
     static constexpr int kStepPages = 1;
-    static constexpr bool kCap = false;
+    static constexpr int kCap = kCapNone;
 };
 struct KvE4m3 {
     static constexpr int kElemBytes = 1;
     static constexpr int kSuffixWarps = 12;
     static constexpr int kStepPages = 2;
-    static constexpr bool kCap = false;
+    static constexpr int kCap = kCapNone;
 };
 
 // The same formats under a logit cap (instantiations of their own: the others
 // keep their registers and code).
 template <class KV>
-struct Capped : KV {
-    static constexpr bool kCap = true;
+struct CappedFree : KV {
+    static constexpr int kCap = kCapFree;
+};
+template <class KV>
+struct CappedRef : KV {
+    static constexpr int kCap = kCapRef;
 };
 
 template <int D, class KV>
@@ -186,17 +190,17 @@ __device__ __forceinline__ int out_col(int nt, int e, int tig) {
 // rescale o; returns P packed as the A operand of the PV MMA.
 template <int D, class KV>
 __device__ __forceinline__ void softmax_page(float (&sc)[2][4], int valid, float scale_log2,
-                                             float cap_log2, WarpState<D> &st, int tig,
-                                             uint32_t (&pa)[4]) {
+                                             float cap_log2, bool &cap_large, WarpState<D> &st,
+                                             int tig, uint32_t (&pa)[4]) {
     // (under a cap scale_log2 is the factor into the tanh)
-    if constexpr (KV::kCap) cap_scores<2, 4, float>(sc, scale_log2, cap_log2);
+    if constexpr (KV::kCap == kCapRef) cap_scores(sc, cap_large, CapFactors(scale_log2, cap_log2));
     float x[2][4];
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int tok = nt * 8 + 2 * tig + (e & 1);
-            x[nt][e] = tok < valid ? (KV::kCap ? sc[nt][e] : sc[nt][e] * scale_log2) : -INFINITY;
+            x[nt][e] = tok < valid ? (KV::kCap != kCapNone ? sc[nt][e] : sc[nt][e] * scale_log2) : -INFINITY;
         }
     float mx0 = fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1]));
     float mx1 = fmaxf(fmaxf(x[0][2], x[0][3]), fmaxf(x[1][2], x[1][3]));
@@ -249,11 +253,34 @@ __device__ __forceinline__ void softmax_page(float (&sc)[2][4], int valid, float
     }
 }
 
+// The same under a cap that needs no reference: P = 2^x, tokens past the last one 0.
+template <int D>
+__device__ __forceinline__ void softmax_page_free(float (&sc)[2][4], int valid, const CapFactors &cap,
+                                                  bool &cap_large, WarpState<D> &st, int tig,
+                                                  uint32_t (&pa)[4]) {
+    LaneP<8> put;
+    cap_free(*reinterpret_cast<const float(*)[8]>(&sc), 8, false, cap_large, cap, put);
+    float(&p)[8] = put.p;
+    if (valid < kPageSize) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if ((e >> 2) * 8 + 2 * tig + (e & 1) >= valid) p[e] = 0.f;
+    }
+    st.m[0] = st.m[1] = 0.f;
+    st.l[0] += p[0] + p[1] + p[4] + p[5];
+    st.l[1] += p[2] + p[3] + p[6] + p[7];
+    pa[0] = dev::pack_bf16(p[0], p[1]);
+    pa[1] = dev::pack_bf16(p[2], p[3]);
+    pa[2] = dev::pack_bf16(p[4], p[5]);
+    pa[3] = dev::pack_bf16(p[6], p[7]);
+}
+
 // One 16-token page: S = Q K^T, online softmax, O += P V.
 template <int D, class KV>
 __device__ __forceinline__ void page_step(uint32_t kbase, uint32_t vbase, int valid,
                                           const uint32_t (&qa)[D / 16][4], WarpState<D> &st,
-                                          float scale_log2, float cap_log2, int lane) {
+                                          float scale_log2, float cap_log2, bool &cap_large,
+                                          int lane) {
     using S = Shape<D, KV>;
     const int gid = lane >> 2, tig = lane & 3;
     const int mi = lane >> 3, r8 = lane & 7;
@@ -293,7 +320,10 @@ __device__ __forceinline__ void page_step(uint32_t kbase, uint32_t vbase, int va
         for (int e = 0; e < 4; ++e) sc[nt][e] += sd[nt][e];
 
     uint32_t pa[4];
-    softmax_page<D, KV>(sc, valid, scale_log2, cap_log2, st, tig, pa);
+    if constexpr (KV::kCap == kCapFree)
+        softmax_page_free<D>(sc, valid, CapFactors(scale_log2, cap_log2), cap_large, st, tig, pa);
+    else
+        softmax_page<D, KV>(sc, valid, scale_log2, cap_log2, cap_large, st, tig, pa);
 
     if constexpr (KV::kElemBytes == 2) {
         // slots past the node's length may hold anything (NaN included): their
@@ -529,23 +559,23 @@ template <int D, class KV, int NP>
 __device__ __forceinline__ void pages_step_t(const uint32_t *kbase, const uint32_t *vbase,
                                              int valid_last, const uint32_t (&qb)[D / 16][2],
                                              WarpStateT<D> &st, float scale_log2, float cap_log2,
-                                             int lane) {
+                                             bool &cap_large, int lane) {
     const int gid = lane >> 2;
     float x[NP][4];
-    if constexpr (KV::kCap) {
+    if constexpr (KV::kCap == kCapRef) {
 #pragma unroll
         for (int p = 0; p < NP; ++p) scores_t<D, KV>(kbase[p], qb, lane, x[p]);
-        cap_scores<NP, 4, float>(x, scale_log2, cap_log2);
+        cap_scores(x, cap_large, CapFactors(scale_log2, cap_log2));
     }
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
         float sp[4];
-        if constexpr (!KV::kCap) scores_t<D, KV>(kbase[p], qb, lane, sp);
+        if constexpr (KV::kCap == kCapNone) scores_t<D, KV>(kbase[p], qb, lane, sp);
         const int valid = p == NP - 1 ? valid_last : kPageSize;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int tok = gid + ((e >> 1) << 3);
-            if constexpr (KV::kCap)
+            if constexpr (KV::kCap != kCapNone)
                 x[p][e] = tok < valid ? x[p][e] : -INFINITY;
             else
                 x[p][e] = tok < valid ? sp[e] * scale_log2 : -INFINITY;
@@ -599,6 +629,34 @@ __device__ __forceinline__ void pages_step_t(const uint32_t *kbase, const uint32
     }
 }
 
+// The same under a cap that needs no reference: P = 2^x, tokens past the last one 0.
+template <int D, class KV, int NP>
+__device__ __forceinline__ void pages_step_t_free(const uint32_t *kbase, const uint32_t *vbase,
+                                                  int valid_last, const uint32_t (&qb)[D / 16][2],
+                                                  WarpStateT<D> &st, const CapFactors &cap,
+                                                  bool &cap_large, int lane) {
+    const int gid = lane >> 2;
+    float x[NP][4];
+#pragma unroll
+    for (int p = 0; p < NP; ++p) scores_t<D, KV>(kbase[p], qb, lane, x[p]);
+    LaneP<4 * NP> put;
+    cap_free(*reinterpret_cast<const float(*)[4 * NP]>(&x), 4 * NP, false, cap_large, cap, put);
+    st.m[0] = st.m[1] = 0.f;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+        const int valid = p == NP - 1 ? valid_last : kPageSize;
+        float(&y)[4] = *reinterpret_cast<float(*)[4]>(put.p + 4 * p);
+        if (valid < kPageSize) {
+            if (gid >= valid) y[0] = y[1] = 0.f;
+            if (gid + 8 >= valid) y[2] = y[3] = 0.f;
+        }
+        st.l[0] += y[0] + y[2];
+        st.l[1] += y[1] + y[3];
+        pv_t<D, KV>(vbase[p], valid, dev::movmatrix_trans(dev::pack_bf16(y[0], y[1])),
+                    dev::movmatrix_trans(dev::pack_bf16(y[2], y[3])), st, lane);
+    }
+}
+
 // Q fragments (A operand, row-major 16 x D) for tile rows {gid, gid+8}:
 // bf16 as stored, or widened to f16 with d permuted as the e4m3 QK^T wants.
 template <int D, class KV>
@@ -640,7 +698,7 @@ __device__ __forceinline__ void load_q_fragments(const AttnArgs &a, const WorkIt
 // factor of its partial o (the kv head's e4m3 scales for K and V; 1 for bf16).
 template <class KV>
 __device__ __forceinline__ float2 item_scales(const AttnArgs &a, const WorkItem &it) {
-    const float scale = KV::kCap ? a.to_cap : a.scale_log2;
+    const float scale = KV::kCap != kCapNone ? a.to_cap : a.scale_log2;
     if constexpr (KV::kElemBytes == 2)
         return make_float2(scale, 1.f);
     else
@@ -815,7 +873,7 @@ __device__ void suffix_warp(const KvMaps &maps, const AttnArgs &a, uint32_t ring
 
     // consume side: the pulled items in order
     int consumed = 0;
-    bool ok = true;
+    bool ok = true, cap_large = false;           // (cap_free)
     for (int k = 0; consumed < issued && ok; ++k) {
         __syncwarp();
         const WorkItem it = grab[k % kGrabSlots];
@@ -845,10 +903,18 @@ __device__ void suffix_warp(const KvMaps &maps, const AttnArgs &a, uint32_t ring
                 }
                 if (!ok) break;
                 const int valid = pg + np == it.num_pages ? it.last_valid : kPageSize;
-                if (kStepPages > 1 && np == kStepPages)
-                    pages_step_t<D, KV, kStepPages>(kb, vb, valid, qb, st, scl.x, a.cap_log2, lane);
-                else
-                    pages_step_t<D, KV, 1>(kb, vb, valid, qb, st, scl.x, a.cap_log2, lane);
+                if constexpr (KV::kCap == kCapFree) {
+                    const CapFactors cap(scl.x, a.cap_log2);
+                    if (kStepPages > 1 && np == kStepPages)
+                        pages_step_t_free<D, KV, kStepPages>(kb, vb, valid, qb, st, cap, cap_large, lane);
+                    else
+                        pages_step_t_free<D, KV, 1>(kb, vb, valid, qb, st, cap, cap_large, lane);
+                } else {
+                    if (kStepPages > 1 && np == kStepPages)
+                        pages_step_t<D, KV, kStepPages>(kb, vb, valid, qb, st, scl.x, a.cap_log2, cap_large, lane);
+                    else
+                        pages_step_t<D, KV, 1>(kb, vb, valid, qb, st, scl.x, a.cap_log2, cap_large, lane);
+                }
                 __syncwarp();
                 for (int p = 0; p < np; ++p) issue_next();
                 pg += np;
@@ -872,7 +938,7 @@ __device__ void suffix_warp(const KvMaps &maps, const AttnArgs &a, uint32_t ring
             const int valid = (pg == it.num_pages - 1) ? it.last_valid : kPageSize;
             page_step<D, KV>(my_ring + s * S::kStageBytes,
                              my_ring + s * S::kStageBytes + S::kPageBytes, valid, qa, st, scl.x,
-                             a.cap_log2, lane);
+                             a.cap_log2, cap_large, lane);
             // refill this slot: its shared-memory reads are complete, since
             // every MMA that consumed them has issued (in order) before this point
             __syncwarp();
@@ -1350,12 +1416,10 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
             const int tokens = (it.num_pages - 1) * kPageSize + it.last_valid;
             const uint32_t tO = lane_base + kTmemO + 128u * (k & 1);
             // e4m3 K: the kv head's scale goes into the logits
-            // (under a cap the scores become logits as they are read, sl is 1)
-            const float scale = KV::kCap ? a.to_cap : a.scale_log2;
-            const float item_scale = kF8 ? scale * a.k_scale[it.kv_head] : scale;
-            const float sl = KV::kCap ? 1.f : item_scale;
-            float m_use = -INFINITY, l = 0.f;
-            bool ok = true;
+            const float sl = item_scales<KV>(a, it).x;
+            const CapFactors cap(sl, a.cap_log2);      // (used under a cap)
+            float m_use = KV::kCap == kCapFree ? 0.f : -INFINITY, l = 0.f;
+            bool ok = true, cap_large = false;
             for (int i = 0; i < nb; ++i) {
                 const int b = blk + i;
                 const int valid = tokens - i * kTcBlockTokens;   // of the block's keys (64 or more: all)
@@ -1365,71 +1429,114 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
                     break;
                 }
                 tc::fence_after_sync();
-                uint32_t sr[2][32];
-                tc::ld32(tS, sr[0]);
-                tc::ld32(tS + 32, sr[1]);
-                tc::wait_ld();
-                // raw scores; keys past the item's last token -inf
-                float x[64];
+                // the row's reference max at least mb less 2^8 (O and l with it)
+                auto raise_reference = [&](float mb) {
+                    if (i == 0) {
+                        m_use = mb;
+                    } else if (__any_sync(0xffffffffu, mb > m_use + kTcRescaleLog2)) {
+                        // O must hold PV(b - 1) before it is rescaled
+                        if (!tc_warp_wait(bar(kBarPvDone + ((b - 1) & 1)), ((b - 1) >> 1) & 1, limit,
+                                          abort_flag, lane)) {
+                            return false;
+                        }
+                        tc::fence_after_sync();
+                        const float m_new = fmaxf(m_use, mb);
+                        const float alpha = m_new == m_use ? 1.f : dev::fast_exp2(m_use - m_new);
 #pragma unroll
-                for (int j = 0; j < 64; ++j) x[j] = __uint_as_float(sr[j >> 5][j & 31]);
-                if constexpr (KV::kCap) cap_scores<64, float>(x, item_scale, a.cap_log2);
-                if (valid < kTcBlockTokens) {
+                        for (int c = 0; c < D / 32; ++c) {
+                            uint32_t ov[32];
+                            tc::ld32(tO + 32 * c, ov);
+                            tc::wait_ld();
 #pragma unroll
-                    for (int j = 0; j < 64; ++j) hide_from(x[j], j, valid);
-                }
-                // the block's max in the log2 domain (sl > 0)
-                float mr = x[0];
-#pragma unroll
-                for (int j = 1; j + 1 < 64; j += 2) mr = dev::max3(mr, x[j], x[j + 1]);
-                mr = fmaxf(mr, x[63]);
-                const float mb = mr * sl;
-                if (i == 0) {
-                    m_use = mb;
-                } else if (__any_sync(0xffffffffu, mb > m_use + kTcRescaleLog2)) {
-                    // O must hold PV(b - 1) before it is rescaled
-                    if (!tc_warp_wait(bar(kBarPvDone + ((b - 1) & 1)), ((b - 1) >> 1) & 1, limit,
-                                      abort_flag, lane)) {
+                            for (int j = 0; j < 32; ++j) ov[j] = __float_as_uint(__uint_as_float(ov[j]) * alpha);
+                            tc::st32(tO + 32 * c, ov);
+                        }
+                        tc::wait_st();
+                        l *= alpha;
+                        m_use = m_new;
+                    }
+                    return true;
+                };
+                if constexpr (KV::kCap == kCapFree) {
+                    // no reference: 32 scores at a time, whose P goes over scores
+                    // that are read.  (Rolled: with all 64 unrolled, beside the suffix
+                    // warps' code, a step of 8 requests took 64 us, not 62, and 76, not
+                    // 66, with logits at the cap.)
+#pragma unroll 1
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t xs[32], ps[16];
+                        tc::ld32(tS + 32 * c, xs);
+                        tc::wait_ld();
+                        PackedRow<false> row{ps};
+                        cap_free(xs, valid - 32 * c, valid < kTcBlockTokens, cap_large, cap, row);
+                        float l0, l1;
+                        dev::f32x2_split(row.sum, l0, l1);
+                        l += l0 + l1;
+                        tc::st16(tS + 16 * c, ps);
+                    }
+                } else if constexpr (KV::kCap == kCapRef) {
+                    uint32_t xs[64], ps[32];
+                    tc::ld32(tS, *reinterpret_cast<uint32_t(*)[32]>(xs));
+                    tc::ld32(tS + 32, *reinterpret_cast<uint32_t(*)[32]>(xs + 32));
+                    tc::wait_ld();
+                    float lo = INFINITY, hi = -INFINITY;
+                    cap_range(xs, valid, lo, hi);
+                    const bool large = __any_sync(0xffffffffu, fmaxf(hi, -lo) * cap.to >= kCapSeries);
+                    if (!raise_reference(cap_one(hi, cap))) {
                         ok = false;
                         break;
                     }
-                    tc::fence_after_sync();
-                    const float m_new = fmaxf(m_use, mb);
-                    const float alpha = m_new == m_use ? 1.f : dev::fast_exp2(m_use - m_new);
-#pragma unroll
-                    for (int c = 0; c < D / 32; ++c) {
-                        uint32_t ov[32];
-                        tc::ld32(tO + 32 * c, ov);
-                        tc::wait_ld();
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) ov[j] = __float_as_uint(__uint_as_float(ov[j]) * alpha);
-                        tc::st32(tO + 32 * c, ov);
-                    }
-                    tc::wait_st();
-                    l *= alpha;
-                    m_use = m_new;
-                }
-                // P = 2^(x - m) as bf16 pairs over the first 32 columns of S
-                const float m_ref = m_use == -INFINITY ? 0.f : m_use;
-                // 2^(x sl - m) with pairs of fp32 lanes: one packed FMA per
-                // two exponents, and two running sums
-                const unsigned long long slp = dev::f32x2(sl, sl), nmp = dev::f32x2(-m_ref, -m_ref);
-                unsigned long long lsum = dev::f32x2(0.f, 0.f);
-                uint32_t pw[32];
-#pragma unroll
-                for (int c = 0; c < 32; ++c) {
-                    float e0, e1;
-                    dev::f32x2_split(dev::fma_f32x2(dev::f32x2(x[2 * c], x[2 * c + 1]), slp, nmp), e0, e1);
-                    const float p0 = dev::fast_exp2(e0), p1 = dev::fast_exp2(e1);
-                    lsum = dev::add_f32x2(lsum, dev::f32x2(p0, p1));
-                    pw[c] = kF8 ? dev::pack_f16(p0, p1) : dev::pack_bf16(p0, p1);
-                }
-                {
+                    PackedRow<kF8> row{ps};
+                    cap_exponentials(xs, valid, valid < kTcBlockTokens, large, dev::f32x2(-m_use, -m_use), cap, row);
                     float l0, l1;
-                    dev::f32x2_split(lsum, l0, l1);
+                    dev::f32x2_split(row.sum, l0, l1);
                     l += l0 + l1;
+                    tc::st32(tS, ps);
+                } else {
+                    uint32_t sr[2][32];
+                    tc::ld32(tS, sr[0]);
+                    tc::ld32(tS + 32, sr[1]);
+                    tc::wait_ld();
+                    // raw scores; keys past the item's last token -inf
+                    float x[64];
+#pragma unroll
+                    for (int j = 0; j < 64; ++j) x[j] = __uint_as_float(sr[j >> 5][j & 31]);
+                    if (valid < kTcBlockTokens) {
+#pragma unroll
+                        for (int j = 0; j < 64; ++j) hide_from(x[j], j, valid);
+                    }
+                    // the block's max in the log2 domain (sl > 0)
+                    float mr = x[0];
+#pragma unroll
+                    for (int j = 1; j + 1 < 64; j += 2) mr = dev::max3(mr, x[j], x[j + 1]);
+                    mr = fmaxf(mr, x[63]);
+                    const float mb = mr * sl;
+                    if (!raise_reference(mb)) {
+                        ok = false;
+                        break;
+                    }
+                    // P = 2^(x - m) as bf16 pairs over the first 32 columns of S
+                    const float m_ref = m_use == -INFINITY ? 0.f : m_use;
+                    // 2^(x sl - m) with pairs of fp32 lanes: one packed FMA per
+                    // two exponents, and two running sums
+                    const unsigned long long slp = dev::f32x2(sl, sl), nmp = dev::f32x2(-m_ref, -m_ref);
+                    unsigned long long lsum = dev::f32x2(0.f, 0.f);
+                    uint32_t pw[32];
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) {
+                        float e0, e1;
+                        dev::f32x2_split(dev::fma_f32x2(dev::f32x2(x[2 * c], x[2 * c + 1]), slp, nmp), e0, e1);
+                        const float p0 = dev::fast_exp2(e0), p1 = dev::fast_exp2(e1);
+                        lsum = dev::add_f32x2(lsum, dev::f32x2(p0, p1));
+                        pw[c] = kF8 ? dev::pack_f16(p0, p1) : dev::pack_bf16(p0, p1);
+                    }
+                    {
+                        float l0, l1;
+                        dev::f32x2_split(lsum, l0, l1);
+                        l += l0 + l1;
+                    }
+                    tc::st32(tS, pw);
                 }
-                tc::st32(tS, pw);
                 tc::wait_st();
                 // V rows past the block's valid tokens may hold anything (NaN
                 // included); P is 0 there but 0 * NaN is NaN, so zero them (the
@@ -1994,7 +2101,9 @@ __device__ void prefix_cta_tc_pair(const KvMaps *maps, const AttnArgs &a, uint8_
                 const WorkItem it = tile_of(m);
                 const int nb = tc_blocks(it.num_pages);
                 const int tokens = (it.num_pages - 1) * kPageSize + it.last_valid;
-                float m_use = -INFINITY, l = 0.f;
+                float m_use = KV::kCap == kCapFree ? 0.f : -INFINITY, l = 0.f;
+                bool cap_large = false;
+                const CapFactors cap(a.to_cap, a.cap_log2);           // (used under a cap)
                 for (int i = 0; i < nb; ++i) {
                     const int buf = u & 1;
                     const uint32_t tS = lane_base + kTmemS + 128u * t + 64u * buf;
@@ -2004,78 +2113,121 @@ __device__ void prefix_cta_tc_pair(const KvMaps *maps, const AttnArgs &a, uint8_
                         break;
                     }
                     tc::fence_after_sync();
-                    uint32_t sr[2][32];
-                    tc::ld32(tS, sr[0]);
-                    tc::ld32(tS + 32, sr[1]);
-                    tc::wait_ld();
+                    // the row's reference max at least mb less 2^8 (O and l with it)
+                    auto raise_reference = [&](float mb) {
+                        if (i == 0) {
+                            m_use = mb;
+                        } else if (__any_sync(0xffffffffu, mb > m_use + kTcRescaleLog2)) {
+                            // O must hold the tile's previous PV before it is rescaled
+                            if (!tc_warp_wait(bar(kPbPvDone + 2 * t + ((u - 1) & 1)), ((u - 1) >> 1) & 1, limit,
+                                              abort_flag, lane)) {
+                                return false;
+                            }
+                            tc::fence_after_sync();
+                            const float m_new = fmaxf(m_use, mb);
+                            const float alpha = m_new == m_use ? 1.f : dev::fast_exp2(m_use - m_new);
+#pragma unroll
+                            for (int c = 0; c < D / 32; ++c) {
+                                uint32_t ov[32];
+                                tc::ld32(tO + 32 * c, ov);
+                                tc::wait_ld();
+#pragma unroll
+                                for (int q = 0; q < 32; ++q)
+                                    ov[q] = __float_as_uint(__uint_as_float(ov[q]) * alpha);
+                                tc::st32(tO + 32 * c, ov);
+                            }
+                            tc::wait_st();
+                            l *= alpha;
+                            m_use = m_new;
+                        }
+                        return true;
+                    };
                     // the tile's last S of the pair is done: its Q buffer takes the
                     // next pair's rows while this block's softmax runs
-                    if (i == nb - 1) {
-                        more = has_pair(k + 1);
-                        if (!ok) break;
-                        if (more && on_in(k + 1)) {
-                            issue_q(k + 1);
-                            loaded_next = true;
+                    auto next_q = [&]() {
+                        if (i == nb - 1) {
+                            more = has_pair(k + 1);
+                            if (!ok) return false;
+                            if (more && on_in(k + 1)) {
+                                issue_q(k + 1);
+                                loaded_next = true;
+                            }
                         }
-                    }
-                    float x[64];
-#pragma unroll
-                    for (int q = 0; q < 64; ++q) x[q] = __uint_as_float(sr[q >> 5][q & 31]);
-                    if constexpr (KV::kCap) cap_scores<64, float>(x, a.to_cap, a.cap_log2);
-                    if (valid < kTcBlockTokens) {
-#pragma unroll
-                        for (int q = 0; q < 64; ++q) hide_from(x[q], q, valid);
-                    }
-                    float mr = x[0];
-#pragma unroll
-                    for (int q = 1; q + 1 < 64; q += 2) mr = dev::max3(mr, x[q], x[q + 1]);
-                    mr = fmaxf(mr, x[63]);
-                    const float sl = KV::kCap ? 1.f : a.scale_log2;
-                    const float mb = mr * sl;
-                    if (i == 0) {
-                        m_use = mb;
-                    } else if (__any_sync(0xffffffffu, mb > m_use + kTcRescaleLog2)) {
-                        // O must hold the tile's previous PV before it is rescaled
-                        if (!tc_warp_wait(bar(kPbPvDone + 2 * t + ((u - 1) & 1)), ((u - 1) >> 1) & 1, limit,
-                                          abort_flag, lane)) {
+                        return true;
+                    };
+                    if constexpr (KV::kCap == kCapFree) {
+                        if (!next_q()) break;
+                        uint32_t xs[64], ps[32];
+                        tc::ld32(tS, *reinterpret_cast<uint32_t(*)[32]>(xs));
+                        tc::ld32(tS + 32, *reinterpret_cast<uint32_t(*)[32]>(xs + 32));
+                        tc::wait_ld();
+                        PackedRow<false> row{ps};
+                        cap_free(xs, valid, valid < kTcBlockTokens, cap_large, cap, row);
+                        float l0, l1;
+                        dev::f32x2_split(row.sum, l0, l1);
+                        l += l0 + l1;
+                        tc::st32(tS, ps);
+                    } else if constexpr (KV::kCap == kCapRef) {
+                        uint32_t xs[64], ps[32];
+                        tc::ld32(tS, *reinterpret_cast<uint32_t(*)[32]>(xs));
+                        tc::ld32(tS + 32, *reinterpret_cast<uint32_t(*)[32]>(xs + 32));
+                        tc::wait_ld();
+                        if (!next_q()) break;
+                        float lo = INFINITY, hi = -INFINITY;
+                        cap_range(xs, valid, lo, hi);
+                        const bool large = __any_sync(0xffffffffu, fmaxf(hi, -lo) * cap.to >= kCapSeries);
+                        if (!raise_reference(cap_one(hi, cap))) {
                             ok = false;
                             break;
                         }
-                        tc::fence_after_sync();
-                        const float m_new = fmaxf(m_use, mb);
-                        const float alpha = m_new == m_use ? 1.f : dev::fast_exp2(m_use - m_new);
-#pragma unroll
-                        for (int c = 0; c < D / 32; ++c) {
-                            uint32_t ov[32];
-                            tc::ld32(tO + 32 * c, ov);
-                            tc::wait_ld();
-#pragma unroll
-                            for (int q = 0; q < 32; ++q)
-                                ov[q] = __float_as_uint(__uint_as_float(ov[q]) * alpha);
-                            tc::st32(tO + 32 * c, ov);
-                        }
-                        tc::wait_st();
-                        l *= alpha;
-                        m_use = m_new;
-                    }
-                    const float m_ref = m_use == -INFINITY ? 0.f : m_use;
-                    const unsigned long long slp = dev::f32x2(sl, sl), nmp = dev::f32x2(-m_ref, -m_ref);
-                    unsigned long long lsum = dev::f32x2(0.f, 0.f);
-                    uint32_t pw[32];
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) {
-                        float e0, e1;
-                        dev::f32x2_split(dev::fma_f32x2(dev::f32x2(x[2 * c], x[2 * c + 1]), slp, nmp), e0, e1);
-                        const float p0 = dev::fast_exp2(e0), p1 = dev::fast_exp2(e1);
-                        lsum = dev::add_f32x2(lsum, dev::f32x2(p0, p1));
-                        pw[c] = dev::pack_bf16(p0, p1);
-                    }
-                    {
+                        PackedRow<false> row{ps};
+                        cap_exponentials(xs, valid, valid < kTcBlockTokens, large, dev::f32x2(-m_use, -m_use), cap, row);
                         float l0, l1;
-                        dev::f32x2_split(lsum, l0, l1);
+                        dev::f32x2_split(row.sum, l0, l1);
                         l += l0 + l1;
+                        tc::st32(tS, ps);
+                    } else {
+                        uint32_t sr[2][32];
+                        tc::ld32(tS, sr[0]);
+                        tc::ld32(tS + 32, sr[1]);
+                        tc::wait_ld();
+                        if (!next_q()) break;
+                        float x[64];
+#pragma unroll
+                        for (int q = 0; q < 64; ++q) x[q] = __uint_as_float(sr[q >> 5][q & 31]);
+                        const float sl = a.scale_log2;
+                        if (valid < kTcBlockTokens) {
+#pragma unroll
+                            for (int q = 0; q < 64; ++q) hide_from(x[q], q, valid);
+                        }
+                        float mr = x[0];
+#pragma unroll
+                        for (int q = 1; q + 1 < 64; q += 2) mr = dev::max3(mr, x[q], x[q + 1]);
+                        mr = fmaxf(mr, x[63]);
+                        const float mb = mr * sl;
+                        if (!raise_reference(mb)) {
+                            ok = false;
+                            break;
+                        }
+                        const float m_ref = m_use == -INFINITY ? 0.f : m_use;
+                        const unsigned long long slp = dev::f32x2(sl, sl), nmp = dev::f32x2(-m_ref, -m_ref);
+                        unsigned long long lsum = dev::f32x2(0.f, 0.f);
+                        uint32_t pw[32];
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) {
+                            float e0, e1;
+                            dev::f32x2_split(dev::fma_f32x2(dev::f32x2(x[2 * c], x[2 * c + 1]), slp, nmp), e0, e1);
+                            const float p0 = dev::fast_exp2(e0), p1 = dev::fast_exp2(e1);
+                            lsum = dev::add_f32x2(lsum, dev::f32x2(p0, p1));
+                            pw[c] = dev::pack_bf16(p0, p1);
+                        }
+                        {
+                            float l0, l1;
+                            dev::f32x2_split(lsum, l0, l1);
+                            l += l0 + l1;
+                        }
+                        tc::st32(tS, pw);
                     }
-                    tc::st32(tS, pw);
                     tc::wait_st();
                     // V rows past the block's valid tokens may hold anything (NaN
                     // included); P is 0 there but 0 * NaN is NaN, so tile A zeroes
@@ -2280,8 +2432,16 @@ static cudaError_t launch_bf16(const AttnArgs &a, const KvMaps &maps, int head_d
     return cudaErrorNotSupported;
 }
 
+template <template <class> class Kind>
+static cudaError_t configure_bf16(int head_dim) {
+    if (head_dim == 64) return configure<64, Kind<KvBf16>>(nullptr);
+    if (head_dim != 128) return cudaErrorNotSupported;
+    const cudaError_t e = configure<128, Kind<KvBf16Deep>>(nullptr);
+    return e != cudaSuccess ? e : configure<128, Kind<KvBf16>>(nullptr);
+}
+
 template <class KV>
-using Plain = KV;
+using Uncapped = KV;
 
 cudaError_t attn_mma_ctas_per_sm(int head_dim, int mode, int *ctas_per_sm) {
     if (mode == PARASON_FP8_E4M3_KV)
@@ -2298,25 +2458,24 @@ cudaError_t attn_mma_ctas_per_sm(int head_dim, int mode, int *ctas_per_sm) {
 cudaError_t launch_attn_bf16(const AttnArgs &a, const KvMaps &maps, int head_dim,
                              cudaStream_t stream) {
     if (a.num_items <= 0 || a.num_ctas <= 0) return cudaSuccess;
-    return a.cap_log2 > 0.f ? launch_bf16<Capped>(a, maps, head_dim, stream)
-                            : launch_bf16<Plain>(a, maps, head_dim, stream);
+    if (a.cap_log2 <= 0.f) return launch_bf16<Uncapped>(a, maps, head_dim, stream);
+    return a.cap_log2 <= kCapFreeLog2 ? launch_bf16<CappedFree>(a, maps, head_dim, stream)
+                                      : launch_bf16<CappedRef>(a, maps, head_dim, stream);
 }
 
 cudaError_t launch_attn_fp8(const AttnArgs &a, const KvMaps &maps, int head_dim,
                             cudaStream_t stream) {
     if (a.num_items <= 0 || a.num_ctas <= 0) return cudaSuccess;
     if (head_dim != 128) return cudaErrorNotSupported;
-    return a.cap_log2 > 0.f ? launch<128, Capped<KvE4m3>>(a, maps, stream)
+    return a.cap_log2 > 0.f ? launch<128, CappedRef<KvE4m3>>(a, maps, stream)
                             : launch<128, KvE4m3>(a, maps, stream);
 }
 
 cudaError_t attn_mma_prepare_cap(int head_dim, int mode) {
     if (mode == PARASON_FP8_E4M3_KV)
-        return head_dim == 128 ? configure<128, Capped<KvE4m3>>(nullptr) : cudaErrorNotSupported;
-    if (head_dim == 64) return configure<64, Capped<KvBf16>>(nullptr);
-    if (head_dim != 128) return cudaErrorNotSupported;
-    const cudaError_t e = configure<128, Capped<KvBf16Deep>>(nullptr);
-    return e != cudaSuccess ? e : configure<128, Capped<KvBf16>>(nullptr);
+        return head_dim == 128 ? configure<128, CappedRef<KvE4m3>>(nullptr) : cudaErrorNotSupported;
+    const cudaError_t e = configure_bf16<CappedFree>(head_dim);
+    return e != cudaSuccess ? e : configure_bf16<CappedRef>(head_dim);
 }
 
 }  // namespace parason

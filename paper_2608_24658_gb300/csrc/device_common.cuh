@@ -199,6 +199,13 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return m;
 }
 
+// min(a, b, c)
+__device__ __forceinline__ float min3(float a, float b, float c) {
+    float m;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+    return m;
+}
+
 // Pairs of fp32 values in one 64-bit register and the packed operations on
 // them.
 __device__ __forceinline__ unsigned long long f32x2(float lo, float hi) {

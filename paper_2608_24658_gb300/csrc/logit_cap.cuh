@@ -11,17 +11,31 @@
 // is at most 5e-7 of tanh(kCapSeries).  Which form a score takes depends on that
 // score alone.
 //
-// What bounds it: the softmax warps' issue slots and the MUFU.  The series is 7
+// A cap also bounds the logits, so where 2^cap_log2 leaves fp32 and bf16 room
+// (kCapFreeLog2) the softmax needs no maximum: P = 2^x, l = sum 2^x, with the
+// partials' reference m = 0.  There is then no pass over the scores before the
+// exponentials, no rescaling of O, and no order in which P has to wait.  f16 P
+// (e4m3 KV) has no such range, and larger caps have none either: they keep the
+// running maximum (kCapRef).
+//
+// What bounds it: the softmax warps' instructions (their issue, and their fetch:
+// long unrolled loops run no faster than they are fetched).  The series is 7
 // packed instructions per two scores and no MUFU; the exponential form adds an
-// exponential and a reciprocal per score to the softmax's own exponential.  Models
-// keep nearly all logits far below their cap, so a warp votes: if no score of
-// the block reaches kCapSeries, it runs the series alone.
+// exponential per score and a reciprocal per two.  Models keep nearly all logits
+// far below their cap, so a warp votes: if no score of the block reaches
+// kCapSeries, it runs the series alone.
 #pragma once
 
 #include "device_common.cuh"
+#include "tile_common.cuh"
 
 namespace parason {
 namespace {
+
+// what an attention kernel does to its logits
+enum : int { kCapNone = 0, kCapFree = 1, kCapRef = 2 };
+// 2^73 is what a cap of 50 needs; sums of 2^20 tokens stay finite for |v| to 2^34
+constexpr float kCapFreeLog2 = 73.f;
 
 constexpr float kCapSeries = 0.4f;
 constexpr float kCapA1 = -0.33331882f, kCapA2 = 0.13277629f, kCapA3 = -0.047794217f;
@@ -35,87 +49,257 @@ __device__ __forceinline__ float fast_rcp(float x) {
 // The factors of one item's scores, in both halves of packed pairs.
 struct CapFactors {
     unsigned long long to_cap, scale;    // u = to_cap <q, k>, scale = cap_log2 to_cap
-    float two_u, cap_log2;               // two_u <q, k> = 2 u log2(e)
-    __device__ __forceinline__ CapFactors(float to, float cap) {
-        const float s = cap * to;
+    unsigned long long a1, a2, a3;       // the series' coefficients times cap_log2
+    unsigned long long two_u;            // two_u <q, k> = 2 u log2(e)
+    float to, cap;
+    __device__ __forceinline__ CapFactors(float to_, float cap_) : to(to_), cap(cap_) {
+        const float s = cap * to, w = 2.f * 1.4426950408889634f * to;
         to_cap = dev::f32x2(to, to);
         scale = dev::f32x2(s, s);
-        two_u = 2.f * 1.4426950408889634f * to;
-        cap_log2 = cap;
+        a1 = dev::f32x2(kCapA1 * cap, kCapA1 * cap);
+        a2 = dev::f32x2(kCapA2 * cap, kCapA2 * cap);
+        a3 = dev::f32x2(kCapA3 * cap, kCapA3 * cap);
+        two_u = dev::f32x2(w, w);
     }
 };
 
-// cap_log2 tanh of two scores by the series; u of both in `u`.
+// cap_log2 tanh - m of two scores by the series (nm: -m in both halves); u^2 of
+// both in `t`.
+__device__ __forceinline__ unsigned long long cap_series(unsigned long long x, unsigned long long nm,
+                                                         const CapFactors &f, unsigned long long &t) {
+    const unsigned long long u = dev::mul_f32x2(x, f.to_cap);
+    t = dev::mul_f32x2(u, u);
+    unsigned long long q = dev::fma_f32x2(t, f.a3, f.a2);
+    q = dev::fma_f32x2(q, t, f.a1);
+    return dev::fma_f32x2(dev::mul_f32x2(u, t), q, dev::fma_f32x2(x, f.scale, nm));
+}
+
+// cap_log2 tanh of two scores, without a reference.
 __device__ __forceinline__ unsigned long long cap_series(unsigned long long x, const CapFactors &f,
-                                                         unsigned long long &u) {
-    u = dev::mul_f32x2(x, f.to_cap);
-    const unsigned long long t = dev::mul_f32x2(u, u);
-    const unsigned long long s = dev::mul_f32x2(x, f.scale);
-    unsigned long long q = dev::fma_f32x2(t, dev::f32x2(kCapA3, kCapA3), dev::f32x2(kCapA2, kCapA2));
-    q = dev::fma_f32x2(q, t, dev::f32x2(kCapA1, kCapA1));
-    return dev::fma_f32x2(dev::mul_f32x2(s, t), q, s);
+                                                         unsigned long long &t) {
+    const unsigned long long u = dev::mul_f32x2(x, f.to_cap);
+    t = dev::mul_f32x2(u, u);
+    unsigned long long q = dev::fma_f32x2(t, f.a3, f.a2);
+    q = dev::fma_f32x2(q, t, f.a1);
+    q = dev::fma_f32x2(q, t, dev::f32x2(f.cap, f.cap));
+    return dev::mul_f32x2(u, q);
 }
 
-// ... of one score by the exponential (x = +-inf gives +-cap_log2).
-__device__ __forceinline__ float cap_exp(float x, const CapFactors &f) {
-    return fmaf(-2.f * f.cap_log2, fast_rcp(1.f + dev::fast_exp2(x * f.two_u)), f.cap_log2);
+// cap_log2 tanh - m of two scores by the exponential (base: cap_log2 - m in both
+// halves).  They share one reciprocal, 1 / (d0 d1), of factors that are cut at 2^60
+// (tanh is 1 there in fp32, infinities included).
+__device__ __forceinline__ unsigned long long cap_exp_pair(float x0, float x1, const CapFactors &f,
+                                                           unsigned long long base) {
+    float w0, w1;
+    dev::f32x2_split(dev::mul_f32x2(dev::f32x2(x0, x1), f.two_u), w0, w1);
+    const float d0 = 1.f + dev::fast_exp2(fminf(w0, 60.f)), d1 = 1.f + dev::fast_exp2(fminf(w1, 60.f));
+    const float r = fast_rcp(d0 * d1);
+    return dev::fma_f32x2(dev::f32x2(r * d1, r * d0), dev::f32x2(-2.f * f.cap, -2.f * f.cap), base);
 }
 
-// ... of one score, either way.
+// The same with every score in the form its own size asks for.
+__device__ __forceinline__ void cap_pair(float x0, float x1, unsigned long long nm, const CapFactors &f,
+                                         float &y0, float &y1) {
+    unsigned long long t;
+    float s0, s1, t0, t1, e0, e1;
+    dev::f32x2_split(cap_series(dev::f32x2(x0, x1), nm, f, t), s0, s1);
+    dev::f32x2_split(t, t0, t1);
+    dev::f32x2_split(cap_exp_pair(x0, x1, f, dev::add_f32x2(dev::f32x2(f.cap, f.cap), nm)), e0, e1);
+    y0 = t0 < kCapSeries * kCapSeries ? s0 : e0;
+    y1 = t1 < kCapSeries * kCapSeries ? s1 : e1;
+}
+
+// One score's logit.
 __device__ __forceinline__ float cap_one(float x, const CapFactors &f) {
-    unsigned long long u;
-    float s, unused, u0;
-    dev::f32x2_split(cap_series(dev::f32x2(x, x), f, u), s, unused);
-    dev::f32x2_split(u, u0, unused);
-    return fabsf(u0) < kCapSeries ? s : cap_exp(x, f);
+    float y, unused;
+    cap_pair(x, x, dev::f32x2(0.f, 0.f), f, y, unused);
+    return y;
 }
 
-__device__ __forceinline__ float score_of(float x) { return x; }
-__device__ __forceinline__ float score_of(uint32_t x) { return __uint_as_float(x); }
-__device__ __forceinline__ void set_score(float &x, float v) { x = v; }
-__device__ __forceinline__ void set_score(uint32_t &x, float v) { x = __float_as_uint(v); }
-
-// M x N scores of a lane (floats or their bits) in place; the whole warp calls.
-template <int M, int N, class X>
-__device__ __forceinline__ void cap_scores(X (&x)[M][N], float to_cap, float cap_log2) {
+// ---------------------------------------------------------------- mma.sync steps
+// A lane's M x N scores to logits in place; the whole warp calls.  large: whether
+// the warp's last scores had one at kCapSeries or past it.  The series runs on
+// trust, and the scores are done again if one turns up.
+template <int M, int N>
+__device__ __forceinline__ void cap_scores(float (&x)[M][N], bool &large, const CapFactors &f) {
     static_assert(N % 2 == 0, "scores come in pairs");
-    const CapFactors f(to_cap, cap_log2);
-    float most = 0.f;
-#pragma unroll
-    for (int i = 0; i < M; ++i)
-#pragma unroll
-        for (int j = 0; j < N; j += 2)
-            most = dev::max3(most, fabsf(score_of(x[i][j])), fabsf(score_of(x[i][j + 1])));
-    if (!__any_sync(0xffffffffu, most * fabsf(to_cap) >= kCapSeries)) {
+    if (!large) {
+        float most = 0.f, y[M][N];
 #pragma unroll
         for (int i = 0; i < M; ++i)
 #pragma unroll
             for (int j = 0; j < N; j += 2) {
-                unsigned long long u;
-                float a, b;
-                dev::f32x2_split(cap_series(dev::f32x2(score_of(x[i][j]), score_of(x[i][j + 1])), f, u), a, b);
-                set_score(x[i][j], a);
-                set_score(x[i][j + 1], b);
+                unsigned long long t;
+                float t0, t1;
+                dev::f32x2_split(cap_series(dev::f32x2(x[i][j], x[i][j + 1]), f, t), y[i][j], y[i][j + 1]);
+                dev::f32x2_split(t, t0, t1);
+                most = dev::max3(most, t0, t1);
             }
-        return;
+        large = __any_sync(0xffffffffu, most >= kCapSeries * kCapSeries);
+        if (!large) {
+#pragma unroll
+            for (int i = 0; i < M; ++i)
+#pragma unroll
+                for (int j = 0; j < N; ++j) x[i][j] = y[i][j];
+            return;
+        }
     }
+    float hi = 0.f, lo = 0.f;
 #pragma unroll
     for (int i = 0; i < M; ++i)
 #pragma unroll
         for (int j = 0; j < N; j += 2) {
-            const float p = score_of(x[i][j]), q = score_of(x[i][j + 1]);
-            unsigned long long u;
-            float a, b, u0, u1;
-            dev::f32x2_split(cap_series(dev::f32x2(p, q), f, u), a, b);
-            dev::f32x2_split(u, u0, u1);
-            set_score(x[i][j], fabsf(u0) < kCapSeries ? a : cap_exp(p, f));
-            set_score(x[i][j + 1], fabsf(u1) < kCapSeries ? b : cap_exp(q, f));
+            const float x0 = x[i][j], x1 = x[i][j + 1];
+            hi = dev::max3(hi, x0, x1);
+            lo = dev::min3(lo, x0, x1);
+            if (f.cap <= kCapFreeLog2)
+                dev::f32x2_split(cap_exp_pair(x0, x1, f, dev::f32x2(f.cap, f.cap)), x[i][j], x[i][j + 1]);
+            else
+                cap_pair(x0, x1, dev::f32x2(0.f, 0.f), f, x[i][j], x[i][j + 1]);
         }
+    large = __any_sync(0xffffffffu, fmaxf(hi, -lo) * f.to >= kCapSeries);
 }
 
+// ---------------------------------------------------------------- no reference
+// P = 2^x (caps up to kCapFreeLog2).  The exponential form serves all scores of a
+// block where one is large: its absolute error, 2e-7 cap, is 1e-5 at most there.
+
+__device__ __forceinline__ float score_of(float x) { return x; }
+__device__ __forceinline__ float score_of(uint32_t x) { return __uint_as_float(x); }
+
+// Where a tile's P goes: packed 16-bit pairs and the row's sum.
+template <bool F16>
+struct PackedRow {
+    uint32_t *pw;
+    unsigned long long sum;
+    __device__ __forceinline__ void start() { sum = 0ull; }
+    __device__ __forceinline__ void operator()(int c, float p0, float p1) {
+        sum = dev::add_f32x2(sum, dev::f32x2(p0, p1));
+        pw[c] = F16 ? dev::pack_f16(p0, p1) : dev::pack_bf16(p0, p1);
+    }
+};
+
+// The P of a lane's N scores as they are (mma.sync steps).
+template <int N>
+struct LaneP {
+    float p[N];
+    __device__ __forceinline__ void start() {}
+    __device__ __forceinline__ void operator()(int c, float p0, float p1) {
+        p[2 * c] = p0;
+        p[2 * c + 1] = p1;
+    }
+};
+
+// P of N scores, the first `seen` of which count (hidden: for some lane of the warp
+// not all), handed pair by pair to `put`
+// (again from `start()` on where a block is done twice); the whole warp calls.
+// large: whether the warp's last block had a score at kCapSeries or past it.  The
+// series runs on trust, and the block is done again if one turns up.
+template <int N, class X, class Put>
+__device__ __forceinline__ void cap_free(const X (&x)[N], int seen, bool hidden, bool &large, const CapFactors &f,
+                                         Put &put) {
+    const unsigned long long base = dev::f32x2(f.cap, f.cap);
+    put.start();
+    if (hidden) {
+#pragma unroll
+        for (int c = 0; c < N / 2; ++c) {
+            float e0, e1;
+            dev::f32x2_split(cap_exp_pair(score_of(x[2 * c]), score_of(x[2 * c + 1]), f, base), e0, e1);
+            const float p0 = dev::fast_exp2(e0), p1 = dev::fast_exp2(e1);
+            put(c, 2 * c < seen ? p0 : 0.f, 2 * c + 1 < seen ? p1 : 0.f);
+        }
+        return;
+    }
+    if (!large) {
+        float most = 0.f;
+#pragma unroll
+        for (int c = 0; c < N / 2; ++c) {
+            const float x0 = score_of(x[2 * c]), x1 = score_of(x[2 * c + 1]);
+            unsigned long long t;
+            float e0, e1, t0, t1;
+            dev::f32x2_split(cap_series(dev::f32x2(x0, x1), f, t), e0, e1);
+            dev::f32x2_split(t, t0, t1);
+            most = dev::max3(most, t0, t1);
+            put(c, dev::fast_exp2(e0), dev::fast_exp2(e1));
+        }
+        large = __any_sync(0xffffffffu, most >= kCapSeries * kCapSeries);
+        if (!large) return;
+        put.start();
+    }
+    float hi = 0.f, lo = 0.f;
+#pragma unroll
+    for (int c = 0; c < N / 2; ++c) {
+        const float x0 = score_of(x[2 * c]), x1 = score_of(x[2 * c + 1]);
+        float e0, e1;
+        dev::f32x2_split(cap_exp_pair(x0, x1, f, base), e0, e1);
+        hi = dev::max3(hi, x0, x1);
+        lo = dev::min3(lo, x0, x1);
+        put(c, dev::fast_exp2(e0), dev::fast_exp2(e1));
+    }
+    large = __any_sync(0xffffffffu, fmaxf(hi, -lo) * f.to >= kCapSeries);
+}
+
+// ---------------------------------------------------------------- tiles
+// A tile's softmax keeps a row's scores as they come from TMEM and caps them
+// inside the loop that takes their exponentials, where the series (FMA pipe)
+// runs beside the exponentials (MUFU); tanh is monotone, so the row's largest
+// logit is that of its largest score, and no pass over the logits is needed
+// before.  Keys a row does not see (from `seen` on) are left out of the range
+// and get P = 0, whatever their score.
+
+// Widen [lo, hi] by N scores of which the first `seen` count.
 template <int N, class X>
-__device__ __forceinline__ void cap_scores(X (&x)[N], float to_cap, float cap_log2) {
-    cap_scores<1, N, X>(*reinterpret_cast<X(*)[1][N]>(&x), to_cap, cap_log2);
+__device__ __forceinline__ void cap_range(const X (&x)[N], int seen, float &lo, float &hi) {
+    if (seen >= N) {
+#pragma unroll
+        for (int j = 0; j < N; j += 2) {
+            hi = dev::max3(hi, score_of(x[j]), score_of(x[j + 1]));
+            lo = dev::min3(lo, score_of(x[j]), score_of(x[j + 1]));
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            float s = score_of(x[j]);
+            hide_from(s, j, seen);                     // -inf from `seen` on
+            hi = fmaxf(hi, s);
+            lo = j < seen ? fminf(lo, score_of(x[j])) : lo;
+        }
+    }
+}
+
+// P of N scores, the first `seen` of which count (hidden: for some lane of the warp
+// not all), against the reference (nm: its negative in both halves), handed to
+// `put`.  large: some score of the warp's block reaches kCapSeries; caps up to
+// kCapFreeLog2 then take the exponential form for all of it.
+template <int N, class X, class Put>
+__device__ __forceinline__ void cap_exponentials(const X (&x)[N], int seen, bool hidden, bool large,
+                                                 unsigned long long nm, const CapFactors &f, Put &put) {
+    put.start();
+    if (!hidden && !large) {
+#pragma unroll
+        for (int c = 0; c < N / 2; ++c) {
+            unsigned long long t;
+            float e0, e1;
+            dev::f32x2_split(cap_series(dev::f32x2(score_of(x[2 * c]), score_of(x[2 * c + 1])), nm, f, t), e0, e1);
+            put(c, dev::fast_exp2(e0), dev::fast_exp2(e1));
+        }
+    } else if (!hidden && f.cap <= kCapFreeLog2) {
+        const unsigned long long base = dev::add_f32x2(dev::f32x2(f.cap, f.cap), nm);
+#pragma unroll
+        for (int c = 0; c < N / 2; ++c) {
+            float e0, e1;
+            dev::f32x2_split(cap_exp_pair(score_of(x[2 * c]), score_of(x[2 * c + 1]), f, base), e0, e1);
+            put(c, dev::fast_exp2(e0), dev::fast_exp2(e1));
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < N / 2; ++c) {
+            float e0, e1;
+            cap_pair(score_of(x[2 * c]), score_of(x[2 * c + 1]), nm, f, e0, e1);
+            const float p0 = dev::fast_exp2(e0), p1 = dev::fast_exp2(e1);
+            put(c, 2 * c < seen ? p0 : 0.f, 2 * c + 1 < seen ? p1 : 0.f);
+        }
+    }
 }
 
 }  // namespace

@@ -204,14 +204,15 @@ __device__ __forceinline__ void widen_block(uint32_t src, uint32_t dst, int v0, 
     }
 }
 
-// CAP: the logits are capped (logit_cap.cuh).
+// CAP: how the logits are capped (logit_cap.cuh).
 // DIRECT: every pair holds its rows' whole paths, and the kernel writes the
 // result itself (an instantiation of its own: a run-time test cost the join
 // 3%).
-template <bool F8, bool DIRECT, bool CAP>
+template <bool F8, bool DIRECT, int CAP>
 __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
     prefill_kernel(const __grid_constant__ KvMaps maps, const AttnArgs a) {
     using C = Cfg<F8>;
+    static_assert(!F8 || CAP != kCapFree, "f16 P needs a reference");
     extern __shared__ uint8_t smem_raw[];
     __shared__ int abort_flag;
     __shared__ uint32_t tmem_base;
@@ -331,12 +332,12 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                 const int key0 = t == 0 ? m.key0 : m.key0B;
                 // the row's last visible key, relative to the item's first
                 const int t_rel = key0 == kNoKey0 ? (1 << 30) : (it.row0 + r) / a.group - key0;
-                // (under a cap the scores become logits as they are read, sl is 1)
                 const float scale = CAP ? a.to_cap : a.scale_log2;
-                const float item_scale = F8 ? scale * a.k_scale[it.kv_head] : scale;
-                const float sl = CAP ? 1.f : item_scale;
+                const float sl = F8 ? scale * a.k_scale[it.kv_head] : scale;
+                const CapFactors cap(sl, a.cap_log2);                 // (used under a cap)
                 const unsigned long long slp = dev::f32x2(sl, sl);
-                float m_use = -INFINITY, l = 0.f;
+                float m_use = CAP == kCapFree ? 0.f : -INFINITY, l = 0.f;
+                bool cap_large = false;                               // (cap_free)
                 for (int i = 0; i < nb; ++i, ++u) {
                     if (!tc_warp_wait(bar(kSFull + t), u & 1, limit, abort, lane)) {
                         ok = false;
@@ -344,6 +345,147 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                     }
                     tc::fence_after_sync();
                     const int vv = valid_ring[(blk + i) % kValidRing];
+                    // keys of half h that the row sees: to the half's last token, or to
+                    // the row's own
+                    const int valid[2] = {vv & 0xff, vv >> 8};
+                    auto valid_in = [&](int h) { return h == 0 ? valid[0] : valid[1]; };
+                    auto seen_in = [&](int h) {
+                        return min(valid_in(h), t_rel - (i * kBlockTokens + h * kHalfTokens) + 1);
+                    };
+                    // half h of P is stored: announce it
+                    auto finish_half = [&](int h) {
+                        // V rows past the half's valid tokens may hold anything
+                        // (NaN included): P is 0 there, but 0 * NaN is NaN, so
+                        // each tile zeroes them before its PV (the same zeros
+                        // twice; the e4m3 converters write them as zeros)
+                        if (!F8 && valid_in(h) < kHalfTokens) {
+                            const int vs = (pos + 2 * i + 1) % C::kSlots;
+                            if (!tc_warp_wait(bar(kFull + vs), ((pos + 2 * i + 1) / C::kSlots) & 1, limit,
+                                              abort, lane)) {
+                                return false;
+                            }
+                            const uint32_t vst = ring + vs * kSlotBytes;
+                            const int n16 = (kHalfTokens - valid_in(h)) * 2 * 8;
+                            for (int q = r; q < n16; q += kRows) {
+                                const int row = h * kHalfTokens + valid_in(h) + q / 16, cb = (q / 8) & 1;
+                                const uint32_t at = row / kPageSize * kPagedBytes + cb * (kPagedBytes / 2) +
+                                                    row % kPageSize * 128;
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(
+                                                 vst + at + ((q & 7) << 4)),
+                                             "r"(0u)
+                                             : "memory");
+                            }
+                            tc::fence_proxy_async_smem();
+                        }
+                        tc::wait_st();
+                        tc::fence_before_sync();
+                        warp_arrive(kPFull + 2 * t + h);
+                        return true;
+                    };
+                    // the row's reference max at least mb less 2^8 (O and l with it)
+                    auto raise_reference = [&](float mb) {
+                        if (i == 0) {
+                            m_use = mb;
+                        } else if (__any_sync(0xffffffffu, mb > m_use + kRescaleLog2)) {
+                            // (this block's S follows the last PV of the tile: O is complete)
+                            const float m_new = fmaxf(m_use, mb);
+                            const float alpha = m_new == m_use ? 1.f : dev::fast_exp2(m_use - m_new);
+#pragma unroll
+                            for (int c = 0; c < kDim / 16; ++c) {
+                                uint32_t ov[16];
+                                tc::ld16(tO + 16 * c, ov);
+                                tc::wait_ld();
+#pragma unroll
+                                for (int q = 0; q < 16; ++q)
+                                    ov[q] = __float_as_uint(__uint_as_float(ov[q]) * alpha);
+                                tc::st16(tO + 16 * c, ov);
+                            }
+                            tc::wait_st();
+                            l *= alpha;
+                            m_use = m_new;
+                        }
+                    };
+                    // the pair's last S is done: the Q buffer takes the next
+                    // pair's rows while this block's softmax runs
+                    auto next_q = [&]() {
+                        if (i == nb - 1) {
+                            more = has_pair(k + 1);
+                            if (!ok) return false;
+                            if (!F8 && more && on_in(k + 1)) {
+                                issue_q(k + 1);
+                                loaded_next = true;
+                            }
+                        }
+                        return true;
+                    };
+                    if constexpr (CAP == kCapFree) {
+                        const bool hidden = __any_sync(0xffffffffu, min(seen_in(0), seen_in(1)) < kHalfTokens);
+                        // no reference: P of a half at a time, over scores that are read
+                        // (rolled, for its instructions' fetch)
+                        if (!next_q()) break;
+                        uint32_t xs[64], ps[32];
+                        auto load_half = [&](int h) {
+                            tc::ld32(tS + 64 * h, *reinterpret_cast<uint32_t(*)[32]>(xs));
+                            tc::ld32(tS + 64 * h + 32, *reinterpret_cast<uint32_t(*)[32]>(xs + 32));
+                        };
+#pragma unroll 1
+                        for (int h = 0; h < 2; ++h) {
+                            load_half(h);
+                            tc::wait_ld();
+                            PackedRow<false> row{ps};
+                            cap_free(xs, seen_in(h), hidden, cap_large, cap, row);
+                            float l0, l1;
+                            dev::f32x2_split(row.sum, l0, l1);
+                            l += l0 + l1;
+                            tc::st32(tS + 32 * h, ps);
+                            if (!finish_half(h)) {
+                                ok = false;
+                                break;
+                            }
+                        }
+                        if (!ok) break;
+                        continue;
+                    }
+                    if constexpr (CAP == kCapRef) {
+                        // the range of the scores, then P, a half at a time
+                        float lo = INFINITY, hi = -INFINITY;
+                        uint32_t xs[64];
+                        auto load_half = [&](int h) {
+                            tc::ld32(tS + 64 * h, *reinterpret_cast<uint32_t(*)[32]>(xs));
+                            tc::ld32(tS + 64 * h + 32, *reinterpret_cast<uint32_t(*)[32]>(xs + 32));
+                            tc::wait_ld();
+                        };
+#pragma unroll 1
+                        for (int h = 0; h < 2; ++h) {
+                            load_half(h);
+                            cap_range(xs, seen_in(h), lo, hi);
+                        }
+                        if (!next_q()) break;
+                        const bool hidden = __any_sync(0xffffffffu, min(seen_in(0), seen_in(1)) < kHalfTokens);
+                        const bool large = __any_sync(0xffffffffu, fmaxf(hi, -lo) * cap.to >= kCapSeries);
+                        // (a row that has seen no key has P = 0 against any reference)
+                        raise_reference(hi < lo ? -INFINITY : cap_one(hi, cap));
+                        const float m_ref = m_use == -INFINITY ? 0.f : m_use;
+                        const unsigned long long nmp = dev::f32x2(-m_ref, -m_ref);
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t xc[32], pc[16];
+                            tc::ld32(tS + 32 * c, xc);
+                            tc::wait_ld();
+                            PackedRow<F8> row{pc};
+                            cap_exponentials(xc, seen_in(c >> 1) - 32 * (c & 1), hidden, large, nmp, cap, row);
+                            float l0, l1;
+                            dev::f32x2_split(row.sum, l0, l1);
+                            l += l0 + l1;
+                            tc::st16(tS + 16 * c, pc);
+                            if ((c & 1) && !finish_half(c >> 1)) {
+                                ok = false;
+                                break;
+                            }
+                        }
+                        if (!ok) break;
+                        continue;
+                    }
                     // The scores: bf16 holds all 128 of the row from here to
                     // the exponentials; with e4m3 KV, where the converters take
                     // a third of the registers (and are what the pass waits
@@ -353,17 +495,9 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                         tc::ld32(tS + 64 * h, x0);
                         tc::ld32(tS + 64 * h + 32, x1);
                     };
-                    auto cap_half = [&](uint32_t(&x0)[32], uint32_t(&x1)[32]) {
-                        if constexpr (CAP) {
-                            cap_scores<32, uint32_t>(x0, item_scale, a.cap_log2);
-                            cap_scores<32, uint32_t>(x1, item_scale, a.cap_log2);
-                        }
-                    };
-                    // keys the row does not see (past the last token of a
-                    // half, or past the row's own token): -inf
-                    const int valid[2] = {vv & 0xff, vv >> 8};
+                    // keys the row does not see: -inf
                     auto hide_half = [&](int h, uint32_t(&x0)[32], uint32_t(&x1)[32]) {
-                        const int seen = min(valid[h], t_rel - (i * kBlockTokens + h * kHalfTokens) + 1);
+                        const int seen = seen_in(h);
                         if (seen < kHalfTokens) {
 #pragma unroll
                             for (int q = 0; q < 32; ++q) hide_from(x0[q], q, seen);
@@ -385,12 +519,10 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                     if constexpr (F8) {
                         read_half(0, x[0], x[1]);
                         tc::wait_ld();
-                        cap_half(x[0], x[1]);
                         hide_half(0, x[0], x[1]);
                         mx = max_half(x[0], x[1]);
                         read_half(1, x[0], x[1]);
                         tc::wait_ld();
-                        cap_half(x[0], x[1]);
                         hide_half(1, x[0], x[1]);
                         mx = fmaxf(mx, max_half(x[0], x[1]));
                     } else {
@@ -398,19 +530,8 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                         read_half(1, x[2], x[3]);
                         tc::wait_ld();
                     }
-                    // the pair's last S is done: the Q buffer takes the next
-                    // pair's rows while this block's softmax runs
-                    if (i == nb - 1) {
-                        more = has_pair(k + 1);
-                        if (!ok) break;
-                        if (!F8 && more && on_in(k + 1)) {
-                            issue_q(k + 1);
-                            loaded_next = true;
-                        }
-                    }
+                    if (!next_q()) break;
                     if constexpr (!F8) {
-                        cap_half(x[0], x[1]);
-                        cap_half(x[2], x[3]);
                         hide_half(0, x[0], x[1]);
                         hide_half(1, x[2], x[3]);
                         mx = fmaxf(max_half(x[0], x[1]), max_half(x[2], x[3]));
@@ -439,63 +560,20 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                     uint32_t pw[32];
                     unsigned long long lsum = 0ull;
                     const float mb = mx * sl;
-                    if (i == 0) {
-                        m_use = mb;
-                    } else if (__any_sync(0xffffffffu, mb > m_use + kRescaleLog2)) {
-                        // (this block's S follows the last PV of the tile: O is complete)
-                        const float m_new = fmaxf(m_use, mb);
-                        const float alpha = m_new == m_use ? 1.f : dev::fast_exp2(m_use - m_new);
-#pragma unroll
-                        for (int c = 0; c < kDim / 16; ++c) {
-                            uint32_t ov[16];
-                            tc::ld16(tO + 16 * c, ov);
-                            tc::wait_ld();
-#pragma unroll
-                            for (int q = 0; q < 16; ++q)
-                                ov[q] = __float_as_uint(__uint_as_float(ov[q]) * alpha);
-                            tc::st16(tO + 16 * c, ov);
-                        }
-                        tc::wait_st();
-                        l *= alpha;
-                        m_use = m_new;
-                    }
+                    raise_reference(mb);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         if constexpr (F8) {
                             read_half(h, x[0], x[1]);
                             tc::wait_ld();
-                            cap_half(x[0], x[1]);
                             hide_half(h, x[0], x[1]);
                         }
                         lsum = exponentiate(h, pw, lsum);
                         tc::st32(tS + 32 * h, pw);
-                        // V rows past the half's valid tokens may hold anything
-                        // (NaN included): P is 0 there, but 0 * NaN is NaN, so
-                        // each tile zeroes them before its PV (the same zeros
-                        // twice; the e4m3 converters write them as zeros)
-                        if (!F8 && valid[h] < kHalfTokens) {
-                            const int vs = (pos + 2 * i + 1) % C::kSlots;
-                            if (!tc_warp_wait(bar(kFull + vs), ((pos + 2 * i + 1) / C::kSlots) & 1, limit,
-                                              abort, lane)) {
-                                ok = false;
-                                break;
-                            }
-                            const uint32_t vst = ring + vs * kSlotBytes;
-                            const int n16 = (kHalfTokens - valid[h]) * 2 * 8;
-                            for (int q = r; q < n16; q += kRows) {
-                                const int row = h * kHalfTokens + valid[h] + q / 16, cb = (q / 8) & 1;
-                                const uint32_t at = row / kPageSize * kPagedBytes + cb * (kPagedBytes / 2) +
-                                                    row % kPageSize * 128;
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(
-                                                 vst + at + ((q & 7) << 4)),
-                                             "r"(0u)
-                                             : "memory");
-                            }
-                            tc::fence_proxy_async_smem();
+                        if (!finish_half(h)) {
+                            ok = false;
+                            break;
                         }
-                        tc::wait_st();
-                        tc::fence_before_sync();
-                        warp_arrive(kPFull + 2 * t + h);
                     }
                     if (!ok) break;
                     float l0, l1;
@@ -920,7 +998,7 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
 // Shared memory is configured once per device; the launch needs one CTA per SM.
 constexpr int kMaxConfigDevices = 64;
 
-template <bool F8, bool DIRECT, bool CAP>
+template <bool F8, bool DIRECT, int CAP>
 cudaError_t configure() {
     static std::mutex mu;
     static bool done[kMaxConfigDevices] = {};
@@ -940,7 +1018,7 @@ cudaError_t configure() {
     return cudaSuccess;
 }
 
-template <bool F8, bool DIRECT, bool CAP>
+template <bool F8, bool DIRECT, int CAP>
 cudaError_t launch(const AttnArgs &a, const KvMaps &maps, cudaStream_t stream) {
     const cudaError_t e = configure<F8, DIRECT, CAP>();
     if (e != cudaSuccess) return e;
@@ -948,30 +1026,33 @@ cudaError_t launch(const AttnArgs &a, const KvMaps &maps, cudaStream_t stream) {
                             dim3(Cfg<F8>::kThreads), smem_bytes<F8>(), stream, maps, a);
 }
 
-template <bool F8, bool CAP>
+template <bool F8, int CAP>
 cudaError_t launch_form(const AttnArgs &a, const KvMaps &maps, cudaStream_t stream) {
     return a.out ? launch<F8, true, CAP>(a, maps, stream) : launch<F8, false, CAP>(a, maps, stream);
 }
 
-template <bool F8>
-cudaError_t prepare_cap() {
-    const cudaError_t e = configure<F8, true, true>();
-    return e != cudaSuccess ? e : configure<F8, false, true>();
+template <bool F8, int CAP>
+cudaError_t prepare() {
+    const cudaError_t e = configure<F8, true, CAP>();
+    return e != cudaSuccess ? e : configure<F8, false, CAP>();
 }
 
 }  // namespace
 
 cudaError_t launch_prefill(const AttnArgs &a, const KvMaps &maps, int mode, cudaStream_t stream) {
     if (a.num_items <= 0 || a.num_ctas <= 0) return cudaSuccess;
+    const bool cap = a.cap_log2 > 0.f;
     if (mode == PARASON_FP8_E4M3_KV)
-        return a.cap_log2 > 0.f ? launch_form<true, true>(a, maps, stream)
-                                : launch_form<true, false>(a, maps, stream);
-    return a.cap_log2 > 0.f ? launch_form<false, true>(a, maps, stream)
-                            : launch_form<false, false>(a, maps, stream);
+        return cap ? launch_form<true, kCapRef>(a, maps, stream) : launch_form<true, kCapNone>(a, maps, stream);
+    if (!cap) return launch_form<false, kCapNone>(a, maps, stream);
+    return a.cap_log2 <= kCapFreeLog2 ? launch_form<false, kCapFree>(a, maps, stream)
+                                      : launch_form<false, kCapRef>(a, maps, stream);
 }
 
 cudaError_t prefill_prepare_cap(int mode) {
-    return mode == PARASON_FP8_E4M3_KV ? prepare_cap<true>() : prepare_cap<false>();
+    if (mode == PARASON_FP8_E4M3_KV) return prepare<true, kCapRef>();
+    const cudaError_t e = prepare<false, kCapFree>();
+    return e != cudaSuccess ? e : prepare<false, kCapRef>();
 }
 
 }  // namespace parason
