@@ -457,9 +457,11 @@ typedef struct {
  * its pair of elements (x0, x1) of a head by the angle
  *   a = positions[axis * position_stride + t] * inv_freq[i],
  *   axis = freq_axis ? freq_axis[i] : 0
- * to (x0 cos a - x1 sin a, x0 sin a + x1 cos a).  The product is taken
- * exactly and reduced in 64 bits, so far positions lose nothing.  Elements
- * from rotary_dim on stay as they are. */
+ * to (x0 cos a - x1 sin a, x0 sin a + x1 cos a).  The frequencies are given as
+ * turns a position, inv_freq[i] / (2 pi), modulo 1 in units of 2^-64
+ * (parason_rotary_turns makes them): a position times that is the angle's part
+ * of a turn to 2^-33, at any position, by one integer product.  Elements from
+ * rotary_dim on stay as they are. */
 enum { PARASON_ROTARY_HALVES = 0,       /* pair i is elements i, i + rotary_dim / 2 */
        PARASON_ROTARY_INTERLEAVED = 1 };/* pair i is elements 2 i, 2 i + 1          */
 typedef struct {
@@ -467,10 +469,15 @@ typedef struct {
     int32_t pairs;             /* PARASON_ROTARY_HALVES or _INTERLEAVED             */
     int32_t num_axes;          /* 1..4: e.g. text 1; time, height, width 3          */
     const uint8_t *freq_axis;  /* host [rotary_dim / 2], each < num_axes; NULL: 0   */
-    const float *inv_freq;     /* device [rotary_dim / 2], finite                   */
+    const uint64_t *turns;     /* device [rotary_dim / 2]                           */
     const int32_t *positions;  /* device [num_axes][num_tokens], negative ones too  */
     int64_t position_stride;   /* elements between the axes' rows                   */
 } parason_rotary;
+
+/* turns[i] = inv_freq[i] / (2 pi) modulo 1, in units of 2^-64, rounded to
+ * nearest; n frequencies, host memory.  PARASON_EINVAL for NULL, a negative n,
+ * or a frequency that is not finite or above 2^64 in magnitude. */
+parason_status parason_rotary_turns(const float *inv_freq, int32_t n, uint64_t *turns);
 
 /*
  * Write the keys and values of num_tokens tokens into their slots, and rotate
@@ -478,7 +485,7 @@ typedef struct {
  *   K[slot] = round(rot(k) / k_scale[h]),  V[slot] = round(v / v_scale[h]),
  *   q_out   = round(rot(q))
  * with the scales in PARASON_FP8_E4M3_KV mode only (ignored, may be NULL,
- * otherwise; positive and finite).  Arithmetic is fp32, rounded once (to
+ * otherwise; at least 2^-126, and finite).  Arithmetic is fp32, rounded once (to
  * nearest even); e4m3 saturates at +-448, infinities too, and keeps NaN.
  *
  *   q       rows [num_tokens, H_q, head_dim], or NULL (no queries; q_out unused)
@@ -499,7 +506,7 @@ typedef struct {
  * ones.  PARASON_EINVAL for a bad config, a NULL or misaligned pointer, a
  * negative count, a rotary description outside the above;
  * PARASON_EUNSUPPORTED if num_physical_pages * H_kv * 16 passes int32 (as in
- * parason_attn_plan); PARASON_ECUDA if the launch fails.
+ * parason_attn_plan) or there are more than 16384 heads; PARASON_ECUDA if the launch fails.
  */
 parason_status parason_kv_write(const parason_attn_config *cfg, int64_t num_tokens,
                                 const parason_rows *q, const parason_rows *k,
@@ -536,7 +543,7 @@ parason_status parason_kv_read(const parason_attn_config *cfg, int64_t num_token
  * above 2^63 (infinities too) counts as 2^63.
  *
  * accumulate 0: the scales are set, at least to 2^-126.  accumulate 1: a
- * scale that is larger already stays (they hold positive finite values on
+ * scale that is larger already stays (they are at least 2^-126 and finite on
  * entry), so that the scales of several batches come out the same in any
  * order.  PARASON_FP8_E4M3_KV mode only (PARASON_EINVAL otherwise).  One or
  * two kernels on `stream`; capture and errors as parason_kv_write.

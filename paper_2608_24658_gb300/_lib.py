@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "_build", "libparason.so")
@@ -54,8 +55,15 @@ class Rows(ctypes.Structure):
 class RotaryDesc(ctypes.Structure):
     _fields_ = [("rotary_dim", ctypes.c_int32), ("pairs", ctypes.c_int32),
                 ("num_axes", ctypes.c_int32), ("freq_axis", ctypes.c_void_p),
-                ("inv_freq", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("turns", ctypes.c_void_p), ("positions", ctypes.c_void_p),
                 ("position_stride", ctypes.c_int64)]
+
+
+# the same records as bytes (a step's calls make them anew: packing takes a
+# fraction of a Structure's time)
+ROWS = struct.Struct("@Pqq")
+ROTARY = struct.Struct("@iiiPPPq")
+assert ROWS.size == ctypes.sizeof(Rows) and ROTARY.size == ctypes.sizeof(RotaryDesc)
 
 
 class TraceStats(ctypes.Structure):
@@ -66,9 +74,7 @@ class TraceStats(ctypes.Structure):
                 ("acceleration", ctypes.c_double), ("eta", ctypes.c_double)]
 
 
-_cfg = ctypes.POINTER(AttnConfig)
-_rows = ctypes.POINTER(Rows)
-_rot = ctypes.POINTER(RotaryDesc)
+_cfg = _rows = _rot = _p          # AttnConfig *, Rows *, RotaryDesc *, or their bytes
 
 SIGNATURES = {
     "parason_attn_plan": (ctypes.c_int, [ctypes.POINTER(AttnConfig), _i32, _p, _p, _p, _p, _i32,
@@ -95,6 +101,7 @@ SIGNATURES = {
                                                ctypes.POINTER(ctypes.c_int32),
                                                ctypes.POINTER(ctypes.c_int32)]),
     "parason_lse_merge": (ctypes.c_int, [_p, _p, _p, _p, _p, _p, _i64, _i32, _i32, _p]),
+    "parason_rotary_turns": (ctypes.c_int, [_p, _i32, _p]),
     "parason_kv_write": (ctypes.c_int, [_cfg, _i64, _rows, _rows, _rows, _rot, _p, _p, _p, _p, _p,
                                         _p, _i64, _p]),
     "parason_kv_read": (ctypes.c_int, [_cfg, _i64, _p, _p, _p, _i64, _p, _p, _rows, _rows, _p]),

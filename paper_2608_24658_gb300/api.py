@@ -384,7 +384,8 @@ class Rotary:
     [rotary_dim / 2]) turns the first rotary_dim elements of each head, as pairs
     (i, i + rotary_dim / 2) or, ``interleaved``, (2 i, 2 i + 1).  ``axes`` gives
     each frequency's position axis (0..3; one axis if None): positions are then
-    [number of axes, tokens], e.g. time, height and width of image tokens."""
+    [number of axes, tokens], e.g. time, height and width of image tokens.  The
+    frequencies are read once, here (parason_rotary_turns)."""
 
     def __init__(self, inv_freq: torch.Tensor, axes=None, interleaved: bool = False):
         if (inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_cuda
@@ -394,6 +395,12 @@ class Rotary:
         if half % 8 or not 0 < half <= 64:
             raise ValueError("inv_freq must have a multiple of 8 elements, 64 at most")
         self.inv_freq, self.interleaved = inv_freq, bool(interleaved)
+        self.rotary_dim = 2 * half
+        host = np.ascontiguousarray(inv_freq.cpu().numpy())
+        turns = np.empty(half, dtype=np.uint64)
+        check(_lib.load().parason_rotary_turns(_ptr(host), half, _ptr(turns)), "parason_rotary_turns")
+        self.device = inv_freq.get_device()
+        self._turns = torch.from_numpy(turns.view(np.int64)).to(inv_freq.device)
         self.num_axes, self._axes = 1, None
         if axes is not None:
             a = np.asarray(axes)
@@ -401,76 +408,95 @@ class Rotary:
                 raise ValueError(f"axes must be {half} integers in 0..3")
             self._axes = np.ascontiguousarray(a, dtype=np.uint8)
             self.num_axes = int(self._axes.max()) + 1
+        self._head = (self.rotary_dim, int(self.interleaved), self.num_axes,
+                      0 if self._axes is None else self._axes.ctypes.data, self._turns.data_ptr())
 
-    @property
-    def rotary_dim(self) -> int:
-        return 2 * self.inv_freq.shape[0]
-
-    def _desc(self, positions):
-        d = _lib.RotaryDesc(self.rotary_dim, int(self.interleaved), self.num_axes,
-                            None if self._axes is None else self._axes.ctypes.data,
-                            self.inv_freq.data_ptr(), None, 0)
-        if positions is not None:
-            d.positions = positions.data_ptr()
-            d.position_stride = positions.stride(0) if positions.dim() == 2 else 0
-        return d
+    def _desc(self, positions) -> bytes:
+        if positions is None:
+            return _lib.ROTARY.pack(*self._head, 0, 0)
+        return _lib.ROTARY.pack(*self._head, positions.data_ptr(),
+                                positions.stride(0) if self.num_axes > 1 else 0)
 
 
-def _token_rows(name, t, tokens, heads, dim, dtype, dev, out=False):
+# (small steps wait for this code: tensors are looked at once, devices as
+# numbers; records go to the library as bytes, pointers as integers)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _token_rows(name, t, shape, dtype, dev, out=False) -> bytes:
     """The C view of rows [tokens, heads, dim] with any strides of 16 bytes."""
-    if t.dtype != dtype or t.shape != (tokens, heads, dim) or t.device != dev:
-        raise ValueError(f"{name} must be a {dtype} tensor of shape {(tokens, heads, dim)} on {dev}")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on cuda:{dev}")
     ts, hs, es = t.stride()
-    elem = t.element_size()
-    if tokens == 0:
-        return _lib.Rows(None, 0, 0)
-    if (es != 1 or t.data_ptr() % 16 or (tokens > 1 and ts * elem % 16)
-            or (heads > 1 and hs * elem % 16)):
-        raise ValueError(f"{name} must have contiguous elements and start and strides of 16 bytes")
-    if out and ((tokens > 1 and ts < dim) or (heads > 1 and hs < dim)):
-        raise ValueError(f"{name} must not overlap itself")
-    return _lib.Rows(t.data_ptr(), ts, hs)
+    at = t.data_ptr()
+    if out or es != 1 or at & 15 or (ts | hs) & (3 if dtype is torch.float32 else 7):
+        # (a stride over a dimension of 1 is not used)
+        tokens, heads, dim = shape
+        if tokens == 0:
+            return _lib.ROWS.pack(0, 0, 0)
+        step = 16 // t.element_size()
+        if es != 1 or at % 16 or (ts % step and tokens > 1) or (hs % step and heads > 1):
+            raise ValueError(f"{name} must have contiguous elements and start and strides of 16 bytes")
+        if out and ((ts < dim and tokens > 1) or (hs < dim and heads > 1)):
+            raise ValueError(f"{name} must not overlap itself")
+    return _lib.ROWS.pack(at, ts, hs)
 
 
-def _token_ints(name, t, shape, dev):
-    if t.dtype != torch.int32 or tuple(t.shape) != shape or t.device != dev or (
-            t.numel() > 1 and t.stride(-1) != 1):
-        raise ValueError(f"{name} must be an int32 tensor of shape {shape} on {dev}, contiguous "
+def _token_ints(name, t, shape, dev) -> int:
+    if t.dtype is not torch.int32 or t.shape != shape or t.get_device() != dev or (
+            t.stride(-1) != 1 and t.numel() > 1):
+        raise ValueError(f"{name} must be an int32 tensor of shape {shape} on cuda:{dev}, contiguous "
                          "along the tokens")
-    return t
+    return t.data_ptr()
 
 
-def _pool_config(k_pages, v_pages, num_q_heads):
-    """(mode, config, device) of a pair of pools."""
-    mode = _POOL_MODES.get(k_pages.dtype)
-    if (mode is None or k_pages.dim() != 4 or k_pages.shape[2] != 16 or not k_pages.is_cuda
-            or not k_pages.is_contiguous()):
+_configs = {}
+
+
+def _config(mode, q_heads, kv_heads, dim):
+    """The bytes of a parason_attn_config (one per shape is kept)."""
+    key = (mode, q_heads, kv_heads, dim)
+    cfg = _configs.get(key)
+    if cfg is None:
+        cfg = _configs[key] = bytes(_lib.AttnConfig(q_heads, kv_heads, dim, 16, _lib.MODES[mode], 0.0))
+    return cfg
+
+
+def _pools(k_pages, v_pages):
+    """(mode, device number, pages, kv heads, head_dim) of a pair of pools."""
+    dtype, shape, dev = k_pages.dtype, k_pages.shape, k_pages.get_device()
+    mode = _POOL_MODES.get(dtype)
+    if mode is None or len(shape) != 4 or shape[2] != 16 or dev < 0 or not k_pages.is_contiguous():
         raise ValueError("k_pages must be a contiguous cuda tensor [pages, kv heads, 16, head_dim] "
                          "in bf16, fp32 or float8_e4m3fn")
-    if (v_pages.dtype != k_pages.dtype or v_pages.shape != k_pages.shape
-            or v_pages.device != k_pages.device or not v_pages.is_contiguous()):
+    if (v_pages.dtype is not dtype or v_pages.shape != shape or v_pages.get_device() != dev
+            or not v_pages.is_contiguous()):
         raise ValueError("v_pages must be like k_pages")
-    heads, d = k_pages.shape[1], k_pages.shape[3]
-    _on_current(k_pages.device)
-    return mode, _lib.AttnConfig(num_q_heads or heads, heads, d, 16, _lib.MODES[mode], 0.0), k_pages.device
+    pages, heads, _, d = shape
+    return mode, dev, pages, heads, d
 
 
-def _on_current(dev):
-    if dev.index != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on {dev}, which is not the current device")
+def _stream_on(stream, dev) -> int:
+    """The handle of `stream`; the tensors' device must be the current one."""
+    if dev != _current_device():
+        raise ValueError(f"the tensors are on cuda:{dev}, which is not the current device")
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(dev)
+    return _stream_int(stream)
 
 
-def _head_scales(scales, heads, dev):
-    for s in scales:
-        if (s is None or s.dtype != torch.float32 or tuple(s.shape) != (heads,) or s.device != dev
+def _head_scales(k_scale, v_scale, heads, dev):
+    for s in (k_scale, v_scale):
+        if (s is None or s.dtype is not torch.float32 or s.shape != (heads,) or s.get_device() != dev
                 or not s.is_contiguous()):
             raise ValueError(f"an e4m3 cache needs k_scale and v_scale: contiguous float32 [{heads}] "
-                             f"on {dev}")
-    return tuple(s.data_ptr() for s in scales)
+                             f"on cuda:{dev}")
+    return k_scale.data_ptr(), v_scale.data_ptr()
 
 
 def _new(stream, shape, dtype, dev):
     """A new tensor whose memory belongs to the stream that will write it."""
+    dev = torch.device("cuda", dev)
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=dev)
     if not isinstance(stream, torch.cuda.Stream):
@@ -493,45 +519,54 @@ def kv_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: t
     whose slot is outside the pool (-1, say) is not written.  positions: cuda
     int32 [T], or [axes, T] as ``rotary`` has axes.  ``q_out`` may be ``q``
     itself where that is contiguous."""
-    mode, cfg, dev = _pool_config(k_pages, v_pages, None if q is None else q.shape[1])
-    dtype, heads, d = _Q_DTYPES[mode], cfg.num_kv_heads, cfg.head_dim
-    tokens = k.shape[0]
-    ck = _token_rows("k", k, tokens, heads, d, dtype, dev)
-    cv = _token_rows("v", v, tokens, heads, d, dtype, dev)
-    _token_ints("slots", slots, (tokens,), dev)
+    mode, dev, pages, heads, d = _pools(k_pages, v_pages)
+    dtype = _Q_DTYPES[mode]
+    shape = k.shape
+    if shape[1:] != (heads, d):
+        raise ValueError(f"k must be [T, {heads}, {d}]")
+    tokens = shape[0]
+    ck = _token_rows("k", k, shape, dtype, dev)
+    cv = _token_rows("v", v, shape, dtype, dev)
+    at = _token_ints("slots", slots, (tokens,), dev)
     ks = vs = None
     if mode == "fp8":
-        ks, vs = _head_scales((k_scale, v_scale), heads, dev)
+        ks, vs = _head_scales(k_scale, v_scale, heads, dev)
     rot = None
     if rotary is not None:
         if positions is None:
             raise ValueError("rotary needs positions")
-        if rotary.inv_freq.device != dev or rotary.rotary_dim > d:
-            raise ValueError(f"rotary must be on {dev} and turn at most {d} elements")
-        _token_ints("positions", positions, (tokens,) if positions.dim() == 1 and rotary.num_axes == 1
-                    else (rotary.num_axes, tokens), dev)
-        rot = ctypes.byref(rotary._desc(positions))
+        if rotary.device != dev or rotary.rotary_dim > d:
+            raise ValueError(f"rotary must be on cuda:{dev} and turn at most {d} elements")
+        axes = rotary.num_axes
+        _token_ints("positions", positions, (tokens,) if axes == 1 and positions.dim() == 1
+                    else (axes, tokens), dev)
+        rot = rotary._desc(positions)
     elif positions is not None:
         raise ValueError("positions need a rotary")
-    cq = None
+    cq = qo = None
+    q_heads = heads
     if q is not None:
-        if q.dim() != 3 or q.shape[1] == 0 or q.shape[1] % heads:
+        q_shape = q.shape
+        if len(q_shape) != 3 or q_shape[1] == 0 or q_shape[1] % heads:
             raise ValueError(f"q must be [T, a multiple of {heads} heads, {d}]")
-        cq = ctypes.byref(_token_rows("q", q, tokens, cfg.num_q_heads, d, dtype, dev))
+        q_heads = q_shape[1]
+        cq = _token_rows("q", q, (tokens, q_heads, d), dtype, dev)
         if q_out is None:
-            q_out = _new(stream, q.shape, dtype, dev)
-        elif (q_out.dtype != dtype or q_out.shape != q.shape or q_out.device != dev
-              or not q_out.is_contiguous() or q_out.data_ptr() % 16):
-            raise ValueError(f"q_out must be a contiguous {dtype} tensor of q's shape on {dev}, "
-                             "16-byte aligned")
-        elif q_out.data_ptr() == q.data_ptr() and not q.is_contiguous():
-            raise ValueError("q_out may be q itself only where q is contiguous")
+            q_out = _new(stream, q_shape, dtype, dev)
+            qo = q_out.data_ptr()
+        else:
+            qo = q_out.data_ptr()
+            if (q_out.dtype is not dtype or q_out.shape != q_shape or q_out.get_device() != dev
+                    or not q_out.is_contiguous() or qo & 15):
+                raise ValueError(f"q_out must be a contiguous {dtype} tensor of q's shape on cuda:{dev}, "
+                                 "16-byte aligned")
+            if qo == q.data_ptr() and not q.is_contiguous():
+                raise ValueError("q_out may be q itself only where q is contiguous")
     elif q_out is not None:
         raise ValueError("q_out needs q")
     st = _lib.load().parason_kv_write(
-        ctypes.byref(cfg), tokens, cq, ctypes.byref(ck), ctypes.byref(cv), rot, slots.data_ptr(),
-        ks, vs, None if q is None else q_out.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
-        k_pages.shape[0], _stream_int(stream))
+        _config(mode, q_heads, heads, d), tokens, cq, ck, cv, rot, at, ks, vs, qo,
+        k_pages.data_ptr(), v_pages.data_ptr(), pages, _stream_on(stream, dev))
     if st:
         check(st, "parason_kv_write")
     return q_out
@@ -544,20 +579,23 @@ def kv_read(k_pages: torch.Tensor, v_pages: torch.Tensor, slots: torch.Tensor,
     [T, H_kv, d] in bf16 (fp32 from an fp32 cache), e4m3 times its scale
     (``parason_kv_read``).  A slot outside the pool gives zeros.  Given ``k`` and
     ``v`` may be views with strides of 16 bytes.  Asynchronous."""
-    mode, cfg, dev = _pool_config(k_pages, v_pages, None)
-    dtype, heads, d = _Q_DTYPES[mode], cfg.num_kv_heads, cfg.head_dim
-    tokens = slots.shape[0] if slots.dim() == 1 else -1
-    _token_ints("slots", slots, (tokens,), dev)
+    mode, dev, pages, heads, d = _pools(k_pages, v_pages)
+    dtype = _Q_DTYPES[mode]
+    tokens = slots.shape
+    if len(tokens) != 1:
+        raise ValueError("slots must be [T]")
+    shape = (*tokens, heads, d)
+    at = _token_ints("slots", slots, tokens, dev)
     ks = vs = None
     if mode == "fp8":
-        ks, vs = _head_scales((k_scale, v_scale), heads, dev)
-    k = _new(stream, (tokens, heads, d), dtype, dev) if k is None else k
-    v = _new(stream, (tokens, heads, d), dtype, dev) if v is None else v
-    ck = _token_rows("k", k, tokens, heads, d, dtype, dev, out=True)
-    cv = _token_rows("v", v, tokens, heads, d, dtype, dev, out=True)
+        ks, vs = _head_scales(k_scale, v_scale, heads, dev)
+    k = _new(stream, shape, dtype, dev) if k is None else k
+    v = _new(stream, shape, dtype, dev) if v is None else v
+    ck = _token_rows("k", k, shape, dtype, dev, out=True)
+    cv = _token_rows("v", v, shape, dtype, dev, out=True)
     st = _lib.load().parason_kv_read(
-        ctypes.byref(cfg), tokens, slots.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
-        k_pages.shape[0], ks, vs, ctypes.byref(ck), ctypes.byref(cv), _stream_int(stream))
+        _config(mode, heads, heads, d), shape[0], at, k_pages.data_ptr(), v_pages.data_ptr(),
+        pages, ks, vs, ck, cv, _stream_on(stream, dev))
     if st:
         check(st, "parason_kv_read")
     return k, v
@@ -571,30 +609,26 @@ def kv_scales(k: torch.Tensor, v: torch.Tensor, rotary: Optional[Rotary] = None,
     (``parason_kv_scales``).  Tokens with a negative slot do not count.  With
     ``accumulate``, given scales are raised where the tokens need it.
     Asynchronous."""
-    if k.dim() != 3 or not k.is_cuda:
+    shape, dev = k.shape, k.get_device()
+    if len(shape) != 3 or dev < 0:
         raise ValueError("k must be a cuda tensor [T, kv heads, 128]")
-    tokens, heads, d = k.shape
-    dev = k.device
-    _on_current(dev)
-    ck = _token_rows("k", k, tokens, heads, d, torch.bfloat16, dev)
-    cv = _token_rows("v", v, tokens, heads, d, torch.bfloat16, dev)
-    if slots is not None:
-        _token_ints("slots", slots, (tokens,), dev)
+    tokens, heads, d = shape
+    ck = _token_rows("k", k, shape, torch.bfloat16, dev)
+    cv = _token_rows("v", v, shape, torch.bfloat16, dev)
+    at = None if slots is None else _token_ints("slots", slots, (tokens,), dev)
     if accumulate and (k_scale is None or v_scale is None):
         raise ValueError("accumulate needs the scales to raise")
     k_scale = _new(stream, (heads,), torch.float32, dev) if k_scale is None else k_scale
     v_scale = _new(stream, (heads,), torch.float32, dev) if v_scale is None else v_scale
-    ks, vs = _head_scales((k_scale, v_scale), heads, dev)
+    ks, vs = _head_scales(k_scale, v_scale, heads, dev)
     rot = None
     if rotary is not None:
         if rotary.rotary_dim > d:
             raise ValueError(f"rotary must turn at most {d} elements")
-        rot = ctypes.byref(rotary._desc(None))
-    cfg = _lib.AttnConfig(heads, heads, d, 16, _lib.MODES["fp8"], 0.0)
+        rot = rotary._desc(None)
     st = _lib.load().parason_kv_scales(
-        ctypes.byref(cfg), tokens, ctypes.byref(ck), ctypes.byref(cv), rot,
-        None if slots is None else slots.data_ptr(), int(bool(accumulate)), ks, vs,
-        _stream_int(stream))
+        _config("fp8", heads, heads, d), tokens, ck, cv, rot, at, int(bool(accumulate)), ks, vs,
+        _stream_on(stream, dev))
     if st:
         check(st, "parason_kv_scales")
     return k_scale, v_scale

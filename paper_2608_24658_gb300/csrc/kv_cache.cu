@@ -18,6 +18,7 @@ namespace {
 constexpr int kMaxFreqs = 64;            // rotary_dim / 2 at head_dim 128
 constexpr int kMaxAxes = 4;
 constexpr float kE4m3Max = 448.f;
+constexpr int kMaxHeads = 16384;         // of q, and of k: what the kernels' counters hold
 
 struct Rows {
     const void *data;
@@ -25,14 +26,14 @@ struct Rows {
 };
 
 // A rotary description by value: the axis of each frequency travels in the
-// kernel's parameters.
+// kernel's parameters, as 2 bits (an array there would be read lane by lane).
 struct RotaryArgs {
-    const float *inv_freq;
+    const uint64_t *turns;
     const int32_t *positions;
     int64_t position_stride;
     int32_t half;                        // pairs of a head; 0: nothing turns
     int32_t interleaved;
-    uint8_t axis[kMaxFreqs];
+    uint64_t axes[2];                    // of frequencies 0..31 and 32..63
 };
 
 struct WriteArgs {
@@ -44,6 +45,7 @@ struct WriteArgs {
     int64_t num_tokens;
     int64_t num_slots;                   // of the pool
     int32_t num_q_heads, num_kv_heads;   // num_q_heads 0: no queries
+    int32_t parts;                       // warps that share a token
 };
 
 struct ReadArgs {
@@ -52,7 +54,7 @@ struct ReadArgs {
     const float *k_scale, *v_scale;
     Rows k, v;
     int64_t num_tokens, num_slots;
-    int32_t num_kv_heads;
+    int32_t num_kv_heads, parts;
 };
 
 struct ScalesArgs {
@@ -64,35 +66,50 @@ struct ScalesArgs {
 };
 
 // Eight consecutive elements, the unit every kernel here moves: 16 bytes of
-// bf16, 32 of fp32, 8 of e4m3.
-__device__ __forceinline__ void load8(const __nv_bfloat16 *p, float (&x)[8]) {
-    const uint4 u = *reinterpret_cast<const uint4 *>(p);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+// bf16, 32 of fp32, 8 of e4m3; loaded as they are, unpacked when they are used.
+template <class T>
+struct Raw8 {
+    uint32_t w[2 * sizeof(T)];
+};
+
+template <class T>
+__device__ __forceinline__ Raw8<T> load8(const T *p) {
+    Raw8<T> r;
+    if constexpr (sizeof(T) == 1) {
+        const uint2 u = __ldcs(reinterpret_cast<const uint2 *>(p));
+        r.w[0] = u.x;
+        r.w[1] = u.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) {
+            const uint4 u = __ldcs(reinterpret_cast<const uint4 *>(p) + i);
+            r.w[4 * i] = u.x;
+            r.w[4 * i + 1] = u.y;
+            r.w[4 * i + 2] = u.z;
+            r.w[4 * i + 3] = u.w;
+        }
+    }
+    return r;
+}
+
+__device__ __forceinline__ void unpack8(const Raw8<__nv_bfloat16> &r, float (&x)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(w[i] << 16);
-        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        x[2 * i] = __uint_as_float(r.w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(r.w[i] & 0xffff0000u);
     }
 }
 
-__device__ __forceinline__ void load8(const float *p, float (&x)[8]) {
+__device__ __forceinline__ void unpack8(const Raw8<float> &r, float (&x)[8]) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const float4 u = reinterpret_cast<const float4 *>(p)[i];
-        x[4 * i] = u.x;
-        x[4 * i + 1] = u.y;
-        x[4 * i + 2] = u.z;
-        x[4 * i + 3] = u.w;
-    }
+    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(r.w[i]);
 }
 
-__device__ __forceinline__ void load8(const __nv_fp8_e4m3 *p, float (&x)[8]) {
-    const uint2 u = *reinterpret_cast<const uint2 *>(p);
-    const uint32_t w[2] = {u.x, u.y};
+__device__ __forceinline__ void unpack8(const Raw8<__nv_fp8_e4m3> &r, float (&x)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         uint32_t h;
-        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(w[i >> 1] >> (16 * (i & 1)))));
+        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(r.w[i >> 1] >> (16 * (i & 1)))));
         const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
         x[2 * i] = f.x;
         x[2 * i + 1] = f.y;
@@ -124,135 +141,202 @@ __device__ __forceinline__ void store8(__nv_fp8_e4m3 *p, const float (&x)[8]) {
 template <class KV>
 constexpr bool kScaled = sizeof(KV) == 1;
 
-// cos and sin of positions[axis] * inv_freq[i].  A turn's fraction is what
-// counts, so the angle is taken in turns: the product (exact: 31 and 24 bits)
-// times 1 / 2 pi in 64 bits is off by less than 2^-52 of its size, a
-// millionth of a turn at position 2^31 and below fp32's own rounding of the
-// fraction up to position 2^24.
+constexpr int kThreads = 128;            // 4 warps, each of them on its own
+constexpr int kWarps = kThreads / 32;
+
+// Warps that fill the card with a few loads each in flight (152 SMs): work that
+// makes fewer is cut up further.
+constexpr int kFullWarps = 152 * 16;
+
+// cos and sin of positions[axis] * inv_freq[i].  The frequency is held as turns a
+// position modulo 1, in 2^-64: the low 64 bits of its product with the position are
+// the angle's part of a turn (off by 2^-33 at most, at position 2^31), whose upper 32
+// as a signed number are it within half a turn.  (In 64-bit floating point the same
+// took 7 instructions of a pipe that does 2 lanes a cycle: 6 us of a 30 us prompt.)
 __device__ __forceinline__ float2 turn(const RotaryArgs &r, int64_t t, int i) {
-    constexpr double kTurnsPerRadian = 0.15915494309189533577;
-    const double f = static_cast<double>(r.inv_freq[i]) * kTurnsPerRadian;
-    const double turns = static_cast<double>(r.positions[r.axis[i] * r.position_stride + t]) * f;
+    const int axis = static_cast<int>((i < 32 ? r.axes[0] : r.axes[1]) >> (2 * (i & 31))) & 3;
+    const int64_t pos = r.positions[axis * r.position_stride + t];
+    const uint64_t part = static_cast<uint64_t>(pos) * r.turns[i];
     float s, c;
-    sincospif(2.f * static_cast<float>(turns - rint(turns)), &s, &c);
+    sincospif(static_cast<float>(static_cast<int32_t>(part >> 32)) * 0x1p-31f, &s, &c);
     return make_float2(c, s);
 }
 
-constexpr int kThreads = 128;
-
-// One CTA per token: the token's angles into shared memory, then its heads in
-// units of two 8-element chunks that hold whole pairs.
-template <class T, class KV, int D>
-__global__ void __launch_bounds__(kThreads) kv_write_kernel(const WriteArgs a) {
-    __shared__ float2 cs[kMaxFreqs];
-    constexpr int kUnits = D / 16;
-    const int64_t t = blockIdx.x;
-    dev::grid_wait();
-    if (static_cast<int>(threadIdx.x) < a.rot.half) cs[threadIdx.x] = turn(a.rot, t, threadIdx.x);
-    const int64_t slot = a.slots[t];
-    const bool live = slot >= 0 && slot < a.num_slots;
-    __syncthreads();
-    const int heads = a.num_q_heads + 2 * a.num_kv_heads;
-    for (int w = threadIdx.x; w < heads * kUnits; w += kThreads) {
-        const int u = w % kUnits;
-        int h = w / kUnits;
-        const Rows *src;
-        void *pool = nullptr;
-        const float *scale = nullptr;
-        bool turned = true;
-        if (h < a.num_q_heads) {
-            src = &a.q;
-        } else if ((h -= a.num_q_heads) < a.num_kv_heads) {
-            src = &a.k;
-            pool = a.k_pages;
-            scale = a.k_scale;
-        } else {
-            h -= a.num_kv_heads;
-            src = &a.v;
-            pool = a.v_pages;
-            scale = a.v_scale;
-            turned = false;
-        }
-        if (pool && !live) continue;
-        // chunks c0 and c1: where pairs are halves of the rotated part, chunk u
-        // and its partner; else neighbours
-        const bool rotates = turned && 8 * u < a.rot.half;
-        int e0 = 16 * u, e1 = e0 + 8, f0 = 8 * u;
-        if (turned && !a.rot.interleaved && rotates) {
-            e0 = 8 * u;
-            e1 = e0 + a.rot.half;
-        }
-        const T *x = static_cast<const T *>(src->data) + t * src->token_stride + h * src->head_stride;
-        float x0[8], x1[8];
-        load8(x + e0, x0);
-        load8(x + e1, x1);
-        if (rotates) {
-            if (a.rot.interleaved) {
+// Heads of one kind (q, k or v) of a token, steps [s0, s1) of kHeads heads each: this
+// lane's two chunks of each are at src + e and dst + e, e0 and e1 (elements), a step
+// further `src_step` and `dst_step`.  The loads of kBatch steps go together.
+template <class T, class Out, int D, bool ROTATE, int kBatch>
+__device__ __forceinline__ void write_heads(const T *src, int64_t src_step, Out *dst, int64_t dst_step, int s0, int s1,
+                                            int heads, int mine, int e0, int e1, bool interleaved, bool rotates,
+                                            const unsigned long long (&cs)[4], const unsigned long long (&sn)[4],
+                                            const float *scale) {
+    constexpr int kHeads = 32 / (D / 16);
+    src += s0 * src_step;
+    dst += s0 * dst_step;
+    for (int s = s0; s < s1; s += kBatch, src += kBatch * src_step, dst += kBatch * dst_step) {
+        Raw8<T> r0[kBatch], r1[kBatch];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    float(&y)[8] = i < 4 ? x0 : x1;
-                    const float2 c = cs[f0 + i];
-                    const float p = y[2 * (i & 3)], q = y[2 * (i & 3) + 1];
-                    y[2 * (i & 3)] = p * c.x - q * c.y;
-                    y[2 * (i & 3) + 1] = p * c.y + q * c.x;
-                }
-            } else {
+        for (int b = 0; b < kBatch; ++b) {
+            if (s + b >= s1 || (s + b) * kHeads + mine >= heads) break;
+            r0[b] = load8(src + b * src_step + e0);
+            r1[b] = load8(src + b * src_step + e1);
+        }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float2 c = cs[f0 + i];
-                    const float p = x0[i], q = x1[i];
-                    x0[i] = p * c.x - q * c.y;
-                    x1[i] = p * c.y + q * c.x;
+        for (int b = 0; b < kBatch; ++b) {
+            const int h = (s + b) * kHeads + mine;
+            if (s + b >= s1 || h >= heads) break;
+            float x0[8], x1[8];
+            unpack8(r0[b], x0);
+            unpack8(r1[b], x1);
+            if (ROTATE && rotates) {
+                // (p c - q s, p s + q c), two pairs an instruction
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float &p0 = interleaved ? (i < 2 ? x0 : x1)[4 * (i & 1)] : x0[2 * i];
+                    float &p1 = interleaved ? (i < 2 ? x0 : x1)[4 * (i & 1) + 2] : x0[2 * i + 1];
+                    float &q0 = interleaved ? (i < 2 ? x0 : x1)[4 * (i & 1) + 1] : x1[2 * i];
+                    float &q1 = interleaved ? (i < 2 ? x0 : x1)[4 * (i & 1) + 3] : x1[2 * i + 1];
+                    const unsigned long long p = dev::f32x2(p0, p1), q = dev::f32x2(q0, q1);
+                    const unsigned long long nq = dev::f32x2(-q0, -q1);
+                    dev::f32x2_split(dev::fma_f32x2(p, cs[i], dev::mul_f32x2(nq, sn[i])), p0, p1);
+                    dev::f32x2_split(dev::fma_f32x2(p, sn[i], dev::mul_f32x2(q, cs[i])), q0, q1);
                 }
             }
-        }
-        if (!pool) {
-            T *dst = static_cast<T *>(a.q_out) + (t * a.num_q_heads + h) * D;
-            store8(dst + e0, x0);
-            store8(dst + e1, x1);
-        } else {
-            if constexpr (kScaled<KV>) {
-                const float s = scale[h];
+            if constexpr (sizeof(Out) == 1) {
+                // (times the reciprocal: within two fp32 roundings of the quotient)
+                const float inv = 1.f / scale[h];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    x0[i] /= s;
-                    x1[i] /= s;
+                    x0[i] *= inv;
+                    x1[i] *= inv;
                 }
             }
-            KV *dst = static_cast<KV *>(pool) +
-                      ((slot / kPageSize * a.num_kv_heads + h) * kPageSize + slot % kPageSize) * D;
-            store8(dst + e0, x0);
-            store8(dst + e1, x1);
+            store8(dst + b * dst_step + e0, x0);
+            store8(dst + b * dst_step + e1, x1);
         }
     }
 }
 
-// One CTA per token.
+// A token's heads are taken in steps of kHeads, first q's, then k's, then v's; a warp
+// takes one token, or one of `parts` equal parts of its steps.
+//
+// A head is D / 16 lanes, each with two 8-element chunks that hold whole pairs: chunk
+// u of the first half of the rotated part and its partner, or two neighbours.  So no
+// element crosses a lane, rotation is in place for q, and a warp's loads and stores
+// are whole sectors.  The warp makes the angles once for all its heads: the lanes of
+// one u share 8 pairs' angles, make 8 / kHeads each and pass them round (out of shared
+// memory they were read four lanes to a bank).
+template <class T, class KV, int D, bool INTERLEAVED>
+__global__ void __launch_bounds__(kThreads) kv_write_kernel(const WriteArgs a) {
+    constexpr int kLanes = D / 16, kHeads = 32 / kLanes, kMake = 8 / kHeads;
+    constexpr int kBatch = sizeof(T) == 4 ? 2 : 3;            // (1, 2, 4 in bf16: 36, 35, 35 us for 34)
+    const int lane = threadIdx.x % 32;
+    const int64_t job = static_cast<int64_t>(blockIdx.x) * kWarps + threadIdx.x / 32;
+    const int64_t t = a.parts == 1 ? job : job / a.parts;
+    if (t >= a.num_tokens) return;
+    const int part = static_cast<int>(job - t * a.parts);
+    const int q_steps = (a.num_q_heads + kHeads - 1) / kHeads, kv_steps = (a.num_kv_heads + kHeads - 1) / kHeads;
+    const int steps = q_steps + 2 * kv_steps;                 // (2^14 at most)
+    const int first = steps * part / a.parts, last = steps * (part + 1) / a.parts;
+    const int u = lane % kLanes, mine = lane / kLanes;
+    const bool rotates = 8 * u < a.rot.half, halves = rotates && !INTERLEAVED;
+    // the elements of this lane's chunks in q and k; in v: 16 u and 16 u + 8
+    const int e0 = halves ? 8 * u : 16 * u, e1 = e0 + (halves ? a.rot.half : 8);
+    dev::grid_wait();
+    const int64_t slot = a.slots[t];
+
+    unsigned long long cs[4], sn[4];
+    if (a.rot.half && first < q_steps + kv_steps) {
+        float2 own[kMake];
+#pragma unroll
+        for (int i = 0; i < kMake; ++i)
+            own[i] = rotates ? turn(a.rot, t, 8 * u + kMake * mine + i) : make_float2(1.f, 0.f);
+        float c[8], s[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            c[i] = __shfl_sync(0xffffffffu, own[i % kMake].x, i / kMake * kLanes + u);
+            s[i] = __shfl_sync(0xffffffffu, own[i % kMake].y, i / kMake * kLanes + u);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            cs[i] = dev::f32x2(c[2 * i], c[2 * i + 1]);
+            sn[i] = dev::f32x2(s[2 * i], s[2 * i + 1]);
+        }
+    }
+    if (first < q_steps)
+        write_heads<T, T, D, true, kBatch>(
+            static_cast<const T *>(a.q.data) + t * a.q.token_stride + mine * a.q.head_stride,
+            kHeads * a.q.head_stride, static_cast<T *>(a.q_out) + (t * a.num_q_heads + mine) * D, kHeads * D, first,
+            min(last, q_steps), a.num_q_heads, mine, e0, e1, INTERLEAVED, rotates, cs, sn, nullptr);
+    if (slot < 0 || slot >= a.num_slots || last <= q_steps) return;
+    const int64_t row = (slot / kPageSize * a.num_kv_heads + mine) * kPageSize * D + slot % kPageSize * D;
+    const int k0 = max(first, q_steps) - q_steps, k1 = min(last - q_steps, kv_steps);
+    if (k0 < k1)
+        write_heads<T, KV, D, true, kBatch>(
+            static_cast<const T *>(a.k.data) + t * a.k.token_stride + mine * a.k.head_stride,
+            kHeads * a.k.head_stride, static_cast<KV *>(a.k_pages) + row, kHeads * kPageSize * D, k0, k1,
+            a.num_kv_heads, mine, e0, e1, INTERLEAVED, rotates, cs, sn, a.k_scale);
+    const int v0 = max(first - q_steps - kv_steps, 0), v1 = last - q_steps - kv_steps;
+    if (v0 < v1)
+        write_heads<T, KV, D, false, kBatch>(
+            static_cast<const T *>(a.v.data) + t * a.v.token_stride + mine * a.v.head_stride,
+            kHeads * a.v.head_stride, static_cast<KV *>(a.v_pages) + row, kHeads * kPageSize * D, v0, v1,
+            a.num_kv_heads, mine, 16 * u, 16 * u + 8, INTERLEAVED, false, cs, sn, a.v_scale);
+}
+
+// A warp takes one token, or one of `parts` equal parts of its steps, k's and then
+// v's: a lane 8 elements of a head, kBatch steps' loads in flight.  12 CTAs an SM hide
+// the chain from slot to rows to stores (38.8k e4m3 tokens: 39.6 us; 8 steps in flight
+// in 8 CTAs 40.8, 2 steps 43.6).
+
 template <class T, class KV, int D>
-__global__ void __launch_bounds__(kThreads) kv_read_kernel(const ReadArgs a) {
-    constexpr int kUnits = D / 8;
-    const int64_t t = blockIdx.x;
+__global__ void __launch_bounds__(kThreads, 12) kv_read_kernel(const ReadArgs a) {
+    constexpr int kLanes = D / 8, kHeads = 32 / kLanes, kBatch = sizeof(T) == 4 ? 2 : 4;
+    const int lane = threadIdx.x % 32;
+    const int64_t job = static_cast<int64_t>(blockIdx.x) * kWarps + threadIdx.x / 32;
+    const int64_t t = a.parts == 1 ? job : job / a.parts;
+    if (t >= a.num_tokens) return;
+    const int part = static_cast<int>(job - t * a.parts);
+    const int kv_steps = (a.num_kv_heads + kHeads - 1) / kHeads, steps = 2 * kv_steps;
+    const int first = steps * part / a.parts, last = steps * (part + 1) / a.parts;
+    const int u = lane % kLanes, mine = lane / kLanes;
     dev::grid_wait();
     const int64_t slot = a.slots[t];
     const bool live = slot >= 0 && slot < a.num_slots;
-    for (int w = threadIdx.x; w < 2 * a.num_kv_heads * kUnits; w += kThreads) {
-        const int u = w % kUnits;
-        int h = w / kUnits;
-        const bool is_k = h < a.num_kv_heads;
-        if (!is_k) h -= a.num_kv_heads;
-        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (live) {
-            load8(static_cast<const KV *>(is_k ? a.k_pages : a.v_pages) +
-                      ((slot / kPageSize * a.num_kv_heads + h) * kPageSize + slot % kPageSize) * D + 8 * u,
-                  x);
-            if constexpr (kScaled<KV>) {
-                const float s = (is_k ? a.k_scale : a.v_scale)[h];
+    const int64_t row = (slot / kPageSize * a.num_kv_heads * kPageSize + slot % kPageSize) * D + 8 * u;
+    for (int s0 = first; s0 < last; s0 += kBatch) {
+        Raw8<KV> r[kBatch];
+        float scale[kBatch];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] *= s;
+        for (int b = 0; b < kBatch; ++b) {
+            const int s = s0 + b;
+            const bool is_k = s < kv_steps;
+            const int h = (is_k ? s : s - kv_steps) * kHeads + mine;
+            if (s < last && h < a.num_kv_heads && live) {
+                r[b] = load8(static_cast<const KV *>(is_k ? a.k_pages : a.v_pages) + row +
+                             static_cast<int64_t>(h) * kPageSize * D);
+                if constexpr (kScaled<KV>) scale[b] = (is_k ? a.k_scale : a.v_scale)[h];
             }
         }
-        const Rows &dst = is_k ? a.k : a.v;
-        store8(static_cast<T *>(const_cast<void *>(dst.data)) + t * dst.token_stride + h * dst.head_stride + 8 * u, x);
+#pragma unroll
+        for (int b = 0; b < kBatch; ++b) {
+            const int s = s0 + b;
+            const bool is_k = s < kv_steps;
+            const int h = (is_k ? s : s - kv_steps) * kHeads + mine;
+            if (s >= last || h >= a.num_kv_heads) continue;
+            float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (live) {
+                unpack8(r[b], x);
+                if constexpr (kScaled<KV>) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] *= scale[b];
+                }
+            }
+            T *dst = static_cast<T *>(const_cast<void *>(is_k ? a.k.data : a.v.data)) +
+                     t * (is_k ? a.k.token_stride : a.v.token_stride) +
+                     h * (is_k ? a.k.head_stride : a.v.head_stride) + 8 * u;
+            store8(dst, x);
+        }
     }
 }
 
@@ -263,74 +347,127 @@ __global__ void reset_scales_kernel(float *k_scale, float *v_scale, int n) {
 }
 
 // min(|x|, 2^63), 0 for NaN: squares of these add up within fp32.
-__device__ __forceinline__ float magnitude(float x) {
-    return fmaxf(fminf(fabsf(x), 9.2233720369e18f), 0.f) * (x == x ? 1.f : 0.f);
+__device__ __forceinline__ float magnitude(float x) { return x == x ? fminf(fabsf(x), 9.2233720369e18f) : 0.f; }
+
+// The larger magnitudes of two bf16 pairs (signs are not kept apart; NaN loses).
+__device__ __forceinline__ uint32_t most_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t m;
+    asm("max.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+    return m;
 }
 
-// One CTA per (256 tokens, head, K or V).  Positive floats order as their
-// bits do, so the maxima meet in integer atomics, whose order does not matter;
-// max / 448 is the max of the quotients, since rounding is monotone.
+// A warp takes kScaleRows tokens of one head of K or of V, all their loads in flight, a
+// lane 16 elements of a token as kv_write takes them (more tokens a warp: 1024 tokens of
+// 2 heads 3.3 us with 32, 5.0 with 64, for 2.6).  max |x| goes in bf16 pairs, two elements an
+// instruction; squares of pairs in packed fp32.  Squares past 2^127 (elements from
+// 2^63 on, infinities) send the warp over its tokens once more with magnitudes cut
+// at 2^63; a NaN's partner counts in max |x|, which squares below 2^-126 leave to it
+// too.  Positive floats order as their bits do, so the maxima meet in integer
+// atomics, whose order does not matter; max / 448 is the max of the quotients, since
+// rounding is monotone.
+constexpr int kScaleRows = 16;
 template <int D>
-__global__ void __launch_bounds__(kThreads) kv_scales_kernel(const ScalesArgs a) {
-    constexpr int kUnits = D / 16, kTokens = 256;
-    __shared__ float part[kThreads / 32];
+__global__ void __launch_bounds__(kThreads, 8) kv_scales_kernel(const ScalesArgs a) {
+    constexpr int kLanes = D / 16, kRows = 32 / kLanes, kBatch = kScaleRows / kRows;
+    __shared__ float part[kWarps];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int h = blockIdx.y;
     const bool is_k = blockIdx.z == 0;
     const Rows &src = is_k ? a.k : a.v;
     const int half = is_k ? a.half : 0;
-    const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTokens;
+    const int u = lane % kLanes;
+    const bool rotates = 8 * u < half, halves = rotates && !a.interleaved;
+    const int e0 = halves ? 8 * u : 16 * u, e1 = e0 + (halves ? half : 8);
+    const int64_t t0 = (static_cast<int64_t>(blockIdx.x) * kWarps + warp) * kScaleRows + lane / kLanes;
+    const __nv_bfloat16 *x = static_cast<const __nv_bfloat16 *>(src.data) + h * src.head_stride;
     dev::grid_wait();
-    float one = 0.f, pair = 0.f;         // max |x|, max of x0^2 + x1^2
-    for (int w = threadIdx.x; w < kTokens * kUnits; w += kThreads) {
-        const int64_t t = t0 + w / kUnits;
-        const int u = w % kUnits;
-        if (t >= a.num_tokens || (a.slots && a.slots[t] < 0)) continue;
-        const bool rotates = 8 * u < half;
-        int e0 = 16 * u, e1 = e0 + 8;
-        if (rotates && !a.interleaved) {
-            e0 = 8 * u;
-            e1 = e0 + half;
-        }
-        const __nv_bfloat16 *x = static_cast<const __nv_bfloat16 *>(src.data) + t * src.token_stride +
-                                 h * src.head_stride;
-        float x0[8], x1[8];
-        load8(x + e0, x0);
-        load8(x + e1, x1);
+    uint32_t one = 0;                    // max |x| of even and of odd elements
+    float pair = 0.f;                    // max of x0^2 + x1^2
+    Raw8<__nv_bfloat16> r0[kBatch], r1[kBatch];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            x0[i] = magnitude(x0[i]);
-            x1[i] = magnitude(x1[i]);
-            one = fmaxf(one, fmaxf(x0[i], x1[i]));
+    for (int b = 0; b < kBatch; ++b) {
+        const int64_t t = t0 + b * kRows;
+        if (t < a.num_tokens && (!a.slots || a.slots[t] >= 0)) {
+            r0[b] = load8(x + t * src.token_stride + e0);
+            r1[b] = load8(x + t * src.token_stride + e1);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r0[b].w[i] = r1[b].w[i] = 0;
         }
-        if (rotates) {
+    }
+#pragma unroll
+    for (int b = 0; b < kBatch; ++b) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t p = r0[b].w[i], q = r1[b].w[i];
+            one = most_bf16x2(one, most_bf16x2(p, q));
+            if (rotates) {
+                // halves: elements i of both chunks; neighbours: within a word
+                const float p0 = __uint_as_float(p << 16), p1 = __uint_as_float(p & 0xffff0000u);
+                const float q0 = __uint_as_float(q << 16), q1 = __uint_as_float(q & 0xffff0000u);
+                const unsigned long long v = halves ? dev::f32x2(p0, p1) : dev::f32x2(p0, q0);
+                const unsigned long long w = halves ? dev::f32x2(q0, q1) : dev::f32x2(p1, q1);
+                float s0, s1;
+                dev::f32x2_split(dev::fma_f32x2(v, v, dev::mul_f32x2(w, w)), s0, s1);
+                pair = dev::max3(pair, s0, s1);
+            }
+        }
+    }
+    float m = fmaxf(magnitude(__uint_as_float(one << 16)), magnitude(__uint_as_float(one & 0xffff0000u)));
+    if (__any_sync(0xffffffffu, pair > 8.5e37f)) {                     // 2^126 and up
+        pair = 0.f;
+        for (int r = 0; rotates && r < kScaleRows; r += kRows) {
+            const int64_t t = t0 + r;
+            if (t >= a.num_tokens || (a.slots && a.slots[t] < 0)) continue;
+            float x0[8], x1[8];
+            unpack8(load8(x + t * src.token_stride + e0), x0);
+            unpack8(load8(x + t * src.token_stride + e1), x1);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float p = a.interleaved ? (i < 4 ? x0 : x1)[2 * (i & 3)] : x0[i];
-                const float q = a.interleaved ? (i < 4 ? x0 : x1)[2 * (i & 3) + 1] : x1[i];
+                const float p = magnitude(halves ? x0[i] : (i < 4 ? x0 : x1)[2 * (i & 3)]);
+                const float q = magnitude(halves ? x1[i] : (i < 4 ? x0 : x1)[2 * (i & 3) + 1]);
                 pair = fmaxf(pair, p * p + q * q);
             }
         }
     }
-    float m = fmaxf(one, sqrtf(pair));
+    m = fmaxf(m, sqrtf(pair));
 #pragma unroll
     for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = m;
+    if (lane == 0) part[warp] = m;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int i = 1; i < kThreads / 32; ++i) m = fmaxf(m, part[i]);
+        for (int i = 1; i < kWarps; ++i) m = fmaxf(m, part[i]);
         atomicMax(reinterpret_cast<int *>((is_k ? a.k_scale : a.v_scale) + h), __float_as_int(m / kE4m3Max));
     }
 }
 
-template <class T, class KV, int D>
-cudaError_t launch_write(const WriteArgs &a, cudaStream_t s) {
-    return launch_dependent(true, kv_write_kernel<T, KV, D>, dim3(static_cast<unsigned>(a.num_tokens)),
-                            dim3(kThreads), 0, s, a);
+// Parts of a token: one, or as many as it takes to fill the card, of one step at
+// least (16 tokens of a decode step: 1.8 us in parts, 4.5 whole; a prompt whole, whose
+// parts would make the same angles several times).
+int parts_of(int64_t tokens, int steps) {
+    const int64_t want = (kFullWarps + tokens - 1) / tokens;
+    return static_cast<int>(want < steps ? want : steps);
+}
+
+unsigned blocks_of(int64_t tokens, int parts) {
+    return static_cast<unsigned>((tokens * parts + kWarps - 1) / kWarps);
 }
 
 template <class T, class KV, int D>
-cudaError_t launch_read(const ReadArgs &a, cudaStream_t s) {
-    return launch_dependent(true, kv_read_kernel<T, KV, D>, dim3(static_cast<unsigned>(a.num_tokens)),
+cudaError_t launch_write(WriteArgs a, cudaStream_t s) {
+    constexpr int kHeads = 32 / (D / 16);
+    const int steps = (a.num_q_heads + kHeads - 1) / kHeads + 2 * ((a.num_kv_heads + kHeads - 1) / kHeads);
+    a.parts = parts_of(a.num_tokens, steps);
+    return launch_dependent(true,
+                            a.rot.interleaved ? kv_write_kernel<T, KV, D, true> : kv_write_kernel<T, KV, D, false>,
+                            dim3(blocks_of(a.num_tokens, a.parts)), dim3(kThreads), 0, s, a);
+}
+
+template <class T, class KV, int D>
+cudaError_t launch_read(ReadArgs a, cudaStream_t s) {
+    constexpr int kHeads = 32 / (D / 8);
+    a.parts = parts_of(a.num_tokens, 2 * ((a.num_kv_heads + kHeads - 1) / kHeads));
+    return launch_dependent(true, kv_read_kernel<T, KV, D>, dim3(blocks_of(a.num_tokens, a.parts)),
                             dim3(kThreads), 0, s, a);
 }
 
@@ -355,6 +492,7 @@ parason_status check_call(const parason_attn_config *cfg, int64_t tokens, int64_
     const parason_status st = check_config(cfg);
     if (st != PARASON_OK) return st;
     if (tokens < 0 || tokens > INT32_MAX || pages < 0) return PARASON_EINVAL;
+    if (cfg->num_q_heads > kMaxHeads || cfg->num_kv_heads > kMaxHeads) return PARASON_EUNSUPPORTED;
     if (pages > INT32_MAX / kPageSize / cfg->num_kv_heads) return PARASON_EUNSUPPORTED;
     return PARASON_OK;
 }
@@ -371,19 +509,50 @@ parason_status to_rotary(const parason_rotary *r, int32_t d, RotaryArgs *out) {
     if (!r) return PARASON_OK;
     const parason_status st = check_pairs(r, d);
     if (st != PARASON_OK) return st;
-    if (r->num_axes < 1 || r->num_axes > kMaxAxes || !r->inv_freq || !r->positions ||
-        misaligned(r->inv_freq, 4) || misaligned(r->positions, 4) || (r->num_axes > 1 && r->position_stride < 0))
+    if (r->num_axes < 1 || r->num_axes > kMaxAxes || !r->turns || !r->positions ||
+        misaligned(r->turns, 8) || misaligned(r->positions, 4) || (r->num_axes > 1 && r->position_stride < 0))
         return PARASON_EINVAL;
-    out->inv_freq = r->inv_freq;
+    out->turns = r->turns;
     out->positions = r->positions;
     out->position_stride = r->num_axes > 1 ? r->position_stride : 0;
     out->half = r->rotary_dim / 2;
     out->interleaved = r->pairs == PARASON_ROTARY_INTERLEAVED;
     for (int i = 0; r->freq_axis && i < out->half; ++i) {
         if (r->freq_axis[i] >= r->num_axes) return PARASON_EINVAL;
-        out->axis[i] = r->freq_axis[i];
+        out->axes[i / 32] |= static_cast<uint64_t>(r->freq_axis[i]) << (2 * (i % 32));
     }
     return PARASON_OK;
+}
+
+// 1 / (2 pi) in 2^-192, most significant 64 bits first
+constexpr uint64_t kInvTwoPi[3] = {0x28be60db9391054aull, 0x7f09d5f47d4d3770ull, 0x36d8a5664f10e410ull};
+
+// |f| / (2 pi) modulo 1 in 2^-64: f = m 2^e, and m kInvTwoPi 2^(e + 64 - 192) rounded.
+// (kInvTwoPi is off by 2^-192, which e <= 40 takes to 2^-64 at most.)
+uint64_t turns_of(float f) {
+    int e = 0;
+    const uint64_t m = static_cast<uint64_t>(std::ldexp(std::frexp(std::fabs(f), &e), 24));
+    e -= 24;
+    uint64_t w[5] = {0, 0, 0, 0, 0};                     // m kInvTwoPi, least significant first
+    unsigned __int128 carry = 0;
+    for (int i = 0; i < 3; ++i) {
+        carry += static_cast<unsigned __int128>(m) * kInvTwoPi[2 - i];
+        w[i] = static_cast<uint64_t>(carry);
+        carry >>= 64;
+    }
+    w[3] = static_cast<uint64_t>(carry);
+    const int shift = 128 - e;                           // 88 and up for |f| <= 2^64
+    if (shift > 256) return 0;
+    const int half = shift - 1;                          // the bit that rounds
+    unsigned __int128 up = static_cast<unsigned __int128>(1) << (half % 64);
+    for (int i = half / 64; i < 5; ++i) {
+        up += w[i];
+        w[i] = static_cast<uint64_t>(up);
+        up >>= 64;
+    }
+    if (shift == 256) return w[4];
+    const int at = shift / 64, by = shift % 64;
+    return by ? (w[at] >> by) | (w[at + 1] << (64 - by)) : w[at];
 }
 
 parason_status launched(cudaError_t e) { return e == cudaSuccess ? PARASON_OK : PARASON_ECUDA; }
@@ -392,6 +561,17 @@ parason_status launched(cudaError_t e) { return e == cudaSuccess ? PARASON_OK : 
 }  // namespace parason
 
 using namespace parason;
+
+extern "C" parason_status parason_rotary_turns(const float *inv_freq, int32_t n, uint64_t *turns) {
+    if (n < 0 || (n > 0 && (!inv_freq || !turns))) return PARASON_EINVAL;
+    for (int32_t i = 0; i < n; ++i)
+        if (!(std::fabs(inv_freq[i]) <= 0x1p64f)) return PARASON_EINVAL;
+    for (int32_t i = 0; i < n; ++i) {
+        const uint64_t t = turns_of(inv_freq[i]);
+        turns[i] = inv_freq[i] < 0.f ? 0 - t : t;
+    }
+    return PARASON_OK;
+}
 
 extern "C" parason_status parason_kv_write(const parason_attn_config *cfg, int64_t num_tokens,
                                            const parason_rows *q, const parason_rows *k,
@@ -510,7 +690,8 @@ extern "C" parason_status parason_kv_scales(const parason_attn_config *cfg, int6
     }
     if (num_tokens == 0) return PARASON_OK;
     return launched(launch_dependent(true, kv_scales_kernel<128>,
-                                     dim3(static_cast<unsigned>((num_tokens + 255) / 256),
+                                     dim3(static_cast<unsigned>((num_tokens + kWarps * kScaleRows - 1) /
+                                                                (kWarps * kScaleRows)),
                                           static_cast<unsigned>(cfg->num_kv_heads), 2),
                                      dim3(kThreads), 0, s, a));
 }

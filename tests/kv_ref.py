@@ -55,8 +55,8 @@ def rotated(x, rotary, table, positions):
 
 def bound(ref, size, dtype, steps=1):
     """One rounding to `dtype` of a value that fp32 arithmetic has off by a few
-    2^-24 of what went into it: cos and sin are off by at most 2^-22 (the
-    fraction of a turn rounds to 2^-25, times 2 pi, and two units of sincospi),
+    2^-24 of what went into it: cos and sin are off by at most 2^-22 (half a turn's
+    fraction rounds to 2^-26 of a turn, times 2 pi, and two units of sincospi),
     a product and a sum round twice, a division or product with a scale `steps`
     times more."""
     off = 2.0 ** -21 * size + steps * 2.0 ** -24 * ref.abs()

@@ -58,7 +58,8 @@ def check_write(seed, mode, h_q, h_kv, d, tokens, kind, pad=0, heads_first=False
             ref, size = R.stored(ref, size, scale)
         got = R.at(pool, slots[live]).view(pool.dtype).double() if mode != "fp8" else \
             R.at(pool, slots[live]).view(pool.dtype).float().double()
-        assert ((got - ref[live]).abs() <= R.bound(ref, size, pool.dtype)[live]).all()
+        # (a scale's reciprocal and the product with it round)
+        assert ((got - ref[live]).abs() <= R.bound(ref, size, pool.dtype, 2)[live]).all()
         rest = torch.arange(pages * R.PAGE, device="cuda")[untouched]
         assert torch.equal(R.at(pool, rest), R.at(old, rest))
 
@@ -103,8 +104,8 @@ def test_write_far_positions(lo, hi):
 
 
 def test_write_farthest_positions():
-    """At the ends of int32 the angle in turns, up to 2^29, rounds to 2^-24 turns in
-    64 bits twice: 2^-21 radians more than elsewhere (2 pi 2^-24 < 2^-21)."""
+    """At the ends of int32 the reference's angle, up to 2^31 radians in 64 bits, is off
+    by 2^-22 radians itself; the kernel's is as near as elsewhere."""
     rotary, table = R.rotary_of(HALVES)
     gen = R.generator(6)
     positions = torch.tensor([2 ** 31 - 1, -2 ** 31, 2 ** 31 - 2, 0], dtype=torch.int32, device="cuda")
@@ -113,7 +114,7 @@ def test_write_farthest_positions():
     out = kv_write(k, k, *pools, torch.full((4,), -1, dtype=torch.int32, device="cuda"), q=q, rotary=rotary,
                    positions=positions)
     ref, size = R.rotated(q, rotary, table, positions)
-    assert ((out.double() - ref).abs() <= R.bound(ref, size, torch.float32) + 2.0 ** -21 * size).all()
+    assert ((out.double() - ref).abs() <= R.bound(ref, size, torch.float32) + 2.0 ** -22 * size).all()
 
 
 def test_write_special_values():
@@ -330,7 +331,7 @@ def test_replay_with_new_slots_and_positions():
         got_scale = ks.clone()
         held, held_size = R.stored(ref, size, got_scale)
         stored = R.at(pools[0], slots).view(torch.float8_e4m3fn).float()
-        assert ((stored.double() - held).abs() <= R.bound(held, held_size, torch.float8_e4m3fn)).all()
+        assert ((stored.double() - held).abs() <= R.bound(held, held_size, torch.float8_e4m3fn, 2)).all()
         want = stored.double() * got_scale.double().view(-1, 1)
         assert ((back[0].double() - want).abs() <= R.bound(want, 0 * want, torch.bfloat16)).all()
         ref, size = R.rotated(q, rotary, table, pos)

@@ -28,7 +28,7 @@ def _rows(data=A, ts=1024, hs=128):
 
 
 def _rot(**kw):
-    f = dict(rotary_dim=128, pairs=0, num_axes=1, freq_axis=None, inv_freq=A, positions=A, position_stride=0)
+    f = dict(rotary_dim=128, pairs=0, num_axes=1, freq_axis=None, turns=A, positions=A, position_stride=0)
     f.update(kw)
     return _lib.RotaryDesc(**f)
 
@@ -71,6 +71,10 @@ def test_shapes_without_a_kernel(lib):
     assert _write(lib, pages=most + 1) == _lib.EUNSUPPORTED
     assert _read(lib, pages=most + 1) == _lib.EUNSUPPORTED
     assert _scales(lib, _cfg("bf16")) == _lib.EINVAL
+    many = dict(num_q_heads=16386, num_kv_heads=2)
+    assert _write(lib, _cfg(**many)) == _lib.EUNSUPPORTED
+    assert _read(lib, _cfg(num_q_heads=16385, num_kv_heads=16385), pages=1) == _lib.EUNSUPPORTED
+    assert _scales(lib, _cfg("fp8", num_q_heads=16385, num_kv_heads=16385)) == _lib.EUNSUPPORTED
 
 
 @pytest.mark.parametrize("bad", [
@@ -90,8 +94,8 @@ def test_e4m3_needs_scales(lib, bad):
 
 @pytest.mark.parametrize("bad", [
     dict(rotary_dim=0), dict(rotary_dim=136), dict(rotary_dim=24), dict(rotary_dim=-16), dict(pairs=2),
-    dict(pairs=-1), dict(num_axes=0), dict(num_axes=5), dict(inv_freq=None), dict(positions=None),
-    dict(inv_freq=A + 2), dict(positions=A + 1), dict(num_axes=2, position_stride=-4)])
+    dict(pairs=-1), dict(num_axes=0), dict(num_axes=5), dict(turns=None), dict(positions=None),
+    dict(turns=A + 4), dict(positions=A + 1), dict(num_axes=2, position_stride=-4)])
 def test_rotary_refusals(lib, bad):
     assert _write(lib, rot=_rot(**bad)) == _lib.EINVAL
     if "rotary_dim" in bad or "pairs" in bad:
@@ -130,3 +134,37 @@ def test_null_config(lib):
                                 None) == _lib.EINVAL
     assert lib.parason_kv_read(None, 0, None, None, None, 0, None, None, None, None, None) == _lib.EINVAL
     assert lib.parason_kv_scales(None, 0, None, None, None, None, 0, None, None, None) == _lib.EINVAL
+
+
+def test_turns_of_frequencies(lib):
+    """inv_freq / (2 pi) modulo 1 in 2^-64, against exact integers; and the angles they give."""
+    def pi_times_2_to(bits):
+        def arctan_inverse(x):
+            one = term = (1 << (bits + 64)) // x
+            n, sign = 3, -1
+            while term:
+                term //= x * x
+                one += sign * (term // n)
+                n, sign = n + 2, -sign
+            return one
+        return (4 * (4 * arctan_inverse(5) - arctan_inverse(239))) >> 64
+
+    rng = np.random.default_rng(0)
+    f = np.concatenate([(1e4 ** (-np.arange(64) / 64)), [0.0, -0.5, 1e-45, 1e-38, 2.0 ** 40, -2.0 ** 64, 123456.789],
+                        rng.standard_normal(50) * 10.0 ** rng.integers(-20, 15, 50)]).astype(np.float32)
+    turns = np.empty(len(f), np.uint64)
+    assert lib.parason_rotary_turns(f.ctypes.data, len(f), turns.ctypes.data) == _lib.OK
+    pi = pi_times_2_to(600)
+    for x, got in zip(f, turns):
+        m, e = np.frexp(np.float64(x))
+        n = int(m * 2 ** 53)                     # x = n 2^(e - 53)
+        shift = int(e) - 53 + 64 + 600           # x / 2 pi in 2^-64 = n 2^(e - 53 + 64) 2^600 / (2 pi 2^600)
+        want = ((n << shift if shift >= 0 else 0) + pi) // (2 * pi) if shift >= 0 else 0
+        assert (int(got) - want) % 2 ** 64 in (0, 1, 2 ** 64 - 1), (x, got, want % 2 ** 64)
+    for bad in (np.inf, -np.inf, np.nan, 2.0 ** 65):
+        one = np.array([0.5, bad], np.float32)
+        assert lib.parason_rotary_turns(one.ctypes.data, 2, turns.ctypes.data) == _lib.EINVAL
+    assert lib.parason_rotary_turns(None, 1, turns.ctypes.data) == _lib.EINVAL
+    assert lib.parason_rotary_turns(f.ctypes.data, 1, None) == _lib.EINVAL
+    assert lib.parason_rotary_turns(f.ctypes.data, -1, turns.ctypes.data) == _lib.EINVAL
+    assert lib.parason_rotary_turns(None, 0, None) == _lib.OK
