@@ -8,8 +8,9 @@
 // (1.2e-7 before rounding, 1.8e-7 in fp32): the logit keeps the relative
 // accuracy of the plain product, so a cap far above the scores costs nothing.
 // Elsewhere tanh(u) = 1 - 2 / (1 + e^(2u)), whose absolute error of about 2e-7
-// is at most 5e-7 of tanh(kCapSeries).  Which form a score takes depends on that
-// score alone.
+// is at most 5e-7 of tanh(kCapSeries).  With caps above kCapFreeLog2 every score
+// takes the form its own size asks for; below, where that error is 1e-5 at most, a
+// block with a large score takes the exponential for all of them.
 //
 // A cap also bounds the logits, so where 2^cap_log2 leaves fp32 and bf16 room
 // (kCapFreeLog2) the softmax needs no maximum: P = 2^x, l = sum 2^x, with the
@@ -19,7 +20,7 @@
 // running maximum (kCapRef).
 //
 // What bounds it: the softmax warps' instructions (their issue, and their fetch:
-// long unrolled loops run no faster than they are fetched).  The series is 7
+// long unrolled loops run no faster than they are fetched).  The series is 6
 // packed instructions per two scores and no MUFU; the exponential form adds an
 // exponential per score and a reciprocal per two.  Models keep nearly all logits
 // far below their cap, so a warp votes: if no score of the block reaches
@@ -48,14 +49,14 @@ __device__ __forceinline__ float fast_rcp(float x) {
 
 // The factors of one item's scores, in both halves of packed pairs.
 struct CapFactors {
-    unsigned long long to_cap, scale;    // u = to_cap <q, k>, scale = cap_log2 to_cap
-    unsigned long long a1, a2, a3;       // the series' coefficients times cap_log2
+    unsigned long long to_cap;           // u = to_cap <q, k>
+    unsigned long long c0, a1, a2, a3;   // cap_log2, and the series' coefficients times it
     unsigned long long two_u;            // two_u <q, k> = 2 u log2(e)
     float to, cap;
     __device__ __forceinline__ CapFactors(float to_, float cap_) : to(to_), cap(cap_) {
-        const float s = cap * to, w = 2.f * 1.4426950408889634f * to;
+        const float w = 2.f * 1.4426950408889634f * to;
         to_cap = dev::f32x2(to, to);
-        scale = dev::f32x2(s, s);
+        c0 = dev::f32x2(cap, cap);
         a1 = dev::f32x2(kCapA1 * cap, kCapA1 * cap);
         a2 = dev::f32x2(kCapA2 * cap, kCapA2 * cap);
         a3 = dev::f32x2(kCapA3 * cap, kCapA3 * cap);
@@ -71,18 +72,8 @@ __device__ __forceinline__ unsigned long long cap_series(unsigned long long x, u
     t = dev::mul_f32x2(u, u);
     unsigned long long q = dev::fma_f32x2(t, f.a3, f.a2);
     q = dev::fma_f32x2(q, t, f.a1);
-    return dev::fma_f32x2(dev::mul_f32x2(u, t), q, dev::fma_f32x2(x, f.scale, nm));
-}
-
-// cap_log2 tanh of two scores, without a reference.
-__device__ __forceinline__ unsigned long long cap_series(unsigned long long x, const CapFactors &f,
-                                                         unsigned long long &t) {
-    const unsigned long long u = dev::mul_f32x2(x, f.to_cap);
-    t = dev::mul_f32x2(u, u);
-    unsigned long long q = dev::fma_f32x2(t, f.a3, f.a2);
-    q = dev::fma_f32x2(q, t, f.a1);
-    q = dev::fma_f32x2(q, t, dev::f32x2(f.cap, f.cap));
-    return dev::mul_f32x2(u, q);
+    q = dev::fma_f32x2(q, t, f.c0);
+    return dev::fma_f32x2(u, q, nm);
 }
 
 // cap_log2 tanh - m of two scores by the exponential (base: cap_log2 - m in both
@@ -131,7 +122,7 @@ __device__ __forceinline__ void cap_scores(float (&x)[M][N], bool &large, const 
             for (int j = 0; j < N; j += 2) {
                 unsigned long long t;
                 float t0, t1;
-                dev::f32x2_split(cap_series(dev::f32x2(x[i][j], x[i][j + 1]), f, t), y[i][j], y[i][j + 1]);
+                dev::f32x2_split(cap_series(dev::f32x2(x[i][j], x[i][j + 1]), 0ull, f, t), y[i][j], y[i][j + 1]);
                 dev::f32x2_split(t, t0, t1);
                 most = dev::max3(most, t0, t1);
             }
@@ -217,7 +208,7 @@ __device__ __forceinline__ void cap_free(const X (&x)[N], int seen, bool hidden,
             const float x0 = score_of(x[2 * c]), x1 = score_of(x[2 * c + 1]);
             unsigned long long t;
             float e0, e1, t0, t1;
-            dev::f32x2_split(cap_series(dev::f32x2(x0, x1), f, t), e0, e1);
+            dev::f32x2_split(cap_series(dev::f32x2(x0, x1), 0ull, f, t), e0, e1);
             dev::f32x2_split(t, t0, t1);
             most = dev::max3(most, t0, t1);
             put(c, dev::fast_exp2(e0), dev::fast_exp2(e1));

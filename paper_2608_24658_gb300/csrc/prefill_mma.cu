@@ -141,13 +141,16 @@ enum Bar : int {
     kMetaFull = kOEmpty + 2,         // [kMeta] scheduler -> every role
     kMetaEmpty = kMetaFull + kMeta,  // [kMeta] the 8 tile warps -> scheduler
     kDrain = kMetaEmpty + kMeta,     // MMA commit -> issuer, before TMEM is freed
-    kBars
+    kBars,
+    // caps without a reference: kSFull is the first half of S, this the second
+    kSFull2 = kBars,                 // [2]
+    kFreeBars = kSFull2 + 2
 };
 
 __host__ __device__ constexpr int bar_count(int i, bool f8) {
     if (i >= kFull && i < kEmpty) return f8 ? 4 : 1;
     if (i >= kRawEmpty && i < kSFull) return 4;
-    if (i >= kSFull && i < kPFull) return 2;
+    if ((i >= kSFull && i < kPFull) || i >= kSFull2) return 2;
     if (i >= kPFull && i < kOFull) return 4;
     if (i >= kOEmpty && i < kMetaFull) return 4;
     if (i >= kMetaEmpty && i < kDrain) return 8;
@@ -218,7 +221,8 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
     __shared__ uint32_t tmem_base;
     __shared__ volatile int progress;                // pairs the producer is at the end of
     __shared__ int valid_ring[kValidRing];           // valid keys of a block's halves (low bytes)
-    __shared__ __align__(8) uint64_t bar_mem[kBars];
+    constexpr int kMyBars = CAP == kCapFree ? kFreeBars : kBars;
+    __shared__ __align__(8) uint64_t bar_mem[kMyBars];
     __shared__ Meta meta[kMeta];
     const uint32_t q_smem = (dev::smem_addr(smem_raw) + 1023) & ~1023u;
     const uint32_t ring = q_smem + 2 * kQBytes;
@@ -232,7 +236,7 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
     if (threadIdx.x == 0) {
         abort_flag = 0;
         progress = 0;
-        for (int i = 0; i < kBars; ++i) dev::mbar_init(bar(i), bar_count(i, F8));
+        for (int i = 0; i < kMyBars; ++i) dev::mbar_init(bar(i), bar_count(i, F8));
         dev::fence_mbar_init();
         dev::prefetch_tensormap(F8 ? &maps.k_box : &maps.k);
         dev::prefetch_tensormap(F8 ? &maps.v_box : &maps.v);
@@ -419,25 +423,29 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                         return true;
                     };
                     if constexpr (CAP == kCapFree) {
+                        // no reference: a half's P needs its own scores alone, and goes
+                        // over them (rolled, for its instructions' fetch)
                         const bool hidden = __any_sync(0xffffffffu, min(seen_in(0), seen_in(1)) < kHalfTokens);
-                        // no reference: P of a half at a time, over scores that are read
-                        // (rolled, for its instructions' fetch)
-                        if (!next_q()) break;
                         uint32_t xs[64], ps[32];
-                        auto load_half = [&](int h) {
-                            tc::ld32(tS + 64 * h, *reinterpret_cast<uint32_t(*)[32]>(xs));
-                            tc::ld32(tS + 64 * h + 32, *reinterpret_cast<uint32_t(*)[32]>(xs + 32));
-                        };
 #pragma unroll 1
                         for (int h = 0; h < 2; ++h) {
-                            load_half(h);
+                            if (h == 1) {
+                                if (!tc_warp_wait(bar(kSFull2 + t), u & 1, limit, abort, lane)) {
+                                    ok = false;
+                                    break;
+                                }
+                                tc::fence_after_sync();
+                                if (!next_q()) break;
+                            }
+                            tc::ld32(tS + 64 * h, *reinterpret_cast<uint32_t(*)[32]>(xs));
+                            tc::ld32(tS + 64 * h + 32, *reinterpret_cast<uint32_t(*)[32]>(xs + 32));
                             tc::wait_ld();
                             PackedRow<false> row{ps};
                             cap_free(xs, seen_in(h), hidden, cap_large, cap, row);
                             float l0, l1;
                             dev::f32x2_split(row.sum, l0, l1);
                             l += l0 + l1;
-                            tc::st32(tS + 32 * h, ps);
+                            tc::st32(tS + 64 * h, ps);
                             if (!finish_half(h)) {
                                 ok = false;
                                 break;
@@ -931,6 +939,24 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                     if (last) tc::commit(bar(kEmpty + st));
                 }
             };
+            // half h of S_t of the block whose K is in `slot`
+            auto issue_half = [&](int t, int h, int slot, bool last) {
+                constexpr uint32_t kIdHalf = tc::idesc_bf16_f32(kRows, kHalfTokens, false);
+                const uint64_t kd = desc_k + static_cast<uint64_t>((slot * kSlotBytes + h * (kHalfTokens / 8) * kKGroup) >> 4);
+                const uint64_t qd = desc_q + static_cast<uint64_t>(t * (kQBytes >> 4));
+                const int full = (h == 0 ? kSFull : kSFull2) + t;
+                if (tc::elect_one()) {
+#pragma unroll
+                    for (int ks = 0; ks < kDim / 16; ++ks) {
+                        const uint32_t off = ((ks >> 2) * kQColBlockBytes + (ks & 3) * 32) >> 4;
+                        const uint32_t koff = ((ks >> 2) * kKCol + (ks & 3) * 32) >> 4;
+                        tc::mma_bf16(tmem + kTmemS + 128u * t + 64u * h, qd + off, kd + koff, kIdHalf, ks > 0);
+                    }
+                    tc::commit(bar(full));
+                    dev::mbar_arrive(bar(full));
+                    if (last) tc::commit(bar(kEmpty + slot));
+                }
+            };
             int u[2] = {0, 0}, j[2] = {0, 0};                 // blocks and pairs of each tile so far
             for (int k = 0;; ++k) {
                 wait(kMetaFull + k % kMeta, k / kMeta);
@@ -943,6 +969,47 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                 if (last) wait(kQReady + 1, j[1]);
                 wait(kFull + st, ph);
                 tc::fence_after_sync();
+                if constexpr (CAP == kCapFree) {
+                    // Caps without a reference: the halves of a block go their own ways,
+                    // S, P, PV, and the next block's S of the half over its P, so that a
+                    // tile's softmax has one half while the tensor core has the other
+                    // (join prefill 682 -> 642 us; half by half of both tiles 652).
+                    for (int h = 0; h < 2; ++h)
+                        for (int t = 0; t <= last; ++t) issue_half(t, h, st, h == 1 && t == last);
+                    advance();
+                    for (int i = 0; i < nb; ++i) {
+                        if (failed()) break;
+                        const int sv = st;
+                        const uint64_t vd = desc_v + static_cast<uint64_t>(sv * (kSlotBytes >> 4));
+                        wait(kFull + st, ph);
+                        advance();
+                        const int sk = st;
+                        if (i + 1 < nb) wait(kFull + sk, ph);
+                        for (int t = 0; t <= last; ++t)
+#pragma unroll
+                            for (int hf = 0; hf < 2; ++hf) {
+                                const uint32_t tO = tmem + kTmemO + 128u * t;
+                                const uint32_t tP = tmem + kTmemS + 128u * t + 64u * hf;
+                                if (i == 0 && hf == 0 && j[t] > 0) wait(kOEmpty + t, j[t] - 1);
+                                wait(kPFull + 2 * t + hf, u[t]);
+                                tc::fence_after_sync();
+                                if (tc::elect_one()) {
+#pragma unroll
+                                    for (int kk = 0; kk < 4; ++kk)
+                                        tc::mma_bf16_tmem_a(tO, tP + 8u * kk, vd + (((4 * hf + kk) * kVStep) >> 4),
+                                                            kIdPV, i > 0 || hf > 0 || kk > 0);
+                                    if (hf == 1 && t == last) tc::commit(bar(kEmpty + sv));
+                                    if (hf == 1 && i == nb - 1) tc::commit(bar(kOFull + t));
+                                }
+                                if (i + 1 < nb) issue_half(t, hf, sk, hf == 1 && t == last);
+                                if (hf == 1) ++u[t];
+                            }
+                        if (i + 1 < nb) advance();
+                    }
+                    ++j[0];
+                    j[1] += last;
+                    continue;
+                }
                 issue_s(0, last == 0);
                 if (last) issue_s(1, true);
                 advance();
