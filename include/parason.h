@@ -418,12 +418,15 @@ parason_status parason_lse_merge(const void *o_a, const float *lse_a, const void
  * instead of s_t = sm_scale * <q, k_t>; softmax, out and lse as before.  The
  * paper has no counterpart: it is the attention of models that bound their
  * logits.  cap is 0 (none; what a new plan has) or in [2^-10, 2^20];
- * PARASON_EINVAL otherwise (NaN included), for NULL, and for a
- * current device that is not the plan's.  Nothing is launched: a decode takes
+ * PARASON_EINVAL otherwise (NaN included), for NULL, for an sm_scale / cap that
+ * is not finite, and for a current device that is not the plan's.  Nothing is launched: a decode takes
  * the cap that is set when it is called, and a captured decode keeps the one it
  * was captured with.  Plans of every mode and kind take a cap, and it
  * stays through appends and forks.  lse_merge of two capped results over
  * disjoint keys is their capped result over both.
+ * With bf16 KV and caps up to 50 the kernels sum e^s as it is, without a
+ * running maximum: results are finite for V up to a magnitude of 2^34 where all
+ * of 2^20 keys are at the cap, and e^(cap - s) times more where they are below.
  */
 parason_status parason_plan_set_logit_cap(parason_plan plan, float cap);
 
@@ -439,7 +442,7 @@ parason_status parason_plan_set_logit_cap(parason_plan plan, float cap);
  * A slot is page * 16 + offset in the page: token t of a node sits in slot
  * 16 * page_ids[node_page_ptr[node] + t / 16] + t % 16.  `cfg` gives the head
  * counts, head_dim, page size and mode of the cache (sm_scale is not used),
- * validated as by parason_attn_plan.  Rows of tokens are bf16 (PARASON_BF16
+ * validated as by parason_attn_plan; the current device is the memory's.  Rows of tokens are bf16 (PARASON_BF16
  * and PARASON_FP8_E4M3_KV) or fp32 (PARASON_FP32).
  * ------------------------------------------------------------------------ */
 

@@ -396,7 +396,7 @@ class Rotary:
             raise ValueError("inv_freq must have a multiple of 8 elements, 64 at most")
         self.inv_freq, self.interleaved = inv_freq, bool(interleaved)
         self.rotary_dim = 2 * half
-        host = np.ascontiguousarray(inv_freq.cpu().numpy())
+        host = np.ascontiguousarray(inv_freq.detach().cpu().numpy())
         turns = np.empty(half, dtype=np.uint64)
         check(_lib.load().parason_rotary_turns(_ptr(host), half, _ptr(turns)), "parason_rotary_turns")
         self.device = inv_freq.get_device()

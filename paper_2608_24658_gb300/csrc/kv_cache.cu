@@ -15,7 +15,6 @@
 namespace parason {
 namespace {
 
-constexpr int kMaxFreqs = 64;            // rotary_dim / 2 at head_dim 128
 constexpr int kMaxAxes = 4;
 constexpr float kE4m3Max = 448.f;
 constexpr int kMaxHeads = 16384;         // of q, and of k: what the kernels' counters hold
@@ -26,7 +25,8 @@ struct Rows {
 };
 
 // A rotary description by value: the axis of each frequency travels in the
-// kernel's parameters, as 2 bits (an array there would be read lane by lane).
+// kernel's parameters, as 2 bits (an array there would be read lane by lane); 64
+// frequencies at most, at head_dim 128.
 struct RotaryArgs {
     const uint64_t *turns;
     const int32_t *positions;

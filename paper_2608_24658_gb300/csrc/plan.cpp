@@ -2376,6 +2376,7 @@ parason_status parason_plan_set_debug(parason_plan p, uint32_t flags, int64_t wa
 parason_status parason_plan_set_logit_cap(parason_plan p, float cap) {
     // (a NaN fails every comparison)
     if (!p || !(cap == 0.0f || (cap >= 0x1p-10f && cap <= 0x1p20f))) return PARASON_EINVAL;
+    if (cap > 0.0f && !std::isfinite(p->cfg.sm_scale / cap)) return PARASON_EINVAL;
     if (cap > 0.0f && p->on_device && p->cfg.mode != PARASON_FP32) {
         int dev = -1;
         if (cudaGetDevice(&dev) != cudaSuccess) return PARASON_ECUDA;

@@ -338,16 +338,16 @@ def test_replay_with_new_slots_and_positions():
         assert ((q_out.double() - ref).abs() <= R.bound(ref, size, torch.bfloat16)).all()
 
 
-@pytest.mark.parametrize("as_int", [False, True])
-def test_another_stream(as_int):
+@pytest.mark.parametrize("which", ["stream", "handle", "default"])
+def test_another_stream(which):
     """New outputs belong to the stream that writes them."""
     gen = R.generator(15)
     k, v = (R.rows(gen, 100, 2, 128, torch.bfloat16) for _ in range(2))
     pools = R.pool(gen, 8, 2, 128, "bf16")
     slots = torch.randperm(128, generator=gen, device="cuda")[:100].to(torch.int32)
-    side = torch.cuda.Stream()
+    side = torch.cuda.default_stream() if which == "default" else torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
-    handle = side.cuda_stream if as_int else side
+    handle = {"stream": side, "handle": side.cuda_stream, "default": 0}[which]
     q = kv_write(k, v, *pools, slots, q=k, stream=handle)
     rk, rv = kv_read(*pools, slots, stream=handle)
     ks, vs = kv_scales(k, v, stream=handle)

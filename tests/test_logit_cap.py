@@ -27,6 +27,14 @@ def test_refused_caps(bad):
     assert _lib.load().parason_plan_set_logit_cap(None, 30.0) == _lib.EINVAL
 
 
+def test_scale_that_a_cap_overflows():
+    with Plan.for_tree(W.figure3_tree(values=False, sm_scale=3e38), host_only=True) as plan:
+        plan.set_logit_cap(4.0)
+        with pytest.raises(ParasonError) as e:
+            plan.set_logit_cap(0.5)
+        assert e.value.status == _lib.EINVAL
+
+
 @pytest.mark.parametrize("good", [0.0, 2.0 ** -10, 1.0, 50.0, 2.0 ** 20])
 def test_caps_leave_the_plan_as_it_is(good):
     tree = W.pair_fixture(values=False)

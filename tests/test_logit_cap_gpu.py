@@ -203,3 +203,60 @@ def test_small_scores_beside_large_ones(mode):
                         head_dim=128, mode=mode, seed=6, q_std=0.5, device="cuda")
     tree.q[1::2] *= 3000.0
     C.check(tree, 1000.0, *decode(tree, 1000.0))
+
+
+@pytest.mark.parametrize("mode", ["bf16", "fp8", "fp32"])
+@pytest.mark.parametrize("cap", [50.0, 50.59, 50.61, 90.0])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_every_key_at_the_cap(mode, cap, sign):
+    """All weights near e^cap, or near e^-cap: the mean of V, lse = ln n + s.  (50.6 is where the kernels go from
+    sums of e^s to a running maximum.)"""
+    tree = W.build_tree("sat", [-1, 0, 0, 0], [700, 33, 1, 100], [1, 2, 3], num_q_heads=16, num_kv_heads=2,
+                        head_dim=128, mode=mode, seed=7, device="cuda", tail_value=math.nan)
+    tree.q.fill_(8.0)
+    if mode == "fp8":
+        tree.k_pages.view(torch.uint8).copy_(torch.full_like(tree.k_pages.float(), 256.0 * sign).to(
+            torch.float8_e4m3fn).view(torch.uint8))
+    else:
+        tree.k_pages.fill_(16.0 * sign)
+    out, lse = decode(tree, cap)
+    C.check(tree, cap, out, lse)
+    # every key's logit: <q, k> = 128 * 8 * k (in e4m3 tanh is not quite 1 there)
+    n = torch.tensor([733, 701, 800], device="cuda").double()[:, None]
+    key = 256.0 * sign * tree.k_scale.double() if mode == "fp8" else torch.full((2,), 16.0 * sign, device="cuda").double()
+    at = (cap * torch.tanh(128 * 8 * key / math.sqrt(128) / cap)).repeat_interleave(8)
+    assert ((lse.double() - (n.log() + at)).abs() <= 2.0 ** -18 * (cap + n.log())).all()
+
+
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+def test_scores_past_fp32(mode):
+    """A score that overflows to infinity is at the cap."""
+    tree = W.build_tree("inf", [-1, 0, 0], [600, 40, 40], [1, 2], num_q_heads=16, num_kv_heads=2, head_dim=128,
+                        mode=mode, seed=8, device="cuda")
+    tree.q.fill_(2.0 ** 62)
+    signs = torch.where(torch.arange(tree.k_pages.shape[2], device="cuda") % 3 == 0, -1.0, 1.0)
+    tree.k_pages.copy_((2.0 ** 62 * signs).view(1, 1, -1, 1).expand_as(tree.k_pages))
+    for cap in (20.0, 100.0):
+        out, lse = decode(tree, cap)
+        ref_o, ref_l, tol_o, tol_l = C.capped(tree, cap)
+        # (the bound's A is infinite here: the logits are +-cap exactly)
+        assert ((lse.double() - ref_l).abs() <= 2.0 ** -18 * ref_l.abs()).all()
+        rel = ((out.double() - ref_o).norm() / ref_o.norm()).item()
+        assert rel <= (2.0 ** -7 if mode == "bf16" else 2.0 ** -18)
+
+
+@pytest.mark.parametrize("mode", ["bf16", "fp8"])
+def test_prefill_every_key_at_minus_the_cap(mode):
+    tree = W.build_prefill("satp", [-1, 0], [300, 90], [1], num_q_heads=8, num_kv_heads=2, head_dim=128, mode=mode,
+                           seed=9, device="cuda", tail_value=math.nan)
+    tree.q.fill_(-8.0)
+    if mode == "fp8":
+        tree.k_pages.view(torch.uint8).copy_(torch.full_like(tree.k_pages.float(), 256.0).to(
+            torch.float8_e4m3fn).view(torch.uint8))
+    else:
+        tree.k_pages.fill_(16.0)
+    for cap in (50.0, 80.0):
+        with Plan.for_prefill(tree, logit_cap=cap) as plan:
+            out, lse = plan.decode_tree(tree)
+            plan.check()
+        C.check(tree, cap, out, lse, prefill=True)
