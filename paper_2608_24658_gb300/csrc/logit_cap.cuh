@@ -83,7 +83,10 @@ __device__ __forceinline__ unsigned long long cap_exp_pair(float x0, float x1, c
                                                            unsigned long long base) {
     float w0, w1;
     dev::f32x2_split(dev::mul_f32x2(dev::f32x2(x0, x1), f.two_u), w0, w1);
-    const float d0 = 1.f + dev::fast_exp2(fminf(w0, 60.f)), d1 = 1.f + dev::fast_exp2(fminf(w1, 60.f));
+    float d0, d1;
+    dev::f32x2_split(dev::add_f32x2(dev::f32x2(dev::fast_exp2(fminf(w0, 60.f)), dev::fast_exp2(fminf(w1, 60.f))),
+                                    dev::f32x2(1.f, 1.f)),
+                     d0, d1);
     const float r = fast_rcp(d0 * d1);
     return dev::fma_f32x2(dev::f32x2(r * d1, r * d0), dev::f32x2(-2.f * f.cap, -2.f * f.cap), base);
 }
@@ -135,20 +138,19 @@ __device__ __forceinline__ void cap_scores(float (&x)[M][N], bool &large, const 
             return;
         }
     }
-    float hi = 0.f, lo = 0.f;
+    float most = 0.f;
 #pragma unroll
     for (int i = 0; i < M; ++i)
 #pragma unroll
         for (int j = 0; j < N; j += 2) {
             const float x0 = x[i][j], x1 = x[i][j + 1];
-            hi = dev::max3(hi, x0, x1);
-            lo = dev::min3(lo, x0, x1);
+            most = dev::max3(most, fabsf(x0), fabsf(x1));
             if (f.cap <= kCapFreeLog2)
                 dev::f32x2_split(cap_exp_pair(x0, x1, f, dev::f32x2(f.cap, f.cap)), x[i][j], x[i][j + 1]);
             else
                 cap_pair(x0, x1, dev::f32x2(0.f, 0.f), f, x[i][j], x[i][j + 1]);
         }
-    large = __any_sync(0xffffffffu, fmaxf(hi, -lo) * f.to >= kCapSeries);
+    large = __any_sync(0xffffffffu, most * f.to >= kCapSeries);
 }
 
 // ---------------------------------------------------------------- no reference
@@ -217,17 +219,16 @@ __device__ __forceinline__ void cap_free(const X (&x)[N], int seen, bool hidden,
         if (!large) return;
         put.start();
     }
-    float hi = 0.f, lo = 0.f;
+    float most = 0.f;
 #pragma unroll
     for (int c = 0; c < N / 2; ++c) {
         const float x0 = score_of(x[2 * c]), x1 = score_of(x[2 * c + 1]);
         float e0, e1;
         dev::f32x2_split(cap_exp_pair(x0, x1, f, base), e0, e1);
-        hi = dev::max3(hi, x0, x1);
-        lo = dev::min3(lo, x0, x1);
+        most = dev::max3(most, fabsf(x0), fabsf(x1));
         put(c, dev::fast_exp2(e0), dev::fast_exp2(e1));
     }
-    large = __any_sync(0xffffffffu, fmaxf(hi, -lo) * f.to >= kCapSeries);
+    large = __any_sync(0xffffffffu, most * f.to >= kCapSeries);
 }
 
 // ---------------------------------------------------------------- tiles
