@@ -55,6 +55,7 @@ struct ReadArgs {
     Rows k, v;
     int64_t num_tokens, num_slots;
     int32_t num_kv_heads, parts;
+    bool aligned;                        // k's and v's rows to 32 bytes
 };
 
 struct ScalesArgs {
@@ -75,19 +76,13 @@ struct Raw8 {
 template <class T>
 __device__ __forceinline__ Raw8<T> load8(const T *p) {
     Raw8<T> r;
-    if constexpr (sizeof(T) == 1) {
-        const uint2 u = __ldcs(reinterpret_cast<const uint2 *>(p));
-        r.w[0] = u.x;
-        r.w[1] = u.y;
-    } else {
 #pragma unroll
-        for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) {
-            const uint4 u = __ldcs(reinterpret_cast<const uint4 *>(p) + i);
-            r.w[4 * i] = u.x;
-            r.w[4 * i + 1] = u.y;
-            r.w[4 * i + 2] = u.z;
-            r.w[4 * i + 3] = u.w;
-        }
+    for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) {
+        const uint4 u = __ldcs(reinterpret_cast<const uint4 *>(p) + i);
+        r.w[4 * i] = u.x;
+        r.w[4 * i + 1] = u.y;
+        r.w[4 * i + 2] = u.z;
+        r.w[4 * i + 3] = u.w;
     }
     return r;
 }
@@ -103,17 +98,6 @@ __device__ __forceinline__ void unpack8(const Raw8<__nv_bfloat16> &r, float (&x)
 __device__ __forceinline__ void unpack8(const Raw8<float> &r, float (&x)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(r.w[i]);
-}
-
-__device__ __forceinline__ void unpack8(const Raw8<__nv_fp8_e4m3> &r, float (&x)[8]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint32_t h;
-        asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(static_cast<uint16_t>(r.w[i >> 1] >> (16 * (i & 1)))));
-        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
-        x[2 * i] = f.x;
-        x[2 * i + 1] = f.y;
-    }
 }
 
 __device__ __forceinline__ void store8(__nv_bfloat16 *p, const float (&x)[8]) {
@@ -284,14 +268,74 @@ __global__ void __launch_bounds__(kThreads) kv_write_kernel(const WriteArgs a) {
             a.num_kv_heads, mine, 16 * u, 16 * u + 8, INTERLEAVED, false, cs, sn, a.v_scale);
 }
 
-// A warp takes one token, or one of `parts` equal parts of its steps, k's and then
-// v's: a lane 8 elements of a head, kBatch steps' loads in flight.  12 CTAs an SM hide
-// the chain from slot to rows to stores (38.8k e4m3 tokens: 39.6 us; 8 steps in flight
-// in 8 CTAs 40.8, 2 steps 43.6).
+// Sixteen consecutive elements, as two of the units above.
+template <class T>
+struct Raw16 {
+    Raw8<T> h[2];
+};
 
+template <class T>
+__device__ __forceinline__ Raw16<T> load16(const T *p) {
+    Raw16<T> r;
+    if constexpr (sizeof(T) == 1) {
+        const uint4 u = __ldcs(reinterpret_cast<const uint4 *>(p));
+        r.h[0].w[0] = u.x;
+        r.h[0].w[1] = u.y;
+        r.h[1].w[0] = u.z;
+        r.h[1].w[1] = u.w;
+    } else {
+        r.h[0] = load8(p);
+        r.h[1] = load8(p + 8);
+    }
+    return r;
+}
+
+// 32 bytes in one store where they are aligned so (whole sectors), else 16 and 16.
+__device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8], bool aligned) {
+    if (aligned) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]),
+                     "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                     : "memory");
+    } else {
+        reinterpret_cast<uint4 *>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4 *>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+}
+
+// 16 elements of the cache as the caller's: bits where the types are the same.
+template <class T, class KV>
+__device__ __forceinline__ void store_read16(T *dst, const Raw16<KV> &r, float scale, bool aligned) {
+    if constexpr (kScaled<KV>) {
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t h;
+            asm("cvt.rn.f16x2.e4m3x2 %0, %1;"
+                : "=r"(h)
+                : "h"(static_cast<uint16_t>(r.h[i >> 2].w[(i >> 1) & 1] >> (16 * (i & 1)))));
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+            float lo, hi;
+            dev::f32x2_split(dev::mul_f32x2(dev::f32x2(f.x, f.y), dev::f32x2(scale, scale)), lo, hi);
+            w[i] = dev::pack_bf16(lo, hi);
+        }
+        store32(dst, w, aligned);
+    } else if constexpr (sizeof(T) == 2) {
+        const uint32_t w[8] = {r.h[0].w[0], r.h[0].w[1], r.h[0].w[2], r.h[0].w[3],
+                               r.h[1].w[0], r.h[1].w[1], r.h[1].w[2], r.h[1].w[3]};
+        store32(dst, w, aligned);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) store32(dst + 8 * i, r.h[i].w, aligned);
+    }
+}
+
+// A warp takes one token, or one of `parts` equal parts of its steps, k's and then
+// v's: a lane 16 elements of a head, kBatch steps' loads in flight.  38.8k e4m3 tokens:
+// 37.7 us (35.2 us of bytes); 8 elements a lane, whose scales and addresses then come
+// twice as often, 39.6; 12 CTAs an SM of 2 steps 38.0.
 template <class T, class KV, int D>
-__global__ void __launch_bounds__(kThreads, 12) kv_read_kernel(const ReadArgs a) {
-    constexpr int kLanes = D / 8, kHeads = 32 / kLanes, kBatch = sizeof(T) == 4 ? 2 : 4;
+__global__ void __launch_bounds__(kThreads, 8) kv_read_kernel(const ReadArgs a) {
+    constexpr int kLanes = D / 16, kHeads = 32 / kLanes, kBatch = sizeof(T) == 4 ? 2 : 4;
     const int lane = threadIdx.x % 32;
     const int64_t job = static_cast<int64_t>(blockIdx.x) * kWarps + threadIdx.x / 32;
     const int64_t t = a.parts == 1 ? job : job / a.parts;
@@ -303,19 +347,24 @@ __global__ void __launch_bounds__(kThreads, 12) kv_read_kernel(const ReadArgs a)
     dev::grid_wait();
     const int64_t slot = a.slots[t];
     const bool live = slot >= 0 && slot < a.num_slots;
-    const int64_t row = (slot / kPageSize * a.num_kv_heads * kPageSize + slot % kPageSize) * D + 8 * u;
+    const int64_t row = (slot / kPageSize * a.num_kv_heads * kPageSize + slot % kPageSize) * D + 16 * u;
     for (int s0 = first; s0 < last; s0 += kBatch) {
-        Raw8<KV> r[kBatch];
+        Raw16<KV> r[kBatch];
         float scale[kBatch];
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
             const int s = s0 + b;
             const bool is_k = s < kv_steps;
             const int h = (is_k ? s : s - kv_steps) * kHeads + mine;
-            if (s < last && h < a.num_kv_heads && live) {
-                r[b] = load8(static_cast<const KV *>(is_k ? a.k_pages : a.v_pages) + row +
-                             static_cast<int64_t>(h) * kPageSize * D);
-                if constexpr (kScaled<KV>) scale[b] = (is_k ? a.k_scale : a.v_scale)[h];
+            if (s < last && h < a.num_kv_heads) {
+                if (live) {
+                    r[b] = load16(static_cast<const KV *>(is_k ? a.k_pages : a.v_pages) + row +
+                                  static_cast<int64_t>(h) * kPageSize * D);
+                    if constexpr (kScaled<KV>) scale[b] = (is_k ? a.k_scale : a.v_scale)[h];
+                } else {
+                    r[b] = Raw16<KV>{};
+                    scale[b] = 0.f;
+                }
             }
         }
 #pragma unroll
@@ -324,18 +373,10 @@ __global__ void __launch_bounds__(kThreads, 12) kv_read_kernel(const ReadArgs a)
             const bool is_k = s < kv_steps;
             const int h = (is_k ? s : s - kv_steps) * kHeads + mine;
             if (s >= last || h >= a.num_kv_heads) continue;
-            float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (live) {
-                unpack8(r[b], x);
-                if constexpr (kScaled<KV>) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] *= scale[b];
-                }
-            }
             T *dst = static_cast<T *>(const_cast<void *>(is_k ? a.k.data : a.v.data)) +
                      t * (is_k ? a.k.token_stride : a.v.token_stride) +
-                     h * (is_k ? a.k.head_stride : a.v.head_stride) + 8 * u;
-            store8(dst, x);
+                     h * (is_k ? a.k.head_stride : a.v.head_stride) + 16 * u;
+            store_read16<T, KV>(dst, r[b], scale[b], a.aligned);
         }
     }
 }
@@ -465,7 +506,12 @@ cudaError_t launch_write(WriteArgs a, cudaStream_t s) {
 
 template <class T, class KV, int D>
 cudaError_t launch_read(ReadArgs a, cudaStream_t s) {
-    constexpr int kHeads = 32 / (D / 8);
+    constexpr int kHeads = 32 / (D / 16);
+    uintptr_t odd = 0;
+    for (const Rows *r : {&a.k, &a.v})
+        odd |= reinterpret_cast<uintptr_t>(r->data) | static_cast<uintptr_t>(r->token_stride * sizeof(T)) |
+               static_cast<uintptr_t>(r->head_stride * sizeof(T));
+    a.aligned = odd % 32 == 0;
     a.parts = parts_of(a.num_tokens, 2 * ((a.num_kv_heads + kHeads - 1) / kHeads));
     return launch_dependent(true, kv_read_kernel<T, KV, D>, dim3(blocks_of(a.num_tokens, a.parts)),
                             dim3(kThreads), 0, s, a);
