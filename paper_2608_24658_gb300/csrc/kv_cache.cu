@@ -54,7 +54,10 @@ struct ReadArgs {
     const float *k_scale, *v_scale;
     Rows k, v;
     int64_t num_tokens, num_slots;
-    int32_t num_kv_heads, parts;
+    int32_t num_kv_heads;
+    uint32_t heads_magic;                // n / heads is the high word of n times it (below 2^32 / heads;
+                                         // 0: one head)
+    bool short_rows;                     // rows fit 32 bits
     bool aligned;                        // k's and v's rows to 32 bytes
 };
 
@@ -135,8 +138,8 @@ constexpr int kFullWarps = 152 * 16;
 // cos and sin of positions[axis] * inv_freq[i].  The frequency is held as turns a
 // position modulo 1, in 2^-64: the low 64 bits of its product with the position are
 // the angle's part of a turn (off by 2^-33 at most, at position 2^31), whose upper 32
-// as a signed number are it within half a turn.  (In 64-bit floating point the same
-// took 7 instructions of a pipe that does 2 lanes a cycle: 6 us of a 30 us prompt.)
+// as a signed number are it within half a turn: integers, as 64-bit floating point
+// has a pipe of 2 lanes a cycle here.
 __device__ __forceinline__ float2 turn(const RotaryArgs &r, int64_t t, int i) {
     const int axis = static_cast<int>((i < 32 ? r.axes[0] : r.axes[1]) >> (2 * (i & 31))) & 3;
     const int64_t pos = r.positions[axis * r.position_stride + t];
@@ -146,28 +149,27 @@ __device__ __forceinline__ float2 turn(const RotaryArgs &r, int64_t t, int i) {
     return make_float2(c, s);
 }
 
-// Heads of one kind (q, k or v) of a token, steps [s0, s1) of kHeads heads each: this
-// lane's two chunks of each are at src + e and dst + e, e0 and e1 (elements), a step
-// further `src_step` and `dst_step`.  The loads of kBatch steps go together.
-template <class T, class Out, int D, bool ROTATE, int kBatch>
+// Heads of one kind (q, k or v) of a token, steps [s0, s1) of G heads each: this lane's
+// two chunks of each are at src + e and dst + e, e0 and e1 (elements), a step further
+// `src_step` and `dst_step`.  The loads of kBatch steps go together.
+template <class T, class Out, int G, bool ROTATE, int kBatch>
 __device__ __forceinline__ void write_heads(const T *src, int64_t src_step, Out *dst, int64_t dst_step, int s0, int s1,
                                             int heads, int mine, int e0, int e1, bool interleaved, bool rotates,
                                             const unsigned long long (&cs)[4], const unsigned long long (&sn)[4],
                                             const float *scale) {
-    constexpr int kHeads = 32 / (D / 16);
     src += s0 * src_step;
     dst += s0 * dst_step;
     for (int s = s0; s < s1; s += kBatch, src += kBatch * src_step, dst += kBatch * dst_step) {
         Raw8<T> r0[kBatch], r1[kBatch];
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
-            if (s + b >= s1 || (s + b) * kHeads + mine >= heads) break;
+            if (s + b >= s1 || (s + b) * G + mine >= heads) break;
             r0[b] = load8(src + b * src_step + e0);
             r1[b] = load8(src + b * src_step + e1);
         }
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
-            const int h = (s + b) * kHeads + mine;
+            const int h = (s + b) * G + mine;
             if (s + b >= s1 || h >= heads) break;
             float x0[8], x1[8];
             unpack8(r0[b], x0);
@@ -201,45 +203,50 @@ __device__ __forceinline__ void write_heads(const T *src, int64_t src_step, Out 
     }
 }
 
-// A token's heads are taken in steps of kHeads, first q's, then k's, then v's; a warp
-// takes one token, or one of `parts` equal parts of its steps.
+// A warp is 512 / D groups of D / 16 lanes, a group a head: each lane has two 8-element
+// chunks of it that hold whole pairs, chunk u of the first half of the rotated part and
+// its partner, or two neighbours.  So no element crosses a lane, rotation is in place
+// for q, and a warp's loads and stores are whole sectors.  G groups share a token and
+// take its heads G at a step, first q's, then k's, then v's: a warp takes as many tokens
+// as it has such teams, or one of `parts` equal parts of one token's steps.
 //
-// A head is D / 16 lanes, each with two 8-element chunks that hold whole pairs: chunk
-// u of the first half of the rotated part and its partner, or two neighbours.  So no
-// element crosses a lane, rotation is in place for q, and a warp's loads and stores
-// are whole sectors.  The warp makes the angles once for all its heads: the lanes of
-// one u share 8 pairs' angles, make 8 / kHeads each and pass them round (out of shared
-// memory they were read four lanes to a bank).
-template <class T, class KV, int D, bool INTERLEAVED>
+// The angles are made once for all heads of a token: the G lanes of one u share 8
+// pairs' angles, make 8 / G each and pass them round (out of shared memory they were
+// read four lanes to a bank).
+template <class T, class KV, int D, bool INTERLEAVED, int G>
 __global__ void __launch_bounds__(kThreads) kv_write_kernel(const WriteArgs a) {
-    constexpr int kLanes = D / 16, kHeads = 32 / kLanes, kMake = 8 / kHeads;
+    constexpr int kLanes = D / 16, kTeams = 32 / kLanes / G, kMake = 8 / G;
     constexpr int kBatch = sizeof(T) == 4 ? 2 : 3;            // (1, 2, 4 in bf16: 36, 35, 35 us for 34)
     const int lane = threadIdx.x % 32;
     const int64_t job = static_cast<int64_t>(blockIdx.x) * kWarps + threadIdx.x / 32;
-    const int64_t t = a.parts == 1 ? job : job / a.parts;
-    if (t >= a.num_tokens) return;
-    const int part = static_cast<int>(job - t * a.parts);
-    const int q_steps = (a.num_q_heads + kHeads - 1) / kHeads, kv_steps = (a.num_kv_heads + kHeads - 1) / kHeads;
-    const int steps = q_steps + 2 * kv_steps;                 // (2^14 at most)
-    const int first = steps * part / a.parts, last = steps * (part + 1) / a.parts;
-    const int u = lane % kLanes, mine = lane / kLanes;
+    const int64_t t0 = a.parts == 1 ? job : job / a.parts;
+    if (t0 * kTeams >= a.num_tokens) return;
+    const int part = static_cast<int>(job - t0 * a.parts);
+    const int q_steps = (a.num_q_heads + G - 1) / G, kv_steps = (a.num_kv_heads + G - 1) / G;
+    const int steps = q_steps + 2 * kv_steps;                 // (3 * 2^14 at most)
+    const int first = a.parts == 1 ? 0 : static_cast<int>(static_cast<int64_t>(steps) * part / a.parts);
+    const int last = a.parts == 1 ? steps : static_cast<int>(static_cast<int64_t>(steps) * (part + 1) / a.parts);
+    const int u = lane % kLanes, team = lane / kLanes / G, mine = lane / kLanes % G;
+    const int64_t t = t0 * kTeams + team;
+    const bool there = t < a.num_tokens;
     const bool rotates = 8 * u < a.rot.half, halves = rotates && !INTERLEAVED;
     // the elements of this lane's chunks in q and k; in v: 16 u and 16 u + 8
     const int e0 = halves ? 8 * u : 16 * u, e1 = e0 + (halves ? a.rot.half : 8);
     dev::grid_wait();
-    const int64_t slot = a.slots[t];
+    const int64_t slot = there ? a.slots[t] : -1;
 
     unsigned long long cs[4], sn[4];
     if (a.rot.half && first < q_steps + kv_steps) {
         float2 own[kMake];
 #pragma unroll
         for (int i = 0; i < kMake; ++i)
-            own[i] = rotates ? turn(a.rot, t, 8 * u + kMake * mine + i) : make_float2(1.f, 0.f);
+            own[i] = rotates && there ? turn(a.rot, t, 8 * u + kMake * mine + i) : make_float2(1.f, 0.f);
         float c[8], s[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            c[i] = __shfl_sync(0xffffffffu, own[i % kMake].x, i / kMake * kLanes + u);
-            s[i] = __shfl_sync(0xffffffffu, own[i % kMake].y, i / kMake * kLanes + u);
+            const int from = (team * G + i / kMake) * kLanes + u;
+            c[i] = G == 1 ? own[i % kMake].x : __shfl_sync(0xffffffffu, own[i % kMake].x, from);
+            s[i] = G == 1 ? own[i % kMake].y : __shfl_sync(0xffffffffu, own[i % kMake].y, from);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -247,25 +254,26 @@ __global__ void __launch_bounds__(kThreads) kv_write_kernel(const WriteArgs a) {
             sn[i] = dev::f32x2(s[2 * i], s[2 * i + 1]);
         }
     }
+    if (!there) return;
     if (first < q_steps)
-        write_heads<T, T, D, true, kBatch>(
-            static_cast<const T *>(a.q.data) + t * a.q.token_stride + mine * a.q.head_stride,
-            kHeads * a.q.head_stride, static_cast<T *>(a.q_out) + (t * a.num_q_heads + mine) * D, kHeads * D, first,
-            min(last, q_steps), a.num_q_heads, mine, e0, e1, INTERLEAVED, rotates, cs, sn, nullptr);
+        write_heads<T, T, G, true, kBatch>(
+            static_cast<const T *>(a.q.data) + t * a.q.token_stride + mine * a.q.head_stride, G * a.q.head_stride,
+            static_cast<T *>(a.q_out) + (t * a.num_q_heads + mine) * D, G * D, first, min(last, q_steps),
+            a.num_q_heads, mine, e0, e1, INTERLEAVED, rotates, cs, sn, nullptr);
     if (slot < 0 || slot >= a.num_slots || last <= q_steps) return;
     const int64_t row = (slot / kPageSize * a.num_kv_heads + mine) * kPageSize * D + slot % kPageSize * D;
     const int k0 = max(first, q_steps) - q_steps, k1 = min(last - q_steps, kv_steps);
     if (k0 < k1)
-        write_heads<T, KV, D, true, kBatch>(
-            static_cast<const T *>(a.k.data) + t * a.k.token_stride + mine * a.k.head_stride,
-            kHeads * a.k.head_stride, static_cast<KV *>(a.k_pages) + row, kHeads * kPageSize * D, k0, k1,
-            a.num_kv_heads, mine, e0, e1, INTERLEAVED, rotates, cs, sn, a.k_scale);
+        write_heads<T, KV, G, true, kBatch>(
+            static_cast<const T *>(a.k.data) + t * a.k.token_stride + mine * a.k.head_stride, G * a.k.head_stride,
+            static_cast<KV *>(a.k_pages) + row, G * kPageSize * D, k0, k1, a.num_kv_heads, mine, e0, e1,
+            INTERLEAVED, rotates, cs, sn, a.k_scale);
     const int v0 = max(first - q_steps - kv_steps, 0), v1 = last - q_steps - kv_steps;
     if (v0 < v1)
-        write_heads<T, KV, D, false, kBatch>(
-            static_cast<const T *>(a.v.data) + t * a.v.token_stride + mine * a.v.head_stride,
-            kHeads * a.v.head_stride, static_cast<KV *>(a.v_pages) + row, kHeads * kPageSize * D, v0, v1,
-            a.num_kv_heads, mine, 16 * u, 16 * u + 8, INTERLEAVED, false, cs, sn, a.v_scale);
+        write_heads<T, KV, G, false, kBatch>(
+            static_cast<const T *>(a.v.data) + t * a.v.token_stride + mine * a.v.head_stride, G * a.v.head_stride,
+            static_cast<KV *>(a.v_pages) + row, G * kPageSize * D, v0, v1, a.num_kv_heads, mine, 16 * u,
+            16 * u + 8, INTERLEAVED, false, cs, sn, a.v_scale);
 }
 
 // Sixteen consecutive elements, as two of the units above.
@@ -329,55 +337,55 @@ __device__ __forceinline__ void store_read16(T *dst, const Raw16<KV> &r, float s
     }
 }
 
-// A warp takes one token, or one of `parts` equal parts of its steps, k's and then
-// v's: a lane 16 elements of a head, kBatch steps' loads in flight.  38.8k e4m3 tokens:
-// 37.7 us (35.2 us of bytes); 8 elements a lane, whose scales and addresses then come
-// twice as often, 39.6; 12 CTAs an SM of 2 steps 38.0.
+// Rows (token, head) in order: a warp takes kSteps x (32 / kLanes) of them, K and V of
+// each, a lane 16 elements, all loads in flight.  38.8k e4m3 tokens of 8 heads: 36.5 us
+// (35.2 us of bytes); 8 elements a lane, whose scales and addresses then come twice as
+// often, 39.6; a warp to a token leaves lanes without a head where there are few (38.4k
+// bf16 tokens of one head 6.2 us, 13.1 so).
 template <class T, class KV, int D>
 __global__ void __launch_bounds__(kThreads, 8) kv_read_kernel(const ReadArgs a) {
-    constexpr int kLanes = D / 16, kHeads = 32 / kLanes, kBatch = sizeof(T) == 4 ? 2 : 4;
-    const int lane = threadIdx.x % 32;
-    const int64_t job = static_cast<int64_t>(blockIdx.x) * kWarps + threadIdx.x / 32;
-    const int64_t t = a.parts == 1 ? job : job / a.parts;
-    if (t >= a.num_tokens) return;
-    const int part = static_cast<int>(job - t * a.parts);
-    const int kv_steps = (a.num_kv_heads + kHeads - 1) / kHeads, steps = 2 * kv_steps;
-    const int first = steps * part / a.parts, last = steps * (part + 1) / a.parts;
-    const int u = lane % kLanes, mine = lane / kLanes;
+    constexpr int kLanes = D / 16, kGroups = 32 / kLanes, kSteps = sizeof(T) == 4 ? 1 : 2;
+    const int lane = threadIdx.x % 32, u = lane % kLanes, mine = lane / kLanes;
+    // the warp's first row: token t0, head h0
+    const int64_t row0 = (static_cast<int64_t>(blockIdx.x) * kWarps + threadIdx.x / 32) * (kGroups * kSteps);
+    int64_t t0;
+    if (a.short_rows)
+        t0 = static_cast<uint32_t>(row0) / static_cast<uint32_t>(a.num_kv_heads);
+    else
+        t0 = row0 / a.num_kv_heads;
+    const uint32_t h0 = static_cast<uint32_t>(row0 - t0 * a.num_kv_heads);
     dev::grid_wait();
-    const int64_t slot = a.slots[t];
-    const bool live = slot >= 0 && slot < a.num_slots;
-    const int64_t row = (slot / kPageSize * a.num_kv_heads * kPageSize + slot % kPageSize) * D + 16 * u;
-    for (int s0 = first; s0 < last; s0 += kBatch) {
-        Raw16<KV> r[kBatch];
-        float scale[kBatch];
+    Raw16<KV> rk[kSteps], rv[kSteps];
+    float ks[kSteps], vs[kSteps];
+    int64_t t[kSteps];
+    int h[kSteps];
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-            const int s = s0 + b;
-            const bool is_k = s < kv_steps;
-            const int h = (is_k ? s : s - kv_steps) * kHeads + mine;
-            if (s < last && h < a.num_kv_heads) {
-                if (live) {
-                    r[b] = load16(static_cast<const KV *>(is_k ? a.k_pages : a.v_pages) + row +
-                                  static_cast<int64_t>(h) * kPageSize * D);
-                    if constexpr (kScaled<KV>) scale[b] = (is_k ? a.k_scale : a.v_scale)[h];
-                } else {
-                    r[b] = Raw16<KV>{};
-                    scale[b] = 0.f;
-                }
+    for (int b = 0; b < kSteps; ++b) {
+        const uint32_t at = h0 + b * kGroups + mine, over = a.heads_magic ? __umulhi(at, a.heads_magic) : at;
+        t[b] = t0 + over;
+        h[b] = static_cast<int>(at - over * a.num_kv_heads);
+        if (t[b] >= a.num_tokens) continue;
+        const int64_t slot = a.slots[t[b]];
+        if (slot >= 0 && slot < a.num_slots) {
+            const int64_t at_row = ((slot / kPageSize * a.num_kv_heads + h[b]) * kPageSize + slot % kPageSize) * D + 16 * u;
+            rk[b] = load16(static_cast<const KV *>(a.k_pages) + at_row);
+            rv[b] = load16(static_cast<const KV *>(a.v_pages) + at_row);
+            if constexpr (kScaled<KV>) {
+                ks[b] = a.k_scale[h[b]];
+                vs[b] = a.v_scale[h[b]];
             }
+        } else {
+            rk[b] = rv[b] = Raw16<KV>{};
+            ks[b] = vs[b] = 0.f;
         }
+    }
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b) {
-            const int s = s0 + b;
-            const bool is_k = s < kv_steps;
-            const int h = (is_k ? s : s - kv_steps) * kHeads + mine;
-            if (s >= last || h >= a.num_kv_heads) continue;
-            T *dst = static_cast<T *>(const_cast<void *>(is_k ? a.k.data : a.v.data)) +
-                     t * (is_k ? a.k.token_stride : a.v.token_stride) +
-                     h * (is_k ? a.k.head_stride : a.v.head_stride) + 16 * u;
-            store_read16<T, KV>(dst, r[b], scale[b], a.aligned);
-        }
+    for (int b = 0; b < kSteps; ++b) {
+        if (t[b] >= a.num_tokens) continue;
+        T *k = static_cast<T *>(const_cast<void *>(a.k.data)) + t[b] * a.k.token_stride + h[b] * a.k.head_stride;
+        T *v = static_cast<T *>(const_cast<void *>(a.v.data)) + t[b] * a.v.token_stride + h[b] * a.v.head_stride;
+        store_read16<T, KV>(k + 16 * u, rk[b], ks[b], a.aligned);
+        store_read16<T, KV>(v + 16 * u, rv[b], vs[b], a.aligned);
     }
 }
 
@@ -482,39 +490,58 @@ __global__ void __launch_bounds__(kThreads, 8) kv_scales_kernel(const ScalesArgs
     }
 }
 
-// Parts of a token: one, or as many as it takes to fill the card, of one step at
-// least (16 tokens of a decode step: 1.8 us in parts, 4.5 whole; a prompt whole, whose
-// parts would make the same angles several times).
+// Parts of a token: as many as one wave of warps has room for, of one step at least
+// (1200 tokens of 32 / 8 heads: 5.5 us in 2 parts, 7.1 in 3, whose warps wait for a
+// place and make the same angles again).
 int parts_of(int64_t tokens, int steps) {
-    const int64_t want = (kFullWarps + tokens - 1) / tokens;
-    return static_cast<int>(want < steps ? want : steps);
+    const int64_t room = kFullWarps / tokens;
+    return static_cast<int>(room < 1 ? 1 : room < steps ? room : steps);
 }
 
 unsigned blocks_of(int64_t tokens, int parts) {
     return static_cast<unsigned>((tokens * parts + kWarps - 1) / kWarps);
 }
 
-template <class T, class KV, int D>
+template <class T, class KV, int D, int G>
 cudaError_t launch_write(WriteArgs a, cudaStream_t s) {
-    constexpr int kHeads = 32 / (D / 16);
-    const int steps = (a.num_q_heads + kHeads - 1) / kHeads + 2 * ((a.num_kv_heads + kHeads - 1) / kHeads);
-    a.parts = parts_of(a.num_tokens, steps);
-    return launch_dependent(true,
-                            a.rot.interleaved ? kv_write_kernel<T, KV, D, true> : kv_write_kernel<T, KV, D, false>,
-                            dim3(blocks_of(a.num_tokens, a.parts)), dim3(kThreads), 0, s, a);
+    constexpr int kTeams = 512 / D / G;
+    const int steps = (a.num_q_heads + G - 1) / G + 2 * ((a.num_kv_heads + G - 1) / G);
+    a.parts = kTeams == 1 ? parts_of(a.num_tokens, steps) : 1;
+    return launch_dependent(
+        true, a.rot.interleaved ? kv_write_kernel<T, KV, D, true, G> : kv_write_kernel<T, KV, D, false, G>,
+        dim3(blocks_of((a.num_tokens + kTeams - 1) / kTeams, a.parts)), dim3(kThreads), 0, s, a);
+}
+
+// A token to a warp, or two or four of them where a token is fewer than 10 steps and
+// the card stays full: a short warp spends its life on its slot, its angles and its
+// first loads (9728 bf16 tokens of 128 elements, a token, two and four to a warp: 15.0,
+// 12.1, 10.6 us at 8 / 2 heads, 4 to 12 steps; 22.8, 19.7, 19.7 at 16 / 4; 35, 36, 36
+// at 24 / 8, 10 to 40 steps).
+template <class T, class KV, int D>
+cudaError_t launch_write(const WriteArgs &a, cudaStream_t s) {
+    constexpr int kGroups = 512 / D;
+    auto few = [&](int g) {
+        return (a.num_q_heads + g - 1) / g + 2 * ((a.num_kv_heads + g - 1) / g) < 10 &&
+               a.num_tokens >= static_cast<int64_t>(2 * kGroups / g) * kFullWarps;
+    };
+    if (!few(kGroups)) return launch_write<T, KV, D, kGroups>(a, s);
+    return few(kGroups / 2) ? launch_write<T, KV, D, kGroups / 4>(a, s)
+                            : launch_write<T, KV, D, kGroups / 2>(a, s);
 }
 
 template <class T, class KV, int D>
 cudaError_t launch_read(ReadArgs a, cudaStream_t s) {
-    constexpr int kHeads = 32 / (D / 16);
+    constexpr int kRowsOfCta = kWarps * (32 / (D / 16)) * (sizeof(T) == 4 ? 1 : 2);
     uintptr_t odd = 0;
     for (const Rows *r : {&a.k, &a.v})
         odd |= reinterpret_cast<uintptr_t>(r->data) | static_cast<uintptr_t>(r->token_stride * sizeof(T)) |
                static_cast<uintptr_t>(r->head_stride * sizeof(T));
     a.aligned = odd % 32 == 0;
-    a.parts = parts_of(a.num_tokens, 2 * ((a.num_kv_heads + kHeads - 1) / kHeads));
-    return launch_dependent(true, kv_read_kernel<T, KV, D>, dim3(blocks_of(a.num_tokens, a.parts)),
-                            dim3(kThreads), 0, s, a);
+    a.heads_magic = static_cast<uint32_t>(((1ull << 32) + a.num_kv_heads - 1) / a.num_kv_heads);
+    const int64_t rows = a.num_tokens * a.num_kv_heads, ctas = (rows + kRowsOfCta - 1) / kRowsOfCta;
+    if (ctas > INT32_MAX) return cudaErrorInvalidValue;
+    a.short_rows = ctas * kRowsOfCta <= UINT32_MAX;
+    return launch_dependent(true, kv_read_kernel<T, KV, D>, dim3(static_cast<unsigned>(ctas)), dim3(kThreads), 0, s, a);
 }
 
 // ---------------------------------------------------------------- arguments
