@@ -97,6 +97,22 @@ def test_write_strides(mode, pad, heads_first):
     check_write(4, mode, 8, 2, 128, 40, HALVES, pad=pad, heads_first=heads_first)
 
 
+@pytest.mark.parametrize("mode,d", [("bf16", 128), ("bf16", 64), ("fp32", 128), ("fp32", 64), ("fp8", 128)])
+@pytest.mark.parametrize("heads,kind", [((8, 2), MIXED), ((1, 1), AXES), ((5, 1), None), ((12, 3), (16, 4, False))])
+@pytest.mark.parametrize("tokens", [4865, 9733])
+def test_write_many_tokens_of_few_heads(mode, d, heads, kind, tokens):
+    """Two and four tokens share a warp; the last warp lacks some."""
+    if kind is not None and kind[0] > d:
+        pytest.skip("rotary_dim above head_dim")
+    check_write(tokens, mode, *heads, d, tokens, kind, pad=8)
+
+
+@pytest.mark.parametrize("tokens,heads", [(700, 32), (1217, 16), (2433, 24), (3041, 8)])
+def test_write_around_a_wave_of_warps(tokens, heads):
+    """Where the parts of a token change in number, and end."""
+    check_write(9, "bf16", heads, 8, 128, tokens, HALVES)
+
+
 @pytest.mark.parametrize("lo,hi", [(2 ** 20, 2 ** 20 + 5000), (-2 ** 24, 2 ** 24)])
 def test_write_far_positions(lo, hi):
     """Up to 2^24 the reduced angle is as near as at the origin."""
@@ -193,6 +209,25 @@ def test_read(mode, d, tokens):
         else:
             assert torch.equal(rows[live].double(), ref)
         assert (rows[~live] == 0).all()
+
+
+@pytest.mark.parametrize("mode,d", [("bf16", 128), ("bf16", 64), ("fp32", 128), ("fp32", 64), ("fp8", 128)])
+@pytest.mark.parametrize("heads", [1, 2, 5, 17, 33, 300])
+@pytest.mark.parametrize("tokens", [1, 3, 131])
+def test_read_head_counts(mode, d, heads, tokens):
+    """A warp's rows begin at any head, end in another token, and pass several."""
+    gen = R.generator(heads)
+    pools = [x.to(R.POOL[mode]) for x in torch.randn((2, 5, heads, R.PAGE, d), generator=gen, device="cuda")]
+    scales = [torch.full((heads,), 1.0, device="cuda") * 2.0 ** torch.randint(-3, 4, (heads,), generator=gen,
+                                                                             device="cuda") for _ in range(2)]
+    slots = torch.randint(-1, 5 * R.PAGE + 1, (tokens,), generator=gen, device="cuda", dtype=torch.int32)
+    live = (slots >= 0) & (slots < 5 * R.PAGE)
+    got = kv_read(*pools, slots, k_scale=scales[0], v_scale=scales[1])
+    for pool, scale, rows in zip(pools, scales, got):
+        ref = R.at(pool, slots[live]).view(pool.dtype).float()
+        if mode == "fp8":
+            ref = ref * scale.view(-1, 1)            # (a power of 2: the product is exact in bf16)
+        assert torch.equal(rows[live].float(), ref) and (rows[~live] == 0).all()
 
 
 @pytest.mark.parametrize("mode", ["bf16", "fp8", "fp32"])
