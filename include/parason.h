@@ -523,8 +523,8 @@ parason_status parason_kv_write(const parason_attn_config *cfg, int64_t num_toke
  * k_scale[h]), v_out likewise, in the type of the mode's rows (an exact copy
  * in PARASON_BF16 and PARASON_FP32 modes).  A slot outside the pool gives a
  * row of zeros; a slot may be read any number of times.  k_out and v_out are
- * rows [num_tokens, H_kv, head_dim] whose strides keep them apart (at least
- * head_dim elements between heads and between tokens).  Keys come out as they
+ * rows [num_tokens, H_kv, head_dim] whose strides keep them apart: the smaller
+ * one at least head_dim, the larger one past all rows of the smaller.  Keys come out as they
  * were written: parason_kv_write with the difference of positions moves them
  * to others.  Launch, capture and errors as parason_kv_write.
  */

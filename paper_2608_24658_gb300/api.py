@@ -437,8 +437,13 @@ def _token_rows(name, t, shape, dtype, dev, out=False) -> bytes:
         step = 16 // t.element_size()
         if es != 1 or at % 16 or (ts % step and tokens > 1) or (hs % step and heads > 1):
             raise ValueError(f"{name} must have contiguous elements and start and strides of 16 bytes")
-        if out and ((ts < dim and tokens > 1) or (hs < dim and heads > 1)):
-            raise ValueError(f"{name} must not overlap itself")
+        if out:
+            # the nearer dimension's stride is a row at least, the other's its whole reach
+            reach = dim
+            for stride, n in sorted(((ts, tokens), (hs, heads))):
+                if n > 1 and stride < reach:
+                    raise ValueError(f"{name} must not overlap itself")
+                reach += (n - 1) * stride
     return _lib.ROWS.pack(at, ts, hs)
 
 

@@ -553,7 +553,13 @@ parason_status check_rows(const parason_rows *r, int64_t tokens, int32_t heads, 
     const int64_t strides[2] = {tokens > 1 ? r->token_stride : d, heads > 1 ? r->head_stride : d};
     for (int64_t st : strides) {
         if (st < 0 || st * elem % 16 != 0) return PARASON_EINVAL;
-        if (out && st < d) return PARASON_EINVAL;
+    }
+    if (out) {
+        // rows apart: the nearer dimension's stride is a row at least, the other's its whole reach
+        const int64_t counts[2] = {tokens, heads};
+        const int near = (tokens > 1 && strides[0] <= strides[1]) || heads <= 1 ? 0 : 1;
+        if (strides[near] < d) return PARASON_EINVAL;
+        if (counts[1 - near] > 1 && (strides[1 - near] - d) / strides[near] < counts[near] - 1) return PARASON_EINVAL;
     }
     return PARASON_OK;
 }

@@ -245,6 +245,18 @@ def test_read_into_views(mode):
         assert torch.equal(rows.float(), R.at(pool, slots).view(pool.dtype).float())
 
 
+@pytest.mark.parametrize("mode", ["bf16", "fp8", "fp32"])
+def test_read_into_heads_first(mode):
+    gen = R.generator(12)
+    pools = [x.to(R.POOL[mode]) for x in torch.randn((2, 4, 2, R.PAGE, 128), generator=gen, device="cuda")]
+    one = torch.ones(2, device="cuda")
+    slots = torch.randint(0, 64, (20,), generator=gen, device="cuda", dtype=torch.int32)
+    k, v = (torch.empty((2, 20, 136), dtype=R.ROWS[mode], device="cuda")[..., 8:].transpose(0, 1) for _ in range(2))
+    kv_read(*pools, slots, k=k, v=v, k_scale=one, v_scale=one)
+    for pool, rows in zip(pools, (k, v)):
+        assert torch.equal(rows.float(), R.at(pool, slots).view(pool.dtype).float())
+
+
 def test_read_every_e4m3_code():
     codes = torch.arange(256, dtype=torch.uint8, device="cuda").view(2, 1, 1, 128).expand(2, 1, R.PAGE, 128)
     pool = codes.contiguous().view(torch.float8_e4m3fn)
@@ -440,6 +452,10 @@ def test_refusals_of_the_binding():
         kv_read(*pools, slots.view(2, 2))
     with pytest.raises(ValueError):
         kv_read(*pools, slots, k=k[:1].expand(4, 2, 128))
+    for strides in ((128, 128, 1), (248, 128, 1), (136, 528, 1), (256, 256, 1)):
+        with pytest.raises(ValueError):
+            kv_read(*pools, slots, k=torch.zeros(2048, dtype=torch.bfloat16,
+                                                 device="cuda").as_strided((4, 2, 128), strides))
     with pytest.raises(ValueError):
         kv_scales(k.float(), k.float())
     with pytest.raises(ValueError):

@@ -114,7 +114,10 @@ def test_axis_past_the_axes(lib):
 
 @pytest.mark.parametrize("bad", [
     dict(n=-1), dict(slots=None), dict(kp=None), dict(vp=A + 8), dict(k=None), dict(v=_rows(A + 4)),
-    dict(k=_rows(ts=64)), dict(v=_rows(hs=64)), dict(k=_rows(ts=0)), dict(k=_rows(hs=0))])
+    dict(k=_rows(ts=64)), dict(v=_rows(hs=64)), dict(k=_rows(ts=0)), dict(k=_rows(hs=0)),
+    # rows that reach into the next token's, or the next head's (heads first)
+    dict(k=_rows(ts=128, hs=128)), dict(v=_rows(ts=248, hs=128)), dict(k=_rows(ts=136, hs=528)),
+    dict(v=_rows(ts=1024, hs=1024))])
 def test_read_refusals(lib, bad):
     assert _read(lib, **bad) == _lib.EINVAL
     assert _read(lib, n=0, slots=None, kp=None, vp=None, k=None, v=None) == _lib.OK
