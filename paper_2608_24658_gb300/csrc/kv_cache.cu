@@ -149,31 +149,41 @@ __device__ __forceinline__ float2 turn(const RotaryArgs &r, int64_t t, int i) {
     return make_float2(c, s);
 }
 
-// Heads of one kind (q, k or v) of a token, steps [s0, s1) of G heads each: this lane's
-// two chunks of each are at src + e and dst + e, e0 and e1 (elements), a step further
-// `src_step` and `dst_step`.  The loads of kBatch steps go together.
-template <class T, class Out, int G, bool ROTATE, int kBatch>
-__device__ __forceinline__ void write_heads(const T *src, int64_t src_step, Out *dst, int64_t dst_step, int s0, int s1,
-                                            int heads, int mine, int e0, int e1, bool interleaved, bool rotates,
-                                            const unsigned long long (&cs)[4], const unsigned long long (&sn)[4],
-                                            const float *scale) {
-    src += s0 * src_step;
-    dst += s0 * dst_step;
-    for (int s = s0; s < s1; s += kBatch, src += kBatch * src_step, dst += kBatch * dst_step) {
-        Raw8<T> r0[kBatch], r1[kBatch];
+// This lane's two chunks of kBatch steps (of G heads of one kind, q, k or v, of a token)
+// from step s on, loaded together: src + e0 and src + e1, a step further `src_step`.
+template <class T, int kBatch>
+struct Batch {
+    Raw8<T> r0[kBatch], r1[kBatch];
+    template <int G>
+    __device__ __forceinline__ void load(const T *src, int64_t src_step, int s, int s1, int heads, int mine, int e0,
+                                         int e1) {
+        src += s * src_step;
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
             if (s + b >= s1 || (s + b) * G + mine >= heads) break;
             r0[b] = load8(src + b * src_step + e0);
             r1[b] = load8(src + b * src_step + e1);
         }
+    }
+};
+
+// Heads of one kind, steps [s0, s1): rotated, scaled, rounded, stored at dst + e0 and
+// dst + e1, a step further `dst_step`.  `batch` holds the first steps already.
+template <class T, class Out, int G, bool ROTATE, int kBatch>
+__device__ __forceinline__ void write_heads(Batch<T, kBatch> &batch, const T *src, int64_t src_step, Out *dst,
+                                            int64_t dst_step, int s0, int s1, int heads, int mine, int e0, int e1,
+                                            bool interleaved, bool rotates, const unsigned long long (&cs)[4],
+                                            const unsigned long long (&sn)[4], const float *scale) {
+    dst += s0 * dst_step;
+    for (int s = s0; s < s1; s += kBatch, dst += kBatch * dst_step) {
+        if (s != s0) batch.template load<G>(src, src_step, s, s1, heads, mine, e0, e1);
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
             const int h = (s + b) * G + mine;
             if (s + b >= s1 || h >= heads) break;
             float x0[8], x1[8];
-            unpack8(r0[b], x0);
-            unpack8(r1[b], x1);
+            unpack8(batch.r0[b], x0);
+            unpack8(batch.r1[b], x1);
             if (ROTATE && rotates) {
                 // (p c - q s, p s + q c), two pairs an instruction
 #pragma unroll
@@ -235,6 +245,21 @@ __global__ void __launch_bounds__(kThreads) kv_write_kernel(const WriteArgs a) {
     dev::grid_wait();
     const int64_t slot = there ? a.slots[t] : -1;
 
+    // the first loads go out before the angles are made
+    const T *q = static_cast<const T *>(a.q.data) + t * a.q.token_stride + mine * a.q.head_stride;
+    const T *k = static_cast<const T *>(a.k.data) + t * a.k.token_stride + mine * a.k.head_stride;
+    const T *v = static_cast<const T *>(a.v.data) + t * a.v.token_stride + mine * a.v.head_stride;
+    const int64_t q_step = G * a.q.head_stride, k_step = G * a.k.head_stride, v_step = G * a.v.head_stride;
+    const int k0 = max(first, q_steps) - q_steps, k1 = min(last - q_steps, kv_steps);
+    const int v0 = max(first - q_steps - kv_steps, 0), v1 = last - q_steps - kv_steps;
+    Batch<T, kBatch> batch;
+    if (there) {
+        if (first < q_steps)
+            batch.template load<G>(q, q_step, first, min(last, q_steps), a.num_q_heads, mine, e0, e1);
+        else if (k0 < k1)
+            batch.template load<G>(k, k_step, k0, k1, a.num_kv_heads, mine, e0, e1);
+    }
+
     unsigned long long cs[4], sn[4];
     if (a.rot.half && first < q_steps + kv_steps) {
         float2 own[kMake];
@@ -256,24 +281,22 @@ __global__ void __launch_bounds__(kThreads) kv_write_kernel(const WriteArgs a) {
     }
     if (!there) return;
     if (first < q_steps)
-        write_heads<T, T, G, true, kBatch>(
-            static_cast<const T *>(a.q.data) + t * a.q.token_stride + mine * a.q.head_stride, G * a.q.head_stride,
-            static_cast<T *>(a.q_out) + (t * a.num_q_heads + mine) * D, G * D, first, min(last, q_steps),
-            a.num_q_heads, mine, e0, e1, INTERLEAVED, rotates, cs, sn, nullptr);
+        write_heads<T, T, G, true, kBatch>(batch, q, q_step, static_cast<T *>(a.q_out) + (t * a.num_q_heads + mine) * D,
+                                           G * D, first, min(last, q_steps), a.num_q_heads, mine, e0, e1, INTERLEAVED,
+                                           rotates, cs, sn, nullptr);
     if (slot < 0 || slot >= a.num_slots || last <= q_steps) return;
     const int64_t row = (slot / kPageSize * a.num_kv_heads + mine) * kPageSize * D + slot % kPageSize * D;
-    const int k0 = max(first, q_steps) - q_steps, k1 = min(last - q_steps, kv_steps);
-    if (k0 < k1)
-        write_heads<T, KV, G, true, kBatch>(
-            static_cast<const T *>(a.k.data) + t * a.k.token_stride + mine * a.k.head_stride, G * a.k.head_stride,
-            static_cast<KV *>(a.k_pages) + row, G * kPageSize * D, k0, k1, a.num_kv_heads, mine, e0, e1,
-            INTERLEAVED, rotates, cs, sn, a.k_scale);
-    const int v0 = max(first - q_steps - kv_steps, 0), v1 = last - q_steps - kv_steps;
-    if (v0 < v1)
-        write_heads<T, KV, G, false, kBatch>(
-            static_cast<const T *>(a.v.data) + t * a.v.token_stride + mine * a.v.head_stride, G * a.v.head_stride,
-            static_cast<KV *>(a.v_pages) + row, G * kPageSize * D, v0, v1, a.num_kv_heads, mine, 16 * u,
-            16 * u + 8, INTERLEAVED, false, cs, sn, a.v_scale);
+    if (k0 < k1) {
+        if (first < q_steps) batch.template load<G>(k, k_step, k0, k1, a.num_kv_heads, mine, e0, e1);
+        write_heads<T, KV, G, true, kBatch>(batch, k, k_step, static_cast<KV *>(a.k_pages) + row, G * kPageSize * D, k0,
+                                            k1, a.num_kv_heads, mine, e0, e1, INTERLEAVED, rotates, cs, sn, a.k_scale);
+    }
+    if (v0 < v1) {
+        batch.template load<G>(v, v_step, v0, v1, a.num_kv_heads, mine, 16 * u, 16 * u + 8);
+        write_heads<T, KV, G, false, kBatch>(batch, v, v_step, static_cast<KV *>(a.v_pages) + row, G * kPageSize * D,
+                                             v0, v1, a.num_kv_heads, mine, 16 * u, 16 * u + 8, INTERLEAVED, false, cs,
+                                             sn, a.v_scale);
+    }
 }
 
 // Sixteen consecutive elements, as two of the units above.
