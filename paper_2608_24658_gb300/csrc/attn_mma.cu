@@ -186,6 +186,22 @@ __device__ __forceinline__ int out_col(int nt, int e, int tig) {
         return 16 * (2 * tig + (e & 1)) + nt;
 }
 
+// Scores of tokens past the page's last one, which may be anything, to 0: a capped
+// score can share its reciprocal with its neighbour.
+__device__ __forceinline__ void clear_past(float (&sc)[2][4], int valid, int tig) {
+    if (valid >= kPageSize) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if ((e >> 2) * 8 + 2 * tig + (e & 1) >= valid) sc[e >> 2][e & 3] = 0.f;
+}
+
+// The same of a transposed step's scores.
+__device__ __forceinline__ void clear_past_t(float (&x)[4], int valid, int gid) {
+    if (valid >= kPageSize) return;
+    if (gid >= valid) x[0] = x[1] = 0.f;
+    if (gid + 8 >= valid) x[2] = x[3] = 0.f;
+}
+
 // Online softmax over one page's scores s (two n-tiles of 8 tokens), then
 // rescale o; returns P packed as the A operand of the PV MMA.
 template <int D, class KV>
@@ -193,7 +209,10 @@ __device__ __forceinline__ void softmax_page(float (&sc)[2][4], int valid, float
                                              float cap_log2, bool &cap_large, WarpState<D> &st,
                                              int tig, uint32_t (&pa)[4]) {
     // (under a cap scale_log2 is the factor into the tanh)
-    if constexpr (KV::kCap == kCapRef) cap_scores(sc, cap_large, CapFactors(scale_log2, cap_log2));
+    if constexpr (KV::kCap == kCapRef) {
+        clear_past(sc, valid, tig);
+        cap_scores<1>(sc, cap_large, CapFactors(scale_log2, cap_log2));
+    }
     float x[2][4];
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt)
@@ -258,9 +277,9 @@ template <int D>
 __device__ __forceinline__ void softmax_page_free(float (&sc)[2][4], int valid, const CapFactors &cap,
                                                   bool &cap_large, WarpState<D> &st, int tig,
                                                   uint32_t (&pa)[4]) {
-    LaneP<8> put;
-    cap_free(*reinterpret_cast<const float(*)[8]>(&sc), 8, false, cap_large, cap, put);
-    float(&p)[8] = put.p;
+    clear_past(sc, valid, tig);
+    cap_free_scores<1>(sc, cap_large, cap);
+    float(&p)[8] = *reinterpret_cast<float(*)[8]>(&sc);
     if (valid < kPageSize) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -565,7 +584,8 @@ __device__ __forceinline__ void pages_step_t(const uint32_t *kbase, const uint32
     if constexpr (KV::kCap == kCapRef) {
 #pragma unroll
         for (int p = 0; p < NP; ++p) scores_t<D, KV>(kbase[p], qb, lane, x[p]);
-        cap_scores(x, cap_large, CapFactors(scale_log2, cap_log2));
+        clear_past_t(x[NP - 1], valid_last, lane >> 2);
+        cap_scores<2>(x, cap_large, CapFactors(scale_log2, cap_log2));
     }
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
@@ -639,13 +659,13 @@ __device__ __forceinline__ void pages_step_t_free(const uint32_t *kbase, const u
     float x[NP][4];
 #pragma unroll
     for (int p = 0; p < NP; ++p) scores_t<D, KV>(kbase[p], qb, lane, x[p]);
-    LaneP<4 * NP> put;
-    cap_free(*reinterpret_cast<const float(*)[4 * NP]>(&x), 4 * NP, false, cap_large, cap, put);
+    clear_past_t(x[NP - 1], valid_last, gid);
+    cap_free_scores<2>(x, cap_large, cap);
     st.m[0] = st.m[1] = 0.f;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
         const int valid = p == NP - 1 ? valid_last : kPageSize;
-        float(&y)[4] = *reinterpret_cast<float(*)[4]>(put.p + 4 * p);
+        float(&y)[4] = x[p];
         if (valid < kPageSize) {
             if (gid >= valid) y[0] = y[1] = 0.f;
             if (gid + 8 >= valid) y[2] = y[3] = 0.f;
@@ -1486,8 +1506,9 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
                         ok = false;
                         break;
                     }
+                    const float m_ref = cap_reference(m_use, hi);
                     PackedRow<kF8> row{ps};
-                    cap_exponentials(xs, valid, valid < kTcBlockTokens, large, dev::f32x2(-m_use, -m_use), cap, row);
+                    cap_exponentials(xs, valid, valid < kTcBlockTokens, large, dev::f32x2(-m_ref, -m_ref), cap, row);
                     float l0, l1;
                     dev::f32x2_split(row.sum, l0, l1);
                     l += l0 + l1;
@@ -2180,8 +2201,9 @@ __device__ void prefix_cta_tc_pair(const KvMaps *maps, const AttnArgs &a, uint8_
                             ok = false;
                             break;
                         }
+                        const float m_ref = cap_reference(m_use, hi);
                         PackedRow<false> row{ps};
-                        cap_exponentials(xs, valid, valid < kTcBlockTokens, large, dev::f32x2(-m_use, -m_use), cap, row);
+                        cap_exponentials(xs, valid, valid < kTcBlockTokens, large, dev::f32x2(-m_ref, -m_ref), cap, row);
                         float l0, l1;
                         dev::f32x2_split(row.sum, l0, l1);
                         l += l0 + l1;

@@ -199,6 +199,20 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return m;
 }
 
+// max(a, b, c), NaN if one of them is
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+    float m;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(m) : "f"(a), "f"(b), "f"(c));
+    return m;
+}
+
+// min(a, b), NaN if one of them is
+__device__ __forceinline__ float min_nan(float a, float b) {
+    float m;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+    return m;
+}
+
 // min(a, b, c)
 __device__ __forceinline__ float min3(float a, float b, float c) {
     float m;

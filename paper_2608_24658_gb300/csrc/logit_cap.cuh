@@ -76,29 +76,37 @@ __device__ __forceinline__ unsigned long long cap_series(unsigned long long x, u
     return dev::fma_f32x2(u, q, nm);
 }
 
-// cap_log2 tanh - m of two scores by the exponential (base: cap_log2 - m in both
-// halves).  They share one reciprocal, 1 / (d0 d1), of factors that are cut at 2^60
-// (tanh is 1 there in fp32, infinities included).
-__device__ __forceinline__ unsigned long long cap_exp_pair(float x0, float x1, const CapFactors &f,
-                                                           unsigned long long base) {
+// 1 + e^(2u) of two scores, whose factors are cut at 2^60 (tanh is 1 there in fp32,
+// infinities included).  A NaN stays one, or with CUT is cut like infinity.
+template <bool CUT>
+__device__ __forceinline__ void cap_divisors(float x0, float x1, const CapFactors &f, float &d0, float &d1) {
     float w0, w1;
     dev::f32x2_split(dev::mul_f32x2(dev::f32x2(x0, x1), f.two_u), w0, w1);
+    w0 = CUT ? fminf(w0, 60.f) : dev::min_nan(w0, 60.f);
+    w1 = CUT ? fminf(w1, 60.f) : dev::min_nan(w1, 60.f);
+    dev::f32x2_split(dev::add_f32x2(dev::f32x2(dev::fast_exp2(w0), dev::fast_exp2(w1)), dev::f32x2(1.f, 1.f)), d0, d1);
+}
+
+// cap_log2 tanh - m of two scores by the exponential (base: cap_log2 - m in both
+// halves).  They share one reciprocal, 1 / (d0 d1), and so a NaN, which only scores of
+// one row may that both count; with CUT the caller makes the row NaN.
+template <bool CUT>
+__device__ __forceinline__ unsigned long long cap_exp_pair(float x0, float x1, const CapFactors &f,
+                                                           unsigned long long base) {
     float d0, d1;
-    dev::f32x2_split(dev::add_f32x2(dev::f32x2(dev::fast_exp2(fminf(w0, 60.f)), dev::fast_exp2(fminf(w1, 60.f))),
-                                    dev::f32x2(1.f, 1.f)),
-                     d0, d1);
+    cap_divisors<CUT>(x0, x1, f, d0, d1);
     const float r = fast_rcp(d0 * d1);
     return dev::fma_f32x2(dev::f32x2(r * d1, r * d0), dev::f32x2(-2.f * f.cap, -2.f * f.cap), base);
 }
 
-// The same with every score in the form its own size asks for.
+// The same (with CUT) with every score in the form its own size asks for.
 __device__ __forceinline__ void cap_pair(float x0, float x1, unsigned long long nm, const CapFactors &f,
                                          float &y0, float &y1) {
     unsigned long long t;
     float s0, s1, t0, t1, e0, e1;
     dev::f32x2_split(cap_series(dev::f32x2(x0, x1), nm, f, t), s0, s1);
     dev::f32x2_split(t, t0, t1);
-    dev::f32x2_split(cap_exp_pair(x0, x1, f, dev::add_f32x2(dev::f32x2(f.cap, f.cap), nm)), e0, e1);
+    dev::f32x2_split(cap_exp_pair<true>(x0, x1, f, dev::add_f32x2(dev::f32x2(f.cap, f.cap), nm)), e0, e1);
     y0 = t0 < kCapSeries * kCapSeries ? s0 : e0;
     y1 = t1 < kCapSeries * kCapSeries ? s1 : e1;
 }
@@ -110,19 +118,34 @@ __device__ __forceinline__ float cap_one(float x, const CapFactors &f) {
     return y;
 }
 
+// Four scores of an mma.sync accumulator, in place, by the exponential.  Scores 0 and
+// 1, and 2 and 3, are of one row (APART 1), or 0 and 2, and 1 and 3 (APART 2).
+template <int APART>
+__device__ __forceinline__ void cap_exp_quad(float (&x)[4], const CapFactors &f) {
+    const unsigned long long base = dev::f32x2(f.cap, f.cap), twice = dev::f32x2(-2.f * f.cap, -2.f * f.cap);
+    float d[4];
+    cap_divisors<false>(x[0], x[1], f, d[0], d[1]);
+    cap_divisors<false>(x[2], x[3], f, d[2], d[3]);
+    const float ra = fast_rcp(d[0] * d[APART]), rb = fast_rcp(d[3] * d[3 - APART]);
+    const float n0 = ra * d[APART], n1 = APART == 1 ? ra * d[0] : rb * d[3];
+    const float n2 = APART == 1 ? rb * d[3] : ra * d[0], n3 = rb * d[3 - APART];
+    dev::f32x2_split(dev::fma_f32x2(dev::f32x2(n0, n1), twice, base), x[0], x[1]);
+    dev::f32x2_split(dev::fma_f32x2(dev::f32x2(n2, n3), twice, base), x[2], x[3]);
+}
+
 // ---------------------------------------------------------------- mma.sync steps
-// A lane's M x N scores to logits in place; the whole warp calls.  large: whether
-// the warp's last scores had one at kCapSeries or past it.  The series runs on
-// trust, and the scores are done again if one turns up.
-template <int M, int N>
-__device__ __forceinline__ void cap_scores(float (&x)[M][N], bool &large, const CapFactors &f) {
-    static_assert(N % 2 == 0, "scores come in pairs");
+// A lane's M accumulators of scores to logits in place; the whole warp calls.
+// Scores that do not count are finite.  large: whether the warp's last scores had one
+// at kCapSeries or past it.  The series runs on trust, and the scores are done again
+// if one turns up.
+template <int APART, int M>
+__device__ __forceinline__ void cap_scores(float (&x)[M][4], bool &large, const CapFactors &f) {
     if (!large) {
-        float most = 0.f, y[M][N];
+        float most = 0.f, y[M][4];
 #pragma unroll
         for (int i = 0; i < M; ++i)
 #pragma unroll
-            for (int j = 0; j < N; j += 2) {
+            for (int j = 0; j < 4; j += 2) {
                 unsigned long long t;
                 float t0, t1;
                 dev::f32x2_split(cap_series(dev::f32x2(x[i][j], x[i][j + 1]), 0ull, f, t), y[i][j], y[i][j + 1]);
@@ -134,28 +157,50 @@ __device__ __forceinline__ void cap_scores(float (&x)[M][N], bool &large, const 
 #pragma unroll
             for (int i = 0; i < M; ++i)
 #pragma unroll
-                for (int j = 0; j < N; ++j) x[i][j] = y[i][j];
+                for (int j = 0; j < 4; ++j) x[i][j] = y[i][j];
             return;
         }
     }
     float most = 0.f;
 #pragma unroll
-    for (int i = 0; i < M; ++i)
+    for (int i = 0; i < M; ++i) {
+        most = dev::max3(dev::max3(most, fabsf(x[i][0]), fabsf(x[i][1])), fabsf(x[i][2]), fabsf(x[i][3]));
+        float e[4] = {x[i][0], x[i][1], x[i][2], x[i][3]};
+        cap_exp_quad<APART>(e, f);
+        if (f.cap > kCapFreeLog2) {
 #pragma unroll
-        for (int j = 0; j < N; j += 2) {
-            const float x0 = x[i][j], x1 = x[i][j + 1];
-            most = dev::max3(most, fabsf(x0), fabsf(x1));
-            if (f.cap <= kCapFreeLog2)
-                dev::f32x2_split(cap_exp_pair(x0, x1, f, dev::f32x2(f.cap, f.cap)), x[i][j], x[i][j + 1]);
-            else
-                cap_pair(x0, x1, dev::f32x2(0.f, 0.f), f, x[i][j], x[i][j + 1]);
+            for (int j = 0; j < 4; j += 2) {
+                unsigned long long t;
+                float s0, s1, t0, t1;
+                dev::f32x2_split(cap_series(dev::f32x2(x[i][j], x[i][j + 1]), 0ull, f, t), s0, s1);
+                dev::f32x2_split(t, t0, t1);
+                if (t0 < kCapSeries * kCapSeries) e[j] = s0;
+                if (t1 < kCapSeries * kCapSeries) e[j + 1] = s1;
+            }
         }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[i][j] = e[j];
+    }
     large = __any_sync(0xffffffffu, most * f.to >= kCapSeries);
 }
 
-// ---------------------------------------------------------------- no reference
-// P = 2^x (caps up to kCapFreeLog2).  The exponential form serves all scores of a
-// block where one is large: its absolute error, 2e-7 cap, is 1e-5 at most there.
+// The same to P = 2^x (caps up to kCapFreeLog2).
+template <int APART, int M>
+__device__ __forceinline__ void cap_free_scores(float (&x)[M][4], bool &large, const CapFactors &f) {
+    cap_scores<APART>(x, large, f);
+#pragma unroll
+    for (int i = 0; i < M; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[i][j] = dev::fast_exp2(x[i][j]);
+}
+
+// ---------------------------------------------------------------- tiles
+// A tile's softmax keeps a row's scores as they come from TMEM and caps them
+// inside the loop that takes their exponentials, where the series (FMA pipe)
+// runs beside the exponentials (MUFU); tanh is monotone, so the row's largest
+// logit is that of its largest score, and no pass over the logits is needed
+// before.  Keys a row does not see (from `seen` on) are left out of the range
+// and get P = 0, whatever their score.
 
 __device__ __forceinline__ float score_of(float x) { return x; }
 __device__ __forceinline__ float score_of(uint32_t x) { return __uint_as_float(x); }
@@ -172,22 +217,12 @@ struct PackedRow {
     }
 };
 
-// The P of a lane's N scores as they are (mma.sync steps).
-template <int N>
-struct LaneP {
-    float p[N];
-    __device__ __forceinline__ void start() {}
-    __device__ __forceinline__ void operator()(int c, float p0, float p1) {
-        p[2 * c] = p0;
-        p[2 * c + 1] = p1;
-    }
-};
-
-// P of N scores, the first `seen` of which count (hidden: for some lane of the warp
-// not all), handed pair by pair to `put`
-// (again from `start()` on where a block is done twice); the whole warp calls.
-// large: whether the warp's last block had a score at kCapSeries or past it.  The
-// series runs on trust, and the block is done again if one turns up.
+// P = 2^x (caps up to kCapFreeLog2) of N scores, the first `seen` of which count
+// (hidden: for some lane of the warp not all), handed pair by pair to `put` (again from
+// `start()` on where a block is done twice); the whole warp calls.  large: whether the
+// warp's last block had a score at kCapSeries or past it.  The series runs on trust,
+// and the block is done again if one turns up; the exponential form then serves all of
+// its scores: its absolute error, 2e-7 cap, is 1e-5 at most there.
 template <int N, class X, class Put>
 __device__ __forceinline__ void cap_free(const X (&x)[N], int seen, bool hidden, bool &large, const CapFactors &f,
                                          Put &put) {
@@ -196,9 +231,10 @@ __device__ __forceinline__ void cap_free(const X (&x)[N], int seen, bool hidden,
     if (hidden) {
 #pragma unroll
         for (int c = 0; c < N / 2; ++c) {
+            const float x0 = score_of(x[2 * c]), x1 = score_of(x[2 * c + 1]);
             float e0, e1;
-            dev::f32x2_split(cap_exp_pair(score_of(x[2 * c]), score_of(x[2 * c + 1]), f, base), e0, e1);
-            const float p0 = dev::fast_exp2(e0), p1 = dev::fast_exp2(e1);
+            dev::f32x2_split(cap_exp_pair<true>(x0, x1, f, base), e0, e1);
+            const float p0 = x0 == x0 ? dev::fast_exp2(e0) : x0, p1 = x1 == x1 ? dev::fast_exp2(e1) : x1;
             put(c, 2 * c < seen ? p0 : 0.f, 2 * c + 1 < seen ? p1 : 0.f);
         }
         return;
@@ -224,28 +260,21 @@ __device__ __forceinline__ void cap_free(const X (&x)[N], int seen, bool hidden,
     for (int c = 0; c < N / 2; ++c) {
         const float x0 = score_of(x[2 * c]), x1 = score_of(x[2 * c + 1]);
         float e0, e1;
-        dev::f32x2_split(cap_exp_pair(x0, x1, f, base), e0, e1);
+        dev::f32x2_split(cap_exp_pair<false>(x0, x1, f, base), e0, e1);
         most = dev::max3(most, fabsf(x0), fabsf(x1));
         put(c, dev::fast_exp2(e0), dev::fast_exp2(e1));
     }
     large = __any_sync(0xffffffffu, most * f.to >= kCapSeries);
 }
 
-// ---------------------------------------------------------------- tiles
-// A tile's softmax keeps a row's scores as they come from TMEM and caps them
-// inside the loop that takes their exponentials, where the series (FMA pipe)
-// runs beside the exponentials (MUFU); tanh is monotone, so the row's largest
-// logit is that of its largest score, and no pass over the logits is needed
-// before.  Keys a row does not see (from `seen` on) are left out of the range
-// and get P = 0, whatever their score.
-
-// Widen [lo, hi] by N scores of which the first `seen` count.
+// Widen [lo, hi] by N scores of which the first `seen` count; hi is NaN from the
+// first NaN on, and cap_reference then too.
 template <int N, class X>
 __device__ __forceinline__ void cap_range(const X (&x)[N], int seen, float &lo, float &hi) {
     if (seen >= N) {
 #pragma unroll
         for (int j = 0; j < N; j += 2) {
-            hi = dev::max3(hi, score_of(x[j]), score_of(x[j + 1]));
+            hi = dev::max3_nan(hi, score_of(x[j]), score_of(x[j + 1]));
             lo = dev::min3(lo, score_of(x[j]), score_of(x[j + 1]));
         }
     } else {
@@ -253,10 +282,15 @@ __device__ __forceinline__ void cap_range(const X (&x)[N], int seen, float &lo, 
         for (int j = 0; j < N; ++j) {
             float s = score_of(x[j]);
             hide_from(s, j, seen);                     // -inf from `seen` on
-            hi = fmaxf(hi, s);
+            hi = dev::max3_nan(hi, s, s);
             lo = j < seen ? fminf(lo, score_of(x[j])) : lo;
         }
     }
+}
+
+// What a row's P is taken against: 0 if it has seen no key, NaN if one is.
+__device__ __forceinline__ float cap_reference(float m_use, float hi) {
+    return hi != hi ? hi : m_use == -INFINITY ? 0.f : m_use;
 }
 
 // P of N scores, the first `seen` of which count (hidden: for some lane of the warp
@@ -280,7 +314,7 @@ __device__ __forceinline__ void cap_exponentials(const X (&x)[N], int seen, bool
 #pragma unroll
         for (int c = 0; c < N / 2; ++c) {
             float e0, e1;
-            dev::f32x2_split(cap_exp_pair(score_of(x[2 * c]), score_of(x[2 * c + 1]), f, base), e0, e1);
+            dev::f32x2_split(cap_exp_pair<true>(score_of(x[2 * c]), score_of(x[2 * c + 1]), f, base), e0, e1);
             put(c, dev::fast_exp2(e0), dev::fast_exp2(e1));
         }
     } else {

@@ -473,7 +473,7 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                         const bool large = __any_sync(0xffffffffu, fmaxf(hi, -lo) * cap.to >= kCapSeries);
                         // (a row that has seen no key has P = 0 against any reference)
                         raise_reference(hi < lo ? -INFINITY : cap_one(hi, cap));
-                        const float m_ref = m_use == -INFINITY ? 0.f : m_use;
+                        const float m_ref = cap_reference(m_use, hi);
                         const unsigned long long nmp = dev::f32x2(-m_ref, -m_ref);
 #pragma unroll 1
                         for (int c = 0; c < 4; ++c) {

@@ -260,3 +260,60 @@ def test_prefill_every_key_at_minus_the_cap(mode):
             out, lse = plan.decode_tree(tree)
             plan.check()
         C.check(tree, cap, out, lse, prefill=True)
+
+
+def nan_key(tree, node, token, head):
+    """One element of a key becomes NaN."""
+    page = int(tree.page_ids[int(tree.node_page_ptr[node]) + token // 16])
+    if tree.mode == "fp8":
+        tree.k_pages.view(torch.uint8)[page, head, token % 16, 5] = 0x7F
+    else:
+        tree.k_pages[page, head, token % 16, 5] = math.nan
+
+
+def check_with_nans(tree, cap, out, lse, rows, prefill=False, all_nan=False):
+    """NaN exactly where 64-bit arithmetic has it (`rows` heads of rows), the rest as near as ever.  (The merge gives
+    a row whose sum is NaN lse = -inf, and one whose every score is NaN may pass for one without keys: without a cap
+    too.)"""
+    ref_o, ref_l, tol_o, tol_l = C.capped(tree, cap, prefill)
+    lost = ref_l.isnan()
+    assert int(lost.sum()) == rows
+    assert (out[lost].isnan() | (all_nan & (out[lost] == 0))).all() and not lse[lost].isfinite().any()
+    assert ((out.double() - ref_o).abs() <= tol_o)[~lost].all() and ((lse.double() - ref_l).abs() <= tol_l)[~lost].all()
+
+
+NAN_CAPS = [(0.0, 1.0), (50.0, 1.0), (10.0, 8.0), (90.0, 1.0), (60.0, 30.0)]
+
+
+@pytest.mark.parametrize("mode", ["bf16", "fp8", "fp32"])
+@pytest.mark.parametrize("heads", [(8, 2), (32, 2)])
+@pytest.mark.parametrize("cap,q_std", NAN_CAPS)
+def test_nan_stays_in_its_rows(mode, heads, cap, q_std):
+    """A NaN score is no score at the cap: it makes its own row NaN and no other."""
+    def tree():
+        return W.build_tree("nan", [-1] + [0] * 6, [600, 40, 33, 5, 70, 16, 1], [1, 2, 3, 4, 5, 6],
+                            num_q_heads=heads[0], num_kv_heads=heads[1], head_dim=128, mode=mode, seed=11, q_std=q_std,
+                            device="cuda", tail_value=math.nan)
+    group = heads[0] // heads[1]
+    own, shared, query = tree(), tree(), tree()
+    nan_key(own, 2, 32, 1)                       # the last key of one branch
+    check_with_nans(own, cap, *decode(own, cap), group)
+    nan_key(shared, 0, 577, 0)
+    check_with_nans(shared, cap, *decode(shared, cap), 6 * group)
+    if mode != "fp8":
+        query.q[3, 1, 7] = math.nan
+        check_with_nans(query, cap, *decode(query, cap), 1, all_nan=True)
+
+
+@pytest.mark.parametrize("mode", ["bf16", "fp8"])
+@pytest.mark.parametrize("cap,q_std", NAN_CAPS)
+def test_prefill_nan_stays_in_its_rows(mode, cap, q_std):
+    """Of a chunk's NaN key: in the rows that see it."""
+    for node, token, rows in ((0, 130, (90 + 30) * 4), (1, 70, (90 - 70) * 4), (2, 0, 30 * 4)):
+        tree = W.build_prefill("nanp", [-1, 0, 0], [300, 90, 30], [1, 2], num_q_heads=8, num_kv_heads=2, head_dim=128,
+                               mode=mode, seed=12, q_std=q_std, device="cuda", tail_value=math.nan)
+        nan_key(tree, node, token, 1)
+        with Plan.for_prefill(tree, logit_cap=cap) as plan:
+            out, lse = plan.decode_tree(tree)
+            plan.check()
+        check_with_nans(tree, cap, out, lse, rows, prefill=True)
