@@ -52,7 +52,10 @@
 //    gives each thread one 16-byte chunk of V's columns.
 //
 // Scores are kept in the log2 domain: x = scale*log2(e)*<q,k>, so a partial
-// is m = max x, l = sum 2^(x-m), o = sum 2^(x-m) v (unnormalised).
+// is m = max x, l = sum 2^(x-m), o = sum 2^(x-m) v (unnormalised).  Under a logit
+// cap (logit_cap.cuh) x = cap*log2(e)*tanh(scale/cap*<q,k>); bf16 KV with caps up
+// to 50 then keeps m = 0 (CappedFree), everything else the running maximum
+// (CappedRef).
 #include <mutex>
 
 #include "device_common.cuh"

@@ -25,6 +25,17 @@
 // exponential per score and a reciprocal per two.  Models keep nearly all logits
 // far below their cap, so a warp votes: if no score of the block reaches
 // kCapSeries, it runs the series alone.
+//
+// Measured, one GB300, uncapped -> capped with scores of N(0, 1) -> with scores 8
+// times that, at a cap of 50: 16 trials of a request 30.6 -> 31.6 -> 32.6 us; 128
+// branches of a 32k prefix 130 -> 144 -> 186; 64 branches in e4m3 97 -> 127 -> 170;
+// join prefill 505 -> 635 -> 775, in e4m3 662 -> 893 -> 1141; fork prefill 39 -> 50 ->
+// 57.  The compiler's tanhf for every score took 45 us for the 16 trials and 1687
+// for the join.
+//
+// A NaN score makes its row NaN, as it does without a cap.  The exponential form
+// shares a reciprocal between two scores, so they are of one row, or the NaN is cut
+// in it and put back (CUT).
 #pragma once
 
 #include "device_common.cuh"
@@ -35,7 +46,8 @@ namespace {
 
 // what an attention kernel does to its logits
 enum : int { kCapNone = 0, kCapFree = 1, kCapRef = 2 };
-// 2^73 is what a cap of 50 needs; sums of 2^20 tokens stay finite for |v| to 2^34
+// 2^73 is what a cap of 50 needs; sums of 2^20 tokens stay finite for |v| to 2^34.
+// (The join takes 635 us below and 826 above, 128 branches of a 32k prefix 144 and 180.)
 constexpr float kCapFreeLog2 = 73.f;
 
 constexpr float kCapSeries = 0.4f;

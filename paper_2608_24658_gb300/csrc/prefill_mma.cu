@@ -58,6 +58,16 @@
 // warps (832 us), or widening over the raw bytes in a ring of 5 slots (932
 // us), are slower than a ring of 4 raw and 3 widened slots.
 //
+// Logit caps (logit_cap.cuh) have instantiations of their own.  Without a
+// reference (kCapFree) a half of a block has nothing to wait for but its own S:
+// the issuer sends the halves of S apart, and the S of the next block's half right
+// behind the PV of this one's, so that a tile's softmax has one half while the
+// tensor core has the other.  The join takes 635 us (682 with whole blocks), the
+// fork 50; with e4m3 KV, whose P needs a reference, the join takes 893.  The softmax
+// warps' instructions bound it: 6 packed ones per two scores come to those without
+// a cap, the maxima go.  Tried and slower: two warpgroups a tile (643 -> 682 us),
+// both halves unrolled (760), the next scores loaded early (698).
+//
 // Every wait is bounded (%globaltimer); on expiry the error is recorded, the
 // copies in flight land, TMEM is freed and the CTA exits.
 #include <mutex>

@@ -144,19 +144,6 @@ __device__ __forceinline__ void st32(uint32_t taddr, const uint32_t (&r)[32]) {
 }
 
 // The same for 16 columns.
-// Wait for the warp's tcgen05.ld, which wrote `r`: what uses the values comes
-// after (for loads that run while the warp works on other registers).
-__device__ __forceinline__ void wait_ld(uint32_t (&r)[64]) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-    // (an empty statement that every value passes through, 16 at a time)
-#pragma unroll
-    for (int i = 0; i < 64; i += 16)
-        asm volatile(""
-                     : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]),
-                       "+r"(r[i + 6]), "+r"(r[i + 7]), "+r"(r[i + 8]), "+r"(r[i + 9]), "+r"(r[i + 10]),
-                       "+r"(r[i + 11]), "+r"(r[i + 12]), "+r"(r[i + 13]), "+r"(r[i + 14]), "+r"(r[i + 15]));
-}
-
 __device__ __forceinline__ void ld16(uint32_t taddr, uint32_t (&r)[16]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
