@@ -131,9 +131,8 @@ constexpr bool kScaled = sizeof(KV) == 1;
 constexpr int kThreads = 128;            // 4 warps, each of them on its own
 constexpr int kWarps = kThreads / 32;
 
-// Warps that fill the card with a few loads each in flight (152 SMs): work that
-// makes fewer is cut up further.
-constexpr int kFullWarps = 152 * 16;
+// Warps of kv_write that run at once, one wave (152 SMs, 5 CTAs each by registers).
+constexpr int kWaveWarps = 152 * 5 * kWarps;
 
 // cos and sin of positions[axis] * inv_freq[i].  The frequency is held as turns a
 // position modulo 1, in 2^-64: the low 64 bits of its product with the position are
@@ -517,7 +516,7 @@ __global__ void __launch_bounds__(kThreads, 8) kv_scales_kernel(const ScalesArgs
 // (1200 tokens of 32 / 8 heads: 5.5 us in 2 parts, 7.1 in 3, whose warps wait for a
 // place and make the same angles again).
 int parts_of(int64_t tokens, int steps) {
-    const int64_t room = kFullWarps / tokens;
+    const int64_t room = kWaveWarps / tokens;
     return static_cast<int>(room < 1 ? 1 : room < steps ? room : steps);
 }
 
@@ -536,7 +535,7 @@ cudaError_t launch_write(WriteArgs a, cudaStream_t s) {
 }
 
 // A token to a warp, or two or four of them where a token is fewer than 10 steps and
-// the card stays full: a short warp spends its life on its slot, its angles and its
+// their warps would pass one wave: a short warp spends its life on its slot, its angles and its
 // first loads (9728 bf16 tokens of 128 elements, a token, two and four to a warp: 15.0,
 // 12.1, 10.6 us at 8 / 2 heads, 4 to 12 steps; 22.8, 19.7, 19.7 at 16 / 4; 35, 36, 36
 // at 24 / 8, 10 to 40 steps).
@@ -545,7 +544,7 @@ cudaError_t launch_write(const WriteArgs &a, cudaStream_t s) {
     constexpr int kGroups = 512 / D;
     auto few = [&](int g) {
         return (a.num_q_heads + g - 1) / g + 2 * ((a.num_kv_heads + g - 1) / g) < 10 &&
-               a.num_tokens >= static_cast<int64_t>(2 * kGroups / g) * kFullWarps;
+               a.num_tokens > static_cast<int64_t>(kGroups / g) * kWaveWarps;
     };
     if (!few(kGroups)) return launch_write<T, KV, D, kGroups>(a, s);
     return few(kGroups / 2) ? launch_write<T, KV, D, kGroups / 4>(a, s)
