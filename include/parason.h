@@ -509,7 +509,8 @@ parason_status parason_rotary_turns(const float *inv_freq, int32_t n, uint64_t *
  * ones.  PARASON_EINVAL for a bad config, a NULL or misaligned pointer, a
  * negative count, a rotary description outside the above;
  * PARASON_EUNSUPPORTED if num_physical_pages * H_kv * 16 passes int32 (as in
- * parason_attn_plan) or there are more than 16384 heads; PARASON_ECUDA if the launch fails.
+ * parason_attn_plan), there are more than 16384 heads, or (parason_kv_read, _scales)
+ * num_tokens * H_kv passes 2^34; PARASON_ECUDA if the launch fails.
  */
 parason_status parason_kv_write(const parason_attn_config *cfg, int64_t num_tokens,
                                 const parason_rows *q, const parason_rows *k,

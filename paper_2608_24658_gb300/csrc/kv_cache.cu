@@ -18,6 +18,7 @@ namespace {
 constexpr int kMaxAxes = 4;
 constexpr float kE4m3Max = 448.f;
 constexpr int kMaxHeads = 16384;         // of q, and of k: what the kernels' counters hold
+constexpr int64_t kMaxRows = 1ll << 34;  // tokens times kv heads: what a grid holds (16 and more a CTA)
 
 struct Rows {
     const void *data;
@@ -435,21 +436,24 @@ __device__ __forceinline__ uint32_t most_bf16x2(uint32_t a, uint32_t b) {
 // at 2^63; a NaN's partner counts in max |x|, which squares below 2^-126 leave to it
 // too.  Positive floats order as their bits do, so the maxima meet in integer
 // atomics, whose order does not matter; max / 448 is the max of the quotients, since
-// rounding is monotone.
+// rounding is monotone.  A CTA's warps meet first: an atomic a warp took 33 us for the
+// 21.3 of 32768 tokens of 8 heads (19.8 us of bytes).  CTAs go over the heads of the
+// same tokens first, whose rows are neighbours (head by head 22.3 us).
 constexpr int kScaleRows = 16;
 template <int D>
 __global__ void __launch_bounds__(kThreads, 8) kv_scales_kernel(const ScalesArgs a) {
     constexpr int kLanes = D / 16, kRows = 32 / kLanes, kBatch = kScaleRows / kRows;
     __shared__ float part[kWarps];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int h = blockIdx.y;
-    const bool is_k = blockIdx.z == 0;
+    const uint32_t rest = blockIdx.x / static_cast<uint32_t>(a.num_kv_heads);
+    const int h = blockIdx.x - rest * a.num_kv_heads;
+    const bool is_k = rest % 2 == 0;
     const Rows &src = is_k ? a.k : a.v;
     const int half = is_k ? a.half : 0;
     const int u = lane % kLanes;
     const bool rotates = 8 * u < half, halves = rotates && !a.interleaved;
     const int e0 = halves ? 8 * u : 16 * u, e1 = e0 + (halves ? half : 8);
-    const int64_t t0 = (static_cast<int64_t>(blockIdx.x) * kWarps + warp) * kScaleRows + lane / kLanes;
+    const int64_t t0 = (static_cast<int64_t>(rest / 2) * kWarps + warp) * kScaleRows + lane / kLanes;
     const __nv_bfloat16 *x = static_cast<const __nv_bfloat16 *>(src.data) + h * src.head_stride;
     dev::grid_wait();
     uint32_t one = 0;                    // max |x| of even and of odd elements
@@ -502,8 +506,7 @@ __global__ void __launch_bounds__(kThreads, 8) kv_scales_kernel(const ScalesArgs
         }
     }
     m = fmaxf(m, sqrtf(pair));
-#pragma unroll
-    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    m = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(m)));
     if (lane == 0) part[warp] = m;
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -561,7 +564,6 @@ cudaError_t launch_read(ReadArgs a, cudaStream_t s) {
     a.aligned = odd % 32 == 0;
     a.heads_magic = static_cast<uint32_t>(((1ull << 32) + a.num_kv_heads - 1) / a.num_kv_heads);
     const int64_t rows = a.num_tokens * a.num_kv_heads, ctas = (rows + kRowsOfCta - 1) / kRowsOfCta;
-    if (ctas > INT32_MAX) return cudaErrorInvalidValue;
     a.short_rows = ctas * kRowsOfCta <= UINT32_MAX;
     return launch_dependent(true, kv_read_kernel<T, KV, D>, dim3(static_cast<unsigned>(ctas)), dim3(kThreads), 0, s, a);
 }
@@ -749,6 +751,7 @@ extern "C" parason_status parason_kv_read(const parason_attn_config *cfg, int64_
     a.num_tokens = num_tokens;
     a.num_slots = num_physical_pages * kPageSize;
     a.num_kv_heads = cfg->num_kv_heads;
+    if (num_tokens * cfg->num_kv_heads > kMaxRows) return PARASON_EUNSUPPORTED;
     const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     if (cfg->mode == PARASON_FP8_E4M3_KV) return launched(launch_read<__nv_bfloat16, __nv_fp8_e4m3, 128>(a, s));
     if (cfg->mode == PARASON_FP32)
@@ -769,6 +772,7 @@ extern "C" parason_status parason_kv_scales(const parason_attn_config *cfg, int6
     if (accumulate != 0 && accumulate != 1) return PARASON_EINVAL;
     if (!k_scale || !v_scale || misaligned(k_scale, 4) || misaligned(v_scale, 4) || misaligned(slots, 4))
         return PARASON_EINVAL;
+    if (num_tokens * cfg->num_kv_heads > kMaxRows) return PARASON_EUNSUPPORTED;
     ScalesArgs a{};
     if (num_tokens > 0) {
         if ((st = check_rows(k, num_tokens, cfg->num_kv_heads, cfg->head_dim, 2, false)) != PARASON_OK) return st;
@@ -790,9 +794,7 @@ extern "C" parason_status parason_kv_scales(const parason_attn_config *cfg, int6
         if (e != cudaSuccess) return PARASON_ECUDA;
     }
     if (num_tokens == 0) return PARASON_OK;
-    return launched(launch_dependent(true, kv_scales_kernel<128>,
-                                     dim3(static_cast<unsigned>((num_tokens + kWarps * kScaleRows - 1) /
-                                                                (kWarps * kScaleRows)),
-                                          static_cast<unsigned>(cfg->num_kv_heads), 2),
-                                     dim3(kThreads), 0, s, a));
+    const int64_t ctas = (num_tokens + kWarps * kScaleRows - 1) / (kWarps * kScaleRows) * 2 * cfg->num_kv_heads;
+    return launched(launch_dependent(true, kv_scales_kernel<128>, dim3(static_cast<unsigned>(ctas)), dim3(kThreads), 0,
+                                     s, a));
 }

@@ -112,6 +112,14 @@ def test_axis_past_the_axes(lib):
     assert _write(lib, n=0, k=None, v=None, slots=None, kp=None, vp=None) == _lib.OK
 
 
+def test_more_rows_than_a_grid(lib):
+    n = 2 ** 31 - 1
+    big = [_rows(ts=4096, hs=128) for _ in range(2)]
+    for mode, call in (("bf16", _read), ("fp8", _scales)):
+        cfg = _cfg(mode, num_q_heads=16, num_kv_heads=16)
+        assert call(lib, cfg, n=n, k=big[0], v=big[1]) == _lib.EUNSUPPORTED
+
+
 @pytest.mark.parametrize("bad", [
     dict(n=-1), dict(slots=None), dict(kp=None), dict(vp=A + 8), dict(k=None), dict(v=_rows(A + 4)),
     dict(k=_rows(ts=64)), dict(v=_rows(hs=64)), dict(k=_rows(ts=0)), dict(k=_rows(hs=0)),
