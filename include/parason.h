@@ -426,7 +426,8 @@ parason_status parason_lse_merge(const void *o_a, const float *lse_a, const void
  * disjoint keys is their capped result over both.
  * With bf16 KV and caps up to 50 the kernels sum e^s as it is, without a
  * running maximum: results are finite for V up to a magnitude of 2^34 where all
- * of 2^20 keys are at the cap, and e^(cap - s) times more where they are below.
+ * of 2^20 keys are at the cap, and e^(cap - s) times more where they are below;
+ * where all of a row's keys are at minus the cap, V below 2^-53 may count as 0.
  */
 parason_status parason_plan_set_logit_cap(parason_plan plan, float cap);
 
