@@ -474,7 +474,8 @@ typedef struct {
     int32_t num_axes;          /* 1..4: e.g. text 1; time, height, width 3          */
     const uint8_t *freq_axis;  /* host [rotary_dim / 2], each < num_axes; NULL: 0   */
     const uint64_t *turns;     /* device [rotary_dim / 2]                           */
-    const int32_t *positions;  /* device [num_axes][num_tokens], negative ones too  */
+    const int32_t *positions;  /* device [num_axes][num_tokens], negative ones too
+                                  (not looked at without tokens)                    */
     int64_t position_stride;   /* elements between the axes' rows                   */
 } parason_rotary;
 

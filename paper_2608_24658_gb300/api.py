@@ -385,7 +385,8 @@ class Rotary:
     (i, i + rotary_dim / 2) or, ``interleaved``, (2 i, 2 i + 1).  ``axes`` gives
     each frequency's position axis (0..3; one axis if None): positions are then
     [number of axes, tokens], e.g. time, height and width of image tokens.  The
-    frequencies are read once, here (parason_rotary_turns)."""
+    frequencies are read once, here (parason_rotary_turns).  It owns device
+    memory that a captured write reads at every replay."""
 
     def __init__(self, inv_freq: torch.Tensor, axes=None, interleaved: bool = False):
         if (inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_cuda

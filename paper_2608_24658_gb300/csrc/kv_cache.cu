@@ -607,12 +607,12 @@ parason_status check_pairs(const parason_rotary *r, int32_t d) {
     return PARASON_OK;
 }
 
-parason_status to_rotary(const parason_rotary *r, int32_t d, RotaryArgs *out) {
+parason_status to_rotary(const parason_rotary *r, int64_t tokens, int32_t d, RotaryArgs *out) {
     *out = RotaryArgs{};
     if (!r) return PARASON_OK;
     const parason_status st = check_pairs(r, d);
     if (st != PARASON_OK) return st;
-    if (r->num_axes < 1 || r->num_axes > kMaxAxes || !r->turns || !r->positions ||
+    if (r->num_axes < 1 || r->num_axes > kMaxAxes || !r->turns || (!r->positions && tokens > 0) ||
         misaligned(r->turns, 8) || misaligned(r->positions, 4) || (r->num_axes > 1 && r->position_stride < 0))
         return PARASON_EINVAL;
     out->turns = r->turns;
@@ -688,7 +688,7 @@ extern "C" parason_status parason_kv_write(const parason_attn_config *cfg, int64
     const int32_t d = cfg->head_dim;
     const int elem = cfg->mode == PARASON_FP32 ? 4 : 2;
     WriteArgs a{};
-    if ((st = to_rotary(rotary, d, &a.rot)) != PARASON_OK) return st;
+    if ((st = to_rotary(rotary, num_tokens, d, &a.rot)) != PARASON_OK) return st;
     if (num_tokens == 0) return PARASON_OK;
     if ((st = check_rows(k, num_tokens, cfg->num_kv_heads, d, elem, false)) != PARASON_OK) return st;
     if ((st = check_rows(v, num_tokens, cfg->num_kv_heads, d, elem, false)) != PARASON_OK) return st;

@@ -191,6 +191,19 @@ def test_empty_batch_and_empty_pool():
     assert all((t == 0).all() for t in kv_read(*empty, slots))
 
 
+@pytest.mark.parametrize("mode", ["bf16", "fp8", "fp32"])
+@pytest.mark.parametrize("kind", [HALVES, AXES])
+def test_empty_batch_with_positions(mode, kind):
+    rotary, _ = R.rotary_of(kind)
+    k = torch.empty((0, 2, 128), dtype=R.ROWS[mode], device="cuda")
+    pools = R.pool(R.generator(10), 2, 2, 128, mode)
+    one = torch.ones(2, device="cuda")
+    shape = (0,) if rotary.num_axes == 1 else (rotary.num_axes, 0)
+    out = kv_write(k, k, *pools, torch.empty(0, dtype=torch.int32, device="cuda"), q=k, rotary=rotary,
+                   positions=torch.empty(shape, dtype=torch.int32, device="cuda"), k_scale=one, v_scale=one)
+    assert out.shape == (0, 2, 128)
+
+
 @pytest.mark.parametrize("mode,d", [("bf16", 128), ("bf16", 64), ("fp32", 128), ("fp32", 64), ("fp8", 128)])
 @pytest.mark.parametrize("tokens", [1, 2, 15, 64, 129, 1000])
 def test_read(mode, d, tokens):

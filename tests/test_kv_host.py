@@ -110,6 +110,7 @@ def test_axis_past_the_axes(lib):
     # the rotary part is checked for an empty batch too, which launches nothing
     assert _write(lib, n=0, rot=rot) == _lib.EINVAL
     assert _write(lib, n=0, k=None, v=None, slots=None, kp=None, vp=None) == _lib.OK
+    assert _write(lib, n=0, k=None, v=None, slots=None, kp=None, vp=None, rot=_rot(positions=None)) == _lib.OK
 
 
 def test_more_rows_than_a_grid(lib):
