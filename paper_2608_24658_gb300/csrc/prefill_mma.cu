@@ -983,7 +983,7 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                     // Caps without a reference: the halves of a block go their own ways,
                     // S, P, PV, and the next block's S of the half over its P, so that a
                     // tile's softmax has one half while the tensor core has the other
-                    // (join prefill 682 -> 642 us; half by half of both tiles 652).
+                    // (join prefill 682 -> 635 us; half by half of both tiles 652).
                     for (int h = 0; h < 2; ++h)
                         for (int t = 0; t <= last; ++t) issue_half(t, h, st, h == 1 && t == last);
                     advance();
