@@ -1491,7 +1491,7 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
                         tc::ld32(tS + 32 * c, xs);
                         tc::wait_ld();
                         PackedRow<false> row{ps};
-                        cap_free(xs, valid - 32 * c, valid < kTcBlockTokens, cap_large, cap, row);
+                        cap_free<1>(xs, valid - 32 * c, valid < kTcBlockTokens, cap_large, cap, row);
                         float l0, l1;
                         dev::f32x2_split(row.sum, l0, l1);
                         l += l0 + l1;
@@ -2186,7 +2186,7 @@ __device__ void prefix_cta_tc_pair(const KvMaps *maps, const AttnArgs &a, uint8_
                         tc::ld32(tS + 32, *reinterpret_cast<uint32_t(*)[32]>(xs + 32));
                         tc::wait_ld();
                         PackedRow<false> row{ps};
-                        cap_free(xs, valid, valid < kTcBlockTokens, cap_large, cap, row);
+                        cap_free<1>(xs, valid, valid < kTcBlockTokens, cap_large, cap, row);
                         float l0, l1;
                         dev::f32x2_split(row.sum, l0, l1);
                         l += l0 + l1;

@@ -76,16 +76,33 @@ struct CapFactors {
     }
 };
 
-// cap_log2 tanh - m of two scores by the series (nm: -m in both halves); u^2 of
-// both in `t`.
+// cap_log2 tanh - m of K pairs of scores by the series (nm: -m in both halves), in place,
+// step by step; u^2 of them in `t`.
+template <int K>
+__device__ __forceinline__ void cap_series(unsigned long long (&x)[K], unsigned long long nm, const CapFactors &f,
+                                           unsigned long long (&t)[K]) {
+    unsigned long long q[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) x[k] = dev::mul_f32x2(x[k], f.to_cap);
+#pragma unroll
+    for (int k = 0; k < K; ++k) t[k] = dev::mul_f32x2(x[k], x[k]);
+#pragma unroll
+    for (int k = 0; k < K; ++k) q[k] = dev::fma_f32x2(t[k], f.a3, f.a2);
+#pragma unroll
+    for (int k = 0; k < K; ++k) q[k] = dev::fma_f32x2(q[k], t[k], f.a1);
+#pragma unroll
+    for (int k = 0; k < K; ++k) q[k] = dev::fma_f32x2(q[k], t[k], f.c0);
+#pragma unroll
+    for (int k = 0; k < K; ++k) x[k] = dev::fma_f32x2(x[k], q[k], nm);
+}
+
+// One pair.
 __device__ __forceinline__ unsigned long long cap_series(unsigned long long x, unsigned long long nm,
                                                          const CapFactors &f, unsigned long long &t) {
-    const unsigned long long u = dev::mul_f32x2(x, f.to_cap);
-    t = dev::mul_f32x2(u, u);
-    unsigned long long q = dev::fma_f32x2(t, f.a3, f.a2);
-    q = dev::fma_f32x2(q, t, f.a1);
-    q = dev::fma_f32x2(q, t, f.c0);
-    return dev::fma_f32x2(u, q, nm);
+    unsigned long long y[1] = {x}, t1[1];
+    cap_series<1>(y, nm, f, t1);
+    t = t1[0];
+    return y[0];
 }
 
 // 1 + e^(2u) of two scores, whose factors are cut at 2^60 (tanh is 1 there in fp32,
@@ -234,8 +251,11 @@ struct PackedRow {
 // `start()` on where a block is done twice); the whole warp calls.  large: whether the
 // warp's last block had a score at kCapSeries or past it.  The series runs on trust,
 // and the block is done again if one turns up; the exponential form then serves all of
-// its scores: its absolute error, 2e-7 cap, is 1e-5 at most there.
-template <int N, class X, class Put>
+// its scores: its absolute error, 2e-7 cap, is 1e-5 at most there.  K pairs go through
+// the series side by side: 8 in the prefill, whose registers hold them (join 636 us with
+// 1, 651 with 4, 626 with 8, 628 with 16), 1 in the decode tiles (128 branches of a 32k
+// prefix 144 with 1, 149 with 8).
+template <int K, int N, class X, class Put>
 __device__ __forceinline__ void cap_free(const X (&x)[N], int seen, bool hidden, bool &large, const CapFactors &f,
                                          Put &put) {
     const unsigned long long base = dev::f32x2(f.cap, f.cap);
@@ -254,14 +274,19 @@ __device__ __forceinline__ void cap_free(const X (&x)[N], int seen, bool hidden,
     if (!large) {
         float most = 0.f;
 #pragma unroll
-        for (int c = 0; c < N / 2; ++c) {
-            const float x0 = score_of(x[2 * c]), x1 = score_of(x[2 * c + 1]);
-            unsigned long long t;
-            float e0, e1, t0, t1;
-            dev::f32x2_split(cap_series(dev::f32x2(x0, x1), 0ull, f, t), e0, e1);
-            dev::f32x2_split(t, t0, t1);
-            most = dev::max3(most, t0, t1);
-            put(c, dev::fast_exp2(e0), dev::fast_exp2(e1));
+        for (int c = 0; c < N / 2; c += K) {
+            unsigned long long y[K], t[K];
+#pragma unroll
+            for (int k = 0; k < K; ++k) y[k] = dev::f32x2(score_of(x[2 * (c + k)]), score_of(x[2 * (c + k) + 1]));
+            cap_series<K>(y, 0ull, f, t);
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                float e0, e1, t0, t1;
+                dev::f32x2_split(y[k], e0, e1);
+                dev::f32x2_split(t[k], t0, t1);
+                most = dev::max3(most, t0, t1);
+                put(c + k, dev::fast_exp2(e0), dev::fast_exp2(e1));
+            }
         }
         large = __any_sync(0xffffffffu, most >= kCapSeries * kCapSeries);
         if (!large) return;

@@ -451,7 +451,7 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                             tc::ld32(tS + 64 * h + 32, *reinterpret_cast<uint32_t(*)[32]>(xs + 32));
                             tc::wait_ld();
                             PackedRow<false> row{ps};
-                            cap_free(xs, seen_in(h), hidden, cap_large, cap, row);
+                            cap_free<8>(xs, seen_in(h), hidden, cap_large, cap, row);
                             float l0, l1;
                             dev::f32x2_split(row.sum, l0, l1);
                             l += l0 + l1;
