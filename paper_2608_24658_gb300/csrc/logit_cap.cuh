@@ -29,8 +29,8 @@
 // Measured, one GB300, uncapped -> capped with scores of N(0, 1) -> with scores 8
 // times that, at a cap of 50: 16 trials of a request 30.6 -> 31.6 -> 32.6 us; 128
 // branches of a 32k prefix 130 -> 144 -> 186; 64 branches in e4m3 97 -> 127 -> 170;
-// join prefill 505 -> 635 -> 775, in e4m3 662 -> 893 -> 1141; fork prefill 39 -> 50 ->
-// 57.  The compiler's tanhf for every score took 45 us for the 16 trials and 1687
+// join prefill 505 -> 626 -> 783, in e4m3 662 -> 893 -> 1141; fork prefill 39 -> 49 ->
+// 58.  The compiler's tanhf for every score took 45 us for the 16 trials and 1687
 // for the join.
 //
 // A NaN score makes its row NaN, as it does without a cap.  The exponential form
@@ -47,7 +47,7 @@ namespace {
 // what an attention kernel does to its logits
 enum : int { kCapNone = 0, kCapFree = 1, kCapRef = 2 };
 // 2^73 is what a cap of 50 needs; sums of 2^20 tokens stay finite for |v| to 2^34.
-// (The join takes 635 us below and 826 above, 128 branches of a 32k prefix 144 and 180.)
+// (The join takes 626 us below and 826 above, 128 branches of a 32k prefix 144 and 180.)
 constexpr float kCapFreeLog2 = 73.f;
 
 constexpr float kCapSeries = 0.4f;

@@ -62,7 +62,7 @@
 // reference (kCapFree) a half of a block has nothing to wait for but its own S:
 // the issuer sends the halves of S apart, and the S of the next block's half right
 // behind the PV of this one's, so that a tile's softmax has one half while the
-// tensor core has the other.  The join takes 635 us (682 with whole blocks), the
+// tensor core has the other.  The join takes 626 us (682 with whole blocks), the
 // fork 50; with e4m3 KV, whose P needs a reference, the join takes 893.  The softmax
 // warps' instructions bound it: 6 packed ones per two scores come to those without
 // a cap, the maxima go.  Tried and slower: two warpgroups a tile (643 -> 682 us),
@@ -983,7 +983,7 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                     // Caps without a reference: the halves of a block go their own ways,
                     // S, P, PV, and the next block's S of the half over its P, so that a
                     // tile's softmax has one half while the tensor core has the other
-                    // (join prefill 682 -> 635 us; half by half of both tiles 652).
+                    // (join prefill 682 -> 626 us; half by half of both tiles 652).
                     for (int h = 0; h < 2; ++h)
                         for (int t = 0; t <= last; ++t) issue_half(t, h, st, h == 1 && t == last);
                     advance();
