@@ -63,9 +63,9 @@
 // the issuer sends the halves of S apart, and the S of the next block's half right
 // behind the PV of this one's, so that a tile's softmax has one half while the
 // tensor core has the other.  The join takes 626 us (682 with whole blocks), the
-// fork 50; with e4m3 KV, whose P needs a reference, the join takes 893.  The softmax
-// warps' instructions bound it: 6 packed ones per two scores come to those without
-// a cap, the maxima go.  Tried and slower: two warpgroups a tile (643 -> 682 us),
+// fork 49; with e4m3 KV, whose P needs a reference, the join takes 893.  The softmax
+// warps' chain bounds it, not one pipe: half of the issue slots, 46% of the FMA pipe,
+// and a series with an instruction less takes as long (632).  Tried and slower: two warpgroups a tile (643 -> 682 us),
 // both halves unrolled (760), the next scores loaded early (698).
 //
 // Every wait is bounded (%globaltimer); on expiry the error is recorded, the
