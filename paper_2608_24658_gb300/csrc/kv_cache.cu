@@ -694,6 +694,11 @@ extern "C" parason_status parason_kv_write(const parason_attn_config *cfg, int64
     if ((st = check_rows(v, num_tokens, cfg->num_kv_heads, d, elem, false)) != PARASON_OK) return st;
     if (q && (st = check_rows(q, num_tokens, cfg->num_q_heads, d, elem, false)) != PARASON_OK) return st;
     if (q && (!q_out || misaligned(q_out, 16))) return PARASON_EINVAL;
+    // (in place: the rows as q_out has them, or a row would be written before it is read)
+    if (q && q_out == q->data &&
+        ((num_tokens > 1 && q->token_stride != static_cast<int64_t>(cfg->num_q_heads) * d) ||
+         (cfg->num_q_heads > 1 && q->head_stride != d)))
+        return PARASON_EINVAL;
     if (!slots || misaligned(slots, 4)) return PARASON_EINVAL;
     if (num_physical_pages > 0 && (!k_pages || !v_pages || misaligned(k_pages, 16) || misaligned(v_pages, 16)))
         return PARASON_EINVAL;

@@ -81,7 +81,9 @@ def test_shapes_without_a_kernel(lib):
     dict(n=-1), dict(n=2 ** 31), dict(pages=-1), dict(k=None), dict(v=None), dict(slots=None),
     dict(slots=A + 2), dict(kp=None), dict(vp=None), dict(kp=A + 8), dict(vp=A + 4),
     dict(k=_rows(None)), dict(k=_rows(A + 2)), dict(v=_rows(ts=1028)), dict(v=_rows(hs=100)),
-    dict(k=_rows(ts=-1024)), dict(q=_rows()), dict(q=_rows(), q_out=A + 2), dict(q=_rows(A + 8), q_out=A)])
+    dict(k=_rows(ts=-1024)), dict(q=_rows()), dict(q=_rows(), q_out=A + 2), dict(q=_rows(A + 8), q_out=A),
+    # in place, but not as q_out lies
+    dict(q=_rows(ts=1032), q_out=A), dict(q=_rows(ts=128, hs=512), q_out=A)])
 def test_write_refusals(lib, bad):
     assert _write(lib, **bad) == _lib.EINVAL
 
