@@ -73,7 +73,9 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
         : "memory");
 }
 
-// CAP: x = cap_log2 tanh(to_cap <q, k>) in place of scale_log2 <q, k>.
+// CAP: x = cap_log2 tanh(to_cap <q, k>) in place of scale_log2 <q, k>.  tanhf keeps fp32's
+// accuracy at every size, and two of them a lane and step take 1 to 3% (137 -> 141 us for
+// 35 branches of five 5.9k prefixes).
 template <int D, bool CAP>
 __global__ void __launch_bounds__(kThreads, kCtasPerSm)
     attn_fp32_kernel(const AttnArgs a, const float *__restrict__ kp, const float *__restrict__ vp) {
