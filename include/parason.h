@@ -491,7 +491,9 @@ parason_status parason_rotary_turns(const float *inv_freq, int32_t n, uint64_t *
  *   q_out   = round(rot(q))
  * with the scales in PARASON_FP8_E4M3_KV mode only (ignored, may be NULL,
  * otherwise; at least 2^-126, and finite).  Arithmetic is fp32, rounded once (to
- * nearest even); e4m3 saturates at +-448, infinities too, and keeps NaN.
+ * nearest even); e4m3 rounds the fp32 quotient (itself rounded to nearest for
+ * scales from 2^-92 to 2^126, within a last place outside), saturates at +-448,
+ * infinities too, and keeps NaN.
  *
  *   q       rows [num_tokens, H_q, head_dim], or NULL (no queries; q_out unused)
  *   k, v    rows [num_tokens, H_kv, head_dim]

@@ -167,6 +167,31 @@ struct Batch {
     }
 };
 
+// x / s in place, rounded to nearest: the product q with the rounded reciprocal y and its
+// remainder q s - x, which an FMA gives exactly, make q - (q s - x) y the rounded quotient
+// (P. Markstein, Computation of elementary functions on the IBM RISC System/6000,
+// 1990); for s outside [2^-92, 2^126], where the remainder or y may be subnormal,
+// within a last place.  In this order a zero keeps its sign.
+//
+// e4m3 needs it to the bit: a scale of amax / 448 puts many quotients on its ties, and
+// with the product alone up to one value in fifty of a head came out a step off.  The
+// product is cut at +-512, so that infinities leave no NaN (the remainder takes the
+// quotient on).  20000 tokens of 64 / 8 heads 121.3 us with the product alone, 122.2 so,
+// 129.3 with the compiler's division; of 8 heads without queries, where all is
+// quotients, 25.8, 27.6 and 38.8.
+__device__ __forceinline__ void quotients8(float (&x)[8], float s) {
+    const float y = 1.f / s;
+    const unsigned long long y2 = dev::f32x2(y, y), ny2 = dev::f32x2(-y, -y), s2 = dev::f32x2(s, s);
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+        float q0, q1;
+        dev::f32x2_split(dev::mul_f32x2(dev::f32x2(x[i], x[i + 1]), y2), q0, q1);
+        const unsigned long long q = dev::f32x2(fminf(fmaxf(q0, -512.f), 512.f), fminf(fmaxf(q1, -512.f), 512.f));
+        const unsigned long long r = dev::fma_f32x2(q, s2, dev::f32x2(-x[i], -x[i + 1]));
+        dev::f32x2_split(dev::fma_f32x2(r, ny2, q), x[i], x[i + 1]);
+    }
+}
+
 // Heads of one kind, steps [s0, s1): rotated, scaled, rounded, stored at dst + e0 and
 // dst + e1, a step further `dst_step`.  `batch` holds the first steps already.
 template <class T, class Out, int G, bool ROTATE, int kBatch>
@@ -199,13 +224,9 @@ __device__ __forceinline__ void write_heads(Batch<T, kBatch> &batch, const T *sr
                 }
             }
             if constexpr (sizeof(Out) == 1) {
-                // (times the reciprocal: within two fp32 roundings of the quotient)
-                const float inv = 1.f / scale[h];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    x0[i] *= inv;
-                    x1[i] *= inv;
-                }
+                const float div = scale[h];
+                quotients8(x0, div);
+                quotients8(x1, div);
             }
             store8(dst + b * dst_step + e0, x0);
             store8(dst + b * dst_step + e1, x1);
@@ -220,11 +241,14 @@ __device__ __forceinline__ void write_heads(Batch<T, kBatch> &batch, const T *sr
 // take its heads G at a step, first q's, then k's, then v's: a warp takes as many tokens
 // as it has such teams, or one of `parts` equal parts of one token's steps.
 //
+// (e4m3: 5 CTAs an SM asked for, as the quotients otherwise took 105 registers for 96:
+// 300 tokens of 64 / 8 heads 3.5 us, 4.5 so.)
+//
 // The angles are made once for all heads of a token: the G lanes of one u share 8
 // pairs' angles, make 8 / G each and pass them round (out of shared memory they were
 // read four lanes to a bank).
 template <class T, class KV, int D, bool INTERLEAVED, int G>
-__global__ void __launch_bounds__(kThreads) kv_write_kernel(const WriteArgs a) {
+__global__ void __launch_bounds__(kThreads, kScaled<KV> ? 5 : 1) kv_write_kernel(const WriteArgs a) {
     constexpr int kLanes = D / 16, kTeams = 32 / kLanes / G, kMake = 8 / G;
     constexpr int kBatch = sizeof(T) == 4 ? 2 : 3;            // (1, 2, 4 in bf16: 36, 35, 35 us for 34)
     const int lane = threadIdx.x % 32;
