@@ -455,14 +455,16 @@ __device__ __forceinline__ uint32_t most_bf16x2(uint32_t a, uint32_t b) {
 // A warp takes kScaleRows tokens of one head of K or of V, all their loads in flight, a
 // lane 16 elements of a token as kv_write takes them (more tokens a warp: 1024 tokens of
 // 2 heads 3.3 us with 32, 5.0 with 64, for 2.6).  max |x| goes in bf16 pairs, two elements an
-// instruction; squares of pairs in packed fp32.  Squares past 2^127 (elements from
-// 2^63 on, infinities) send the warp over its tokens once more with magnitudes cut
-// at 2^63; a NaN's partner counts in max |x|, which squares below 2^-126 leave to it
-// too.  Positive floats order as their bits do, so the maxima meet in integer
-// atomics, whose order does not matter; max / 448 is the max of the quotients, since
-// rounding is monotone.  A CTA's warps meet first: an atomic a warp took 33 us for the
-// 21.3 of 32768 tokens of 8 heads (19.8 us of bytes).  CTAs go over the heads of the
-// same tokens first, whose rows are neighbours (head by head 22.3 us).
+// instruction; squares of pairs in packed fp32.  Where their largest sum is past 2^126
+// (elements from 2^62 on, infinities) or below 2^-100 (squares that lose bits, or are
+// 0), the warp goes over its tokens once more, with magnitudes cut at 2^63, or taken
+// times 2^100 before they are squared.  A NaN's partner counts in max |x|.
+//
+// Positive floats order as their bits do, so the maxima meet in integer atomics, whose
+// order does not matter; max / 448 is the max of the quotients, since rounding is
+// monotone.  A CTA's warps meet first: an atomic a warp took 33 us for the 21.1 of 32768
+// tokens of 8 heads (19.8 us of bytes).  CTAs go over the heads of the same tokens
+// first, whose rows are neighbours (head by head 22.3 us).
 constexpr int kScaleRows = 16;
 template <int D>
 __global__ void __launch_bounds__(kThreads, 8) kv_scales_kernel(const ScalesArgs a) {
@@ -513,23 +515,31 @@ __global__ void __launch_bounds__(kThreads, 8) kv_scales_kernel(const ScalesArgs
         }
     }
     float m = fmaxf(magnitude(__uint_as_float(one << 16)), magnitude(__uint_as_float(one & 0xffff0000u)));
-    if (__any_sync(0xffffffffu, pair > 8.5e37f)) {                     // 2^126 and up
-        pair = 0.f;
-        for (int r = 0; rotates && r < kScaleRows; r += kRows) {
-            const int64_t t = t0 + r;
-            if (t >= a.num_tokens || (a.slots && a.slots[t] < 0)) continue;
-            float x0[8], x1[8];
-            unpack8(load8(x + t * src.token_stride + e0), x0);
-            unpack8(load8(x + t * src.token_stride + e1), x1);
+    if (half > 0) {
+        const float most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(pair)));
+        const bool tiny = most < 0x1p-100f && __any_sync(0xffffffffu, m > 0.f);
+        if (tiny || most > 0x1p126f) {
+            const float up = tiny ? 0x1p100f : 1.f;
+            pair = 0.f;
+            for (int r = 0; rotates && r < kScaleRows; r += kRows) {
+                const int64_t t = t0 + r;
+                if (t >= a.num_tokens || (a.slots && a.slots[t] < 0)) continue;
+                float x0[8], x1[8];
+                unpack8(load8(x + t * src.token_stride + e0), x0);
+                unpack8(load8(x + t * src.token_stride + e1), x1);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float p = magnitude(halves ? x0[i] : (i < 4 ? x0 : x1)[2 * (i & 3)]);
-                const float q = magnitude(halves ? x1[i] : (i < 4 ? x0 : x1)[2 * (i & 3) + 1]);
-                pair = fmaxf(pair, p * p + q * q);
+                for (int i = 0; i < 8; ++i) {
+                    const float p = magnitude(up * (halves ? x0[i] : (i < 4 ? x0 : x1)[2 * (i & 3)]));
+                    const float q = magnitude(up * (halves ? x1[i] : (i < 4 ? x0 : x1)[2 * (i & 3) + 1]));
+                    pair = fmaxf(pair, p * p + q * q);
+                }
             }
+            pair = sqrtf(pair) * (tiny ? 0x1p-100f : 1.f);
+        } else {
+            pair = sqrtf(pair);
         }
+        m = fmaxf(m, pair);
     }
-    m = fmaxf(m, sqrtf(pair));
     m = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(m)));
     if (lane == 0) part[warp] = m;
     __syncthreads();
