@@ -29,7 +29,8 @@
  *   k_pages   [num_physical_pages, H_kv, page_size, head_dim]
  *   v_pages   same as k_pages
  *   out       [num_leaves, H_q, head_dim]   same dtype as q
- *   lse       [num_leaves, H_q] fp32, natural log of sum_t exp(s_t)
+ *   lse       [num_leaves, H_q] fp32, natural log of sum_t exp(s_t); a row
+ *             without keys has out 0 and lse -inf, one with a NaN score NaN in both
  *   q head h reads kv head h / (H_q / H_kv)  (grouped-query attention)
  *   s_t = sm_scale * <q, k_t>, sm_scale = 1/sqrt(head_dim) unless given
  *   (capped by a tanh after parason_plan_set_logit_cap).

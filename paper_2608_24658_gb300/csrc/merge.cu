@@ -135,7 +135,7 @@ __global__ void __launch_bounds__(kMergeThreads)
         float mb = m;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, o));
-        const float Mn = fmaxf(M, mb);             // finite: the pass has a valid entry
+        const float Mn = fmaxf(M, mb);             // finite: a valid entry (or all its scores NaN)
         const float s_old = exp2f(M - Mn);
         const float wgt = valid ? exp2f(m - Mn) : 0.f;
         float lw = l * wgt;
@@ -184,19 +184,19 @@ __global__ void __launch_bounds__(kMergeThreads)
         L = 0.f;
 #pragma unroll
         for (int c = 0; c < N; ++c) acc[c] = 0.f;
-        if (Mg != -INFINITY) {
+        // (a warp without entries has M = -inf and sums 0; one whose every score is
+        // NaN has M = -inf and NaN sums, which a weight of 0 keeps)
 #pragma unroll
-            for (int u = 0; u < W; ++u) {
-                const float su = s_m[base + u] == -INFINITY ? 0.f : exp2f(s_m[base + u] - Mg);
-                L += s_l[base + u] * su;
+        for (int u = 0; u < W; ++u) {
+            const float su = s_m[base + u] == -INFINITY ? 0.f : exp2f(s_m[base + u] - Mg);
+            L += s_l[base + u] * su;
 #pragma unroll
-                for (int c = 0; c < N; ++c) acc[c] += su * s_acc[base + u][lane * N + c];
-            }
+            for (int c = 0; c < N; ++c) acc[c] += su * s_acc[base + u][lane * N + c];
         }
         M = Mg;
     }
     if (!active) return;
-    const bool empty = !(L > 0.f);
+    const bool empty = L == 0.f;                    // (NaN is no empty row)
     const float inv = empty ? 0.f : 1.f / L;
 #pragma unroll
     for (int c = 0; c < N; ++c) acc[c] *= inv;
@@ -256,7 +256,7 @@ __global__ void __launch_bounds__(kMergeThreads)
             float mb = m;
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, o));
-            const float Mn = fmaxf(M[r], mb);       // finite: the pass has a valid entry
+            const float Mn = fmaxf(M[r], mb);       // finite: a valid entry (or all its scores NaN)
             const float s_old = exp2f(M[r] - Mn);
             wgt[r] = valid ? exp2f(m - Mn) : 0.f;
             float lw = l * wgt[r];
@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(kMergeThreads)
 #pragma unroll
     for (int r = 0; r < G; ++r) {
         const int64_t row = pair * G + r;            // b * H_q + j * G + r
-        const bool empty = !(L[r] > 0.f);
+        const bool empty = L[r] == 0.f;              // (NaN is no empty row)
         const float inv = empty ? 0.f : 1.f / L[r];
 #pragma unroll
         for (int c = 0; c < N; ++c) acc[r][c] *= inv;

@@ -612,7 +612,7 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                     const int nr = live ? it.row0 + r : 0;
                     out_row = static_cast<int64_t>(it.leaf_lo + nr / a.group) * a.num_q_heads +
                               it.kv_head * a.group + nr % a.group;
-                    const bool empty = !(l > 0.f);
+                    const bool empty = l == 0.f;             // (NaN is no empty row)
                     inv = empty ? 0.f : 1.f / l;
                     if (live && a.lse) a.lse[out_row] = empty ? -INFINITY : (m_use + log2f(l)) * kLn2;
                 } else if (live) {
