@@ -7,6 +7,7 @@
 // of dependent loads (slot or position, then rows) on short ones.
 #include <cuda_fp8.h>
 
+#include <atomic>
 #include <cmath>
 
 #include "device_common.cuh"
@@ -18,6 +19,7 @@ namespace {
 constexpr int kMaxAxes = 4;
 constexpr float kE4m3Max = 448.f;
 constexpr int kMaxHeads = 16384;         // of q, and of k: what the kernels' counters hold
+constexpr int kMaxDevices = 64;
 constexpr int64_t kMaxRows = 1ll << 34;  // tokens times kv heads: what a grid holds (16 and more a CTA)
 
 struct Rows {
@@ -132,8 +134,11 @@ constexpr bool kScaled = sizeof(KV) == 1;
 constexpr int kThreads = 128;            // 4 warps, each of them on its own
 constexpr int kWarps = kThreads / 32;
 
-// Warps of kv_write that run at once, one wave (152 SMs, 5 CTAs each by registers).
-constexpr int kWaveWarps = 152 * 5 * kWarps;
+// CTAs of kv_write to ask an SM's registers for: bf16 and e4m3 rows fit 5 without
+// spills (e4m3 took 105 registers unasked, and 300 tokens of 64 / 8 heads 4.5 us for
+// 3.5); fp32 rows do not everywhere, and are left to themselves (96 to 104).
+template <class T>
+constexpr int kAskedCtas = sizeof(T) == 2 ? 5 : 0;
 
 // cos and sin of positions[axis] * inv_freq[i].  The frequency is held as turns a
 // position modulo 1, in 2^-64: the low 64 bits of its product with the position are
@@ -241,14 +246,11 @@ __device__ __forceinline__ void write_heads(Batch<T, kBatch> &batch, const T *sr
 // take its heads G at a step, first q's, then k's, then v's: a warp takes as many tokens
 // as it has such teams, or one of `parts` equal parts of one token's steps.
 //
-// (e4m3: 5 CTAs an SM asked for, as the quotients otherwise took 105 registers for 96:
-// 300 tokens of 64 / 8 heads 3.5 us, 4.5 so.)
-//
 // The angles are made once for all heads of a token: the G lanes of one u share 8
 // pairs' angles, make 8 / G each and pass them round (out of shared memory they were
 // read four lanes to a bank).
 template <class T, class KV, int D, bool INTERLEAVED, int G>
-__global__ void __launch_bounds__(kThreads, kScaled<KV> ? 5 : 1) kv_write_kernel(const WriteArgs a) {
+__global__ void __launch_bounds__(kThreads, kAskedCtas<T>) kv_write_kernel(const WriteArgs a) {
     constexpr int kLanes = D / 16, kTeams = 32 / kLanes / G, kMake = 8 / G;
     constexpr int kBatch = sizeof(T) == 4 ? 2 : 3;            // (1, 2, 4 in bf16: 36, 35, 35 us for 34)
     const int lane = threadIdx.x % 32;
@@ -549,11 +551,35 @@ __global__ void __launch_bounds__(kThreads, 8) kv_scales_kernel(const ScalesArgs
     }
 }
 
+// Warps of kv_write (a token to a warp) that run at once on the current device, one
+// wave: asked for once a device.
+template <class T, class KV, int D, bool INTERLEAVED>
+cudaError_t wave_warps(int64_t *warps) {
+    static std::atomic<int> known[kMaxDevices];          // 0: not asked yet
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices) return cudaErrorNotSupported;
+    int n = known[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        int sms = 0, ctas = 0;
+        e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+        if (e == cudaSuccess)
+            e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ctas, kv_write_kernel<T, KV, D, INTERLEAVED, 512 / D>,
+                                                              kThreads, 0);
+        if (e != cudaSuccess) return e;
+        n = sms * ctas * kWarps;
+        known[dev].store(n, std::memory_order_relaxed);
+    }
+    *warps = n;
+    return cudaSuccess;
+}
+
 // Parts of a token: as many as one wave of warps has room for, of one step at least
 // (1200 tokens of 32 / 8 heads: 5.5 us in 2 parts, 7.1 in 3, whose warps wait for a
 // place and make the same angles again).
-int parts_of(int64_t tokens, int steps) {
-    const int64_t room = kWaveWarps / tokens;
+int parts_of(int64_t tokens, int steps, int64_t wave) {
+    const int64_t room = wave / tokens;
     return static_cast<int>(room < 1 ? 1 : room < steps ? room : steps);
 }
 
@@ -562,10 +588,10 @@ unsigned blocks_of(int64_t tokens, int parts) {
 }
 
 template <class T, class KV, int D, int G>
-cudaError_t launch_write(WriteArgs a, cudaStream_t s) {
+cudaError_t launch_write(WriteArgs a, int64_t wave, cudaStream_t s) {
     constexpr int kTeams = 512 / D / G;
     const int steps = (a.num_q_heads + G - 1) / G + 2 * ((a.num_kv_heads + G - 1) / G);
-    a.parts = kTeams == 1 ? parts_of(a.num_tokens, steps) : 1;
+    a.parts = kTeams == 1 ? parts_of(a.num_tokens, steps, wave) : 1;
     return launch_dependent(
         true, a.rot.interleaved ? kv_write_kernel<T, KV, D, true, G> : kv_write_kernel<T, KV, D, false, G>,
         dim3(blocks_of((a.num_tokens + kTeams - 1) / kTeams, a.parts)), dim3(kThreads), 0, s, a);
@@ -579,13 +605,16 @@ cudaError_t launch_write(WriteArgs a, cudaStream_t s) {
 template <class T, class KV, int D>
 cudaError_t launch_write(const WriteArgs &a, cudaStream_t s) {
     constexpr int kGroups = 512 / D;
+    int64_t wave = 0;
+    const cudaError_t e = a.rot.interleaved ? wave_warps<T, KV, D, true>(&wave) : wave_warps<T, KV, D, false>(&wave);
+    if (e != cudaSuccess) return e;
     auto few = [&](int g) {
         return (a.num_q_heads + g - 1) / g + 2 * ((a.num_kv_heads + g - 1) / g) < 10 &&
-               a.num_tokens > static_cast<int64_t>(kGroups / g) * kWaveWarps;
+               a.num_tokens > kGroups / g * wave;
     };
-    if (!few(kGroups)) return launch_write<T, KV, D, kGroups>(a, s);
-    return few(kGroups / 2) ? launch_write<T, KV, D, kGroups / 4>(a, s)
-                            : launch_write<T, KV, D, kGroups / 2>(a, s);
+    if (!few(kGroups)) return launch_write<T, KV, D, kGroups>(a, wave, s);
+    return few(kGroups / 2) ? launch_write<T, KV, D, kGroups / 4>(a, wave, s)
+                            : launch_write<T, KV, D, kGroups / 2>(a, wave, s);
 }
 
 template <class T, class KV, int D>
