@@ -2377,10 +2377,13 @@ parason_status parason_plan_set_logit_cap(parason_plan p, float cap) {
     // (a NaN fails every comparison)
     if (!p || !(cap == 0.0f || (cap >= 0x1p-10f && cap <= 0x1p20f))) return PARASON_EINVAL;
     if (cap > 0.0f && !std::isfinite(p->cfg.sm_scale / cap)) return PARASON_EINVAL;
-    if (cap > 0.0f && p->on_device && p->cfg.mode != PARASON_FP32) {
+    if (p->on_device) {
         int dev = -1;
         if (cudaGetDevice(&dev) != cudaSuccess) return PARASON_ECUDA;
         if (dev != p->device) return PARASON_EINVAL;
+    }
+    // (the fp32 kernels set theirs at each launch)
+    if (cap > 0.0f && p->on_device && p->cfg.mode != PARASON_FP32) {
         const cudaError_t e = p->prefill ? parason::prefill_prepare_cap(p->cfg.mode)
                                          : parason::attn_mma_prepare_cap(p->cfg.head_dim, p->cfg.mode);
         if (e != cudaSuccess) return PARASON_ECUDA;
