@@ -507,12 +507,14 @@ parason_status parason_rotary_turns(const float *inv_freq, int32_t n, uint64_t *
  *   q_out   device [num_tokens, H_q, head_dim], contiguous, 16-byte aligned,
  *           the layout parason_attn_decode takes; may be q's own memory if q
  *           has that layout, and overlaps nothing else here
- *   k_pages, v_pages  the pools of parason_attn_decode
+ *   k_pages, v_pages  the pools of parason_attn_decode, apart from each other; q, k
+ *           and v may be rows of a pool, but not of a slot that this call writes
  *
  * One kernel on `stream`, no allocation, capturable.  It reads positions,
  * slots and scales on the device, so a captured step can be replayed with new
  * ones.  PARASON_EINVAL for a bad config, a NULL or misaligned pointer, a
- * negative count, a rotary description outside the above;
+ * negative count, a rotary description outside the above, k_pages = v_pages, q_out
+ * at the start of k or v (other overlaps are the caller's to avoid);
  * PARASON_EUNSUPPORTED if num_physical_pages * H_kv * 16 passes int32 (as in
  * parason_attn_plan), there are more than 16384 heads, or (parason_kv_read, _scales)
  * num_tokens * H_kv passes 2^34; PARASON_ECUDA if the launch fails.
@@ -530,7 +532,9 @@ parason_status parason_kv_write(const parason_attn_config *cfg, int64_t num_toke
  * in PARASON_BF16 and PARASON_FP32 modes).  A slot outside the pool gives a
  * row of zeros; a slot may be read any number of times.  k_out and v_out are
  * rows [num_tokens, H_kv, head_dim] whose strides keep them apart: the smaller
- * one at least head_dim, the larger one past all rows of the smaller.  Keys come out as they
+ * one at least head_dim, the larger one past all rows of the smaller.  They may be
+ * views of one buffer whose rows lie apart, and overlap neither each other
+ * (PARASON_EINVAL for the same start) nor the pools.  Keys come out as they
  * were written: parason_kv_write with the difference of positions moves them
  * to others.  Launch, capture and errors as parason_kv_write.
  */

@@ -768,6 +768,9 @@ extern "C" parason_status parason_kv_write(const parason_attn_config *cfg, int64
     if (cfg->mode == PARASON_FP8_E4M3_KV &&
         (!k_scale || !v_scale || misaligned(k_scale, 4) || misaligned(v_scale, 4)))
         return PARASON_EINVAL;
+    // (outputs in one place: two warps would write it, or one before another has read it)
+    if (num_physical_pages > 0 && k_pages == v_pages) return PARASON_EINVAL;
+    if (q && (q_out == k->data || q_out == v->data)) return PARASON_EINVAL;
     if (q) a.q = to_rows(q);
     a.k = to_rows(k);
     a.v = to_rows(v);
@@ -820,6 +823,7 @@ extern "C" parason_status parason_kv_read(const parason_attn_config *cfg, int64_
     a.num_slots = num_physical_pages * kPageSize;
     a.num_kv_heads = cfg->num_kv_heads;
     if (num_tokens * cfg->num_kv_heads > kMaxRows) return PARASON_EUNSUPPORTED;
+    if (k_out->data == v_out->data) return PARASON_EINVAL;
     const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     if (cfg->mode == PARASON_FP8_E4M3_KV) return launched(launch_read<__nv_bfloat16, __nv_fp8_e4m3, 128>(a, s));
     if (cfg->mode == PARASON_FP32)
