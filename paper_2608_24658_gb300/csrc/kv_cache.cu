@@ -694,7 +694,8 @@ parason_status to_rotary(const parason_rotary *r, int64_t tokens, int32_t d, Rot
 constexpr uint64_t kInvTwoPi[3] = {0x28be60db9391054aull, 0x7f09d5f47d4d3770ull, 0x36d8a5664f10e410ull};
 
 // |f| / (2 pi) modulo 1 in 2^-64: f = m 2^e, and m kInvTwoPi 2^(e + 64 - 192) rounded.
-// (kInvTwoPi is off by 2^-192, which e <= 40 takes to 2^-64 at most.)
+// (kInvTwoPi is below 1 / (2 pi) by less than 2^-192, so the product by less than
+// 2^24 2^(e - 192): 2^-127 of a turn at e = 41, the largest.)
 uint64_t turns_of(float f) {
     int e = 0;
     const uint64_t m = static_cast<uint64_t>(std::ldexp(std::frexp(std::fabs(f), &e), 24));
@@ -707,7 +708,7 @@ uint64_t turns_of(float f) {
         carry >>= 64;
     }
     w[3] = static_cast<uint64_t>(carry);
-    const int shift = 128 - e;                           // 88 and up for |f| <= 2^64
+    const int shift = 128 - e;                           // 87 and up for |f| <= 2^64
     if (shift > 256) return 0;
     const int half = shift - 1;                          // the bit that rounds
     unsigned __int128 up = static_cast<unsigned __int128>(1) << (half % 64);
