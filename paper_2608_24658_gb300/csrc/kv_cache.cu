@@ -246,13 +246,17 @@ __device__ __forceinline__ void write_heads(Batch<T, kBatch> &batch, const T *sr
 // take its heads G at a step, first q's, then k's, then v's: a warp takes as many tokens
 // as it has such teams, or one of `parts` equal parts of one token's steps.
 //
+// Three steps of a head are loaded ahead in bf16: with 1, 2, 3, 4 the prompt of 8192
+// tokens takes 40.6, 34.5, 33.5, 33.1 us and the e4m3 batch of 2500 22.2, 19.0, 18.7,
+// 19.5.
+//
 // The angles are made once for all heads of a token: the G lanes of one u share 8
 // pairs' angles, make 8 / G each and pass them round (out of shared memory they were
 // read four lanes to a bank).
 template <class T, class KV, int D, bool INTERLEAVED, int G>
 __global__ void __launch_bounds__(kThreads, kAskedCtas<T>) kv_write_kernel(const WriteArgs a) {
     constexpr int kLanes = D / 16, kTeams = 32 / kLanes / G, kMake = 8 / G;
-    constexpr int kBatch = sizeof(T) == 4 ? 2 : 3;            // (1, 2, 4 in bf16: 36, 35, 35 us for 34)
+    constexpr int kBatch = sizeof(T) == 4 ? 2 : 3;            // (steps in flight; below)
     const int lane = threadIdx.x % 32;
     const int64_t job = static_cast<int64_t>(blockIdx.x) * kWarps + threadIdx.x / 32;
     const int64_t t0 = a.parts == 1 ? job : job / a.parts;
@@ -387,9 +391,9 @@ __device__ __forceinline__ void store_read16(T *dst, const Raw16<KV> &r, float s
 }
 
 // Rows (token, head) in order: a warp takes kSteps x (32 / kLanes) of them, K and V of
-// each, a lane 16 elements, all loads in flight.  38.8k e4m3 tokens of 8 heads: 36.5 us
-// (35.2 us of bytes); 8 elements a lane, whose scales and addresses then come twice as
-// often, 39.6; a warp to a token leaves lanes without a head where there are few (38.4k
+// each, a lane 16 elements, all loads in flight.  38.8k e4m3 tokens of 8 heads: 37.3 us
+// (35.2 us of bytes), fp32 95.5 (93.8); 8 elements a lane, whose scales and addresses
+// then come twice as often, 39.6; a warp to a token leaves lanes without a head where there are few (38.4k
 // bf16 tokens of one head 6.2 us, 13.1 so).
 template <class T, class KV, int D>
 __global__ void __launch_bounds__(kThreads, 8) kv_read_kernel(const ReadArgs a) {
@@ -599,9 +603,9 @@ cudaError_t launch_write(WriteArgs a, int64_t wave, cudaStream_t s) {
 
 // A token to a warp, or two or four of them where a token is fewer than 10 steps and
 // their warps would pass one wave: a short warp spends its life on its slot, its angles and its
-// first loads (9728 bf16 tokens of 128 elements, a token, two and four to a warp: 15.0,
-// 12.1, 10.6 us at 8 / 2 heads, 4 to 12 steps; 22.8, 19.7, 19.7 at 16 / 4; 35, 36, 36
-// at 24 / 8, 10 to 40 steps).
+// first loads (9728 bf16 tokens of 128 elements, a token, two and four to a warp: 14.1,
+// 11.9, 10.0 us at 8 / 2 heads, 4 to 12 steps; 22.0, 19.2, 19.0 at 16 / 4; 34.1, 35.0,
+// 34.5 at 24 / 8, 10 to 40 steps).
 template <class T, class KV, int D>
 cudaError_t launch_write(const WriteArgs &a, cudaStream_t s) {
     constexpr int kGroups = 512 / D;

@@ -29,7 +29,7 @@
 // Measured, one GB300, uncapped -> capped with scores of N(0, 1) -> with scores 8
 // times that, at a cap of 50: 16 trials of a request 30.6 -> 31.6 -> 32.6 us; 128
 // branches of a 32k prefix 130 -> 144 -> 186; 64 branches in e4m3 97 -> 127 -> 170;
-// join prefill 505 -> 626 -> 783, in e4m3 662 -> 893 -> 1141; fork prefill 39 -> 49 ->
+// join prefill 509 -> 626 -> 783, in e4m3 662 -> 894 -> 1142; fork prefill 39 -> 49 ->
 // 58.  The compiler's tanhf for every score took 45 us for the 16 trials and 1687
 // for the join.
 //
@@ -47,7 +47,7 @@ namespace {
 // what an attention kernel does to its logits
 enum : int { kCapNone = 0, kCapFree = 1, kCapRef = 2 };
 // 2^73 is what a cap of 50 needs; sums of 2^20 tokens stay finite for |v| to 2^34.
-// (The join takes 626 us below and 826 above, 128 branches of a 32k prefix 144 and 180.)
+// (The join takes 626 us below and 825 above, 128 branches of a 32k prefix 144 and 180.)
 constexpr float kCapFreeLog2 = 73.f;
 
 constexpr float kCapSeries = 0.4f;
@@ -251,9 +251,10 @@ struct PackedRow {
 // `start()` on where a block is done twice); the whole warp calls.  large: whether the
 // warp's last block had a score at kCapSeries or past it.  The series runs on trust,
 // and the block is done again if one turns up; the exponential form then serves all of
-// its scores: its absolute error, 2e-7 cap, is 1e-5 at most there.  K pairs go through
-// the series side by side: 8 in the prefill, whose registers hold them (join 636 us with
-// 1, 651 with 4, 626 with 8, 628 with 16), 1 in the decode tiles (128 branches of a 32k
+// its scores: its absolute error, 2e-7 cap, is 1e-5 at most there.  K pairs go
+// through the series side by side: 8 in the prefill, whose registers hold them (calls
+// back to back, in turn on one GPU: the join 635 us with 1, 649 with 4, 625 with 8 and
+// 16; the fork 50.3, 49.5, 49.4, 50.0), 1 in the decode tiles (128 branches of a 32k
 // prefix 144 with 1, 149 with 8).
 template <int K, int N, class X, class Put>
 __device__ __forceinline__ void cap_free(const X (&x)[N], int seen, bool hidden, bool &large, const CapFactors &f,

@@ -62,11 +62,11 @@
 // reference (kCapFree) a half of a block has nothing to wait for but its own S:
 // the issuer sends the halves of S apart, and the S of the next block's half right
 // behind the PV of this one's, so that a tile's softmax has one half while the
-// tensor core has the other.  The join takes 626 us (682 with whole blocks), the
-// fork 49; with e4m3 KV, whose P needs a reference, the join takes 893.  The softmax
-// warps' chain bounds it, not one pipe: half of the issue slots, 46% of the FMA pipe,
-// and a series with an instruction less takes as long (632).  Tried and slower: two warpgroups a tile (643 -> 682 us),
-// both halves unrolled (760), the next scores loaded early (698).
+// tensor core has the other.  The join takes 626 us, the fork 49; with e4m3 KV, whose
+// P needs a reference, the join takes 894.  The softmax warps' chain bounds it, not one
+// pipe: half of the issue slots, less than half of the FMA and tensor pipes.  Tried and
+// slower, from 643 us at that time: two warpgroups a tile (682), both halves unrolled
+// (760), the next scores loaded early (698); a series with an instruction less was level.
 //
 // Every wait is bounded (%globaltimer); on expiry the error is recorded, the
 // copies in flight land, TMEM is freed and the CTA exits.
@@ -983,7 +983,7 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                     // Caps without a reference: the halves of a block go their own ways,
                     // S, P, PV, and the next block's S of the half over its P, so that a
                     // tile's softmax has one half while the tensor core has the other
-                    // (join prefill 682 -> 626 us; half by half of both tiles 652).
+                    // (join prefill 682 -> 636 us; half by half of both tiles 652).
                     for (int h = 0; h < 2; ++h)
                         for (int t = 0; t <= last; ++t) issue_half(t, h, st, h == 1 && t == last);
                     advance();
