@@ -256,7 +256,7 @@ __device__ __forceinline__ void write_heads(Batch<T, kBatch> &batch, const T *sr
 template <class T, class KV, int D, bool INTERLEAVED, int G>
 __global__ void __launch_bounds__(kThreads, kAskedCtas<T>) kv_write_kernel(const WriteArgs a) {
     constexpr int kLanes = D / 16, kTeams = 32 / kLanes / G, kMake = 8 / G;
-    constexpr int kBatch = sizeof(T) == 4 ? 2 : 3;            // (steps in flight; below)
+    constexpr int kBatch = sizeof(T) == 4 ? 2 : 3;            // (steps in flight, as above)
     const int lane = threadIdx.x % 32;
     const int64_t job = static_cast<int64_t>(blockIdx.x) * kWarps + threadIdx.x / 32;
     const int64_t t0 = a.parts == 1 ? job : job / a.parts;
@@ -391,10 +391,10 @@ __device__ __forceinline__ void store_read16(T *dst, const Raw16<KV> &r, float s
 }
 
 // Rows (token, head) in order: a warp takes kSteps x (32 / kLanes) of them, K and V of
-// each, a lane 16 elements, all loads in flight.  38.8k e4m3 tokens of 8 heads: 37.3 us
+// each, a lane 16 elements, all loads in flight.  38.8k e4m3 tokens of 8 heads: 37.2 us
 // (35.2 us of bytes), fp32 95.5 (93.8); 8 elements a lane, whose scales and addresses
-// then come twice as often, 39.6; a warp to a token leaves lanes without a head where there are few (38.4k
-// bf16 tokens of one head 6.2 us, 13.1 so).
+// then come twice as often, 39.6 in e4m3; a warp to a token leaves lanes without a head
+// where there are few (38.4k bf16 tokens of one head 6.2 us, 13.1 so).
 template <class T, class KV, int D>
 __global__ void __launch_bounds__(kThreads, 8) kv_read_kernel(const ReadArgs a) {
     constexpr int kLanes = D / 16, kGroups = 32 / kLanes, kSteps = sizeof(T) == 4 ? 1 : 2;
