@@ -29,6 +29,8 @@
  *   k_pages   [num_physical_pages, H_kv, page_size, head_dim]
  *   v_pages   same as k_pages
  *   out       [num_leaves, H_q, head_dim]   same dtype as q
+ *             (PARASON_FP4_KV: [num_physical_pages, H_kv, 9 head_dim] bytes, see
+ *             "Filling and reading the paged cache")
  *   lse       [num_leaves, H_q] fp32, natural log of sum_t exp(s_t); a row
  *             without keys has out 0 and lse -inf, one with a NaN score NaN in both
  *   q head h reads kv head h / (H_q / H_kv)  (grouped-query attention)
@@ -58,14 +60,17 @@ typedef enum {
     PARASON_EUNSUPPORTED = 5, /* valid but not implemented (shape / mode) */
     PARASON_ENOSPACE = 6,     /* the plan has no room for an update: build a new one */
     PARASON_ERANGE = 7        /* an input value outside what the mode's kernels hold
-                                 (e4m3 KV: |q| >= 65520, see parason_attn_decode) */
+                                 (e4m3 or 4-bit KV: |q| >= 65520, see parason_attn_decode) */
 } parason_status;
 
 typedef enum {
     PARASON_BF16 = 0,         /* q, K, V, out bf16; fp32 accumulation     */
     PARASON_FP32 = 1,         /* q, K, V, out fp32; fp32 FMA throughout   */
-    PARASON_FP8_E4M3_KV = 2   /* q, out bf16; K, V OCP e4m3 bytes with one
+    PARASON_FP8_E4M3_KV = 2,  /* q, out bf16; K, V OCP e4m3 bytes with one
                                  fp32 scale per kv head for K and for V   */
+    PARASON_FP4_KV = 3        /* q, out bf16; K, V OCP e2m1, 4 bits an
+                                 element, with an e4m3 scale for every 16 of
+                                 a row and one fp32 scale per kv head     */
 } parason_mode;
 
 typedef struct {
@@ -104,7 +109,7 @@ typedef struct parason_plan_s *parason_plan;
  * parent out of range or not smaller than its child, a negative length, a
  * page count that is not ceil(len/page_size), a page id out of range or owned
  * twice, a leaf out of range, repeated or with children, or a NULL pointer.
- * PARASON_EUNSUPPORTED for e4m3 KV with head_dim 64 (only 128 has a kernel).
+ * PARASON_EUNSUPPORTED for e4m3 or 4-bit KV with head_dim 64 (only 128 has a kernel).
  * PARASON_ENOMEM / PARASON_ECUDA if the metadata cannot be allocated or
  * copied.  On success *out owns host and device memory until
  * parason_plan_destroy.  The plan may be used by any number of decode calls,
@@ -149,8 +154,8 @@ parason_status parason_attn_plan_host(const parason_attn_config *cfg, int32_t nu
  * The plan is run with parason_attn_decode: q [num_queries, H_q, head_dim],
  * out the same shape, lse [num_queries, H_q]; parason_plan_info reports
  * num_queries as num_leaves.  The kernel is a tcgen05 tile pair:
- * PARASON_EUNSUPPORTED unless head_dim is 128 and the mode is PARASON_BF16
- * or PARASON_FP8_E4M3_KV (k_scale / v_scale as for decode), and
+ * PARASON_EUNSUPPORTED unless head_dim is 128 and the mode is PARASON_BF16,
+ * PARASON_FP8_E4M3_KV or PARASON_FP4_KV (k_scale / v_scale as for decode), and
  * parason_plan_append on a prefill plan returns PARASON_EUNSUPPORTED.  Other
  * errors, ownership and concurrency as parason_attn_plan.
  */
@@ -239,10 +244,10 @@ size_t parason_plan_workspace_bytes(parason_plan plan);
  *            16-byte aligned; or page-locked host memory the device can
  *            address (cudaHostAlloc / cudaHostRegister), read in place
  *   k_pages  device, [num_physical_pages, H_kv, 16, head_dim], bf16 / fp32 /
- *            e4m3 bytes by mode, 16-byte aligned
+ *            e4m3 bytes by mode (4-bit: the bytes of pages), 16-byte aligned
  *   v_pages  device, same layout and dtype as k_pages
- *   k_scale, v_scale  device fp32 [H_kv] in FP8 mode (k = e4m3 * k_scale),
- *            ignored otherwise (may be NULL)
+ *   k_scale, v_scale  device fp32 [H_kv] in FP8 mode (k = e4m3 * k_scale) and
+ *            FP4 mode (k = e2m1 * e4m3 * k_scale), ignored otherwise (may be NULL)
  *   out      device, [num_leaves, H_q, head_dim], dtype of q, 16-byte
  *            aligned; or page-locked host memory the device can address
  *            (cudaHostAlloc / cudaHostRegister): the plan's last kernel
@@ -260,8 +265,9 @@ size_t parason_plan_workspace_bytes(parason_plan plan);
  * also reach up to 2 floor(128 / g) + 14 queries before the token in its chunk
  * (g = H_q / H_kv), whose weight for it is 0: they share its tiles and pages.
  *
- * With e4m3 KV the kernels multiply q by the widened keys and values in f16
- * (f16 holds every e4m3 value exactly): q is narrowed from bf16 to f16,
+ * With e4m3 and 4-bit KV the kernels multiply q by the widened keys and values in
+ * f16 (f16 holds every e4m3 value, and every e2m1 value times its e4m3 scale,
+ * exactly; a NaN scale makes its 16 elements NaN): q is narrowed from bf16 to f16,
  * which is exact for |q| < 65504 except in the low bits of values below
  * 2^-14.  A q element of magnitude 65520 or more (inf included) cannot be
  * narrowed: the kernel records PARASON_ERANGE, which the next
@@ -403,8 +409,8 @@ parason_status parason_plan_fork(parason_plan plan, int32_t branch, int32_t num_
  *   o = (e^{lse_a} o_a + e^{lse_b} o_b) / (e^{lse_a} + e^{lse_b})
  *   lse = ln(e^{lse_a} + e^{lse_b})
  * A side with lse = -inf is empty; both empty gives o = 0, lse = -inf.
- * o_a, o_b, o_out: device [rows, head_dim], bf16 (PARASON_BF16 and
- * PARASON_FP8_E4M3_KV) or fp32 (PARASON_FP32); lse_*: device fp32 [rows].
+ * o_a, o_b, o_out: device [rows, head_dim], bf16 (PARASON_BF16,
+ * PARASON_FP8_E4M3_KV and PARASON_FP4_KV) or fp32 (PARASON_FP32); lse_*: device fp32 [rows].
  * o_out / lse_out may alias the inputs row for row.  Asynchronous on stream.
  */
 parason_status parason_lse_merge(const void *o_a, const float *lse_a, const void *o_b,
@@ -441,11 +447,18 @@ parason_status parason_plan_set_logit_cap(parason_plan plan, float cap);
  * again, for example to move them.  The paper leaves positions and the cache
  * to its engine (Sec. 3.4); these calls are what that engine has to do.
  *
+ * In PARASON_FP4_KV mode a page of one kv head is 9 head_dim bytes: the values of
+ * its 16 tokens, head_dim / 2 bytes each (OCP e2m1, element 2 i in the low four bits of
+ * byte i, element 2 i + 1 in the high ones), then their scales, head_dim / 16 bytes
+ * each (OCP e4m3, scale j for elements 16 j .. 16 j + 15).  Element i is
+ *   e2m1[i] * e4m3[i / 16] * scale,  scale the kv head's fp32 one.
+ * Pages lie as [num_physical_pages][H_kv][9 head_dim], 16-byte aligned.
+ *
  * A slot is page * 16 + offset in the page: token t of a node sits in slot
  * 16 * page_ids[node_page_ptr[node] + t / 16] + t % 16.  `cfg` gives the head
  * counts, head_dim, page size and mode of the cache (sm_scale is not used),
- * validated as by parason_attn_plan; the current device is the memory's.  Rows of tokens are bf16 (PARASON_BF16
- * and PARASON_FP8_E4M3_KV) or fp32 (PARASON_FP32).
+ * validated as by parason_attn_plan; the current device is the memory's.  Rows of tokens are bf16 (PARASON_BF16,
+ * PARASON_FP8_E4M3_KV and PARASON_FP4_KV) or fp32 (PARASON_FP32).
  * ------------------------------------------------------------------------ */
 
 /* Rows of num_tokens tokens by some heads of head_dim elements: element i of
@@ -490,11 +503,17 @@ parason_status parason_rotary_turns(const float *inv_freq, int32_t n, uint64_t *
  * their queries on the way:
  *   K[slot] = round(rot(k) / k_scale[h]),  V[slot] = round(v / v_scale[h]),
  *   q_out   = round(rot(q))
- * with the scales in PARASON_FP8_E4M3_KV mode only (ignored, may be NULL,
- * otherwise; at least 2^-126, and finite).  Arithmetic is fp32, rounded once (to
+ * with the scales in PARASON_FP8_E4M3_KV and PARASON_FP4_KV mode only (ignored, may
+ * be NULL, otherwise; at least 2^-126, and finite).  Arithmetic is fp32, rounded once (to
  * nearest even); e4m3 rounds the fp32 quotient (itself rounded to nearest for
  * scales from 2^-92 to 2^126, within a last place outside), saturates at +-448,
  * infinities too, and keeps NaN.
+ *
+ * PARASON_FP4_KV, for each 16 elements x of a row and the head's scale g in
+ * [2^-100, 2^100]: s = e4m3(max |x| r) with r = 1 / (6 g), and the codes are
+ * e2m1(x y) with y = 1 / (s g), 0 where s is 0; products and reciprocals are fp32,
+ * rounded to nearest each, both formats round to nearest even and saturate (at 448,
+ * +-6).  A NaN makes s NaN, and so all 16 elements.
  *
  *   q       rows [num_tokens, H_q, head_dim], or NULL (no queries; q_out unused)
  *   k, v    rows [num_tokens, H_kv, head_dim]
@@ -526,6 +545,82 @@ parason_status parason_kv_write(const parason_attn_config *cfg, int64_t num_toke
                                 void *q_out, void *k_pages, void *v_pages,
                                 int64_t num_physical_pages, parason_stream_t stream);
 
+/* The norm of each head of q and of k, before its rotation: over the head's d =
+ * head_dim elements
+ *   y_i = x_i / sqrt(sum_j x_j^2 / d + eps) * (weight_offset + w_i)
+ * in fp32, not rounded in between (finite for |x| up to 2^59). */
+typedef struct {
+    const void *q_weight;      /* device, the type of the rows, 16-byte aligned: w of   */
+    const void *k_weight;      /* head h at element h * head_stride; NULL: no norm      */
+    int64_t q_head_stride;     /* elements, a multiple of 16 bytes; 0: the same weight  */
+    int64_t k_head_stride;     /* for every head                                        */
+    float eps;                 /* at least 2^-126, finite                               */
+    float weight_offset;       /* 0, or 1 for weights that are kept as w - 1            */
+} parason_head_norm;
+
+/*
+ * parason_kv_write with q and k normed head by head on the way (norm NULL:
+ * parason_kv_write):
+ *   K[slot] = round(rot(norm(k)) / k_scale[h]),  q_out = round(rot(norm(q))),
+ * V as there.  Errors as there, and PARASON_EINVAL for a norm without weights, a
+ * misaligned weight, a stride that is negative or no multiple of 16 bytes, or an
+ * eps or weight_offset outside the above.  The weights are read on the device.
+ */
+parason_status parason_kv_write_norm(const parason_attn_config *cfg, int64_t num_tokens,
+                                     const parason_rows *q, const parason_rows *k,
+                                     const parason_rows *v, const parason_head_norm *norm,
+                                     const parason_rotary *rotary, const int32_t *slots,
+                                     const float *k_scale, const float *v_scale, void *q_out,
+                                     void *k_pages, void *v_pages, int64_t num_physical_pages,
+                                     parason_stream_t stream);
+
+/*
+ * The slots and positions of the tokens that a batch of sequences (nodes of trees, or
+ * whole requests) adds, from lengths and page tables in device memory; new pages
+ * come out of a list of free ones.  Sequence r holds held[r] tokens, and adds added[r]:
+ * tokens x = held[r], held[r] + 1, ..., which take rows one after another, sequence by
+ * sequence:
+ *   slots[row] = 16 * page + x % 16,  positions[row] = first[r] + x,
+ * page the table's entry x / 16 of the sequence.  With free_pages, the pages that
+ * sequence r opens (entries from ceil(held[r] / 16) on) are the list's next ones, in
+ * order of r from entry free_used on, and are written into the table.
+ *
+ * A token without a page has slot -1, for which parason_kv_write writes nothing: the
+ * list was used up, the table is too narrow, or its entry is negative.  Rows past the
+ * last token have slot -1 and position 0.  Tokens past num_rows are not added.
+ * Negative lengths count as 0, and added[r] as at most 2^31 - 1 - held[r].
+ */
+typedef struct {
+    int32_t num_seqs;            /* at most 16384                                          */
+    int32_t num_rows;            /* rows of slots and positions                            */
+    const int32_t *held;         /* device [num_seqs]                                      */
+    const int32_t *added;        /* device [num_seqs]; NULL: one token each                */
+    const int32_t *first;        /* device [num_seqs]; NULL: 0 (tokens of the nodes above) */
+    int32_t *page_table;         /* device [num_seqs][table_pages], rows table_stride apart */
+    int64_t table_stride;
+    int32_t table_pages;
+    int32_t num_free;            /* entries of free_pages                                  */
+    const int32_t *free_pages;   /* device; NULL: the table has every page already         */
+    const int32_t *free_used;    /* device [1], entries taken before; NULL: 0              */
+    int32_t *slots;              /* device [num_rows]                                      */
+    int32_t *positions;          /* device [num_rows], or NULL                             */
+    int32_t *token_ptr;          /* device [num_seqs + 1], or NULL: first row of each
+                                    sequence, then the rows in use                         */
+    int32_t *held_out;           /* device [num_seqs], or NULL: tokens held afterwards, as
+                                    far as there are pages (the table's width, without a
+                                    free list); may be held                                */
+    int32_t *used_out;           /* device [1], or NULL: entries taken afterwards; may be
+                                    free_used                                              */
+} parason_slot_map;
+
+/* One kernel on `stream`, no allocation, capturable: it reads lengths, table and list
+ * on the device.  Other than held_out and used_out, outputs overlap nothing here.
+ * PARASON_EINVAL for a negative count, a missing or misaligned (4 bytes) array, a
+ * table_stride below table_pages, slots = positions, or what belongs to a free list
+ * without one; PARASON_EUNSUPPORTED for more than 16384 sequences or (about) 2^31 rows;
+ * PARASON_ECUDA if the launch fails. */
+parason_status parason_kv_slots(const parason_slot_map *map, parason_stream_t stream);
+
 /*
  * Take num_tokens tokens out of the cache: k_out[t] = round(K[slots[t]] *
  * k_scale[h]), v_out likewise, in the type of the mode's rows (an exact copy
@@ -545,20 +640,21 @@ parason_status parason_kv_read(const parason_attn_config *cfg, int64_t num_token
                                const parason_rows *v_out, parason_stream_t stream);
 
 /*
- * e4m3 scales per kv head that hold the given tokens:
- *   v_scale[h] = max |v| / 448 over the tokens,
+ * The scales per kv head, of an e4m3 or a 4-bit cache, that hold the given tokens:
+ *   v_scale[h] = max |v| / 448 over the tokens (PARASON_FP4_KV: / 2688),
  *   k_scale[h] = max over the pairs that `rotary` turns of sqrt(x0^2 + x1^2),
- *                and of |x| of the other elements, / 448.
+ *                and of |x| of the other elements, / 448 (/ 2688).
  * No rotation takes an element of a pair past its sqrt, so the K scale holds
  * at every position, after a join has moved the keys too.  Of `rotary` only
  * rotary_dim and pairs are used (NULL: no pairs).  slots may be NULL; tokens
  * with a negative slot do not count.  NaN does not count, and a magnitude
  * above 2^63 (infinities too) counts as 2^63.
  *
- * accumulate 0: the scales are set, at least to 2^-126.  accumulate 1: a
- * scale that is larger already stays (they are at least 2^-126 and finite on
- * entry), so that the scales of several batches come out the same in any
- * order.  PARASON_FP8_E4M3_KV mode only (PARASON_EINVAL otherwise).  One or
+ * accumulate 0: the scales are set, at least to 2^-126 (2^-100).  accumulate 1: a
+ * scale that is larger already stays (they are at least 2^-126, or 2^-100, and finite
+ * on entry), so that the scales of several batches come out the same in any
+ * order.  PARASON_FP8_E4M3_KV and PARASON_FP4_KV modes only (PARASON_EINVAL
+ * otherwise).  Keys that parason_kv_write_norm will norm: from the normed ones.  One or
  * two kernels on `stream`; capture and errors as parason_kv_write.
  */
 parason_status parason_kv_scales(const parason_attn_config *cfg, int64_t num_tokens,
@@ -569,7 +665,7 @@ parason_status parason_kv_scales(const parason_attn_config *cfg, int64_t num_tok
 
 /* Synchronise `stream`, then read and clear the plan's device error word:
  * PARASON_ETIMEOUT if a kernel gave up a bounded wait since the last check,
- * PARASON_ERANGE if an e4m3-KV decode met a q element of magnitude 65520 or
+ * PARASON_ERANGE if an e4m3- or 4-bit-KV decode met a q element of magnitude 65520 or
  * more (the first error recorded wins), PARASON_ECUDA if the stream reports
  * an error, else PARASON_OK. */
 parason_status parason_plan_check(parason_plan plan, parason_stream_t stream);

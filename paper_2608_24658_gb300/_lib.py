@@ -13,7 +13,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "_build", "libparason.so")
 
 OK, EINVAL, ENOMEM, ECUDA, ETIMEOUT, EUNSUPPORTED, ENOSPACE, ERANGE = range(8)
-MODES = {"bf16": 0, "fp32": 1, "fp8": 2}
+MODES = {"bf16": 0, "fp32": 1, "fp8": 2, "fp4": 3}
 (TABLE_ITEMS, TABLE_DFS_LEAVES, TABLE_MERGE_RANGES, TABLE_MERGE, TABLE_WIDE_QUEUE,
  TABLE_NARROW_QUEUE, TABLE_ITEM_ROWS, TABLE_STREAM_ROWS, TABLE_ITEM_KEY0,
  TABLE_SHARD_BRANCHES) = range(10)
@@ -59,11 +59,31 @@ class RotaryDesc(ctypes.Structure):
                 ("position_stride", ctypes.c_int64)]
 
 
+class HeadNormDesc(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("q_head_stride", ctypes.c_int64), ("k_head_stride", ctypes.c_int64),
+                ("eps", ctypes.c_float), ("weight_offset", ctypes.c_float)]
+
+
+class SlotMap(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("num_rows", ctypes.c_int32),
+                ("held", ctypes.c_void_p), ("added", ctypes.c_void_p), ("first", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p), ("table_stride", ctypes.c_int64),
+                ("table_pages", ctypes.c_int32), ("num_free", ctypes.c_int32),
+                ("free_pages", ctypes.c_void_p), ("free_used", ctypes.c_void_p),
+                ("slots", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("token_ptr", ctypes.c_void_p), ("held_out", ctypes.c_void_p),
+                ("used_out", ctypes.c_void_p)]
+
+
 # the same records as bytes (a step's calls make them anew: packing takes a
 # fraction of a Structure's time)
 ROWS = struct.Struct("@Pqq")
 ROTARY = struct.Struct("@iiiPPPq")
+HEAD_NORM = struct.Struct("@PPqqff")
+SLOT_MAP = struct.Struct("@iiPPPPqiiPPPPPPP")
 assert ROWS.size == ctypes.sizeof(Rows) and ROTARY.size == ctypes.sizeof(RotaryDesc)
+assert HEAD_NORM.size == ctypes.sizeof(HeadNormDesc) and SLOT_MAP.size == ctypes.sizeof(SlotMap)
 
 
 class TraceStats(ctypes.Structure):
@@ -74,7 +94,7 @@ class TraceStats(ctypes.Structure):
                 ("acceleration", ctypes.c_double), ("eta", ctypes.c_double)]
 
 
-_cfg = _rows = _rot = _p          # AttnConfig *, Rows *, RotaryDesc *, or their bytes
+_cfg = _rows = _rot = _norm = _map = _p   # AttnConfig *, Rows *, RotaryDesc *, ..., or their bytes
 
 SIGNATURES = {
     "parason_attn_plan": (ctypes.c_int, [ctypes.POINTER(AttnConfig), _i32, _p, _p, _p, _p, _i32,
@@ -104,6 +124,9 @@ SIGNATURES = {
     "parason_rotary_turns": (ctypes.c_int, [_p, _i32, _p]),
     "parason_kv_write": (ctypes.c_int, [_cfg, _i64, _rows, _rows, _rows, _rot, _p, _p, _p, _p, _p,
                                         _p, _i64, _p]),
+    "parason_kv_write_norm": (ctypes.c_int, [_cfg, _i64, _rows, _rows, _rows, _norm, _rot, _p, _p,
+                                             _p, _p, _p, _p, _i64, _p]),
+    "parason_kv_slots": (ctypes.c_int, [_map, _p]),
     "parason_kv_read": (ctypes.c_int, [_cfg, _i64, _p, _p, _p, _i64, _p, _p, _rows, _rows, _p]),
     "parason_kv_scales": (ctypes.c_int, [_cfg, _i64, _rows, _rows, _rot, _p, _i32, _p, _p, _p]),
     "parason_plan_check": (ctypes.c_int, [_p, _p]),

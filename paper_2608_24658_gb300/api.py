@@ -16,8 +16,15 @@ import torch
 from . import _lib
 from ._lib import ParasonError, check
 
-_KV_DTYPES = {"bf16": torch.bfloat16, "fp32": torch.float32, "fp8": torch.float8_e4m3fn}
-_Q_DTYPES = {"bf16": torch.bfloat16, "fp32": torch.float32, "fp8": torch.bfloat16}
+_KV_DTYPES = {"bf16": torch.bfloat16, "fp32": torch.float32, "fp8": torch.float8_e4m3fn,
+              "fp4": torch.uint8}
+_Q_DTYPES = {"bf16": torch.bfloat16, "fp32": torch.float32, "fp8": torch.bfloat16,
+             "fp4": torch.bfloat16}
+
+
+def _page_shape(mode, heads, dim) -> tuple:
+    """The shape of a page: fp4 pages are bytes (parason.h, PARASON_FP4_KV)."""
+    return (heads, 9 * dim) if mode == "fp4" else (heads, 16, dim)
 
 
 def _stream_handle(stream) -> ctypes.c_void_p:
@@ -220,12 +227,13 @@ class Plan:
             raise ValueError(f"q must be a contiguous cuda (or pinned host) {qd} tensor of "
                              f"shape {(L, Hq, d)}")
         dev = k_pages.device
+        page = (Hkv, 9 * d) if kvd is torch.uint8 else (Hkv, 16, d)
         for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
             shape = t.shape
-            if (t.dtype != kvd or shape[1:] != (Hkv, 16, d) or shape[0] < self.num_physical_pages
+            if (t.dtype != kvd or shape[1:] != page or shape[0] < self.num_physical_pages
                     or not t.is_contiguous() or not t.is_cuda or t.device != dev):
                 raise ValueError(f"{name} must be a contiguous cuda {kvd} tensor "
-                                 f"[>= {self.num_physical_pages}, {Hkv}, 16, {d}] on one device")
+                                 f"[>= {self.num_physical_pages}, {', '.join(map(str, page))}] on one device")
         if q_cuda and q.device != dev:
             raise ValueError(f"q must be on {dev}")
         if out is None:
@@ -236,9 +244,9 @@ class Plan:
         if workspace is None:
             workspace = self.workspace(dev)
         ks = vs = None
-        if self.mode == "fp8":
+        if self.mode in ("fp8", "fp4"):
             if k_scale is None or v_scale is None:
-                raise ValueError("fp8 mode needs k_scale and v_scale")
+                raise ValueError(f"{self.mode} mode needs k_scale and v_scale")
             for s in (k_scale, v_scale):
                 if s.dtype != torch.float32 or s.numel() != Hkv or not s.is_cuda:
                     raise ValueError(f"scales must be cuda float32 [{Hkv}]")
@@ -265,18 +273,19 @@ class Plan:
         for name, t in (("q", q), ("out", out)):
             if t.dtype != qd or tuple(t.shape) != (L, Hq, d) or not t.is_cuda or not t.is_contiguous():
                 raise ValueError(f"{name} must be a contiguous cuda {qd} tensor of shape {(L, Hq, d)}")
+        page = _page_shape(self.mode, Hkv, d)
         for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
-            if (t.dtype != kvd or t.dim() != 4 or tuple(t.shape[1:]) != (Hkv, 16, d)
+            if (t.dtype != kvd or tuple(t.shape[1:]) != page
                     or t.shape[0] < self.num_physical_pages or not t.is_contiguous()
                     or t.device != q.device):
                 raise ValueError(f"{name} must be a contiguous {kvd} tensor "
-                                 f"[>= {self.num_physical_pages}, {Hkv}, 16, {d}] on {q.device}")
+                                 f"[>= {self.num_physical_pages}, {', '.join(map(str, page))}] on {q.device}")
         if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (L, Hq)
                                 or not lse.is_cuda or not lse.is_contiguous()):
             raise ValueError(f"lse must be a contiguous cuda float32 tensor of shape {(L, Hq)}")
-        if self.mode == "fp8":
+        if self.mode in ("fp8", "fp4"):
             if k_scale is None or v_scale is None:
-                raise ValueError("fp8 mode needs k_scale and v_scale")
+                raise ValueError(f"{self.mode} mode needs k_scale and v_scale")
             for s in (k_scale, v_scale):
                 if s.dtype != torch.float32 or s.numel() != Hkv or not s.is_cuda:
                     raise ValueError(f"scales must be cuda float32 [{Hkv}]")
@@ -373,7 +382,7 @@ def lse_merge(o_a: torch.Tensor, lse_a: torch.Tensor, o_b: torch.Tensor, lse_b: 
 
 
 # ---------------------------------------------------------------------------
-# the paged cache: filling it, reading it, its e4m3 scales
+# the paged cache: filling it, reading it, its scales per head, its slots
 # ---------------------------------------------------------------------------
 
 _POOL_MODES = {dtype: mode for mode, dtype in _KV_DTYPES.items()}
@@ -417,6 +426,38 @@ class Rotary:
             return _lib.ROTARY.pack(*self._head, 0, 0)
         return _lib.ROTARY.pack(*self._head, positions.data_ptr(),
                                 positions.stride(0) if self.num_axes > 1 else 0)
+
+
+class HeadNorm:
+    """The norm of each head of q and k before its rotation (C type
+    ``parason_head_norm``): x / sqrt(mean x^2 + eps) * w in fp32.  ``q_weight`` and
+    ``k_weight``: cuda [head_dim] for all heads or [heads, head_dim], in the rows' dtype;
+    None leaves q (or k) as it is.  ``unit_offset``: the weights are kept less 1.  The
+    weights are read at every write (a captured one's replays too)."""
+
+    def __init__(self, q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                 eps: float = 1e-6, unit_offset: bool = False):
+        given = [w for w in (q_weight, k_weight) if w is not None]
+        if not given:
+            raise ValueError("a norm needs q_weight or k_weight")
+        for w in given:
+            if (w.dtype not in (torch.bfloat16, torch.float32) or w.dim() not in (1, 2) or not w.is_cuda
+                    or w.dtype != given[0].dtype or w.device != given[0].device
+                    or w.shape[-1] != given[0].shape[-1]):
+                raise ValueError("weights must be cuda [head_dim] or [heads, head_dim] tensors, bf16 or "
+                                 "fp32, alike in dtype, device and head_dim")
+            if (w.stride(-1) != 1 or w.data_ptr() % 16
+                    or (w.dim() == 2 and (w.stride(0) * w.element_size() % 16 or w.stride(0) < 0))):
+                raise ValueError("weights must have contiguous elements and start and rows of 16 bytes")
+        self.q_weight, self.k_weight = q_weight, k_weight
+        self.eps, self.unit_offset = float(eps), bool(unit_offset)
+        self.dtype, self.device, self.head_dim = given[0].dtype, given[0].get_device(), given[0].shape[-1]
+        # heads a weight is for; None: any number
+        self.q_heads, self.k_heads = (None if w is None or w.dim() == 1 or w.stride(0) == 0 and w.shape[0] == 1
+                                      else w.shape[0] for w in (q_weight, k_weight))
+        at = [0 if w is None else w.data_ptr() for w in (q_weight, k_weight)]
+        step = [0 if w is None or w.dim() == 1 else w.stride(0) for w in (q_weight, k_weight)]
+        self._desc = _lib.HEAD_NORM.pack(*at, *step, self.eps, 1.0 if self.unit_offset else 0.0)
 
 
 # (small steps wait for this code: tensors are looked at once, devices as
@@ -472,12 +513,15 @@ def _pools(k_pages, v_pages):
     """(mode, device number, pages, kv heads, head_dim) of a pair of pools."""
     dtype, shape, dev = k_pages.dtype, k_pages.shape, k_pages.get_device()
     mode = _POOL_MODES.get(dtype)
-    if mode is None or len(shape) != 4 or shape[2] != 16 or dev < 0 or not k_pages.is_contiguous():
+    if (mode is None or (mode != "fp4" and (len(shape) != 4 or shape[2] != 16)) or dev < 0
+            or not k_pages.is_contiguous() or (mode == "fp4" and (len(shape) != 3 or shape[2] % 9))):
         raise ValueError("k_pages must be a contiguous cuda tensor [pages, kv heads, 16, head_dim] "
-                         "in bf16, fp32 or float8_e4m3fn")
+                         "in bf16, fp32 or float8_e4m3fn, or uint8 [pages, kv heads, 9 head_dim]")
     if (v_pages.dtype is not dtype or v_pages.shape != shape or v_pages.get_device() != dev
             or not v_pages.is_contiguous()):
         raise ValueError("v_pages must be like k_pages")
+    if mode == "fp4":
+        return mode, dev, shape[0], shape[1], shape[2] // 9
     pages, heads, _, d = shape
     return mode, dev, pages, heads, d
 
@@ -495,7 +539,7 @@ def _head_scales(k_scale, v_scale, heads, dev):
     for s in (k_scale, v_scale):
         if (s is None or s.dtype is not torch.float32 or s.shape != (heads,) or s.get_device() != dev
                 or not s.is_contiguous()):
-            raise ValueError(f"an e4m3 cache needs k_scale and v_scale: contiguous float32 [{heads}] "
+            raise ValueError(f"an e4m3 or 4-bit cache needs k_scale and v_scale: contiguous float32 [{heads}] "
                              f"on cuda:{dev}")
     return k_scale.data_ptr(), v_scale.data_ptr()
 
@@ -514,14 +558,18 @@ def _new(stream, shape, dtype, dev):
 def kv_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
              slots: torch.Tensor, q: Optional[torch.Tensor] = None,
              q_out: Optional[torch.Tensor] = None, rotary: Optional[Rotary] = None,
-             positions: Optional[torch.Tensor] = None, k_scale=None, v_scale=None, stream=None):
+             positions: Optional[torch.Tensor] = None, k_scale=None, v_scale=None, stream=None,
+             norm: Optional[HeadNorm] = None):
     """Keys and values of new tokens into their slots of the paged cache
     (``parason_kv_write``): k is rotated to ``positions``, both are rounded to
-    the cache's type (e4m3: divided by the scales first).  Returns the rotated
-    queries [T, H_q, d] if ``q`` is given, else None.  Asynchronous.
+    the cache's type (e4m3: divided by the scales first; 4 bits: by the scales and
+    those of their blocks).  ``norm``: q and k are normed head by head before their
+    rotation (``parason_kv_write_norm``).  Returns the rotated queries [T, H_q, d] if
+    ``q`` is given, else None.  Asynchronous.
 
-    k, v, q: [T, heads, d] in bf16 (fp32 for an fp32 cache), views with strides
-    of 16 bytes allowed.  slots: cuda int32 [T], page * 16 + offset; a token
+    k_pages, v_pages: the pools of ``Plan.decode``; a 4-bit cache's are uint8 [pages,
+    H_kv, 9 d].  k, v, q: [T, heads, d] in bf16 (fp32 for an fp32 cache), views with
+    strides of 16 bytes allowed.  slots: cuda int32 [T], page * 16 + offset; a token
     whose slot is outside the pool (-1, say) is not written.  positions: cuda
     int32 [T], or [axes, T] as ``rotary`` has axes.  ``q_out`` may be ``q``
     itself where that is contiguous."""
@@ -535,7 +583,7 @@ def kv_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: t
     cv = _token_rows("v", v, shape, dtype, dev)
     at = _token_ints("slots", slots, (tokens,), dev)
     ks = vs = None
-    if mode == "fp8":
+    if mode == "fp8" or mode == "fp4":
         ks, vs = _head_scales(k_scale, v_scale, heads, dev)
     rot = None
     if rotary is not None:
@@ -570,6 +618,19 @@ def kv_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: t
                 raise ValueError("q_out may be q itself only where q is contiguous")
     elif q_out is not None:
         raise ValueError("q_out needs q")
+    if norm is not None:
+        if (norm.dtype is not dtype or norm.device != dev or norm.head_dim != d
+                or norm.k_heads not in (None, heads) or (q is not None and norm.q_heads not in (None, q_heads))):
+            raise ValueError(f"norm must have {dtype} weights of {d} elements on cuda:{dev}, for all heads "
+                             f"or for {q_heads} of q and {heads} of k")
+        if norm.k_weight is None and q is None:
+            raise ValueError("a norm of q alone needs q")
+        st = _lib.load().parason_kv_write_norm(
+            _config(mode, q_heads, heads, d), tokens, cq, ck, cv, norm._desc, rot, at, ks, vs, qo,
+            k_pages.data_ptr(), v_pages.data_ptr(), pages, _stream_on(stream, dev))
+        if st:
+            check(st, "parason_kv_write_norm")
+        return q_out
     st = _lib.load().parason_kv_write(
         _config(mode, q_heads, heads, d), tokens, cq, ck, cv, rot, at, ks, vs, qo,
         k_pages.data_ptr(), v_pages.data_ptr(), pages, _stream_on(stream, dev))
@@ -582,8 +643,8 @@ def kv_read(k_pages: torch.Tensor, v_pages: torch.Tensor, slots: torch.Tensor,
             k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None, k_scale=None,
             v_scale=None, stream=None):
     """The tokens of ``slots`` (cuda int32 [T]) out of the cache: (k, v), each
-    [T, H_kv, d] in bf16 (fp32 from an fp32 cache), e4m3 times its scale
-    (``parason_kv_read``).  A slot outside the pool gives zeros.  Given ``k`` and
+    [T, H_kv, d] in bf16 (fp32 from an fp32 cache), e4m3 and 4 bits times their
+    scales (``parason_kv_read``).  A slot outside the pool gives zeros.  Given ``k`` and
     ``v`` may be views with strides of 16 bytes.  Asynchronous."""
     mode, dev, pages, heads, d = _pools(k_pages, v_pages)
     dtype = _Q_DTYPES[mode]
@@ -593,7 +654,7 @@ def kv_read(k_pages: torch.Tensor, v_pages: torch.Tensor, slots: torch.Tensor,
     shape = (*tokens, heads, d)
     at = _token_ints("slots", slots, tokens, dev)
     ks = vs = None
-    if mode == "fp8":
+    if mode == "fp8" or mode == "fp4":
         ks, vs = _head_scales(k_scale, v_scale, heads, dev)
     k = _new(stream, shape, dtype, dev) if k is None else k
     v = _new(stream, shape, dtype, dev) if v is None else v
@@ -609,13 +670,16 @@ def kv_read(k_pages: torch.Tensor, v_pages: torch.Tensor, slots: torch.Tensor,
 
 def kv_scales(k: torch.Tensor, v: torch.Tensor, rotary: Optional[Rotary] = None,
               slots: Optional[torch.Tensor] = None, k_scale: Optional[torch.Tensor] = None,
-              v_scale: Optional[torch.Tensor] = None, accumulate: bool = False, stream=None):
-    """(k_scale, v_scale), float32 [H_kv]: e4m3 scales that hold the tokens k, v
-    [T, H_kv, 128] (bf16) at any positions ``rotary`` may turn them to
-    (``parason_kv_scales``).  Tokens with a negative slot do not count.  With
+              v_scale: Optional[torch.Tensor] = None, accumulate: bool = False, stream=None,
+              mode: str = "fp8"):
+    """(k_scale, v_scale), float32 [H_kv]: scales of an e4m3 cache (``mode`` "fp8") or of a
+    4-bit one ("fp4") that hold the tokens k, v [T, H_kv, 128] (bf16) at any positions
+    ``rotary`` may turn them to (``parason_kv_scales``).  Tokens with a negative slot do not count.  With
     ``accumulate``, given scales are raised where the tokens need it.
     Asynchronous."""
     shape, dev = k.shape, k.get_device()
+    if mode not in ("fp8", "fp4"):
+        raise ValueError("mode must be fp8 or fp4")
     if len(shape) != 3 or dev < 0:
         raise ValueError("k must be a cuda tensor [T, kv heads, 128]")
     tokens, heads, d = shape
@@ -633,19 +697,88 @@ def kv_scales(k: torch.Tensor, v: torch.Tensor, rotary: Optional[Rotary] = None,
             raise ValueError(f"rotary must turn at most {d} elements")
         rot = rotary._desc(None)
     st = _lib.load().parason_kv_scales(
-        _config("fp8", heads, heads, d), tokens, ck, cv, rot, at, int(bool(accumulate)), ks, vs,
+        _config(mode, heads, heads, d), tokens, ck, cv, rot, at, int(bool(accumulate)), ks, vs,
         _stream_on(stream, dev))
     if st:
         check(st, "parason_kv_scales")
     return k_scale, v_scale
 
 
+def _ints(name, t, shape, dev):
+    if t.dtype is not torch.int32 or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {tuple(shape)} on cuda:{dev}")
+    return t.data_ptr()
+
+
+def kv_slots(page_table: torch.Tensor, held: torch.Tensor, added: Optional[torch.Tensor] = None,
+             tokens: Optional[int] = None, *, first: Optional[torch.Tensor] = None,
+             free_pages: Optional[torch.Tensor] = None, free_used: Optional[torch.Tensor] = None,
+             slots: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+             token_ptr: Optional[torch.Tensor] = None, lens_out: Optional[torch.Tensor] = None,
+             used_out: Optional[torch.Tensor] = None, stream=None):
+    """(slots, positions), int32 [rows]: where the tokens go that sequences add to the
+    cache, for ``kv_write`` and ``kv_read`` (``parason_kv_slots``).  Sequence r holds
+    ``held[r]`` tokens and adds ``added[r]`` (one each if None), its pages are
+    ``page_table[r]``, its token x is at position ``first[r]`` + x.  New pages come from
+    ``free_pages``, in the sequences' order from entry ``free_used[0]`` on, and go into the
+    table; without it the table has them.  (held 0 and added the lengths: the slots of
+    whole sequences.)
+
+    All are cuda int32: page_table [R, pages] (its rows may lie apart), held, added,
+    first and ``lens_out`` [R], ``free_used`` and ``used_out`` [1], ``token_ptr`` [R + 1].
+    ``tokens``: rows of new outputs, as many as the sequences add or more (rows past
+    the last token have slot -1); with neither it nor outputs there are R.  lens_out may
+    be held, and used_out free_used.  Asynchronous."""
+    dev = page_table.get_device()
+    if page_table.dtype is not torch.int32 or page_table.dim() != 2 or dev < 0 or (
+            page_table.stride(1) != 1 and page_table.numel() > 1):
+        raise ValueError("page_table must be a cuda int32 tensor [sequences, pages] with contiguous rows")
+    seqs, width = page_table.shape
+    of_seq = (seqs,)
+    ha = _ints("held", held, of_seq, dev)
+    ad = 0 if added is None else _ints("added", added, of_seq, dev)
+    fi = 0 if first is None else _ints("first", first, of_seq, dev)
+    fp = fu = uo = free = 0
+    if free_pages is not None:
+        free = free_pages.numel()
+        fp = _ints("free_pages", free_pages, (free,), dev)
+        if free == 0:
+            raise ValueError("free_pages must have an entry")
+        fu = 0 if free_used is None else _ints("free_used", free_used, (1,), dev)
+        uo = 0 if used_out is None else _ints("used_out", used_out, (1,), dev)
+    elif free_used is not None or used_out is not None:
+        raise ValueError("free_used and used_out need free_pages")
+    if slots is not None:
+        rows = slots.shape[0] if slots.dim() == 1 else -1
+        if tokens is not None and tokens != rows:
+            raise ValueError(f"slots must be [{tokens}]")
+    elif positions is not None and positions.dim() == 1:
+        rows = positions.shape[0]
+    else:
+        if tokens is None and added is not None:
+            raise ValueError("added needs tokens, the rows of the outputs")
+        rows = seqs if tokens is None else int(tokens)
+    if rows < 0:
+        raise ValueError("the outputs must be [rows]")
+    slots = _new(stream, (rows,), torch.int32, dev) if slots is None else slots
+    positions = _new(stream, (rows,), torch.int32, dev) if positions is None else positions
+    sl, po = _ints("slots", slots, (rows,), dev), _ints("positions", positions, (rows,), dev)
+    tp = 0 if token_ptr is None else _ints("token_ptr", token_ptr, (seqs + 1,), dev)
+    lo = 0 if lens_out is None else _ints("lens_out", lens_out, of_seq, dev)
+    st = _lib.load().parason_kv_slots(
+        _lib.SLOT_MAP.pack(seqs, rows, ha, ad, fi, page_table.data_ptr(), page_table.stride(0) if seqs > 1 else width,
+                           width, free, fp, fu, sl, po, tp, lo, uo), _stream_on(stream, dev))
+    if st:
+        check(st, "parason_kv_slots")
+    return slots, positions
+
+
 def version() -> str:
     return _lib.load().parason_version().decode()
 
 
-__all__ = ["Plan", "Rotary", "kv_read", "kv_scales", "kv_write", "lse_merge", "version",
-           "ParasonError"]
+__all__ = ["HeadNorm", "Plan", "Rotary", "kv_read", "kv_scales", "kv_slots", "kv_write", "lse_merge",
+           "version", "ParasonError"]
 
 
 # ---------------------------------------------------------------------------

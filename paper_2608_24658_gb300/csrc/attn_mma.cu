@@ -57,6 +57,7 @@
 // to 50 then keeps m = 0 (CappedFree), everything else the running maximum
 // (CappedRef).
 #include <mutex>
+#include <type_traits>
 
 #include "device_common.cuh"
 #include "logit_cap.cuh"
@@ -102,6 +103,15 @@ struct KvE4m3 {
     static constexpr int kStepPages = 2;
     static constexpr int kCap = kCapNone;
 };
+// (kElemBytes 1: what the fragments are widened from and q is narrowed for)
+struct KvE2m1 {
+    static constexpr int kElemBytes = 1;
+    static constexpr int kSuffixWarps = 12;
+    static constexpr int kStepPages = 2;
+    static constexpr int kCap = kCapNone;
+};
+template <class KV>
+constexpr bool kFp4 = std::is_base_of_v<KvE2m1, KV>;
 
 // The same formats under a logit cap (instantiations of their own: the others
 // keep their registers and code).
@@ -117,7 +127,7 @@ struct CappedRef : KV {
 template <int D, class KV>
 struct Shape {
     static constexpr int kRowBytes = D * KV::kElemBytes;    // one token of one kv head
-    static constexpr int kPageBytes = kPageSize * kRowBytes; // one page of one kv head
+    static constexpr int kPageBytes = kFp4<KV> ? fp4_page_bytes(D) : kPageSize * kRowBytes; // one page of one kv head
     // a page lands as kSeg column blocks of 16 tokens x 128 bytes, so that 8
     // consecutive tokens hit 8 different 128-byte swizzle rows
     static constexpr int kSeg = kRowBytes / 128;
@@ -131,10 +141,10 @@ struct Shape {
     static constexpr int kNarrowBytes = kSuffixWarps * kWarpRingBytes;
     static constexpr int kNarrowBars = kSuffixWarps * kWarpStages;
 
-    static constexpr int kBars = 64;                        // the larger of both passes' barriers
-    static constexpr int kBodyBytes = kNarrowBytes;
+    static constexpr int kBars = kNarrowBars > 64 ? kNarrowBars : 64;   // the larger of both passes' barriers
+    static constexpr int kBodyBytes = 192 * 1024;
     static constexpr int kSmemBytes = kBodyBytes + kBars * 8 + 1024;   // + alignment slack
-    static_assert(kNarrowBars <= kBars, "barrier area holds the suffix rings' barriers");
+    static_assert(kNarrowBytes <= kBodyBytes, "the suffix rings fit");
     static_assert(kRowBytes % 128 == 0, "token rows are whole 128-byte blocks");
     static_assert(kWarpStages >= 2, "suffix ring depth");
     static_assert(kSuffixWarps <= kMaxSuffixWarps, "suffix-pass warps fit the item rings");
@@ -150,11 +160,15 @@ struct Shape {
 // only, so its lines go first when L2 needs room (the partials written
 // meanwhile stay for the merge).
 template <int D, class KV>
-__device__ __forceinline__ void load_suffix_page(uint32_t dst, const KvMaps &maps, int row,
+__device__ __forceinline__ void load_suffix_page(uint32_t dst, const KvMaps &maps, const AttnArgs &a, int row,
                                                  uint32_t bar) {
     using S = Shape<D, KV>;
     const uint64_t pol = dev::l2_evict_first_policy();
-    if constexpr (S::kSeg > 1) {
+    if constexpr (kFp4<KV>) {
+        const int64_t at = static_cast<int64_t>(row / kPageSize) * S::kPageBytes;
+        dev::bulk_load_hint(dst, a.k_raw + at, S::kPageBytes, bar, pol);
+        dev::bulk_load_hint(dst + S::kPageBytes, a.v_raw + at, S::kPageBytes, bar, pol);
+    } else if constexpr (S::kSeg > 1) {
         const int ph = row / kPageSize;
         dev::tma_load_4d_hint(dst, &maps.k_box, 0, 0, 0, ph, bar, pol);
         dev::tma_load_4d_hint(dst + S::kPageBytes, &maps.v_box, 0, 0, 0, ph, bar, pol);
@@ -189,21 +203,95 @@ __device__ __forceinline__ int out_col(int nt, int e, int tig) {
         return 16 * (2 * tig + (e & 1)) + nt;
 }
 
+// The page's token at MMA index m (0..15) of both products.  4-bit rows are 64
+// bytes: with neighbours swapped in every second pair the tokens that the four
+// lanes of a V load take at once lie in both halves of the banks.
+template <class KV>
+__device__ __forceinline__ int key_of(int m) {
+    return kFp4<KV> ? m ^ ((m >> 1) & 1) : m;
+}
+
 // Scores of tokens past the page's last one, which may be anything, to 0: a capped
 // score can share its reciprocal with its neighbour.
+template <class KV>
 __device__ __forceinline__ void clear_past(float (&sc)[2][4], int valid, int tig) {
     if (valid >= kPageSize) return;
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-        if ((e >> 2) * 8 + 2 * tig + (e & 1) >= valid) sc[e >> 2][e & 3] = 0.f;
+        if (key_of<KV>((e >> 2) * 8 + 2 * tig + (e & 1)) >= valid) sc[e >> 2][e & 3] = 0.f;
 }
 
 // The same of a transposed step's scores.
+template <class KV>
 __device__ __forceinline__ void clear_past_t(float (&x)[4], int valid, int gid) {
     if (valid >= kPageSize) return;
-    if (gid >= valid) x[0] = x[1] = 0.f;
-    if (gid + 8 >= valid) x[2] = x[3] = 0.f;
+    if (key_of<KV>(gid) >= valid) x[0] = x[1] = 0.f;
+    if (key_of<KV>(gid + 8) >= valid) x[2] = x[3] = 0.f;
 }
+
+// 4-bit KV: the f16 fragments of one page.  K: lane (gid, tig) has elements
+// 32 tig .. 32 tig + 31 of tokens key_of(gid) and key_of(gid + 8), a 16-byte
+// chunk of each with two scales; k-step ks takes pairs 4 ks and 4 ks + 2 of
+// them, the slice that load_q_fragments gives it of q.
+struct Fp4Keys {
+    uint32_t w[2][4];        // chunks of both tokens
+    uint32_t s[2][2];        // their scales, as f16 pairs of the same value
+    __device__ __forceinline__ Fp4Keys(uint32_t base, int lane) {
+        const int gid = lane >> 2, tig = lane & 3;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int tok = (gid ^ ((gid >> 1) & 1)) + 8 * h;
+            const uint4 u = lds128(base + tok * 64 + 16 * tig);
+            w[h][0] = u.x;
+            w[h][1] = u.y;
+            w[h][2] = u.z;
+            w[h][3] = u.w;
+            const uint32_t both = e4m3x2_to_f16x2(lds16(base + fp4_value_bytes(128) + tok * 8 + 2 * tig));
+            s[h][0] = __byte_perm(both, 0u, 0x1010);
+            s[h][1] = __byte_perm(both, 0u, 0x3232);
+        }
+    }
+    // word i (k-steps 2 i and 2 i + 1) of token h: two pairs for each step
+    __device__ __forceinline__ void word(int h, int i, uint32_t (&p)[4]) const {
+        e2m1x8_to_f16(w[h][i], p);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) p[j] = mul_f16x2(p[j], s[h][i >> 1]);
+    }
+};
+
+// V: lane (gid, tig) has columns 16 gid .. 16 gid + 15 (one scale) of tokens
+// key_of(2 tig), key_of(2 tig + 1) and the two 8 further; pairs are of tokens, so
+// the bytes of two tokens are regrouped before they are widened.  Tokens from
+// `valid` on may hold anything (NaN scales included): they become zeros.
+struct Fp4Values {
+    uint32_t w[2][4];        // even columns of the chunk's words, odd columns, for each token pair
+    uint32_t s[2];           // the pair's scales
+    __device__ __forceinline__ Fp4Values(uint32_t base, int valid, int lane) {
+        const int gid = lane >> 2, tig = lane & 3;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int t0 = 2 * tig + (tig & 1) + 8 * h, t1 = t0 + 1 - 2 * (tig & 1);
+            uint2 x = lds64(base + t0 * 64 + 8 * gid), y = lds64(base + t1 * 64 + 8 * gid);
+            uint32_t sx = lds8(base + fp4_value_bytes(128) + t0 * 8 + gid);
+            uint32_t sy = lds8(base + fp4_value_bytes(128) + t1 * 8 + gid);
+            if (valid < kPageSize) {
+                if (t0 >= valid) x = make_uint2(0u, 0u), sx = 0u;
+                if (t1 >= valid) y = make_uint2(0u, 0u), sy = 0u;
+            }
+            w[h][0] = (x.x & 0x0f0f0f0fu) | ((y.x << 4) & 0xf0f0f0f0u);
+            w[h][1] = ((x.x >> 4) & 0x0f0f0f0fu) | (y.x & 0xf0f0f0f0u);
+            w[h][2] = (x.y & 0x0f0f0f0fu) | ((y.y << 4) & 0xf0f0f0f0u);
+            w[h][3] = ((x.y >> 4) & 0x0f0f0f0fu) | (y.y & 0xf0f0f0f0u);
+            s[h] = e4m3x2_to_f16x2(sx | (sy << 8));
+        }
+    }
+    // token pair h: columns 8 i, 8 i + 2, 8 i + 4, 8 i + 6 of the lane's 16 (odd 0), or those after them
+    __device__ __forceinline__ void columns(int h, int i, int odd, uint32_t (&p)[4]) const {
+        e2m1x8_to_f16(w[h][2 * i + odd], p);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) p[j] = mul_f16x2(p[j], s[h]);
+    }
+};
 
 // Online softmax over one page's scores s (two n-tiles of 8 tokens), then
 // rescale o; returns P packed as the A operand of the PV MMA.
@@ -213,7 +301,7 @@ __device__ __forceinline__ void softmax_page(float (&sc)[2][4], int valid, float
                                              int tig, uint32_t (&pa)[4]) {
     // (under a cap scale_log2 is the factor into the tanh)
     if constexpr (KV::kCap == kCapRef) {
-        clear_past(sc, valid, tig);
+        clear_past<KV>(sc, valid, tig);
         cap_scores<1>(sc, cap_large, CapFactors(scale_log2, cap_log2));
     }
     float x[2][4];
@@ -221,7 +309,7 @@ __device__ __forceinline__ void softmax_page(float (&sc)[2][4], int valid, float
     for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int tok = nt * 8 + 2 * tig + (e & 1);
+            const int tok = key_of<KV>(nt * 8 + 2 * tig + (e & 1));
             x[nt][e] = tok < valid ? (KV::kCap != kCapNone ? sc[nt][e] : sc[nt][e] * scale_log2) : -INFINITY;
         }
     float mx0 = fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1]));
@@ -280,7 +368,7 @@ template <int D>
 __device__ __forceinline__ void softmax_page_free(float (&sc)[2][4], int valid, const CapFactors &cap,
                                                   bool &cap_large, WarpState<D> &st, int tig,
                                                   uint32_t (&pa)[4]) {
-    clear_past(sc, valid, tig);
+    clear_past<KvBf16>(sc, valid, tig);
     cap_free_scores<1>(sc, cap_large, cap);
     float(&p)[8] = *reinterpret_cast<float(*)[8]>(&sc);
     if (valid < kPageSize) {
@@ -321,6 +409,19 @@ __device__ __forceinline__ void page_step(uint32_t kbase, uint32_t vbase, int va
             float(&acc)[2][4] = ks < D / 32 ? sc : sd;
             dev::mma_bf16_16816(acc[0], qa[ks], b00, b01);
             dev::mma_bf16_16816(acc[1], qa[ks], b10, b11);
+        }
+    } else if constexpr (kFp4<KV>) {
+        const Fp4Keys k(kbase, lane);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            float(&acc)[2][4] = i < D / 64 ? sc : sd;
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) {
+                uint32_t b[4];
+                k.word(nt, i, b);
+                dev::mma_f16_16816(acc[nt], qa[2 * i], b[0], b[1]);
+                dev::mma_f16_16816(acc[nt], qa[2 * i + 1], b[2], b[3]);
+            }
         }
     } else {
         // thread (gid, tig) reads bytes 4tig..4tig+3 of 16-byte chunk ks of token gid
@@ -369,6 +470,17 @@ __device__ __forceinline__ void page_step(uint32_t kbase, uint32_t vbase, int va
             v3 &= keep_hi;
             dev::mma_bf16_16816(st.o[dt], pa, v0, v1);
             dev::mma_bf16_16816(st.o[dt + 1], pa, v2, v3);
+        }
+    } else if constexpr (kFp4<KV>) {
+        const Fp4Values v(vbase, valid, lane);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {                    // columns 8 (c / 2) + c % 2 + {0, 2, 4, 6}
+            uint32_t lo[4], hi[4];
+            v.columns(0, c >> 1, c & 1, lo);
+            v.columns(1, c >> 1, c & 1, hi);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                dev::mma_f16_16816(st.o[8 * (c >> 1) + 2 * j + (c & 1)], pa, lo[j], hi[j]);
         }
     } else {
         // thread gid owns output columns 16gid .. 16gid+15: one 16-byte chunk
@@ -485,6 +597,18 @@ __device__ __forceinline__ void scores_t(uint32_t kbase, const uint32_t (&qb)[D 
                          ka[2], ka[3]);
             dev::mma_bf16_16816(acc, ka, qb[ks][0], qb[ks][1]);
         }
+    } else if constexpr (kFp4<KV>) {
+        const Fp4Keys k(kbase, lane);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            float(&acc)[4] = i < D / 64 ? sc : sd;
+            uint32_t g[4], h[4];
+            k.word(0, i, g);
+            k.word(1, i, h);
+            const uint32_t k0[4] = {g[0], h[0], g[1], h[1]}, k1[4] = {g[2], h[2], g[3], h[3]};
+            dev::mma_f16_16816(acc, k0, qb[2 * i][0], qb[2 * i][1]);
+            dev::mma_f16_16816(acc, k1, qb[2 * i + 1][0], qb[2 * i + 1][1]);
+        }
     } else {
         static_assert(D == 128, "e4m3 KV path is written for head_dim 128");
         // 16-byte chunks 2 tig and 2 tig + 1 of tokens gid and gid + 8 (the
@@ -542,6 +666,22 @@ __device__ __forceinline__ void pv_t(uint32_t vbase, int valid, uint32_t pb0, ui
             va[3] &= keep_hi;
             dev::mma_bf16_16816(st.o[dt], va, pb0, pb1);
         }
+    } else if constexpr (kFp4<KV>) {
+        const Fp4Values v(vbase, valid, lane);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            uint32_t p[2][2][4];                         // [token pair][odd column][column pair]
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                v.columns(h, i, 0, p[h][0]);
+                v.columns(h, i, 1, p[h][1]);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t a4[4] = {p[0][0][j], p[0][1][j], p[1][0][j], p[1][1][j]};
+                dev::mma_f16_16816(st.o[4 * i + j], a4, pb0, pb1);
+            }
+        }
     } else {
         // this lane's output columns are 16 gid .. 16 gid + 15: chunk gid of
         // its four tokens 2tig, 2tig + 1, 2tig + 8, 2tig + 9
@@ -587,7 +727,7 @@ __device__ __forceinline__ void pages_step_t(const uint32_t *kbase, const uint32
     if constexpr (KV::kCap == kCapRef) {
 #pragma unroll
         for (int p = 0; p < NP; ++p) scores_t<D, KV>(kbase[p], qb, lane, x[p]);
-        clear_past_t(x[NP - 1], valid_last, lane >> 2);
+        clear_past_t<KV>(x[NP - 1], valid_last, lane >> 2);
         cap_scores<2>(x, cap_large, CapFactors(scale_log2, cap_log2));
     }
 #pragma unroll
@@ -597,7 +737,7 @@ __device__ __forceinline__ void pages_step_t(const uint32_t *kbase, const uint32
         const int valid = p == NP - 1 ? valid_last : kPageSize;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int tok = gid + ((e >> 1) << 3);
+            const int tok = key_of<KV>(gid + ((e >> 1) << 3));
             if constexpr (KV::kCap != kCapNone)
                 x[p][e] = tok < valid ? x[p][e] : -INFINITY;
             else
@@ -662,7 +802,7 @@ __device__ __forceinline__ void pages_step_t_free(const uint32_t *kbase, const u
     float x[NP][4];
 #pragma unroll
     for (int p = 0; p < NP; ++p) scores_t<D, KV>(kbase[p], qb, lane, x[p]);
-    clear_past_t(x[NP - 1], valid_last, gid);
+    clear_past_t<KV>(x[NP - 1], valid_last, gid);
     cap_free_scores<2>(x, cap_large, cap);
     st.m[0] = st.m[1] = 0.f;
 #pragma unroll
@@ -709,7 +849,9 @@ __device__ __forceinline__ void load_q_fragments(const AttnArgs &a, const WorkIt
                 qa[ks][2 + h] = qrow[h] ? *reinterpret_cast<const uint32_t *>(qrow[h] + c0 + 8) : 0u;
             } else {
                 uint2 u = make_uint2(0u, 0u);
-                if (qrow[h]) u = *reinterpret_cast<const uint2 *>(qrow[h] + ks * 16 + 4 * tig);
+                // (4-bit: the slice of the lane's 32 elements that Fp4Keys gives the step)
+                if (qrow[h])
+                    u = *reinterpret_cast<const uint2 *>(qrow[h] + (kFp4<KV> ? 32 * tig + 4 * ks : ks * 16 + 4 * tig));
                 qa[ks][h] = q_pair_to_f16(u.x, big);
                 qa[ks][2 + h] = q_pair_to_f16(u.y, big);
             }
@@ -887,7 +1029,7 @@ __device__ void suffix_warp(const KvMaps &maps, const AttnArgs &a, uint32_t ring
             const int s = issued % NS;
             const uint32_t bar = my_bar + s * 8;
             dev::mbar_arrive_expect_tx(bar, S::kStageBytes);
-            load_suffix_page<D, KV>(my_ring + s * S::kStageBytes, maps, row, bar);
+            load_suffix_page<D, KV>(my_ring + s * S::kStageBytes, maps, a, row, bar);
         }
         ++iss_pg;
         ++issued;
@@ -1050,6 +1192,8 @@ constexpr int kTcCvStages = 4;
 // conversion, and measured level (head_dim 128) or 1% slower (64) this way.
 constexpr int kTcWantBlocks = 8;
 constexpr int kTcCvOffset = kTcF8Stages * kTcF8StageBytes;    // 64 KB
+constexpr int kTcF4OpBytes = kTcBlockPages * fp4_page_bytes(128);   // 4-bit: K (or V) of a block, as stored
+static_assert(2 * kTcF4OpBytes <= kTcF8StageBytes, "a 4-bit block fits a raw stage");
 static_assert(kTcF8Stages < kTcStages, "raw e4m3 stages and kBarWant use the ring's barriers");
 static_assert(kTcCvOffset + kTcCvStages * kTcStageBytes <= kTcRingBytes, "e4m3 rings fit");
 constexpr int kTcTmemCols = 512;
@@ -1066,6 +1210,7 @@ constexpr int kTcPvWarp = 11;
 static_assert(kTcRingBytes <= Shape<128, KvBf16>::kBodyBytes, "tcgen05 ring fits the CTA's memory");
 static_assert(kTcRingBytes <= Shape<128, KvBf16Deep>::kBodyBytes, "tcgen05 ring fits the CTA's memory");
 static_assert(kTcRingBytes <= Shape<128, KvE4m3>::kBodyBytes, "tcgen05 ring fits the CTA's memory");
+static_assert(kTcRingBytes <= Shape<128, KvE2m1>::kBodyBytes, "tcgen05 ring fits the CTA's memory");
 static_assert(kTcSchedulerWarp < kThreads / 32 && kTcPvWarp < kThreads / 32,
               "every tcgen05 role has a warp");
 static_assert(kMaxSuffixWarps <= kThreads / 32, "every suffix-pass warp exists");
@@ -1165,6 +1310,59 @@ __device__ __forceinline__ void convert_block_e4m3(uint32_t src, uint32_t dst, i
                      "r"(b0), "r"(b1), "r"(b2), "r"(b3)
                      : "memory");
     }
+}
+
+// The same of a 4-bit block, 4 of its 512 16-byte chunks (32 elements, two scales) a
+// thread: pages as they are stored, K of 4 pages, then V.  A chunk fills four
+// 16-byte slots of a row; the quarter warp's two rows of four chunks take eight
+// bank groups when chunks 2 and 3, whose column block is the other one, take their
+// slots in another order.
+__device__ __forceinline__ void convert_block_e2m1(uint32_t src, uint32_t dst, int valid, int t) {
+    constexpr int kPage = fp4_page_bytes(128), kValues = fp4_value_bytes(128);
+    uint4 w[4];
+    uint32_t sc[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int idx = t + kTcRows * q;
+        const int op = idx >> 8;                 // 0: K, 1: V
+        const int r = (idx >> 2) & 63;           // token
+        const int c = idx & 3;                   // elements 32c .. 32c + 31
+        const uint32_t page = src + (op * kTcBlockPages + (r >> 4)) * kPage;
+        w[q] = lds128(page + (r & 15) * 64 + 16 * c);
+        sc[q] = lds16(page + kValues + (r & 15) * 8 + 2 * c);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int idx = t + kTcRows * q;
+        const int op = idx >> 8, r = (idx >> 2) & 63, c = idx & 3;
+        if (r >= valid) w[q] = make_uint4(0u, 0u, 0u, 0u), sc[q] = 0u;
+        const bool turned = (c & 2) != 0;
+        const uint32_t both = e4m3x2_to_f16x2(sc[q]);
+        const uint32_t s0 = __byte_perm(both, 0u, turned ? 0x3232 : 0x1010);
+        const uint32_t s1 = __byte_perm(both, 0u, turned ? 0x1010 : 0x3232);
+        const uint32_t v[4] = {turned ? w[q].z : w[q].x, turned ? w[q].w : w[q].y, turned ? w[q].x : w[q].z,
+                               turned ? w[q].y : w[q].w};
+        const uint32_t row = dst + op * kTcKBytes + (c >> 1) * kTcColBlockBytes + r * 128;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t p[4];
+            e2m1x8_to_f16(v[j], p);
+            const uint32_t s = j < 2 ? s0 : s1;
+            const int slot = 4 * (c & 1) + (turned ? j ^ 2 : j);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + ((slot ^ (r & 7)) << 4)),
+                         "r"(mul_f16x2(p[0], s)), "r"(mul_f16x2(p[1], s)), "r"(mul_f16x2(p[2], s)),
+                         "r"(mul_f16x2(p[3], s))
+                         : "memory");
+        }
+    }
+}
+
+template <class KV>
+__device__ __forceinline__ void convert_block(uint32_t src, uint32_t dst, int valid, int t) {
+    if constexpr (kFp4<KV>)
+        convert_block_e2m1(src, dst, valid, t);
+    else
+        convert_block_e4m3(src, dst, valid, t);
 }
 
 __device__ __forceinline__ int tc_blocks(int num_pages) {
@@ -1268,6 +1466,21 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
                     // thread issuing them all was the tile's bottleneck); the
                     // expected bytes are registered first
                     const uint32_t fb = bar(kBarKvFull + s);
+                    if constexpr (kFp4<KV>) {
+                        // a copy per page and tensor (even lanes K); pages past the
+                        // item's end are not loaded (the converters write zeros)
+                        constexpr uint32_t kBytes = fp4_page_bytes(D);
+                        const int pages = min(kTcBlockPages, np - bi * kTcBlockPages), j = lane >> 1;
+                        if (lane == 0) dev::mbar_arrive_expect_tx(fb, 2 * kBytes * pages);
+                        __syncwarp();
+                        if (j < pages) {
+                            const int64_t at = static_cast<int64_t>(m.rows[bi * kTcBlockPages + j] / kPageSize) * kBytes;
+                            dev::bulk_load_hint(ring + s * kTcF8StageBytes + (lane & 1) * kTcF4OpBytes + j * kBytes,
+                                                ((lane & 1) ? a.v_raw : a.k_raw) + at, kBytes, fb, f8_pol);
+                        }
+                        last_issue[s] = blk;
+                        continue;
+                    }
                     if (lane == 0)
                         dev::mbar_arrive_expect_tx(fb, kF8 ? kTcF8StageBytes : kStageBytes);
                     __syncwarp();
@@ -1672,7 +1885,7 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
                     !tc_warp_wait(bar(kBarCvEmpty + c), ((gb / kTcCvStages) - 1) & 1, limit, abort_flag,
                                   lane))
                     return false;
-                convert_block_e4m3(ring + s * kTcF8StageBytes, ring + kTcCvOffset + c * kStageBytes,
+                convert_block<KV>(ring + s * kTcF8StageBytes, ring + kTcCvOffset + c * kStageBytes,
                                    valid, r);
                 tc::fence_proxy_async_smem();
                 dev::mbar_arrive(bar(kBarCvFull + c));
@@ -2348,8 +2561,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int s = 0; s < S::kNarrowBars; ++s) dev::mbar_init(bars + 8 * s, 1);
         }
         dev::fence_mbar_init();
-        dev::prefetch_tensormap(&maps.k);
-        dev::prefetch_tensormap(&maps.v);
+        if constexpr (!kFp4<KV>) {
+            dev::prefetch_tensormap(&maps.k);
+            dev::prefetch_tensormap(&maps.v);
+        }
         if constexpr (S::kSeg > 1) {
             dev::prefetch_tensormap(&maps.k_box);
             dev::prefetch_tensormap(&maps.v_box);
@@ -2469,6 +2684,8 @@ template <class KV>
 using Uncapped = KV;
 
 cudaError_t attn_mma_ctas_per_sm(int head_dim, int mode, int *ctas_per_sm) {
+    if (mode == PARASON_FP4_KV)
+        return head_dim == 128 ? configure<128, KvE2m1>(ctas_per_sm) : cudaErrorNotSupported;
     if (mode == PARASON_FP8_E4M3_KV)
         return head_dim == 128 ? configure<128, KvE4m3>(ctas_per_sm) : cudaErrorNotSupported;
     if (head_dim == 128) {
@@ -2492,11 +2709,16 @@ cudaError_t launch_attn_fp8(const AttnArgs &a, const KvMaps &maps, int head_dim,
                             cudaStream_t stream) {
     if (a.num_items <= 0 || a.num_ctas <= 0) return cudaSuccess;
     if (head_dim != 128) return cudaErrorNotSupported;
+    if (a.k_raw)
+        return a.cap_log2 > 0.f ? launch<128, CappedRef<KvE2m1>>(a, maps, stream)
+                                : launch<128, KvE2m1>(a, maps, stream);
     return a.cap_log2 > 0.f ? launch<128, CappedRef<KvE4m3>>(a, maps, stream)
                             : launch<128, KvE4m3>(a, maps, stream);
 }
 
 cudaError_t attn_mma_prepare_cap(int head_dim, int mode) {
+    if (mode == PARASON_FP4_KV)
+        return head_dim == 128 ? configure<128, CappedRef<KvE2m1>>(nullptr) : cudaErrorNotSupported;
     if (mode == PARASON_FP8_E4M3_KV)
         return head_dim == 128 ? configure<128, CappedRef<KvE4m3>>(nullptr) : cudaErrorNotSupported;
     const cudaError_t e = configure_bf16<CappedFree>(head_dim);

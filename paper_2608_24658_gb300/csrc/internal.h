@@ -31,6 +31,17 @@ static_assert(sizeof(WorkItem) == 32, "WorkItem is a 32-byte device record");
 
 constexpr int kPageSize = 16;
 
+// 4-bit KV: a page of one kv head is its 16 rows of e2m1 values (two to a byte,
+// the even element in the low bits), then 16 rows of e4m3 scales, one to each
+// kFp4Block elements of a row.
+constexpr int kFp4Block = 16;
+__host__ __device__ constexpr int fp4_value_bytes(int d) { return kPageSize * d / 2; }
+__host__ __device__ constexpr int fp4_page_bytes(int d) { return fp4_value_bytes(d) + kPageSize * d / kFp4Block; }
+
+// Modes whose KV the kernels widen to f16 (q narrowed to f16, fp32 scales per kv
+// head).
+inline bool scaled_kv(int mode) { return mode == PARASON_FP8_E4M3_KV || mode == PARASON_FP4_KV; }
+
 // Suffix-warp item record: 32 words (one 128-byte line, word i read by lane
 // i): the WorkItem, the start of its page rows in the stream, its first rows.
 constexpr int kRecWords = 32;
@@ -103,6 +114,8 @@ struct AttnArgs {
     void *out;
     float *lse;
     int32_t early;          // launch as a programmatic dependent (plan.cpp: early)
+    // 4-bit KV: the pools, whose pages bulk copies address (no tensor map)
+    const uint8_t *k_raw, *v_raw;
 };
 
 struct MergeArgs {
@@ -178,9 +191,10 @@ cudaError_t prefill_prepare_cap(int mode);
 // Kernel launchers; each returns the launch's cudaError_t.
 cudaError_t launch_attn_bf16(const AttnArgs &a, const KvMaps &maps, int head_dim,
                              cudaStream_t stream);
+// e4m3 KV, or 4-bit KV where a.k_raw is set
 cudaError_t launch_attn_fp8(const AttnArgs &a, const KvMaps &maps, int head_dim,
                             cudaStream_t stream);
-// tree-masked prefill (bf16 or e4m3 KV at head_dim 128)
+// tree-masked prefill (bf16, e4m3 or 4-bit KV at head_dim 128)
 cudaError_t launch_prefill(const AttnArgs &a, const KvMaps &maps, int mode, cudaStream_t stream);
 cudaError_t launch_attn_fp32(const AttnArgs &a, const float *k_pages, const float *v_pages,
                              int head_dim, cudaStream_t stream);

@@ -9,15 +9,19 @@
 
 #include <atomic>
 #include <cmath>
+#include <type_traits>
 
 #include "device_common.cuh"
 #include "internal.h"
+#include "tile_common.cuh"
 
 namespace parason {
 namespace {
 
 constexpr int kMaxAxes = 4;
 constexpr float kE4m3Max = 448.f;
+constexpr float kFp4Max = 448.f * 6.f;   // the largest scale of a block times the largest value
+constexpr float kLeastScale = 1.17549435e-38f, kLeastScaleFp4 = 0x1p-100f;   // of a kv head
 constexpr int kMaxHeads = 16384;         // of q, and of k: what the kernels' counters hold
 constexpr int kMaxDevices = 64;
 constexpr int64_t kMaxRows = 1ll << 34;  // tokens times kv heads: what a grid holds (16 and more a CTA)
@@ -39,9 +43,23 @@ struct RotaryArgs {
     uint64_t axes[2];                    // of frequencies 0..31 and 32..63
 };
 
+// The norm of each head of q and k: weights of a row's type, a head's `stride`
+// further (0: one for all heads); null: not normed.
+struct NormArgs {
+    const void *q, *k;
+    int64_t q_stride, k_stride;
+    float eps, offset;
+};
+
+// The type of a 4-bit cache's pools: bytes.
+struct Fp4 {
+    uint8_t byte;
+};
+
 struct WriteArgs {
     Rows q, k, v;
     RotaryArgs rot;
+    NormArgs norm;
     const int32_t *slots;
     const float *k_scale, *v_scale;
     void *q_out, *k_pages, *v_pages;
@@ -70,6 +88,7 @@ struct ScalesArgs {
     float *k_scale, *v_scale;
     int64_t num_tokens;
     int32_t num_kv_heads, half, interleaved;
+    float limit;                         // the largest value that a scale of 1 holds
 };
 
 // Eight consecutive elements, the unit every kernel here moves: 16 bytes of
@@ -85,6 +104,21 @@ __device__ __forceinline__ Raw8<T> load8(const T *p) {
 #pragma unroll
     for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) {
         const uint4 u = __ldcs(reinterpret_cast<const uint4 *>(p) + i);
+        r.w[4 * i] = u.x;
+        r.w[4 * i + 1] = u.y;
+        r.w[4 * i + 2] = u.z;
+        r.w[4 * i + 3] = u.w;
+    }
+    return r;
+}
+
+// The same of weights, which stay in the caches.
+template <class T>
+__device__ __forceinline__ Raw8<T> load_weight8(const T *p) {
+    Raw8<T> r;
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) {
+        const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p) + i);
         r.w[4 * i] = u.x;
         r.w[4 * i + 1] = u.y;
         r.w[4 * i + 2] = u.z;
@@ -130,6 +164,15 @@ __device__ __forceinline__ void store8(__nv_fp8_e4m3 *p, const float (&x)[8]) {
 
 template <class KV>
 constexpr bool kScaled = sizeof(KV) == 1;
+template <class KV>
+constexpr bool kIsFp4 = std::is_same_v<KV, Fp4>;
+
+// Bytes of an element, and elements' distance in a pool between kv heads of a page and
+// between tokens (4-bit: bytes, as values and block scales lie apart in a page).
+template <class KV, int D>
+constexpr int64_t kHeadStep = kIsFp4<KV> ? fp4_page_bytes(D) : kPageSize * D;
+template <class KV, int D>
+constexpr int64_t kTokenStep = kIsFp4<KV> ? D / 2 : D;
 
 constexpr int kThreads = 128;            // 4 warps, each of them on its own
 constexpr int kWarps = kThreads / 32;
@@ -197,13 +240,119 @@ __device__ __forceinline__ void quotients8(float (&x)[8], float s) {
     }
 }
 
-// Heads of one kind, steps [s0, s1): rotated, scaled, rounded, stored at dst + e0 and
-// dst + e1, a step further `dst_step`.  `batch` holds the first steps already.
-template <class T, class Out, int G, bool ROTATE, int kBatch>
+// Where the other 8 elements of a lane's two 16-element blocks are: chunk c is the
+// first or second of lane c % 16 of its group.
+struct BlockMates {
+    int lane0, lane1;                    // of chunks e0 / 8 and e1 / 8
+    bool second0, second1;
+    __device__ __forceinline__ BlockMates(int e0, int e1, int half8, int first_lane) {
+        // (chunks below 2 half8 lie as pairs to rotate, the others as neighbours)
+        auto find = [&](int c, int &lane, bool &second) {
+            second = c < 2 * half8 ? c >= half8 : c & 1;
+            lane = first_lane + (c < 2 * half8 ? (second ? c - half8 : c) : c / 2);
+        };
+        find(e0 / 8 ^ 1, lane0, second0);
+        find(e1 / 8 ^ 1, lane1, second1);
+    }
+};
+
+// max |x|, NaN if one is
+__device__ __forceinline__ float most8(const float (&x)[8]) {
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) m = dev::max3_nan(m, fabsf(x[i]), fabsf(x[i + 1]));
+    return m;
+}
+
+// Two 8-element chunks into a 4-bit page: block scale s = e4m3(max |x| / (6 g)), codes
+// e2m1(x / (s g)), each quotient the product with a rounded reciprocal, so that one
+// division a block does (g, and s g, are between 2^-109 and 2^109).  A block of zeros, or too small
+// for a scale, has s = 0 and codes of 0; a NaN makes s NaN.  `row`: the token's values;
+// scales are `to_scales` bytes further.
+__device__ __forceinline__ void store_fp4(Fp4 *row, int to_scales, const float (&x0)[8], const float (&x1)[8], int e0,
+                                          int e1, bool pairs, const BlockMates &mates, uint32_t group, float g) {
+    float m0 = most8(x0), m1 = most8(x1);
+    if (pairs) {                         // (of q and k: whose blocks may span lanes)
+        const float a0 = __shfl_sync(group, m0, mates.lane0), a1 = __shfl_sync(group, m1, mates.lane0);
+        const float b0 = __shfl_sync(group, m0, mates.lane1), b1 = __shfl_sync(group, m1, mates.lane1);
+        m0 = dev::max3_nan(m0, mates.second0 ? a1 : a0, 0.f);
+        m1 = dev::max3_nan(m1, mates.second1 ? b1 : b0, 0.f);
+    } else {
+        m0 = m1 = dev::max3_nan(m0, m1, 0.f);
+    }
+    const float r = __frcp_rn(6.f * g);
+    const uint32_t s2 = __nv_cvt_float2_to_fp8x2(make_float2(m0 * r, m1 * r), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t h2 = e4m3x2_to_f16x2(s2);
+    const float2 s = __half22float2(*reinterpret_cast<const __half2 *>(&h2));
+    auto codes = [&](const float (&x)[8], float step) {
+        const float y = step > 0.f ? __frcp_rn(step) : 0.f;
+        uint32_t w = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t b;
+            asm("{\n\t.reg .b8 t;\n\t"
+                "cvt.rn.satfinite.e2m1x2.f32 t, %2, %1;\n\t"
+                "cvt.u32.u8 %0, t;\n\t}"
+                : "=r"(b)
+                : "f"(x[2 * i] * y), "f"(x[2 * i + 1] * y));
+            w |= b << (8 * i);
+        }
+        return w;
+    };
+    uint8_t *out = &row->byte;
+    *reinterpret_cast<uint32_t *>(out + e0 / 2) = codes(x0, s.x * g);
+    *reinterpret_cast<uint32_t *>(out + e1 / 2) = codes(x1, s.y * g);
+    if (e0 % 16 == 0) out[to_scales + e0 / 16] = static_cast<uint8_t>(s2);
+    if (e1 % 16 == 0) out[to_scales + e1 / 16] = static_cast<uint8_t>(s2 >> 8);
+}
+
+// x / sqrt(mean x^2 + eps) * (offset + w) over a head of D elements, whose lanes are
+// `group`.
+template <class T, int D>
+__device__ __forceinline__ void norm_head(float (&x0)[8], float (&x1)[8], const Raw8<T> &w0, const Raw8<T> &w1,
+                                          float eps, float offset, uint32_t group) {
+    unsigned long long sum = dev::mul_f32x2(dev::f32x2(x0[0], x0[1]), dev::f32x2(x0[0], x0[1]));
+#pragma unroll
+    for (int i = 2; i < 8; i += 2) sum = dev::fma_f32x2(dev::f32x2(x0[i], x0[i + 1]), dev::f32x2(x0[i], x0[i + 1]), sum);
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) sum = dev::fma_f32x2(dev::f32x2(x1[i], x1[i + 1]), dev::f32x2(x1[i], x1[i + 1]), sum);
+    float lo, hi;
+    dev::f32x2_split(sum, lo, hi);
+    float s = lo + hi;
+#pragma unroll
+    for (int o = 1; o < D / 16; o <<= 1) s += __shfl_xor_sync(group, s, o);
+    const float inv = __frsqrt_rn(s * (1.f / D) + eps);
+    float y0[8], y1[8];
+    unpack8(w0, y0);
+    unpack8(w1, y1);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        x0[i] = x0[i] * inv * (y0[i] + offset);
+        x1[i] = x1[i] * inv * (y1[i] + offset);
+    }
+}
+
+// Heads of one kind, steps [s0, s1): normed, rotated, scaled, rounded, stored at dst + e0
+// and dst + e1, a step further `dst_step`.  `batch` holds the first steps already.
+template <class T, class Out, int D, int G, bool ROTATE, bool NORM, int kBatch>
 __device__ __forceinline__ void write_heads(Batch<T, kBatch> &batch, const T *src, int64_t src_step, Out *dst,
                                             int64_t dst_step, int s0, int s1, int heads, int mine, int e0, int e1,
                                             bool interleaved, bool rotates, const unsigned long long (&cs)[4],
-                                            const unsigned long long (&sn)[4], const float *scale) {
+                                            const unsigned long long (&sn)[4], const float *scale, const T *weight,
+                                            int64_t weight_stride, const WriteArgs &a, int to_scales) {
+    constexpr int kLanes = D / 16;
+    const int first_lane = threadIdx.x % 32 / kLanes * kLanes;
+    const uint32_t group = ((1u << kLanes) - 1) << first_lane;      // the lanes of a head
+    const BlockMates mates(e0, e1, ROTATE && !interleaved ? a.rot.half / 8 : 0, first_lane);
+    // (a weight for all heads stays in registers)
+    Raw8<T> w0 = {}, w1 = {};
+    if constexpr (NORM) {
+        if (weight) {
+            const T *w = weight + (s0 * G + mine < heads ? s0 * G + mine : 0) * weight_stride;
+            w0 = load_weight8(w + e0);
+            w1 = load_weight8(w + e1);
+        }
+    }
     dst += s0 * dst_step;
     for (int s = s0; s < s1; s += kBatch, dst += kBatch * dst_step) {
         if (s != s0) batch.template load<G>(src, src_step, s, s1, heads, mine, e0, e1);
@@ -214,6 +363,15 @@ __device__ __forceinline__ void write_heads(Batch<T, kBatch> &batch, const T *sr
             float x0[8], x1[8];
             unpack8(batch.r0[b], x0);
             unpack8(batch.r1[b], x1);
+            if constexpr (NORM) {
+                if (weight) {
+                    if (weight_stride) {
+                        w0 = load_weight8(weight + h * weight_stride + e0);
+                        w1 = load_weight8(weight + h * weight_stride + e1);
+                    }
+                    norm_head<T, D>(x0, x1, w0, w1, a.norm.eps, a.norm.offset, group);
+                }
+            }
             if (ROTATE && rotates) {
                 // (p c - q s, p s + q c), two pairs an instruction
 #pragma unroll
@@ -228,13 +386,17 @@ __device__ __forceinline__ void write_heads(Batch<T, kBatch> &batch, const T *sr
                     dev::f32x2_split(dev::fma_f32x2(p, sn[i], dev::mul_f32x2(q, cs[i])), q0, q1);
                 }
             }
-            if constexpr (sizeof(Out) == 1) {
-                const float div = scale[h];
-                quotients8(x0, div);
-                quotients8(x1, div);
+            if constexpr (kIsFp4<Out>) {
+                store_fp4(dst + b * dst_step, to_scales, x0, x1, e0, e1, ROTATE && !interleaved, mates, group, scale[h]);
+            } else {
+                if constexpr (sizeof(Out) == 1) {
+                    const float div = scale[h];
+                    quotients8(x0, div);
+                    quotients8(x1, div);
+                }
+                store8(dst + b * dst_step + e0, x0);
+                store8(dst + b * dst_step + e1, x1);
             }
-            store8(dst + b * dst_step + e0, x0);
-            store8(dst + b * dst_step + e1, x1);
         }
     }
 }
@@ -253,7 +415,7 @@ __device__ __forceinline__ void write_heads(Batch<T, kBatch> &batch, const T *sr
 // The angles are made once for all heads of a token: the G lanes of one u share 8
 // pairs' angles, make 8 / G each and pass them round (out of shared memory they were
 // read four lanes to a bank).
-template <class T, class KV, int D, bool INTERLEAVED, int G>
+template <class T, class KV, int D, bool INTERLEAVED, int G, bool NORM>
 __global__ void __launch_bounds__(kThreads, kAskedCtas<T>) kv_write_kernel(const WriteArgs a) {
     constexpr int kLanes = D / 16, kTeams = 32 / kLanes / G, kMake = 8 / G;
     constexpr int kBatch = sizeof(T) == 4 ? 2 : 3;            // (steps in flight, as above)
@@ -311,21 +473,26 @@ __global__ void __launch_bounds__(kThreads, kAskedCtas<T>) kv_write_kernel(const
     }
     if (!there) return;
     if (first < q_steps)
-        write_heads<T, T, G, true, kBatch>(batch, q, q_step, static_cast<T *>(a.q_out) + (t * a.num_q_heads + mine) * D,
-                                           G * D, first, min(last, q_steps), a.num_q_heads, mine, e0, e1, INTERLEAVED,
-                                           rotates, cs, sn, nullptr);
+        write_heads<T, T, D, G, true, NORM, kBatch>(
+            batch, q, q_step, static_cast<T *>(a.q_out) + (t * a.num_q_heads + mine) * D, G * D, first,
+            min(last, q_steps), a.num_q_heads, mine, e0, e1, INTERLEAVED, rotates, cs, sn, nullptr,
+            static_cast<const T *>(a.norm.q), a.norm.q_stride, a, 0);
     if (slot < 0 || slot >= a.num_slots || last <= q_steps) return;
-    const int64_t row = (slot / kPageSize * a.num_kv_heads + mine) * kPageSize * D + slot % kPageSize * D;
+    const int at = static_cast<int>(slot % kPageSize);
+    const int64_t row = (slot / kPageSize * a.num_kv_heads + mine) * kHeadStep<KV, D> + at * kTokenStep<KV, D>;
+    const int to_scales = fp4_value_bytes(D) - at * (D / 2 - D / kFp4Block);   // (4-bit)
     if (k0 < k1) {
         if (first < q_steps) batch.template load<G>(k, k_step, k0, k1, a.num_kv_heads, mine, e0, e1);
-        write_heads<T, KV, G, true, kBatch>(batch, k, k_step, static_cast<KV *>(a.k_pages) + row, G * kPageSize * D, k0,
-                                            k1, a.num_kv_heads, mine, e0, e1, INTERLEAVED, rotates, cs, sn, a.k_scale);
+        write_heads<T, KV, D, G, true, NORM, kBatch>(
+            batch, k, k_step, static_cast<KV *>(a.k_pages) + row, G * kHeadStep<KV, D>, k0, k1, a.num_kv_heads, mine,
+            e0, e1, INTERLEAVED, rotates, cs, sn, a.k_scale, static_cast<const T *>(a.norm.k), a.norm.k_stride, a,
+            to_scales);
     }
     if (v0 < v1) {
         batch.template load<G>(v, v_step, v0, v1, a.num_kv_heads, mine, 16 * u, 16 * u + 8);
-        write_heads<T, KV, G, false, kBatch>(batch, v, v_step, static_cast<KV *>(a.v_pages) + row, G * kPageSize * D,
-                                             v0, v1, a.num_kv_heads, mine, 16 * u, 16 * u + 8, INTERLEAVED, false, cs,
-                                             sn, a.v_scale);
+        write_heads<T, KV, D, G, false, false, kBatch>(
+            batch, v, v_step, static_cast<KV *>(a.v_pages) + row, G * kHeadStep<KV, D>, v0, v1, a.num_kv_heads, mine,
+            16 * u, 16 * u + 8, INTERLEAVED, false, cs, sn, a.v_scale, nullptr, 0, a, to_scales);
     }
 }
 
@@ -390,6 +557,33 @@ __device__ __forceinline__ void store_read16(T *dst, const Raw16<KV> &r, float s
     }
 }
 
+// 16 elements of a 4-bit row: a block, its scale.
+template <>
+struct Raw16<Fp4> {
+    uint2 values;
+    uint32_t scale;
+};
+
+template <class T>
+__device__ __forceinline__ void store_read16(T *dst, const Raw16<Fp4> &r, float scale, bool aligned) {
+    const uint32_t s = __byte_perm(e4m3x2_to_f16x2(r.scale), 0u, 0x1010);
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        uint32_t h[4];
+        e2m1x8_to_f16(i ? r.values.y : r.values.x, h);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t p = mul_f16x2(h[j], s);
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&p));
+            float lo, hi;
+            dev::f32x2_split(dev::mul_f32x2(dev::f32x2(f.x, f.y), dev::f32x2(scale, scale)), lo, hi);
+            w[4 * i + j] = dev::pack_bf16(lo, hi);
+        }
+    }
+    store32(dst, w, aligned);
+}
+
 // Rows (token, head) in order: a warp takes kSteps x (32 / kLanes) of them, K and V of
 // each, a lane 16 elements, all loads in flight.  38.8k e4m3 tokens of 8 heads: 37.2 us
 // (35.2 us of bytes), fp32 95.5 (93.8); 8 elements a lane, whose scales and addresses
@@ -420,9 +614,19 @@ __global__ void __launch_bounds__(kThreads, 8) kv_read_kernel(const ReadArgs a) 
         if (t[b] >= a.num_tokens) continue;
         const int64_t slot = a.slots[t[b]];
         if (slot >= 0 && slot < a.num_slots) {
-            const int64_t at_row = ((slot / kPageSize * a.num_kv_heads + h[b]) * kPageSize + slot % kPageSize) * D + 16 * u;
-            rk[b] = load16(static_cast<const KV *>(a.k_pages) + at_row);
-            rv[b] = load16(static_cast<const KV *>(a.v_pages) + at_row);
+            if constexpr (kIsFp4<KV>) {
+                const int64_t page = (slot / kPageSize * a.num_kv_heads + h[b]) * kHeadStep<KV, D>;
+                const int at = static_cast<int>(slot % kPageSize);
+                const int64_t values = page + at * kTokenStep<KV, D> + 8 * u;
+                const int64_t scales = page + fp4_value_bytes(D) + at * (D / kFp4Block) + u;
+                const uint8_t *k = static_cast<const uint8_t *>(a.k_pages), *v = static_cast<const uint8_t *>(a.v_pages);
+                rk[b] = {__ldcs(reinterpret_cast<const uint2 *>(k + values)), k[scales]};
+                rv[b] = {__ldcs(reinterpret_cast<const uint2 *>(v + values)), v[scales]};
+            } else {
+                const int64_t at_row = ((slot / kPageSize * a.num_kv_heads + h[b]) * kPageSize + slot % kPageSize) * D + 16 * u;
+                rk[b] = load16(static_cast<const KV *>(a.k_pages) + at_row);
+                rv[b] = load16(static_cast<const KV *>(a.v_pages) + at_row);
+            }
             if constexpr (kScaled<KV>) {
                 ks[b] = a.k_scale[h[b]];
                 vs[b] = a.v_scale[h[b]];
@@ -437,15 +641,15 @@ __global__ void __launch_bounds__(kThreads, 8) kv_read_kernel(const ReadArgs a) 
         if (t[b] >= a.num_tokens) continue;
         T *k = static_cast<T *>(const_cast<void *>(a.k.data)) + t[b] * a.k.token_stride + h[b] * a.k.head_stride;
         T *v = static_cast<T *>(const_cast<void *>(a.v.data)) + t[b] * a.v.token_stride + h[b] * a.v.head_stride;
-        store_read16<T, KV>(k + 16 * u, rk[b], ks[b], a.aligned);
-        store_read16<T, KV>(v + 16 * u, rv[b], vs[b], a.aligned);
+        store_read16(k + 16 * u, rk[b], ks[b], a.aligned);
+        store_read16(v + 16 * u, rv[b], vs[b], a.aligned);
     }
 }
 
-// Scales at their least, 2^-126, before the tokens raise them.
-__global__ void reset_scales_kernel(float *k_scale, float *v_scale, int n) {
+// Scales at their least before the tokens raise them.
+__global__ void reset_scales_kernel(float *k_scale, float *v_scale, int n, float least) {
     dev::grid_wait();
-    for (int i = threadIdx.x; i < n; i += blockDim.x) k_scale[i] = v_scale[i] = 1.17549435e-38f;
+    for (int i = threadIdx.x; i < n; i += blockDim.x) k_scale[i] = v_scale[i] = least;
 }
 
 // min(|x|, 2^63), 0 for NaN: squares of these add up within fp32.
@@ -551,13 +755,13 @@ __global__ void __launch_bounds__(kThreads, 8) kv_scales_kernel(const ScalesArgs
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int i = 1; i < kWarps; ++i) m = fmaxf(m, part[i]);
-        atomicMax(reinterpret_cast<int *>((is_k ? a.k_scale : a.v_scale) + h), __float_as_int(m / kE4m3Max));
+        atomicMax(reinterpret_cast<int *>((is_k ? a.k_scale : a.v_scale) + h), __float_as_int(m / a.limit));
     }
 }
 
 // Warps of kv_write (a token to a warp) that run at once on the current device, one
 // wave: asked for once a device.
-template <class T, class KV, int D, bool INTERLEAVED>
+template <class T, class KV, int D, bool INTERLEAVED, bool NORM>
 cudaError_t wave_warps(int64_t *warps) {
     static std::atomic<int> known[kMaxDevices];          // 0: not asked yet
     int dev = 0;
@@ -569,8 +773,8 @@ cudaError_t wave_warps(int64_t *warps) {
         int sms = 0, ctas = 0;
         e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
         if (e == cudaSuccess)
-            e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ctas, kv_write_kernel<T, KV, D, INTERLEAVED, 512 / D>,
-                                                              kThreads, 0);
+            e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(
+                &ctas, kv_write_kernel<T, KV, D, INTERLEAVED, 512 / D, NORM>, kThreads, 0);
         if (e != cudaSuccess) return e;
         n = sms * ctas * kWarps;
         known[dev].store(n, std::memory_order_relaxed);
@@ -591,13 +795,13 @@ unsigned blocks_of(int64_t tokens, int parts) {
     return static_cast<unsigned>((tokens * parts + kWarps - 1) / kWarps);
 }
 
-template <class T, class KV, int D, int G>
+template <class T, class KV, int D, int G, bool NORM>
 cudaError_t launch_write(WriteArgs a, int64_t wave, cudaStream_t s) {
     constexpr int kTeams = 512 / D / G;
     const int steps = (a.num_q_heads + G - 1) / G + 2 * ((a.num_kv_heads + G - 1) / G);
     a.parts = kTeams == 1 ? parts_of(a.num_tokens, steps, wave) : 1;
     return launch_dependent(
-        true, a.rot.interleaved ? kv_write_kernel<T, KV, D, true, G> : kv_write_kernel<T, KV, D, false, G>,
+        true, a.rot.interleaved ? kv_write_kernel<T, KV, D, true, G, NORM> : kv_write_kernel<T, KV, D, false, G, NORM>,
         dim3(blocks_of((a.num_tokens + kTeams - 1) / kTeams, a.parts)), dim3(kThreads), 0, s, a);
 }
 
@@ -606,19 +810,24 @@ cudaError_t launch_write(WriteArgs a, int64_t wave, cudaStream_t s) {
 // first loads (9728 bf16 tokens of 128 elements, a token, two and four to a warp: 14.1,
 // 11.9, 10.0 us at 8 / 2 heads, 4 to 12 steps; 22.0, 19.2, 19.0 at 16 / 4; 34.1, 35.0,
 // 34.5 at 24 / 8, 10 to 40 steps).
-template <class T, class KV, int D>
+template <class T, class KV, int D, bool NORM>
 cudaError_t launch_write(const WriteArgs &a, cudaStream_t s) {
     constexpr int kGroups = 512 / D;
     int64_t wave = 0;
-    const cudaError_t e = a.rot.interleaved ? wave_warps<T, KV, D, true>(&wave) : wave_warps<T, KV, D, false>(&wave);
+    const cudaError_t e = a.rot.interleaved ? wave_warps<T, KV, D, true, NORM>(&wave) : wave_warps<T, KV, D, false, NORM>(&wave);
     if (e != cudaSuccess) return e;
     auto few = [&](int g) {
         return (a.num_q_heads + g - 1) / g + 2 * ((a.num_kv_heads + g - 1) / g) < 10 &&
                a.num_tokens > kGroups / g * wave;
     };
-    if (!few(kGroups)) return launch_write<T, KV, D, kGroups>(a, wave, s);
-    return few(kGroups / 2) ? launch_write<T, KV, D, kGroups / 4>(a, wave, s)
-                            : launch_write<T, KV, D, kGroups / 2>(a, wave, s);
+    if (!few(kGroups)) return launch_write<T, KV, D, kGroups, NORM>(a, wave, s);
+    return few(kGroups / 2) ? launch_write<T, KV, D, kGroups / 4, NORM>(a, wave, s)
+                            : launch_write<T, KV, D, kGroups / 2, NORM>(a, wave, s);
+}
+
+template <class T, class KV, int D>
+cudaError_t launch_write(const WriteArgs &a, cudaStream_t s) {
+    return a.norm.q || a.norm.k ? launch_write<T, KV, D, true>(a, s) : launch_write<T, KV, D, false>(a, s);
 }
 
 template <class T, class KV, int D>
@@ -751,12 +960,36 @@ extern "C" parason_status parason_kv_write(const parason_attn_config *cfg, int64
                                            const float *v_scale, void *q_out, void *k_pages,
                                            void *v_pages, int64_t num_physical_pages,
                                            parason_stream_t stream) {
+    return parason_kv_write_norm(cfg, num_tokens, q, k, v, nullptr, rotary, slots, k_scale, v_scale, q_out, k_pages,
+                                 v_pages, num_physical_pages, stream);
+}
+
+extern "C" parason_status parason_kv_write_norm(const parason_attn_config *cfg, int64_t num_tokens,
+                                                const parason_rows *q, const parason_rows *k,
+                                                const parason_rows *v, const parason_head_norm *norm,
+                                                const parason_rotary *rotary, const int32_t *slots,
+                                                const float *k_scale, const float *v_scale, void *q_out,
+                                                void *k_pages, void *v_pages, int64_t num_physical_pages,
+                                                parason_stream_t stream) {
     parason_status st = check_call(cfg, num_tokens, num_physical_pages);
     if (st != PARASON_OK) return st;
     const int32_t d = cfg->head_dim;
     const int elem = cfg->mode == PARASON_FP32 ? 4 : 2;
     WriteArgs a{};
     if ((st = to_rotary(rotary, num_tokens, d, &a.rot)) != PARASON_OK) return st;
+    if (norm) {
+        if (!(norm->eps >= kLeastScale) || !std::isfinite(norm->eps) || !std::isfinite(norm->weight_offset) ||
+            (!norm->q_weight && !norm->k_weight) || misaligned(norm->q_weight, 16) || misaligned(norm->k_weight, 16))
+            return PARASON_EINVAL;
+        for (int64_t stride : {norm->q_head_stride, norm->k_head_stride})
+            if (stride < 0 || stride * elem % 16 != 0) return PARASON_EINVAL;
+        if (q) a.norm.q = norm->q_weight;
+        a.norm.k = norm->k_weight;
+        a.norm.q_stride = norm->q_head_stride;
+        a.norm.k_stride = norm->k_head_stride;
+        a.norm.eps = norm->eps;
+        a.norm.offset = norm->weight_offset;
+    }
     if (num_tokens == 0) return PARASON_OK;
     if ((st = check_rows(k, num_tokens, cfg->num_kv_heads, d, elem, false)) != PARASON_OK) return st;
     if ((st = check_rows(v, num_tokens, cfg->num_kv_heads, d, elem, false)) != PARASON_OK) return st;
@@ -770,7 +1003,7 @@ extern "C" parason_status parason_kv_write(const parason_attn_config *cfg, int64
     if (!slots || misaligned(slots, 4)) return PARASON_EINVAL;
     if (num_physical_pages > 0 && (!k_pages || !v_pages || misaligned(k_pages, 16) || misaligned(v_pages, 16)))
         return PARASON_EINVAL;
-    if (cfg->mode == PARASON_FP8_E4M3_KV &&
+    if (scaled_kv(cfg->mode) &&
         (!k_scale || !v_scale || misaligned(k_scale, 4) || misaligned(v_scale, 4)))
         return PARASON_EINVAL;
     // (outputs in one place: two warps would write it, or one before another has read it)
@@ -791,6 +1024,7 @@ extern "C" parason_status parason_kv_write(const parason_attn_config *cfg, int64
     a.num_kv_heads = cfg->num_kv_heads;
     const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     if (cfg->mode == PARASON_FP8_E4M3_KV) return launched(launch_write<__nv_bfloat16, __nv_fp8_e4m3, 128>(a, s));
+    if (cfg->mode == PARASON_FP4_KV) return launched(launch_write<__nv_bfloat16, Fp4, 128>(a, s));
     if (cfg->mode == PARASON_FP32)
         return launched(d == 128 ? launch_write<float, float, 128>(a, s) : launch_write<float, float, 64>(a, s));
     return launched(d == 128 ? launch_write<__nv_bfloat16, __nv_bfloat16, 128>(a, s)
@@ -813,7 +1047,7 @@ extern "C" parason_status parason_kv_read(const parason_attn_config *cfg, int64_
     if (!slots || misaligned(slots, 4)) return PARASON_EINVAL;
     if (num_physical_pages > 0 && (!k_pages || !v_pages || misaligned(k_pages, 16) || misaligned(v_pages, 16)))
         return PARASON_EINVAL;
-    if (cfg->mode == PARASON_FP8_E4M3_KV &&
+    if (scaled_kv(cfg->mode) &&
         (!k_scale || !v_scale || misaligned(k_scale, 4) || misaligned(v_scale, 4)))
         return PARASON_EINVAL;
     ReadArgs a{};
@@ -831,6 +1065,7 @@ extern "C" parason_status parason_kv_read(const parason_attn_config *cfg, int64_
     if (k_out->data == v_out->data) return PARASON_EINVAL;
     const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     if (cfg->mode == PARASON_FP8_E4M3_KV) return launched(launch_read<__nv_bfloat16, __nv_fp8_e4m3, 128>(a, s));
+    if (cfg->mode == PARASON_FP4_KV) return launched(launch_read<__nv_bfloat16, Fp4, 128>(a, s));
     if (cfg->mode == PARASON_FP32)
         return launched(d == 128 ? launch_read<float, float, 128>(a, s) : launch_read<float, float, 64>(a, s));
     return launched(d == 128 ? launch_read<__nv_bfloat16, __nv_bfloat16, 128>(a, s)
@@ -844,7 +1079,7 @@ extern "C" parason_status parason_kv_scales(const parason_attn_config *cfg, int6
                                             parason_stream_t stream) {
     parason_status st = check_call(cfg, num_tokens, 0);
     if (st != PARASON_OK) return st;
-    if (cfg->mode != PARASON_FP8_E4M3_KV) return PARASON_EINVAL;
+    if (!scaled_kv(cfg->mode)) return PARASON_EINVAL;
     if (rotary && (st = check_pairs(rotary, cfg->head_dim)) != PARASON_OK) return st;
     if (accumulate != 0 && accumulate != 1) return PARASON_EINVAL;
     if (!k_scale || !v_scale || misaligned(k_scale, 4) || misaligned(v_scale, 4) || misaligned(slots, 4))
@@ -864,10 +1099,12 @@ extern "C" parason_status parason_kv_scales(const parason_attn_config *cfg, int6
     a.num_kv_heads = cfg->num_kv_heads;
     a.half = rotary ? rotary->rotary_dim / 2 : 0;
     a.interleaved = rotary && rotary->pairs == PARASON_ROTARY_INTERLEAVED;
+    a.limit = cfg->mode == PARASON_FP4_KV ? kFp4Max : kE4m3Max;
     const cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     if (!accumulate) {
         const cudaError_t e = launch_dependent(true, reset_scales_kernel, dim3(1), dim3(kThreads), 0, s, k_scale,
-                                               v_scale, static_cast<int>(cfg->num_kv_heads));
+                                               v_scale, static_cast<int>(cfg->num_kv_heads),
+                                               cfg->mode == PARASON_FP4_KV ? kLeastScaleFp4 : kLeastScale);
         if (e != cudaSuccess) return PARASON_ECUDA;
     }
     if (num_tokens == 0) return PARASON_OK;

@@ -35,7 +35,7 @@ constexpr int kNarrowRows = 16;         // nodes with at most this many rows: su
 // autonomous warps per suffix-pass CTA (the kernel's count for the KV format: 6
 // deeper warps for bf16 at head_dim 128 with g <= 4, where they are latency-bound)
 int32_t narrow_warps(int32_t mode, int32_t head_dim, int32_t g) {
-    if (mode == PARASON_FP8_E4M3_KV) return 12;
+    if (parason::scaled_kv(mode)) return 12;
     return (mode == PARASON_BF16 && head_dim == 128 && g <= 4) ? 6 : 8;
 }
 // Suffix-pass pieces are at least kMinPiecePages long (4 against 8: tiny
@@ -481,10 +481,10 @@ parason_status check_config(const parason_attn_config *cfg) {
     if (cfg->head_dim != 64 && cfg->head_dim != 128) return PARASON_EINVAL;
     if (cfg->page_size != kPageSize) return PARASON_EINVAL;
     if (cfg->mode != PARASON_BF16 && cfg->mode != PARASON_FP32 &&
-        cfg->mode != PARASON_FP8_E4M3_KV)
+        cfg->mode != PARASON_FP8_E4M3_KV && cfg->mode != PARASON_FP4_KV)
         return PARASON_EINVAL;
     if (!(cfg->sm_scale >= 0.0f) || !std::isfinite(cfg->sm_scale)) return PARASON_EINVAL;
-    if (cfg->mode == PARASON_FP8_E4M3_KV && cfg->head_dim != 128) return PARASON_EUNSUPPORTED;
+    if (scaled_kv(cfg->mode) && cfg->head_dim != 128) return PARASON_EUNSUPPORTED;
     return PARASON_OK;
 }
 
@@ -556,7 +556,7 @@ parason_status build_host(parason_plan_s *p, const parason_attn_config *cfg, int
                           int64_t num_phys, int32_t num_sms, bool prefill = false) {
     parason_status st = parason::check_config(cfg);
     if (st != PARASON_OK) return st;
-    // the prefill's causal mask is in the tcgen05 tile: bf16 or e4m3 KV at head_dim 128
+    // the prefill's causal mask is in the tcgen05 tile: bf16, e4m3 or 4-bit KV at head_dim 128
     if (prefill && (cfg->mode == PARASON_FP32 || cfg->head_dim != 128)) return PARASON_EUNSUPPORTED;
     p->prefill = prefill;
     if (num_nodes < 0 || num_leaves < 0 || num_phys < 0) return PARASON_EINVAL;
@@ -770,8 +770,8 @@ parason_status build_host(parason_plan_s *p, const parason_attn_config *cfg, int
                 run.leaf_lo = lo[n];
                 run.wide = wide;
                 if (wide)
-                    wide_cost += wide_page_cost(cfg->head_dim, mode == PARASON_FP8_E4M3_KV) *
-                                 static_cast<double>(P + (mode == PARASON_FP8_E4M3_KV
+                    wide_cost += wide_page_cost(cfg->head_dim, parason::scaled_kv(mode)) *
+                                 static_cast<double>(P + (parason::scaled_kv(mode)
                                                               ? std::min<int64_t>(kTcStartPagesE4m3, P / 3)
                                                               : 0));
                 else
@@ -892,7 +892,7 @@ parason_status build_host(parason_plan_s *p, const parason_attn_config *cfg, int
                     longest = std::max(longest, std::min(per, r.pages));
                 }
             const double piece = static_cast<double>(longest * (p->tc_pairs ? 2 : 1)) *
-                                 wide_page_cost(cfg->head_dim, mode == PARASON_FP8_E4M3_KV);
+                                 wide_page_cost(cfg->head_dim, parason::scaled_kv(mode));
             if (e <= n_wide && piece * S <= kLongestPiece * (wide_cost + static_cast<double>(narrow_pages))) {
                 wide_chunk = chunk;
                 n_wide = static_cast<int32_t>(e);
@@ -1035,7 +1035,7 @@ parason_status build_host(parason_plan_s *p, const parason_attn_config *cfg, int
         };
         int64_t narrow_chunk = length_at(kNarrowPiecesPerWarp);
         if (n_narrow_ctas > 0 && length_at(1.0) > narrow_chunk) {
-            const bool e4m3 = mode == PARASON_FP8_E4M3_KV;
+            const bool e4m3 = parason::scaled_kv(mode);
             std::vector<std::pair<int64_t, int64_t>> lens;
             for (const Run &r : runs)
                 if (!r.wide && r.pages > 0) {
@@ -1242,8 +1242,10 @@ parason_status build_host(parason_plan_s *p, const parason_attn_config *cfg, int
         if (p->merge_ent.size() > static_cast<size_t>(INT32_MAX)) return PARASON_EUNSUPPORTED;
         p->merge_rng[k] = make_int2(e0, static_cast<int32_t>(p->merge_ent.size()));
     }
-    const int64_t kv_bytes = 2 * p->unique_tokens * H_kv * cfg->head_dim *
-                             (mode == PARASON_FP32 ? 4 : mode == PARASON_BF16 ? 2 : 1);
+    const int64_t kv_bytes = mode == PARASON_FP4_KV
+                                 ? 2 * p->unique_tokens * H_kv * (parason::fp4_page_bytes(cfg->head_dim) / parason::kPageSize)
+                                 : 2 * p->unique_tokens * H_kv * cfg->head_dim *
+                                       (mode == PARASON_FP32 ? 4 : mode == PARASON_BF16 ? 2 : 1);
     p->early = mode == PARASON_FP32 ||
                (prefill ? wide_units <= 2 * kEarlyPrefillPages * p->num_sms
                         : kv_bytes <= (mode == PARASON_BF16 ? kEarlyKvBytes : kEarlyKvBytesE4m3));
@@ -1766,7 +1768,7 @@ parason_status parason_attn_decode(parason_plan p, const void *q, const void *k_
             return PARASON_EINVAL;
         if (reinterpret_cast<uintptr_t>(k_pages) % 16 || reinterpret_cast<uintptr_t>(v_pages) % 16)
             return PARASON_EINVAL;
-        if (p->cfg.mode == PARASON_FP8_E4M3_KV && (!k_scale || !v_scale)) return PARASON_EINVAL;
+        if (parason::scaled_kv(p->cfg.mode) && (!k_scale || !v_scale)) return PARASON_EINVAL;
     }
     if (reinterpret_cast<uintptr_t>(q) % 16 || reinterpret_cast<uintptr_t>(out) % 16)
         return PARASON_EINVAL;
@@ -1826,6 +1828,12 @@ parason_status parason_attn_decode(parason_plan p, const void *q, const void *k_
         if (p->cfg.mode == PARASON_FP32) {
             e = parason::launch_attn_fp32(a, static_cast<const float *>(k_pages),
                                           static_cast<const float *>(v_pages), d, stream);
+        } else if (p->cfg.mode == PARASON_FP4_KV) {
+            const parason::KvMaps none{};
+            a.k_raw = static_cast<const uint8_t *>(k_pages);
+            a.v_raw = static_cast<const uint8_t *>(v_pages);
+            e = p->prefill ? parason::launch_prefill(a, none, p->cfg.mode, stream)
+                           : parason::launch_attn_fp8(a, none, d, stream);
         } else {
             parason::KvMaps maps;
             {
@@ -1896,7 +1904,7 @@ parason_status parason_lse_merge(const void *o_a, const float *lse_a, const void
                                  const float *lse_b, void *o_out, float *lse_out, int64_t rows,
                                  int32_t head_dim, int32_t mode, parason_stream_t stream) {
     if (rows < 0 || (head_dim != 64 && head_dim != 128)) return PARASON_EINVAL;
-    if (mode != PARASON_BF16 && mode != PARASON_FP32 && mode != PARASON_FP8_E4M3_KV)
+    if (mode != PARASON_BF16 && mode != PARASON_FP32 && mode != PARASON_FP8_E4M3_KV && mode != PARASON_FP4_KV)
         return PARASON_EINVAL;
     if (rows == 0) return PARASON_OK;
     if (!o_a || !lse_a || !o_b || !lse_b || !o_out || !lse_out) return PARASON_EINVAL;

@@ -105,30 +105,37 @@ constexpr int kProducerWarp = 8, kMmaWarp = 9, kSchedulerWarp = 10, kConvertWarp
 // Launch shapes, with the registers a thread at launch and after the split:
 // bf16 384 x 168 = 64512 = 256 x 208 + 128 x 88; e4m3 512 x 128 = 65536 = 256 x
 // 152 + 128 x 88 + 128 x 120.
-template <bool F8>
+enum { kBf16Kv, kE4m3Kv, kE2m1Kv };                 // formats of K and V
+template <int KV>
 struct Cfg;
 template <>
-struct Cfg<false> {
+struct Cfg<kBf16Kv> {
     static constexpr int kThreads = 384;
-    static constexpr int kSlots = 5, kRawSlots = 0;
+    static constexpr int kSlots = 5, kRawSlots = 0, kRawBytes = 0;
     static constexpr int kTileRegs = 208, kAuxRegs = 88, kConvertRegs = 0;
     static_assert(256 * kTileRegs + 128 * kAuxRegs <= kThreads * 168, "register split");
 };
 template <>
-struct Cfg<true> {
+struct Cfg<kE4m3Kv> {
     static constexpr int kThreads = 512;
-    static constexpr int kSlots = 3, kRawSlots = 4;
+    static constexpr int kSlots = 3, kRawSlots = 4, kRawBytes = kRawSlotBytes;
     static constexpr int kTileRegs = 152, kAuxRegs = 88, kConvertRegs = 120;
     static_assert(256 * kTileRegs + 128 * kAuxRegs + 128 * kConvertRegs <= kThreads * 128,
                   "register split");
 };
+// (the raw slots are smaller: one more widened block)
+template <>
+struct Cfg<kE2m1Kv> : Cfg<kE4m3Kv> {
+    static constexpr int kSlots = 4, kRawSlots = 3, kRawBytes = kBlockPages * fp4_page_bytes(kDim);
+};
 
 // shared memory: Q of both tiles, the 16-bit ring, the raw ring
-template <bool F8>
+template <int KV>
 constexpr int smem_bytes() {
-    return 2 * kQBytes + Cfg<F8>::kSlots * kSlotBytes + Cfg<F8>::kRawSlots * kRawSlotBytes + 1024;
+    return 2 * kQBytes + Cfg<KV>::kSlots * kSlotBytes + Cfg<KV>::kRawSlots * Cfg<KV>::kRawBytes + 1024;
 }
-static_assert(smem_bytes<false>() <= 225 * 1024 + 1024 && smem_bytes<true>() <= 225 * 1024 + 1024,
+static_assert(smem_bytes<kBf16Kv>() <= 225 * 1024 + 1024 && smem_bytes<kE4m3Kv>() <= 225 * 1024 + 1024 &&
+                  smem_bytes<kE2m1Kv>() <= 225 * 1024 + 1024,
               "dynamic shared memory, with room for the static part");
 
 struct Meta {
@@ -217,14 +224,55 @@ __device__ __forceinline__ void widen_block(uint32_t src, uint32_t dst, int v0, 
     }
 }
 
+// The same of 4-bit pages as they are stored: 512 16-byte chunks (32 elements, two
+// scales), 4 a thread.  A chunk fills four 16-byte slots of a row; chunks 2 and 3,
+// whose column block is the other one, take them in another order, so that a quarter
+// warp's stores fall into eight bank groups.
+__device__ __forceinline__ void widen_block_e2m1(uint32_t src, uint32_t dst, int v0, int v1, int t) {
+    constexpr int kPage = fp4_page_bytes(kDim), kValues = fp4_value_bytes(kDim);
+    uint4 w[4];
+    uint32_t sc[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int idx = t + kRows * q, r = idx >> 2, c = idx & 3;
+        const uint32_t page = src + (r >> 4) * kPage;
+        w[q] = lds128(page + (r & 15) * 64 + 16 * c);
+        sc[q] = lds16(page + kValues + (r & 15) * 8 + 2 * c);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int idx = t + kRows * q, r = idx >> 2, c = idx & 3;
+        if ((r & 63) >= (r < kHalfTokens ? v0 : v1)) w[q] = make_uint4(0u, 0u, 0u, 0u), sc[q] = 0u;
+        const bool turned = (c & 2) != 0;
+        const uint32_t both = e4m3x2_to_f16x2(sc[q]);
+        const uint32_t s0 = __byte_perm(both, 0u, turned ? 0x3232 : 0x1010);
+        const uint32_t s1 = __byte_perm(both, 0u, turned ? 0x1010 : 0x3232);
+        const uint32_t v[4] = {turned ? w[q].z : w[q].x, turned ? w[q].w : w[q].y, turned ? w[q].x : w[q].z,
+                               turned ? w[q].y : w[q].w};
+        const uint32_t row = dst + (c >> 1) * kColBlockBytes + r * 128;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t p[4];
+            e2m1x8_to_f16(v[j], p);
+            const uint32_t s = j < 2 ? s0 : s1;
+            const int slot = 4 * (c & 1) + (turned ? j ^ 2 : j);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + ((slot ^ (r & 7)) << 4)),
+                         "r"(mul_f16x2(p[0], s)), "r"(mul_f16x2(p[1], s)), "r"(mul_f16x2(p[2], s)),
+                         "r"(mul_f16x2(p[3], s))
+                         : "memory");
+        }
+    }
+}
+
 // CAP: how the logits are capped (logit_cap.cuh).
 // DIRECT: every pair holds its rows' whole paths, and the kernel writes the
 // result itself (an instantiation of its own: a run-time test cost the join
 // 3%).
-template <bool F8, bool DIRECT, int CAP>
-__global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
+template <int KV, bool DIRECT, int CAP>
+__global__ void __launch_bounds__(Cfg<KV>::kThreads, 1)
     prefill_kernel(const __grid_constant__ KvMaps maps, const AttnArgs a) {
-    using C = Cfg<F8>;
+    using C = Cfg<KV>;
+    constexpr bool F8 = KV != kBf16Kv, F4 = KV == kE2m1Kv;   // widened to f16; from 4 bits
     static_assert(!F8 || CAP != kCapFree, "f16 P needs a reference");
     extern __shared__ uint8_t smem_raw[];
     __shared__ int abort_flag;
@@ -248,8 +296,10 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
         progress = 0;
         for (int i = 0; i < kMyBars; ++i) dev::mbar_init(bar(i), bar_count(i, F8));
         dev::fence_mbar_init();
-        dev::prefetch_tensormap(F8 ? &maps.k_box : &maps.k);
-        dev::prefetch_tensormap(F8 ? &maps.v_box : &maps.v);
+        if constexpr (!F4) {
+            dev::prefetch_tensormap(F8 ? &maps.k_box : &maps.k);
+            dev::prefetch_tensormap(F8 ? &maps.v_box : &maps.v);
+        }
     }
     if (warp == kMmaWarp) tc::alloc<kTmemCols>(dev::smem_addr(&tmem_base));
     tc::fence_before_sync();
@@ -689,7 +739,10 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                         break;
                     }
                     const int vv = valid_ring[blk % kValidRing];
-                    widen_block(raw + rs * kRawSlotBytes, ring + cs * kSlotBytes, vv & 0xff, vv >> 8, r);
+                    if constexpr (F4)
+                        widen_block_e2m1(raw + rs * C::kRawBytes, ring + cs * kSlotBytes, vv & 0xff, vv >> 8, r);
+                    else
+                        widen_block(raw + rs * C::kRawBytes, ring + cs * kSlotBytes, vv & 0xff, vv >> 8, r);
                     tc::fence_proxy_async_smem();
                     __syncwarp();
                     if (lane == 0) {
@@ -781,7 +834,7 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
         } else if (warp == kProducerWarp) {
             // -------------------------------------------------------- producer
             constexpr int NS = F8 ? C::kRawSlots : C::kSlots;
-            constexpr int kLoadBytes = F8 ? kRawSlotBytes : kSlotBytes;
+            constexpr int kLoadBytes = F8 ? C::kRawBytes : kSlotBytes;
             constexpr int kFullBar = F8 ? kRawFull : kFull, kEmptyBar = F8 ? kRawEmpty : kEmpty;
             const bool skip_first = a.debug_flags & PARASON_DEBUG_SKIP_FIRST_LOAD;
             const int page_rows = a.num_kv_heads * kPageSize;   // TMA rows between consecutive pages
@@ -848,6 +901,20 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
                         const uint32_t fb = bar(kFullBar + st);
                         const uint32_t dst0 = (F8 ? raw : ring) + st * kLoadBytes;
                         last_issue[st] = pos;
+                        if constexpr (F4) {
+                            // a copy per page (lane: page); padding and pages past the
+                            // item are not loaded (the converters write zeros)
+                            constexpr int kBytes = fp4_page_bytes(kDim);
+                            const uint32_t in = (pool >> w0) & 0xffu;
+                            const int32_t pr = __shfl_sync(0xffffffffu, win, w0 + (lane & 7));
+                            if (lane == 0) dev::mbar_arrive_expect_tx(fb, __popc(in) * kBytes);
+                            __syncwarp();
+                            if (lane < kBlockPages && ((in >> lane) & 1u))
+                                dev::bulk_load_hint(dst0 + lane * kBytes,
+                                                    (op ? a.v_raw : a.k_raw) + static_cast<int64_t>(pr / kPageSize) * kBytes,
+                                                    kBytes, fb, pol);
+                            continue;
+                        }
                         if (lane == 0) dev::mbar_arrive_expect_tx(fb, kLoadBytes);
                         if (whole) {                     // 8 pages in a row: one box
                             if (lane == 0)
@@ -1075,7 +1142,7 @@ __global__ void __launch_bounds__(Cfg<F8>::kThreads, 1)
 // Shared memory is configured once per device; the launch needs one CTA per SM.
 constexpr int kMaxConfigDevices = 64;
 
-template <bool F8, bool DIRECT, int CAP>
+template <int KV, bool DIRECT, int CAP>
 cudaError_t configure() {
     static std::mutex mu;
     static bool done[kMaxConfigDevices] = {};
@@ -1085,33 +1152,33 @@ cudaError_t configure() {
     if (dev < 0 || dev >= kMaxConfigDevices) return cudaErrorNotSupported;
     std::lock_guard<std::mutex> lock(mu);
     if (done[dev]) return cudaSuccess;
-    e = cudaFuncSetAttribute(prefill_kernel<F8, DIRECT, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             smem_bytes<F8>());
+    e = cudaFuncSetAttribute(prefill_kernel<KV, DIRECT, CAP>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             smem_bytes<KV>());
     if (e != cudaSuccess) return e;
-    e = cudaFuncSetAttribute(prefill_kernel<F8, DIRECT, CAP>, cudaFuncAttributePreferredSharedMemoryCarveout,
+    e = cudaFuncSetAttribute(prefill_kernel<KV, DIRECT, CAP>, cudaFuncAttributePreferredSharedMemoryCarveout,
                              cudaSharedmemCarveoutMaxShared);
     if (e != cudaSuccess) return e;
     done[dev] = true;
     return cudaSuccess;
 }
 
-template <bool F8, bool DIRECT, int CAP>
+template <int KV, bool DIRECT, int CAP>
 cudaError_t launch(const AttnArgs &a, const KvMaps &maps, cudaStream_t stream) {
-    const cudaError_t e = configure<F8, DIRECT, CAP>();
+    const cudaError_t e = configure<KV, DIRECT, CAP>();
     if (e != cudaSuccess) return e;
-    return launch_dependent(a.early != 0, prefill_kernel<F8, DIRECT, CAP>, dim3(a.num_ctas),
-                            dim3(Cfg<F8>::kThreads), smem_bytes<F8>(), stream, maps, a);
+    return launch_dependent(a.early != 0, prefill_kernel<KV, DIRECT, CAP>, dim3(a.num_ctas),
+                            dim3(Cfg<KV>::kThreads), smem_bytes<KV>(), stream, maps, a);
 }
 
-template <bool F8, int CAP>
+template <int KV, int CAP>
 cudaError_t launch_form(const AttnArgs &a, const KvMaps &maps, cudaStream_t stream) {
-    return a.out ? launch<F8, true, CAP>(a, maps, stream) : launch<F8, false, CAP>(a, maps, stream);
+    return a.out ? launch<KV, true, CAP>(a, maps, stream) : launch<KV, false, CAP>(a, maps, stream);
 }
 
-template <bool F8, int CAP>
+template <int KV, int CAP>
 cudaError_t prepare() {
-    const cudaError_t e = configure<F8, true, CAP>();
-    return e != cudaSuccess ? e : configure<F8, false, CAP>();
+    const cudaError_t e = configure<KV, true, CAP>();
+    return e != cudaSuccess ? e : configure<KV, false, CAP>();
 }
 
 }  // namespace
@@ -1119,17 +1186,20 @@ cudaError_t prepare() {
 cudaError_t launch_prefill(const AttnArgs &a, const KvMaps &maps, int mode, cudaStream_t stream) {
     if (a.num_items <= 0 || a.num_ctas <= 0) return cudaSuccess;
     const bool cap = a.cap_log2 > 0.f;
+    if (mode == PARASON_FP4_KV)
+        return cap ? launch_form<kE2m1Kv, kCapRef>(a, maps, stream) : launch_form<kE2m1Kv, kCapNone>(a, maps, stream);
     if (mode == PARASON_FP8_E4M3_KV)
-        return cap ? launch_form<true, kCapRef>(a, maps, stream) : launch_form<true, kCapNone>(a, maps, stream);
-    if (!cap) return launch_form<false, kCapNone>(a, maps, stream);
-    return a.cap_log2 <= kCapFreeLog2 ? launch_form<false, kCapFree>(a, maps, stream)
-                                      : launch_form<false, kCapRef>(a, maps, stream);
+        return cap ? launch_form<kE4m3Kv, kCapRef>(a, maps, stream) : launch_form<kE4m3Kv, kCapNone>(a, maps, stream);
+    if (!cap) return launch_form<kBf16Kv, kCapNone>(a, maps, stream);
+    return a.cap_log2 <= kCapFreeLog2 ? launch_form<kBf16Kv, kCapFree>(a, maps, stream)
+                                      : launch_form<kBf16Kv, kCapRef>(a, maps, stream);
 }
 
 cudaError_t prefill_prepare_cap(int mode) {
-    if (mode == PARASON_FP8_E4M3_KV) return prepare<true, kCapRef>();
-    const cudaError_t e = prepare<false, kCapFree>();
-    return e != cudaSuccess ? e : prepare<false, kCapRef>();
+    if (mode == PARASON_FP4_KV) return prepare<kE2m1Kv, kCapRef>();
+    if (mode == PARASON_FP8_E4M3_KV) return prepare<kE4m3Kv, kCapRef>();
+    const cudaError_t e = prepare<kBf16Kv, kCapFree>();
+    return e != cudaSuccess ? e : prepare<kBf16Kv, kCapRef>();
 }
 
 }  // namespace parason
