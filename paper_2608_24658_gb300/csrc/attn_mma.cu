@@ -107,7 +107,6 @@ struct KvE4m3 {
 struct KvE2m1 {
     static constexpr int kElemBytes = 1;
     static constexpr int kSuffixWarps = 12;
-    static constexpr int kStepPages = 2;
     static constexpr int kCap = kCapNone;
 };
 template <class KV>
@@ -132,7 +131,7 @@ struct Shape {
     // consecutive tokens hit 8 different 128-byte swizzle rows
     static constexpr int kSeg = kRowBytes / 128;
     static constexpr int kSegBytes = kPageSize * 128;
-    static constexpr int kStageBytes = 2 * kPageBytes;      // K and V of one page
+    static constexpr int kStageBytes = 2 * kPageBytes * (kFp4<KV> ? 2 : 1);   // K and V of one page (4-bit: of two)
 
     // suffix pass: a private ring per warp
     static constexpr int kSuffixWarps = KV::kSuffixWarps;
@@ -140,6 +139,7 @@ struct Shape {
     static constexpr int kWarpRingBytes = kWarpStages * kStageBytes;
     static constexpr int kNarrowBytes = kSuffixWarps * kWarpRingBytes;
     static constexpr int kNarrowBars = kSuffixWarps * kWarpStages;
+    static constexpr int kPageArrivals = kFp4<KV> ? 32 : 1;   // of a staged page: every lane's copies, or one box's bytes
 
     static constexpr int kBars = kNarrowBars > 64 ? kNarrowBars : 64;   // the larger of both passes' barriers
     static constexpr int kBodyBytes = 192 * 1024;
@@ -160,15 +160,11 @@ struct Shape {
 // only, so its lines go first when L2 needs room (the partials written
 // meanwhile stay for the merge).
 template <int D, class KV>
-__device__ __forceinline__ void load_suffix_page(uint32_t dst, const KvMaps &maps, const AttnArgs &a, int row,
+__device__ __forceinline__ void load_suffix_page(uint32_t dst, const KvMaps &maps, int row,
                                                  uint32_t bar) {
     using S = Shape<D, KV>;
     const uint64_t pol = dev::l2_evict_first_policy();
-    if constexpr (kFp4<KV>) {
-        const int64_t at = static_cast<int64_t>(row / kPageSize) * S::kPageBytes;
-        dev::bulk_load_hint(dst, a.k_raw + at, S::kPageBytes, bar, pol);
-        dev::bulk_load_hint(dst + S::kPageBytes, a.v_raw + at, S::kPageBytes, bar, pol);
-    } else if constexpr (S::kSeg > 1) {
+    if constexpr (S::kSeg > 1) {
         const int ph = row / kPageSize;
         dev::tma_load_4d_hint(dst, &maps.k_box, 0, 0, 0, ph, bar, pol);
         dev::tma_load_4d_hint(dst + S::kPageBytes, &maps.v_box, 0, 0, 0, ph, bar, pol);
@@ -176,6 +172,30 @@ __device__ __forceinline__ void load_suffix_page(uint32_t dst, const KvMaps &map
         dev::tma_load_3d_hint(dst, &maps.k, 0, 0, row, bar, pol);
         dev::tma_load_3d_hint(dst + S::kPageBytes, &maps.v, 0, 0, row, bar, pol);
     }
+}
+
+// A stage of the 4-bit ring, by the whole warp: K and V of the page at row0, then (row1 >=
+// 0) of another, 2 x 72 chunks of 16 bytes each.  k and v: this lane's 16 bytes of the
+// pools' first row, v one page further on, as V's bytes follow K's.
+template <int D>
+__device__ __forceinline__ void load_suffix_pages_fp4(uint32_t dst, const uint8_t *k0, const uint8_t *v0, int row0,
+                                                      int row1, uint32_t bar, uint64_t pol, int lane) {
+    constexpr int kPage = fp4_page_bytes(D), kStep = 32 * 16;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        // (a row of a page: kPage / kPageSize bytes)
+        const int64_t at = static_cast<int64_t>(p ? row1 : row0) * (kPage / kPageSize);
+        const uint8_t *k = k0 + at, *v = v0 + at;
+        if (p == 0 || row1 >= 0) {
+#pragma unroll
+            for (int i = 0; i < 2 * kPage; i += kStep) {
+                const uint8_t *src = i + kStep <= kPage ? k : i >= kPage ? v : i + 16 * lane < kPage ? k : v;
+                if (i + kStep <= 2 * kPage || i + 16 * lane < 2 * kPage)
+                    dev::copy16_hint(dst + 2 * kPage * p + i, src + i, pol);
+            }
+        }
+    }
+    dev::mbar_arrive_copied(bar);
 }
 
 template <int D>
@@ -229,33 +249,46 @@ __device__ __forceinline__ void clear_past_t(float (&x)[4], int valid, int gid) 
     if (key_of<KV>(gid + 8) >= valid) x[2] = x[3] = 0.f;
 }
 
-// 4-bit KV: the f16 fragments of one page.  K: lane (gid, tig) has elements
-// 32 tig .. 32 tig + 31 of tokens key_of(gid) and key_of(gid + 8), a 16-byte
-// chunk of each with two scales; k-step ks takes pairs 4 ks and 4 ks + 2 of
-// them, the slice that load_q_fragments gives it of q.
+// 4-bit KV: where a lane's bytes lie in a page of K (rows of 64 bytes, then the scales)
+// and in one of V.
+struct Fp4Lane {
+    uint32_t k, k_scale;                 // chunk tig of token key_of(gid), its two scales
+    uint32_t v0, v1, v_scale0, v_scale1; // block gid of tokens key_of(2 tig) and key_of(2 tig + 1)
+    __device__ __forceinline__ explicit Fp4Lane(int lane) {
+        const int gid = lane >> 2, tig = lane & 3;
+        const int tok = key_of<KvE2m1>(gid), t0 = key_of<KvE2m1>(2 * tig), t1 = key_of<KvE2m1>(2 * tig + 1);
+        k = tok * 64 + 16 * tig;
+        k_scale = fp4_value_bytes(128) + tok * 8 + 2 * tig;
+        v0 = t0 * 64 + 8 * gid;
+        v1 = t1 * 64 + 8 * gid;
+        v_scale0 = fp4_value_bytes(128) + t0 * 8 + gid;
+        v_scale1 = fp4_value_bytes(128) + t1 * 8 + gid;
+    }
+};
+
+// The f16 fragments of one page.  K: lane (gid, tig) has elements 32 tig .. 32 tig + 31
+// of tokens key_of(gid) and key_of(gid + 8), a 16-byte chunk of each with two scales;
+// k-step ks takes pairs 4 ks and 4 ks + 2 of them, the slice that load_q_fragments gives
+// it of q.
 struct Fp4Keys {
     uint32_t w[2][4];        // chunks of both tokens
-    uint32_t s[2][2];        // their scales, as f16 pairs of the same value
-    __device__ __forceinline__ Fp4Keys(uint32_t base, int lane) {
-        const int gid = lane >> 2, tig = lane & 3;
+    uint32_t s[2];           // their two scales each
+    __device__ __forceinline__ Fp4Keys(uint32_t base, const Fp4Lane &at) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int tok = (gid ^ ((gid >> 1) & 1)) + 8 * h;
-            const uint4 u = lds128(base + tok * 64 + 16 * tig);
+            const uint4 u = lds128(base + at.k + 8 * 64 * h);
             w[h][0] = u.x;
             w[h][1] = u.y;
             w[h][2] = u.z;
             w[h][3] = u.w;
-            const uint32_t both = e4m3x2_to_f16x2(lds16(base + fp4_value_bytes(128) + tok * 8 + 2 * tig));
-            s[h][0] = __byte_perm(both, 0u, 0x1010);
-            s[h][1] = __byte_perm(both, 0u, 0x3232);
+            s[h] = e4m3x2_to_f16x2(lds16(base + at.k_scale + 8 * 8 * h));
         }
     }
     // word i (k-steps 2 i and 2 i + 1) of token h: two pairs for each step
     __device__ __forceinline__ void word(int h, int i, uint32_t (&p)[4]) const {
         e2m1x8_to_f16(w[h][i], p);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) p[j] = mul_f16x2(p[j], s[h][i >> 1]);
+        for (int j = 0; j < 4; ++j) p[j] = i < 2 ? mul_f16x2_by<0>(p[j], s[h]) : mul_f16x2_by<1>(p[j], s[h]);
     }
 };
 
@@ -266,23 +299,22 @@ struct Fp4Keys {
 struct Fp4Values {
     uint32_t w[2][4];        // even columns of the chunk's words, odd columns, for each token pair
     uint32_t s[2];           // the pair's scales
-    __device__ __forceinline__ Fp4Values(uint32_t base, int valid, int lane) {
-        const int gid = lane >> 2, tig = lane & 3;
+    template <bool MASKED>
+    __device__ __forceinline__ void load(uint32_t base, int valid, const Fp4Lane &at, int tig) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int t0 = 2 * tig + (tig & 1) + 8 * h, t1 = t0 + 1 - 2 * (tig & 1);
-            uint2 x = lds64(base + t0 * 64 + 8 * gid), y = lds64(base + t1 * 64 + 8 * gid);
-            uint32_t sx = lds8(base + fp4_value_bytes(128) + t0 * 8 + gid);
-            uint32_t sy = lds8(base + fp4_value_bytes(128) + t1 * 8 + gid);
-            if (valid < kPageSize) {
-                if (t0 >= valid) x = make_uint2(0u, 0u), sx = 0u;
-                if (t1 >= valid) y = make_uint2(0u, 0u), sy = 0u;
+            uint2 x = lds64(base + at.v0 + 8 * 64 * h), y = lds64(base + at.v1 + 8 * 64 * h);
+            uint32_t sx = lds8(base + at.v_scale0 + 8 * 8 * h);
+            uint32_t sy = lds8(base + at.v_scale1 + 8 * 8 * h);
+            if constexpr (MASKED) {
+                if (key_of<KvE2m1>(2 * tig) + 8 * h >= valid) x = make_uint2(0u, 0u), sx = 0u;
+                if (key_of<KvE2m1>(2 * tig + 1) + 8 * h >= valid) y = make_uint2(0u, 0u), sy = 0u;
             }
             w[h][0] = (x.x & 0x0f0f0f0fu) | ((y.x << 4) & 0xf0f0f0f0u);
             w[h][1] = ((x.x >> 4) & 0x0f0f0f0fu) | (y.x & 0xf0f0f0f0u);
             w[h][2] = (x.y & 0x0f0f0f0fu) | ((y.y << 4) & 0xf0f0f0f0u);
             w[h][3] = ((x.y >> 4) & 0x0f0f0f0fu) | (y.y & 0xf0f0f0f0u);
-            s[h] = e4m3x2_to_f16x2(sx | (sy << 8));
+            s[h] = e4m3x2_to_f16x2(__byte_perm(sx, sy, 0x0040));
         }
     }
     // token pair h: columns 8 i, 8 i + 2, 8 i + 4, 8 i + 6 of the lane's 16 (odd 0), or those after them
@@ -411,7 +443,7 @@ __device__ __forceinline__ void page_step(uint32_t kbase, uint32_t vbase, int va
             dev::mma_bf16_16816(acc[1], qa[ks], b10, b11);
         }
     } else if constexpr (kFp4<KV>) {
-        const Fp4Keys k(kbase, lane);
+        const Fp4Keys k(kbase, Fp4Lane(lane));
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
             float(&acc)[2][4] = i < D / 64 ? sc : sd;
@@ -472,7 +504,11 @@ __device__ __forceinline__ void page_step(uint32_t kbase, uint32_t vbase, int va
             dev::mma_bf16_16816(st.o[dt + 1], pa, v2, v3);
         }
     } else if constexpr (kFp4<KV>) {
-        const Fp4Values v(vbase, valid, lane);
+        Fp4Values v;
+        if (valid < kPageSize)
+            v.load<true>(vbase, valid, Fp4Lane(lane), tig);
+        else
+            v.load<false>(vbase, valid, Fp4Lane(lane), tig);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {                    // columns 8 (c / 2) + c % 2 + {0, 2, 4, 6}
             uint32_t lo[4], hi[4];
@@ -597,18 +633,6 @@ __device__ __forceinline__ void scores_t(uint32_t kbase, const uint32_t (&qb)[D 
                          ka[2], ka[3]);
             dev::mma_bf16_16816(acc, ka, qb[ks][0], qb[ks][1]);
         }
-    } else if constexpr (kFp4<KV>) {
-        const Fp4Keys k(kbase, lane);
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-            float(&acc)[4] = i < D / 64 ? sc : sd;
-            uint32_t g[4], h[4];
-            k.word(0, i, g);
-            k.word(1, i, h);
-            const uint32_t k0[4] = {g[0], h[0], g[1], h[1]}, k1[4] = {g[2], h[2], g[3], h[3]};
-            dev::mma_f16_16816(acc, k0, qb[2 * i][0], qb[2 * i][1]);
-            dev::mma_f16_16816(acc, k1, qb[2 * i + 1][0], qb[2 * i + 1][1]);
-        }
     } else {
         static_assert(D == 128, "e4m3 KV path is written for head_dim 128");
         // 16-byte chunks 2 tig and 2 tig + 1 of tokens gid and gid + 8 (the
@@ -634,6 +658,25 @@ __device__ __forceinline__ void scores_t(uint32_t kbase, const uint32_t (&qb)[D 
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) s[e] = sc[e] + sd[e];
+}
+
+// O^T += V^T P^T of one 4-bit page
+template <int D>
+__device__ __forceinline__ void pv_fp4(const Fp4Values &v, uint32_t pb0, uint32_t pb1, WarpStateT<D> &st) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        uint32_t p[2][2][4];                             // [token pair][odd column][column pair]
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            v.columns(h, i, 0, p[h][0]);
+            v.columns(h, i, 1, p[h][1]);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t a4[4] = {p[0][0][j], p[0][1][j], p[1][0][j], p[1][1][j]};
+            dev::mma_f16_16816(st.o[4 * i + j], a4, pb0, pb1);
+        }
+    }
 }
 
 // O^T += V^T P^T of one page
@@ -665,22 +708,6 @@ __device__ __forceinline__ void pv_t(uint32_t vbase, int valid, uint32_t pb0, ui
             va[2] &= keep_hi;
             va[3] &= keep_hi;
             dev::mma_bf16_16816(st.o[dt], va, pb0, pb1);
-        }
-    } else if constexpr (kFp4<KV>) {
-        const Fp4Values v(vbase, valid, lane);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            uint32_t p[2][2][4];                         // [token pair][odd column][column pair]
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                v.columns(h, i, 0, p[h][0]);
-                v.columns(h, i, 1, p[h][1]);
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t a4[4] = {p[0][0][j], p[0][1][j], p[1][0][j], p[1][1][j]};
-                dev::mma_f16_16816(st.o[4 * i + j], a4, pb0, pb1);
-            }
         }
     } else {
         // this lane's output columns are 16 gid .. 16 gid + 15: chunk gid of
@@ -789,6 +816,99 @@ __device__ __forceinline__ void pages_step_t(const uint32_t *kbase, const uint32
             pb1 = dev::movmatrix_trans(dev::pack_f16(p2, p3));
         }
         pv_t<D, KV>(vbase[p], p == NP - 1 ? valid_last : kPageSize, pb0, pb1, st, lane);
+    }
+}
+
+// pages_step_t of the two 4-bit pages of a stage (K, V, K, V from `base`); MASKED: of which
+// `keys` tokens are there, 1 to 32 (with 16 or fewer the second page holds anything).  The
+// row maxima are wanted only where a score passes the reference by 2^8, which a vote of
+// the lanes' own maxima says; and V is regrouped before the exponentials, so that neither
+// waits for the other and the stage is free for its next pages (`refill`).
+template <int D, class KV, bool MASKED, class Refill>
+__device__ __forceinline__ void pages_step_fp4(uint32_t base, int keys, const uint32_t (&qb)[D / 16][2],
+                                               WarpStateT<D> &st, float scale_log2, float cap_log2, bool &cap_large,
+                                               const Fp4Lane &at, int lane, const Refill &refill) {
+    constexpr int kPage = fp4_page_bytes(D), NP = 2;
+    const int gid = lane >> 2, tig = lane & 3;
+    float x[NP][4];
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+        const Fp4Keys k(base + 2 * kPage * p, at);
+        float sc[4], sd[4];                              // first and second half of d
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            float(&acc)[4] = i < D / 64 ? sc : sd;
+            uint32_t g[4], h[4];
+            k.word(0, i, g);
+            k.word(1, i, h);
+            const uint32_t k0[4] = {g[0], h[0], g[1], h[1]}, k1[4] = {g[2], h[2], g[3], h[3]};
+            if (i % (D / 64) == 0)
+                dev::mma_f16_16816_first(acc, k0, qb[2 * i][0], qb[2 * i][1]);
+            else
+                dev::mma_f16_16816(acc, k0, qb[2 * i][0], qb[2 * i][1]);
+            dev::mma_f16_16816(acc, k1, qb[2 * i + 1][0], qb[2 * i + 1][1]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[p][e] = sc[e] + sd[e];
+    }
+    float scale = scale_log2;
+    if constexpr (KV::kCap == kCapRef) {
+        if constexpr (MASKED) {
+            clear_past_t<KV>(x[0], min(keys, kPageSize), gid);
+            clear_past_t<KV>(x[1], max(keys - kPageSize, 0), gid);
+        }
+        cap_scores<2>(x, cap_large, CapFactors(scale_log2, cap_log2));
+        scale = 1.f;
+    }
+    if constexpr (MASKED) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            if (key_of<KV>(gid) + kPageSize * p >= keys) x[p][0] = x[p][1] = -INFINITY;
+            if (key_of<KV>(gid + 8) + kPageSize * p >= keys) x[p][2] = x[p][3] = -INFINITY;
+        }
+    }
+    Fp4Values v[NP];
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+        v[p].template load<MASKED>(base + 2 * kPage * p + kPage, keys - kPageSize * p, at, tig);
+    refill();                            // (the stage is in registers)
+    float mx0 = fmaxf(x[0][0], x[0][2]), mx1 = fmaxf(x[0][1], x[0][3]);
+#pragma unroll
+    for (int p = 1; p < NP; ++p) {
+        mx0 = dev::max3(mx0, x[p][0], x[p][2]);
+        mx1 = dev::max3(mx1, x[p][1], x[p][3]);
+    }
+    mx0 *= scale;
+    mx1 *= scale;
+    if (__any_sync(0xffffffffu, mx0 > st.m[0] + kLazyRescaleLog2 || mx1 > st.m[1] + kLazyRescaleLog2)) {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+            mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, o));
+            mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, o));
+        }
+        const float mn0 = fmaxf(st.m[0], mx0), mn1 = fmaxf(st.m[1], mx1);
+        const float al0 = dev::fast_exp2(st.m[0] - mn0), al1 = dev::fast_exp2(st.m[1] - mn1);
+        st.m[0] = mn0;
+        st.m[1] = mn1;
+        st.l[0] *= al0;
+        st.l[1] *= al1;
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) {
+            st.o[dt][0] *= al0;
+            st.o[dt][1] *= al1;
+            st.o[dt][2] *= al0;
+            st.o[dt][3] *= al1;
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+        const float p0 = dev::fast_exp2(fmaf(x[p][0], scale, -st.m[0]));
+        const float p1 = dev::fast_exp2(fmaf(x[p][1], scale, -st.m[1]));
+        const float p2 = dev::fast_exp2(fmaf(x[p][2], scale, -st.m[0]));
+        const float p3 = dev::fast_exp2(fmaf(x[p][3], scale, -st.m[1]));
+        st.l[0] += p0 + p2;
+        st.l[1] += p1 + p3;
+        pv_fp4<D>(v[p], dev::movmatrix_trans(dev::pack_f16(p0, p1)), dev::movmatrix_trans(dev::pack_f16(p2, p3)), st);
     }
 }
 
@@ -1029,7 +1149,7 @@ __device__ void suffix_warp(const KvMaps &maps, const AttnArgs &a, uint32_t ring
             const int s = issued % NS;
             const uint32_t bar = my_bar + s * 8;
             dev::mbar_arrive_expect_tx(bar, S::kStageBytes);
-            load_suffix_page<D, KV>(my_ring + s * S::kStageBytes, maps, a, row, bar);
+            load_suffix_page<D, KV>(my_ring + s * S::kStageBytes, maps, row, bar);
         }
         ++iss_pg;
         ++issued;
@@ -1111,6 +1231,152 @@ __device__ void suffix_warp(const KvMaps &maps, const AttnArgs &a, uint32_t ring
         }
         if (!ok) break;
         store_warp_partials<D, KV>(a, it, st, lane, scl.y);
+    }
+    if (!ok && lane == 0) dev::record_error(a.err, PARASON_ETIMEOUT, kSiteConsumerFull);
+    // copies still in flight must land before the CTA's shared memory goes
+    if (lane == 0) {
+        for (int q = consumed; q < issued; ++q) {
+            if (skip_first && q == 0) continue;
+            dev::mbar_wait_bounded(my_bar + (q % NS) * 8, (q / NS) & 1, kDrainLimitNs, nullptr);
+        }
+    }
+    __syncwarp();
+}
+
+// The same over 4-bit pages, whose 2304 bytes of K and V are worth 100 cycles of an SM's
+// share of HBM: what is done by the page counts as much as the page's own arithmetic.  So a
+// stage of the ring is two pages, with one wait, one turn of the loop and one softmax
+// update, the whole warp copies (288 chunks of 16 bytes are nine a lane), and tiles of up
+// to 8 rows all take the transposed step.
+template <int D, class KV>
+__device__ void suffix_warp_fp4(const AttnArgs &a, uint32_t ring, uint32_t bars, int warp, int lane, WorkItem *grab) {
+    using S = Shape<D, KV>;
+    constexpr int NS = S::kWarpStages, kPage = S::kPageBytes;
+    const uint32_t my_ring = ring + warp * S::kWarpRingBytes;
+    const uint32_t my_bar = bars + warp * NS * 8;
+    const bool skip_first = (a.debug_flags & PARASON_DEBUG_SKIP_FIRST_LOAD) && warp == 0 &&
+                            static_cast<int>(blockIdx.x) >= a.num_wide_ctas;
+    const Fp4Lane at(lane);
+
+    // Issue side, as in suffix_warp: the next item is claimed, read and switched to over
+    // the current one's last stages.  Lane i holds the row of page win_pg + i (the record's
+    // own at first, then the page stream's, 32 at a time and asked for 32 ahead).
+    constexpr int kFetchPages = 4, kFirstRows = kRecRows & ~1;
+    const uint8_t *k0 = a.k_raw + 16 * lane, *v0 = a.v_raw + 16 * lane - kPage;
+    const uint64_t pol = dev::l2_evict_first_policy();
+    int pulled = 0, iss_pg = 0, iss_np = 0, iss_s = 0, issued = 0;
+    int fetch = 0;
+    const int own_first = static_cast<int>(blockIdx.x) - a.num_wide_ctas;
+    int claimed = own_first >= 0 ? warp * (a.num_ctas - a.num_wide_ctas) + own_first : -1;
+    int nxt_id = 0;                      // -1: the queue is empty
+    int32_t nxt_w = 0;
+    const int32_t *stream = nullptr;
+    int win_pg = 0, win_end = 0;
+    int32_t win = 0, win_next = 0;
+    auto fetch_step = [&]() {
+        if (fetch == 0) {
+            if (lane == 0 && (pulled > 0 || claimed < 0)) claimed = atomicAdd(a.queue_next + 1, 1);
+            fetch = 1;
+        } else if (fetch == 1) {
+            int id = -1;
+            if (lane == 0) id = queue_item(a, 1, claimed);
+            nxt_id = __shfl_sync(0xffffffffu, id, 0);
+            if (nxt_id >= 0) nxt_w = a.item_rec[static_cast<int64_t>(nxt_id) * kRecWords + lane];
+            fetch = 2;
+        }
+    };
+    // an item's last stages, and the switch to the next one; false: no more
+    auto near_end = [&]() {
+        if (nxt_id < 0 && iss_pg >= iss_np) return false;
+        fetch_step();
+        while (iss_pg >= iss_np) {
+            while (fetch < 2) fetch_step();
+            if (nxt_id < 0) return false;
+            fetch = 0;
+            iss_np = __shfl_sync(0xffffffffu, nxt_w, 1);          // WorkItem::num_pages
+            stream = a.stream_rows + __shfl_sync(0xffffffffu, nxt_w, kRecRowsOff) + lane;
+            win = __shfl_sync(0xffffffffu, nxt_w, min(kRecRow0 + lane, kRecWords - 1));
+            iss_pg = win_pg = 0;
+            win_end = kFirstRows;
+            if (iss_np > kFirstRows) win_next = stream[kFirstRows];
+            if (lane < 8) reinterpret_cast<int32_t *>(grab + pulled % kGrabSlots)[lane] = nxt_w;
+            ++pulled;
+        }
+        return true;
+    };
+    auto issue_next = [&]() {
+        if (iss_pg + kFetchPages >= iss_np && !near_end()) return;
+        if (iss_pg >= win_end) {
+            win = win_next;
+            win_pg = iss_pg;
+            win_end = iss_pg + 32;
+            if (iss_np > win_end) win_next = stream[win_end];
+        }
+        const int row0 = __shfl_sync(0xffffffffu, win, iss_pg - win_pg);
+        int row1 = __shfl_sync(0xffffffffu, win, iss_pg - win_pg + 1);
+        if (iss_pg + 1 >= iss_np) row1 = -1;
+        if (!(skip_first && issued == 0))
+            load_suffix_pages_fp4<D>(my_ring + iss_s * S::kStageBytes + 16 * lane, k0, v0, row0, row1,
+                                     my_bar + iss_s * 8, pol, lane);
+        iss_s = iss_s + 1 == NS ? 0 : iss_s + 1;
+        iss_pg += 2;
+        ++issued;
+    };
+    for (int i = 0; i < NS; ++i) issue_next();
+
+    int consumed = 0, con_s = 0, con_ph = 0;             // stages
+    bool ok = true, cap_large = false;                   // (cap_free)
+    auto next_stage = [&]() {
+        __syncwarp();
+        issue_next();
+        ++consumed;
+        if (++con_s == NS) {
+            con_s = 0;
+            con_ph ^= 1;
+        }
+    };
+    for (int k = 0; consumed < issued && ok; ++k) {
+        __syncwarp();
+        const WorkItem it = grab[k % kGrabSlots];
+        const float2 scl = item_scales<KV>(a, it);
+        if (it.nrows <= 8) {
+            uint32_t qb[D / 16][2];
+            load_q_fragments_t<D, KV>(a, it, lane, qb);
+            WarpStateT<D> st;
+            reset<D>(st);
+            for (int left = it.num_pages; left > 0; left -= 2) {
+                if (!dev::mbar_wait_bounded(my_bar + con_s * 8, con_ph, a.wait_limit_ns, nullptr)) {
+                    ok = false;
+                    break;
+                }
+                const uint32_t base = my_ring + con_s * S::kStageBytes;
+                if (left > 2)
+                    pages_step_fp4<D, KV, false>(base, 0, qb, st, scl.x, a.cap_log2, cap_large, at, lane, next_stage);
+                else
+                    pages_step_fp4<D, KV, true>(base, (left - 1) * kPageSize + it.last_valid, qb, st, scl.x,
+                                                a.cap_log2, cap_large, at, lane, next_stage);
+            }
+            if (ok) store_warp_partials_t<D, KV>(a, it, st, lane, scl.y);
+        } else {
+            uint32_t qa[D / 16][4];
+            load_q_fragments<D, KV>(a, it, lane, qa);
+            WarpState<D> st;
+            reset<D>(st);
+            for (int left = it.num_pages; left > 0; left -= 2) {
+                if (!dev::mbar_wait_bounded(my_bar + con_s * 8, con_ph, a.wait_limit_ns, nullptr)) {
+                    ok = false;
+                    break;
+                }
+#pragma unroll 1
+                for (int p = 0; p < min(left, 2); ++p) {
+                    const uint32_t base = my_ring + con_s * S::kStageBytes + 2 * kPage * p;
+                    page_step<D, KV>(base, base + kPage, left == p + 1 ? it.last_valid : kPageSize, qa, st, scl.x,
+                                     a.cap_log2, cap_large, lane);
+                }
+                next_stage();
+            }
+            if (ok) store_warp_partials<D, KV>(a, it, st, lane, scl.y);
+        }
     }
     if (!ok && lane == 0) dev::record_error(a.err, PARASON_ETIMEOUT, kSiteConsumerFull);
     // copies still in flight must land before the CTA's shared memory goes
@@ -2558,7 +2824,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int i = 0; i < kTcBars; ++i)
                 dev::mbar_init(bars + 8 * i, tc_bar_count(i, KV::kElemBytes == 1));
         } else {
-            for (int s = 0; s < S::kNarrowBars; ++s) dev::mbar_init(bars + 8 * s, 1);
+            for (int s = 0; s < S::kNarrowBars; ++s) dev::mbar_init(bars + 8 * s, S::kPageArrivals);
         }
         dev::fence_mbar_init();
         if constexpr (!kFp4<KV>) {
@@ -2606,13 +2872,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int i = threadIdx.x; i < prefix_bars || i < S::kNarrowBars; i += blockDim.x) {
             if (i < prefix_bars)
                 asm volatile("mbarrier.inval.shared::cta.b64 [%0];" ::"r"(bars + 8 * i) : "memory");
-            if (i < S::kNarrowBars) dev::mbar_init(bars + 8 * i, 1);
+            if (i < S::kNarrowBars) dev::mbar_init(bars + 8 * i, S::kPageArrivals);
         }
         dev::fence_mbar_init();
         __syncthreads();
     }
-    if (warp < S::kSuffixWarps)
-        suffix_warp<D, KV>(maps, a, ring, bars, warp, lane, grab_items[warp]);
+    if (warp < S::kSuffixWarps) {
+        if constexpr (kFp4<KV>)
+            suffix_warp_fp4<D, KV>(a, ring, bars, warp, lane, grab_items[warp]);
+        else
+            suffix_warp<D, KV>(maps, a, ring, bars, warp, lane, grab_items[warp]);
+    }
 }
 
 // Shared memory and carveout are set once per device (with that device

@@ -51,6 +51,23 @@ __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
     return c;
 }
 
+// The same with one half of b for both.
+template <int HALF>
+__device__ __forceinline__ uint32_t mul_f16x2_by(uint32_t a, uint32_t b) {
+    uint32_t c;
+    if constexpr (HALF == 0)
+        asm("{\n\t.reg .f16 l, h;\n\t.reg .b32 t;\n\t"
+            "mov.b32 {l, h}, %2;\n\tmov.b32 t, {l, l};\n\tmul.rn.f16x2 %0, %1, t;\n\t}"
+            : "=r"(c)
+            : "r"(a), "r"(b));
+    else
+        asm("{\n\t.reg .f16 l, h;\n\t.reg .b32 t;\n\t"
+            "mov.b32 {l, h}, %2;\n\tmov.b32 t, {h, h};\n\tmul.rn.f16x2 %0, %1, t;\n\t}"
+            : "=r"(c)
+            : "r"(a), "r"(b));
+    return c;
+}
+
 // A bf16 pair of q narrowed to an f16 pair for the e4m3 MMAs.  The f16
 // values are exact for |q| < 65504 (tiny values lose low bits); an element
 // of magnitude 65520 or more (including inf) would round to inf, so `big` is
