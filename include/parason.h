@@ -617,7 +617,7 @@ typedef struct {
  * on the device.  Other than held_out and used_out, outputs overlap nothing here.
  * PARASON_EINVAL for a negative count, a missing or misaligned (4 bytes) array, a
  * table_stride below table_pages, slots = positions, or what belongs to a free list
- * without one; PARASON_EUNSUPPORTED for more than 16384 sequences or (about) 2^31 rows;
+ * without one; PARASON_EUNSUPPORTED for more than 16384 sequences or 2^31 - 1 rows;
  * PARASON_ECUDA if the launch fails. */
 parason_status parason_kv_slots(const parason_slot_map *map, parason_stream_t stream);
 

@@ -180,8 +180,8 @@ constexpr int kWarps = kThreads / 32;
 // CTAs of kv_write to ask an SM's registers for: bf16 and e4m3 rows fit 5 without
 // spills (e4m3 took 105 registers unasked, and 300 tokens of 64 / 8 heads 4.5 us for
 // 3.5); fp32 rows do not everywhere, and are left to themselves (96 to 104).
-template <class T>
-constexpr int kAskedCtas = sizeof(T) == 2 ? 5 : 0;
+template <class T, bool NORM>
+constexpr int kAskedCtas = sizeof(T) == 2 ? (NORM ? 4 : 5) : 0;
 
 // cos and sin of positions[axis] * inv_freq[i].  The frequency is held as turns a
 // position modulo 1, in 2^-64: the low 64 bits of its product with the position are
@@ -306,56 +306,135 @@ __device__ __forceinline__ void store_fp4(Fp4 *row, int to_scales, const float (
     if (e1 % 16 == 0) out[to_scales + e1 / 16] = static_cast<uint8_t>(s2 >> 8);
 }
 
-// x / sqrt(mean x^2 + eps) * (offset + w) over a head of D elements, whose lanes are
-// `group`.
-template <class T, int D>
-__device__ __forceinline__ void norm_head(float (&x0)[8], float (&x1)[8], const Raw8<T> &w0, const Raw8<T> &w1,
-                                          float eps, float offset, uint32_t group) {
-    unsigned long long sum = dev::mul_f32x2(dev::f32x2(x0[0], x0[1]), dev::f32x2(x0[0], x0[1]));
+// This lane's part of sum x^2 of a head.
+template <class T>
+__device__ __forceinline__ float square_sum(const Raw8<T> &r0, const Raw8<T> &r1) {
+    float x0[8], x1[8];
+    unpack8(r0, x0);
+    unpack8(r1, x1);
+    unsigned long long a = dev::mul_f32x2(dev::f32x2(x0[0], x0[1]), dev::f32x2(x0[0], x0[1]));
+    unsigned long long b = dev::mul_f32x2(dev::f32x2(x1[0], x1[1]), dev::f32x2(x1[0], x1[1]));
 #pragma unroll
-    for (int i = 2; i < 8; i += 2) sum = dev::fma_f32x2(dev::f32x2(x0[i], x0[i + 1]), dev::f32x2(x0[i], x0[i + 1]), sum);
-#pragma unroll
-    for (int i = 0; i < 8; i += 2) sum = dev::fma_f32x2(dev::f32x2(x1[i], x1[i + 1]), dev::f32x2(x1[i], x1[i + 1]), sum);
-    float lo, hi;
-    dev::f32x2_split(sum, lo, hi);
-    float s = lo + hi;
-#pragma unroll
-    for (int o = 1; o < D / 16; o <<= 1) s += __shfl_xor_sync(group, s, o);
-    const float inv = __frsqrt_rn(s * (1.f / D) + eps);
-    float y0[8], y1[8];
-    unpack8(w0, y0);
-    unpack8(w1, y1);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        x0[i] = x0[i] * inv * (y0[i] + offset);
-        x1[i] = x1[i] * inv * (y1[i] + offset);
+    for (int i = 2; i < 8; i += 2) {
+        a = dev::fma_f32x2(dev::f32x2(x0[i], x0[i + 1]), dev::f32x2(x0[i], x0[i + 1]), a);
+        b = dev::fma_f32x2(dev::f32x2(x1[i], x1[i + 1]), dev::f32x2(x1[i], x1[i + 1]), b);
     }
+    float lo, hi;
+    dev::f32x2_split(dev::add_f32x2(a, b), lo, hi);
+    return lo + hi;
 }
+
+// x *= w + offset, of weights that are a head's own.
+template <class T>
+__device__ __forceinline__ void weighted8(float (&x)[8], const Raw8<T> &w, float offset) {
+    float y[8];
+    unpack8(w, y);
+    const unsigned long long off2 = dev::f32x2(offset, offset);
+#pragma unroll
+    for (int i = 0; i < 8; i += 2)
+        dev::f32x2_split(dev::mul_f32x2(dev::f32x2(x[i], x[i + 1]), dev::add_f32x2(dev::f32x2(y[i], y[i + 1]), off2)),
+                         x[i], x[i + 1]);
+}
+
+// Element 2 i (+ 1 for j = 1) of a lane's first (q false) or second halves of pairs.
+__device__ __forceinline__ float &pair_of(float (&x0)[8], float (&x1)[8], bool interleaved, int i, int j, bool q) {
+    if (!interleaved) return (q ? x1 : x0)[2 * i + j];
+    return (i < 2 ? x0 : x1)[4 * (i & 1) + 2 * j + (q ? 1 : 0)];
+}
+
+// The norm's weights times cos and sin, made once for all heads of a kind: a pair (p, q)
+// becomes inv (p pc + q qs, p ps + q qc), qs with the minus.  Where nothing turns, p pc and q qc.
+struct TurnedWeights {
+    unsigned long long pc[4], qs[4], ps[4], qc[4];
+    __device__ __forceinline__ TurnedWeights(float (&w0)[8], float (&w1)[8], bool interleaved, bool rotates,
+                                             const unsigned long long (&cs)[4], const unsigned long long (&sn)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const unsigned long long p = dev::f32x2(pair_of(w0, w1, interleaved, i, 0, false), pair_of(w0, w1, interleaved, i, 1, false));
+            const unsigned long long q = dev::f32x2(pair_of(w0, w1, interleaved, i, 0, true), pair_of(w0, w1, interleaved, i, 1, true));
+            pc[i] = p;
+            qc[i] = q;
+            qs[i] = ps[i] = 0ull;
+            if (rotates) {
+                pc[i] = dev::mul_f32x2(p, cs[i]);
+                qs[i] = dev::mul_f32x2(q, sn[i]) ^ 0x8000000080000000ull;
+                ps[i] = dev::mul_f32x2(p, sn[i]);
+                qc[i] = dev::mul_f32x2(q, cs[i]);
+            }
+        }
+    }
+    __device__ __forceinline__ void apply(float (&x0)[8], float (&x1)[8], float inv, bool interleaved, bool rotates) const {
+        const unsigned long long inv2 = dev::f32x2(inv, inv);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float &p0 = pair_of(x0, x1, interleaved, i, 0, false), &p1 = pair_of(x0, x1, interleaved, i, 1, false);
+            float &q0 = pair_of(x0, x1, interleaved, i, 0, true), &q1 = pair_of(x0, x1, interleaved, i, 1, true);
+            const unsigned long long p = dev::mul_f32x2(dev::f32x2(p0, p1), inv2);
+            const unsigned long long q = dev::mul_f32x2(dev::f32x2(q0, q1), inv2);
+            unsigned long long y = dev::mul_f32x2(p, pc[i]), z = dev::mul_f32x2(q, qc[i]);
+            if (rotates) {
+                y = dev::fma_f32x2(q, qs[i], y);
+                z = dev::fma_f32x2(p, ps[i], z);
+            }
+            dev::f32x2_split(y, p0, p1);
+            dev::f32x2_split(z, q0, q1);
+        }
+    }
+};
 
 // Heads of one kind, steps [s0, s1): normed, rotated, scaled, rounded, stored at dst + e0
 // and dst + e1, a step further `dst_step`.  `batch` holds the first steps already.
-template <class T, class Out, int D, int G, bool ROTATE, bool NORM, int kBatch>
+template <class T, class Out, int D, int G, bool ROTATE, bool NORM, int kBatch, bool AHEAD, class Then>
 __device__ __forceinline__ void write_heads(Batch<T, kBatch> &batch, const T *src, int64_t src_step, Out *dst,
                                             int64_t dst_step, int s0, int s1, int heads, int mine, int e0, int e1,
                                             bool interleaved, bool rotates, const unsigned long long (&cs)[4],
                                             const unsigned long long (&sn)[4], const float *scale, const T *weight,
-                                            int64_t weight_stride, const WriteArgs &a, int to_scales) {
+                                            int64_t weight_stride, const WriteArgs &a, int to_scales,
+                                            const Then &then) {
     constexpr int kLanes = D / 16;
     const int first_lane = threadIdx.x % 32 / kLanes * kLanes;
     const uint32_t group = ((1u << kLanes) - 1) << first_lane;      // the lanes of a head
     const BlockMates mates(e0, e1, ROTATE && !interleaved ? a.rot.half / 8 : 0, first_lane);
-    // (a weight for all heads stays in registers)
-    Raw8<T> w0 = {}, w1 = {};
-    if constexpr (NORM) {
-        if (weight) {
-            const T *w = weight + (s0 * G + mine < heads ? s0 * G + mine : 0) * weight_stride;
-            w0 = load_weight8(w + e0);
-            w1 = load_weight8(w + e1);
+    // (weights of all heads go into the rotation)
+    float w0[8], w1[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w0[i] = w1[i] = 1.f;
+    if (NORM && weight && !weight_stride) {
+        unpack8(load_weight8(weight + e0), w0);
+        unpack8(load_weight8(weight + e1), w1);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            w0[i] += a.norm.offset;
+            w1[i] += a.norm.offset;
         }
     }
+    const TurnedWeights turned(w0, w1, interleaved, ROTATE && rotates, cs, sn);
     dst += s0 * dst_step;
     for (int s = s0; s < s1; s += kBatch, dst += kBatch * dst_step) {
-        if (s != s0) batch.template load<G>(src, src_step, s, s1, heads, mine, e0, e1);
+        Batch<T, kBatch> next;
+        if constexpr (AHEAD) {
+            if (s + kBatch < s1)
+                next.template load<G>(src, src_step, s + kBatch, s1, heads, mine, e0, e1);
+            else
+                then(next);
+        } else if (s != s0) {
+            batch.template load<G>(src, src_step, s, s1, heads, mine, e0, e1);
+        }
+        // the batch's sums go through the lanes side by side (one after another, a shuffle
+        // chain a step: XXX)
+        float inv[kBatch];
+        if constexpr (NORM) {
+            if (weight) {
+#pragma unroll
+                for (int b = 0; b < kBatch; ++b) inv[b] = square_sum<T>(batch.r0[b], batch.r1[b]);
+#pragma unroll
+                for (int o = 1; o < kLanes; o <<= 1)
+#pragma unroll
+                    for (int b = 0; b < kBatch; ++b) inv[b] += __shfl_xor_sync(group, inv[b], o);
+#pragma unroll
+                for (int b = 0; b < kBatch; ++b) inv[b] = rsqrtf(inv[b] * (1.f / D) + a.norm.eps);
+            }
+        }
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
             const int h = (s + b) * G + mine;
@@ -364,22 +443,17 @@ __device__ __forceinline__ void write_heads(Batch<T, kBatch> &batch, const T *sr
             unpack8(batch.r0[b], x0);
             unpack8(batch.r1[b], x1);
             if constexpr (NORM) {
-                if (weight) {
-                    if (weight_stride) {
-                        w0 = load_weight8(weight + h * weight_stride + e0);
-                        w1 = load_weight8(weight + h * weight_stride + e1);
-                    }
-                    norm_head<T, D>(x0, x1, w0, w1, a.norm.eps, a.norm.offset, group);
+                if (weight && weight_stride) {
+                    weighted8<T>(x0, load_weight8(weight + h * weight_stride + e0), a.norm.offset);
+                    weighted8<T>(x1, load_weight8(weight + h * weight_stride + e1), a.norm.offset);
                 }
-            }
-            if (ROTATE && rotates) {
+                turned.apply(x0, x1, weight ? inv[b] : 1.f, interleaved, rotates);
+            } else if (ROTATE && rotates) {
                 // (p c - q s, p s + q c), two pairs an instruction
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    float &p0 = interleaved ? (i < 2 ? x0 : x1)[4 * (i & 1)] : x0[2 * i];
-                    float &p1 = interleaved ? (i < 2 ? x0 : x1)[4 * (i & 1) + 2] : x0[2 * i + 1];
-                    float &q0 = interleaved ? (i < 2 ? x0 : x1)[4 * (i & 1) + 1] : x1[2 * i];
-                    float &q1 = interleaved ? (i < 2 ? x0 : x1)[4 * (i & 1) + 3] : x1[2 * i + 1];
+                    float &p0 = pair_of(x0, x1, interleaved, i, 0, false), &p1 = pair_of(x0, x1, interleaved, i, 1, false);
+                    float &q0 = pair_of(x0, x1, interleaved, i, 0, true), &q1 = pair_of(x0, x1, interleaved, i, 1, true);
                     const unsigned long long p = dev::f32x2(p0, p1), q = dev::f32x2(q0, q1);
                     const unsigned long long nq = dev::f32x2(-q0, -q1);
                     dev::f32x2_split(dev::fma_f32x2(p, cs[i], dev::mul_f32x2(nq, sn[i])), p0, p1);
@@ -398,6 +472,7 @@ __device__ __forceinline__ void write_heads(Batch<T, kBatch> &batch, const T *sr
                 store8(dst + b * dst_step + e1, x1);
             }
         }
+        if constexpr (AHEAD) batch = next;
     }
 }
 
@@ -416,9 +491,10 @@ __device__ __forceinline__ void write_heads(Batch<T, kBatch> &batch, const T *sr
 // pairs' angles, make 8 / G each and pass them round (out of shared memory they were
 // read four lanes to a bank).
 template <class T, class KV, int D, bool INTERLEAVED, int G, bool NORM>
-__global__ void __launch_bounds__(kThreads, kAskedCtas<T>) kv_write_kernel(const WriteArgs a) {
+__global__ void __launch_bounds__(kThreads, kAskedCtas<T, NORM>) kv_write_kernel(const WriteArgs a) {
     constexpr int kLanes = D / 16, kTeams = 32 / kLanes / G, kMake = 8 / G;
     constexpr int kBatch = sizeof(T) == 4 ? 2 : 3;            // (steps in flight, as above)
+    constexpr bool kAhead = NORM;                             // the next batch is asked for before this one is used
     const int lane = threadIdx.x % 32;
     const int64_t job = static_cast<int64_t>(blockIdx.x) * kWarps + threadIdx.x / 32;
     const int64_t t0 = a.parts == 1 ? job : job / a.parts;
@@ -471,28 +547,56 @@ __global__ void __launch_bounds__(kThreads, kAskedCtas<T>) kv_write_kernel(const
             sn[i] = dev::f32x2(s[2 * i], s[2 * i + 1]);
         }
     }
+    // (with norms q's and k's weights are in what is kept of the angles: these wait for k)
+    __shared__ unsigned long long angles[NORM ? 8 : 1][kThreads];
+    if constexpr (NORM) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            angles[i][threadIdx.x] = cs[i];
+            angles[4 + i][threadIdx.x] = sn[i];
+        }
+    }
     if (!there) return;
+    // what a kind's last batch asks for ahead: the next kind's first one
+    const bool stores = slot >= 0 && slot < a.num_slots;
+    auto load_v = [&](Batch<T, kBatch> &b) {
+        if (stores && v0 < v1) b.template load<G>(v, v_step, v0, v1, a.num_kv_heads, mine, 16 * u, 16 * u + 8);
+    };
+    auto load_k = [&](Batch<T, kBatch> &b) {
+        if (stores && k0 < k1)
+            b.template load<G>(k, k_step, k0, k1, a.num_kv_heads, mine, e0, e1);
+        else
+            load_v(b);
+    };
+    auto nothing = [](Batch<T, kBatch> &) {};
     if (first < q_steps)
-        write_heads<T, T, D, G, true, NORM, kBatch>(
+        write_heads<T, T, D, G, true, NORM, kBatch, kAhead>(
             batch, q, q_step, static_cast<T *>(a.q_out) + (t * a.num_q_heads + mine) * D, G * D, first,
             min(last, q_steps), a.num_q_heads, mine, e0, e1, INTERLEAVED, rotates, cs, sn, nullptr,
-            static_cast<const T *>(a.norm.q), a.norm.q_stride, a, 0);
-    if (slot < 0 || slot >= a.num_slots || last <= q_steps) return;
+            static_cast<const T *>(a.norm.q), a.norm.q_stride, a, 0, load_k);
+    if (!stores || last <= q_steps) return;
     const int at = static_cast<int>(slot % kPageSize);
     const int64_t row = (slot / kPageSize * a.num_kv_heads + mine) * kHeadStep<KV, D> + at * kTokenStep<KV, D>;
     const int to_scales = fp4_value_bytes(D) - at * (D / 2 - D / kFp4Block);   // (4-bit)
     if (k0 < k1) {
-        if (first < q_steps) batch.template load<G>(k, k_step, k0, k1, a.num_kv_heads, mine, e0, e1);
-        write_heads<T, KV, D, G, true, NORM, kBatch>(
+        if (!kAhead && first < q_steps) load_k(batch);
+        if constexpr (NORM) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                cs[i] = angles[i][threadIdx.x];
+                sn[i] = angles[4 + i][threadIdx.x];
+            }
+        }
+        write_heads<T, KV, D, G, true, NORM, kBatch, kAhead>(
             batch, k, k_step, static_cast<KV *>(a.k_pages) + row, G * kHeadStep<KV, D>, k0, k1, a.num_kv_heads, mine,
             e0, e1, INTERLEAVED, rotates, cs, sn, a.k_scale, static_cast<const T *>(a.norm.k), a.norm.k_stride, a,
-            to_scales);
+            to_scales, load_v);
     }
     if (v0 < v1) {
-        batch.template load<G>(v, v_step, v0, v1, a.num_kv_heads, mine, 16 * u, 16 * u + 8);
-        write_heads<T, KV, D, G, false, false, kBatch>(
+        if (!kAhead || (first >= q_steps && k0 >= k1)) load_v(batch);
+        write_heads<T, KV, D, G, false, false, kBatch, kAhead>(
             batch, v, v_step, static_cast<KV *>(a.v_pages) + row, G * kHeadStep<KV, D>, v0, v1, a.num_kv_heads, mine,
-            16 * u, 16 * u + 8, INTERLEAVED, false, cs, sn, a.v_scale, nullptr, 0, a, to_scales);
+            16 * u, 16 * u + 8, INTERLEAVED, false, cs, sn, a.v_scale, nullptr, 0, a, to_scales, nothing);
     }
 }
 

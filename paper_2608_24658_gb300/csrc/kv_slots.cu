@@ -7,10 +7,10 @@
 //   slot     of token i of sequence r: x = held_r + i, 16 page(r, x / 16) + x % 16
 //
 // A few KB in, 8 bytes a token out: launch and one chain of dependent loads
-// (lengths, two scans, page, stores) are its time.  So it is one launch of one
-// cluster: every CTA makes both scans for itself in shared memory, and the cluster's
-// barrier stands between the last read of the lengths and the first write of an
-// output that may be their own memory.
+// (lengths, two scans, page, stores) are its time.  So it is one launch, whose CTAs
+// make both scans for themselves in shared memory and share the rows.  Where the
+// lengths or the count of taken pages advance in place, the CTAs are one cluster, and its
+// barrier stands between the last read of them and the first write.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -22,8 +22,10 @@ namespace parason {
 namespace {
 
 constexpr int kMaxSeqs = 16384;          // 12 bytes each in shared memory
-constexpr int kMaxCtas = 8;              // of the cluster: the portable size
-constexpr int kMaxThreads = 1024;
+constexpr int kClusterCtas = 8;          // the portable size
+constexpr int kMaxCtas = 128;            // without a cluster: each reads all lengths
+constexpr int kMaxThreads = 1024, kFewThreads = 256;
+constexpr int kFewSeqs = 1024;           // up to this many: kFewThreads a CTA
 constexpr int kTokensPerThread = 4;      // neighbours, stored in 16 bytes
 constexpr int32_t kMaxPage = INT32_MAX / kPageSize;
 
@@ -33,6 +35,7 @@ struct SlotArgs {
     int64_t table_stride;
     int32_t num_seqs, table_pages, num_free, num_rows;
     bool aligned;                        // slots and positions to 16 bytes
+    bool in_place;                       // held_out or used_out are inputs too
 };
 
 // Inclusive sums over the CTA's threads of a and b; `part` holds two values a warp.
@@ -58,8 +61,9 @@ __device__ __forceinline__ void scan_pair(int64_t &a, int64_t &b, int64_t (&part
 
 __device__ __forceinline__ int pages_of(int64_t tokens) { return static_cast<int>((tokens + kPageSize - 1) / kPageSize); }
 
-// Every CTA scans all sequences; the cluster's threads then share the rows, a thread
-// kTokensPerThread neighbours a step, and CTA 0 writes what there is per sequence.
+// Every CTA scans all sequences; the grid's threads then share the rows, a thread
+// kTokensPerThread neighbours a step (mostly of one page: it is looked up when it changes),
+// and CTA 0 writes what there is per sequence.
 __global__ void __launch_bounds__(kMaxThreads) kv_slots_kernel(const SlotArgs a) {
     extern __shared__ int32_t mem[];
     __shared__ int64_t part[2][32];
@@ -111,7 +115,10 @@ __global__ void __launch_bounds__(kMaxThreads) kv_slots_kernel(const SlotArgs a)
             page0[R] = static_cast<int32_t>(min(p, static_cast<int64_t>(INT32_MAX)));
         }
     }
-    cooperative_groups::this_cluster().sync();        // lengths are read, scans written
+    if (a.in_place)
+        cooperative_groups::this_cluster().sync();    // lengths are read, scans written
+    else
+        __syncthreads();
 
     const int left = max(0, a.num_free - used);       // of the list
     const int ctas = gridDim.x, cta = blockIdx.x;
@@ -144,6 +151,8 @@ __global__ void __launch_bounds__(kMaxThreads) kv_slots_kernel(const SlotArgs a)
             r = lo;
         }
         int32_t slot[kTokensPerThread], pos[kTokensPerThread];
+        int64_t known = -1;                           // (sequence, page) that `page` is of
+        int page = -1;
 #pragma unroll
         for (int i = 0; i < kTokensPerThread; ++i) {
             const int64_t q = q0 + i;
@@ -151,16 +160,20 @@ __global__ void __launch_bounds__(kMaxThreads) kv_slots_kernel(const SlotArgs a)
             pos[i] = 0;
             if (q >= total) continue;
             while (row0[r + 1] <= q) ++r;             // (row0[R] = total > q)
-            const int x = held[r] + static_cast<int>(q - row0[r]), j = x / kPageSize, fresh = j - pages_of(held[r]);
-            pos[i] = x + (a.first ? a.first[r] : 0);
-            int page = -1;
-            if (a.free_pages && fresh >= 0) {
-                if (j < a.table_pages && page0[r] + static_cast<int64_t>(fresh) < left) {
-                    page = a.free_pages[used + page0[r] + fresh];
+            const int h = held[r], x = h + static_cast<int>(q - row0[r]), j = x / kPageSize;
+            pos[i] = x + (a.first ? __ldg(a.first + r) : 0);
+            const int64_t id = static_cast<int64_t>(r) << 32 | j;
+            if (id != known) {
+                known = id;
+                page = -1;
+                const int fresh = j - pages_of(h);
+                if (j >= a.table_pages) {
+                } else if (!a.free_pages || fresh < 0) {
+                    page = a.table[r * a.table_stride + j];
+                } else if (page0[r] + static_cast<int64_t>(fresh) < left) {
+                    page = __ldg(a.free_pages + (used + page0[r] + fresh));
                     if (x % kPageSize == 0) a.table[r * a.table_stride + j] = page;
                 }
-            } else if (j < a.table_pages) {
-                page = a.table[r * a.table_stride + j];
             }
             if (page >= 0 && page <= kMaxPage) slot[i] = page * kPageSize + x % kPageSize;
         }
@@ -188,7 +201,7 @@ using namespace parason;
 extern "C" parason_status parason_kv_slots(const parason_slot_map *m, parason_stream_t stream) {
     if (!m || m->num_seqs < 0 || m->num_rows < 0 || m->table_pages < 0 || m->num_free < 0) return PARASON_EINVAL;
     if (m->num_seqs > kMaxSeqs) return PARASON_EUNSUPPORTED;
-    if (m->num_rows > INT32_MAX - kMaxCtas * kMaxThreads * kTokensPerThread) return PARASON_EUNSUPPORTED;
+    if (m->num_rows == INT32_MAX) return PARASON_EUNSUPPORTED;
     for (const void *p : {static_cast<const void *>(m->held), static_cast<const void *>(m->added),
                           static_cast<const void *>(m->first), static_cast<const void *>(m->page_table),
                           static_cast<const void *>(m->free_pages), static_cast<const void *>(m->free_used),
@@ -219,10 +232,17 @@ extern "C" parason_status parason_kv_slots(const parason_slot_map *m, parason_st
     a.num_free = m->num_free;
     a.num_rows = m->num_rows;
     a.aligned = (reinterpret_cast<uintptr_t>(m->slots) | reinterpret_cast<uintptr_t>(m->positions)) % 16 == 0;
-    const int work = std::max(a.num_seqs, (a.num_rows + kTokensPerThread - 1) / kTokensPerThread);
-    const int threads = std::min(kMaxThreads, std::max(32, (work + 31) / 32 * 32));
-    int ctas = 1;
-    while (ctas < kMaxCtas && static_cast<int64_t>(ctas) * threads * kTokensPerThread < a.num_rows) ctas *= 2;
+    a.in_place = (m->held_out && m->held_out == m->held) || (m->used_out && m->used_out == m->free_used);
+    const int64_t groups = (static_cast<int64_t>(a.num_rows) + kTokensPerThread - 1) / kTokensPerThread;
+    const int most = a.in_place || a.num_seqs > kFewSeqs ? kMaxThreads : kFewThreads;
+    const int threads =
+        static_cast<int>(std::min<int64_t>(most, std::max<int64_t>(32, (std::max<int64_t>(a.num_seqs, groups) + 31) / 32 * 32)));
+    const int64_t ctas64 = std::max<int64_t>(1, (groups + threads - 1) / threads);
+    int ctas = static_cast<int>(std::min<int64_t>(ctas64, kMaxCtas));
+    if (a.in_place) {
+        ctas = 1;
+        while (ctas < kClusterCtas && ctas < ctas64) ctas *= 2;
+    }
     const size_t smem = (3 * static_cast<size_t>(a.num_seqs) + 2) * sizeof(int32_t);
     if (smem > 47 * 1024 &&
         cudaFuncSetAttribute(kv_slots_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
@@ -237,7 +257,7 @@ extern "C" parason_status parason_kv_slots(const parason_slot_map *m, parason_st
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = static_cast<unsigned>(ctas);
+    attr[1].val.clusterDim.x = a.in_place ? static_cast<unsigned>(ctas) : 1;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
