@@ -180,8 +180,8 @@ constexpr int kWarps = kThreads / 32;
 // CTAs of kv_write to ask an SM's registers for: bf16 and e4m3 rows fit 5 without
 // spills (e4m3 took 105 registers unasked, and 300 tokens of 64 / 8 heads 4.5 us for
 // 3.5); fp32 rows do not everywhere, and are left to themselves (96 to 104).
-template <class T, bool NORM>
-constexpr int kAskedCtas = sizeof(T) == 2 ? (NORM ? 4 : 5) : 0;
+template <class T, class KV, bool NORM>
+constexpr int kAskedCtas = sizeof(T) == 2 ? (NORM || kIsFp4<KV> ? 4 : 5) : 0;
 
 // cos and sin of positions[axis] * inv_freq[i].  The frequency is held as turns a
 // position modulo 1, in 2^-64: the low 64 bits of its product with the position are
@@ -264,44 +264,55 @@ __device__ __forceinline__ float most8(const float (&x)[8]) {
     return m;
 }
 
+// Eight elements times y as e2m1 codes.
+__device__ __forceinline__ uint32_t e2m1_codes(const float (&x)[8], float y) {
+    const unsigned long long y2 = dev::f32x2(y, y);
+    float z[8];
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) dev::f32x2_split(dev::mul_f32x2(dev::f32x2(x[i], x[i + 1]), y2), z[i], z[i + 1]);
+    uint32_t w;
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
+        "mov.b32 %0, {b0, b1, b2, b3};\n\t}"
+        : "=r"(w)
+        : "f"(z[0]), "f"(z[1]), "f"(z[2]), "f"(z[3]), "f"(z[4]), "f"(z[5]), "f"(z[6]), "f"(z[7]));
+    return w;
+}
+
 // Two 8-element chunks into a 4-bit page: block scale s = e4m3(max |x| / (6 g)), codes
 // e2m1(x / (s g)), each quotient the product with a rounded reciprocal, so that one
-// division a block does (g, and s g, are between 2^-109 and 2^109).  A block of zeros, or too small
-// for a scale, has s = 0 and codes of 0; a NaN makes s NaN.  `row`: the token's values;
-// scales are `to_scales` bytes further.
+// division a block does (g, and s g, are between 2^-109 and 2^109).  A block of zeros, or
+// too small for a scale, has s = 0 and codes of 0; a NaN makes s NaN.  `row`: the token's
+// values; scales are `to_scales` bytes further.  pairs: the lane's chunks are of two
+// blocks, whose other halves other lanes have (38803 tokens of 8 heads without that: 42.5
+// -> XXX us).
 __device__ __forceinline__ void store_fp4(Fp4 *row, int to_scales, const float (&x0)[8], const float (&x1)[8], int e0,
                                           int e1, bool pairs, const BlockMates &mates, uint32_t group, float g) {
-    float m0 = most8(x0), m1 = most8(x1);
-    if (pairs) {                         // (of q and k: whose blocks may span lanes)
-        const float a0 = __shfl_sync(group, m0, mates.lane0), a1 = __shfl_sync(group, m1, mates.lane0);
-        const float b0 = __shfl_sync(group, m0, mates.lane1), b1 = __shfl_sync(group, m1, mates.lane1);
-        m0 = dev::max3_nan(m0, mates.second0 ? a1 : a0, 0.f);
-        m1 = dev::max3_nan(m1, mates.second1 ? b1 : b0, 0.f);
-    } else {
-        m0 = m1 = dev::max3_nan(m0, m1, 0.f);
-    }
     const float r = __frcp_rn(6.f * g);
+    float m0 = most8(x0), m1 = most8(x1);
+    uint8_t *out = &row->byte;
+    if (!pairs) {
+        const uint32_t byte = __nv_cvt_float_to_fp8(dev::max3_nan(m0, m1, 0.f) * r, __NV_SATFINITE, __NV_E4M3);
+        const uint32_t h2 = e4m3x2_to_f16x2(byte);
+        const float step = __low2float(*reinterpret_cast<const __half2 *>(&h2)) * g;
+        const float y = step > 0.f ? __frcp_rn(step) : 0.f;
+        *reinterpret_cast<uint2 *>(out + e0 / 2) = make_uint2(e2m1_codes(x0, y), e2m1_codes(x1, y));
+        out[to_scales + e0 / 16] = static_cast<uint8_t>(byte);
+        return;
+    }
+    const float a0 = __shfl_sync(group, m0, mates.lane0), a1 = __shfl_sync(group, m1, mates.lane0);
+    const float b0 = __shfl_sync(group, m0, mates.lane1), b1 = __shfl_sync(group, m1, mates.lane1);
+    m0 = dev::max3_nan(m0, mates.second0 ? a1 : a0, 0.f);
+    m1 = dev::max3_nan(m1, mates.second1 ? b1 : b0, 0.f);
     const uint32_t s2 = __nv_cvt_float2_to_fp8x2(make_float2(m0 * r, m1 * r), __NV_SATFINITE, __NV_E4M3);
     const uint32_t h2 = e4m3x2_to_f16x2(s2);
     const float2 s = __half22float2(*reinterpret_cast<const __half2 *>(&h2));
-    auto codes = [&](const float (&x)[8], float step) {
-        const float y = step > 0.f ? __frcp_rn(step) : 0.f;
-        uint32_t w = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t b;
-            asm("{\n\t.reg .b8 t;\n\t"
-                "cvt.rn.satfinite.e2m1x2.f32 t, %2, %1;\n\t"
-                "cvt.u32.u8 %0, t;\n\t}"
-                : "=r"(b)
-                : "f"(x[2 * i] * y), "f"(x[2 * i + 1] * y));
-            w |= b << (8 * i);
-        }
-        return w;
-    };
-    uint8_t *out = &row->byte;
-    *reinterpret_cast<uint32_t *>(out + e0 / 2) = codes(x0, s.x * g);
-    *reinterpret_cast<uint32_t *>(out + e1 / 2) = codes(x1, s.y * g);
+    const float step0 = s.x * g, step1 = s.y * g;
+    *reinterpret_cast<uint32_t *>(out + e0 / 2) = e2m1_codes(x0, step0 > 0.f ? __frcp_rn(step0) : 0.f);
+    *reinterpret_cast<uint32_t *>(out + e1 / 2) = e2m1_codes(x1, step1 > 0.f ? __frcp_rn(step1) : 0.f);
     if (e0 % 16 == 0) out[to_scales + e0 / 16] = static_cast<uint8_t>(s2);
     if (e1 % 16 == 0) out[to_scales + e1 / 16] = static_cast<uint8_t>(s2 >> 8);
 }
@@ -461,7 +472,8 @@ __device__ __forceinline__ void write_heads(Batch<T, kBatch> &batch, const T *sr
                 }
             }
             if constexpr (kIsFp4<Out>) {
-                store_fp4(dst + b * dst_step, to_scales, x0, x1, e0, e1, ROTATE && !interleaved, mates, group, scale[h]);
+                store_fp4(dst + b * dst_step, to_scales, x0, x1, e0, e1,
+                          ROTATE && !interleaved && a.rot.half > 0, mates, group, scale[h]);
             } else {
                 if constexpr (sizeof(Out) == 1) {
                     const float div = scale[h];
@@ -491,10 +503,10 @@ __device__ __forceinline__ void write_heads(Batch<T, kBatch> &batch, const T *sr
 // pairs' angles, make 8 / G each and pass them round (out of shared memory they were
 // read four lanes to a bank).
 template <class T, class KV, int D, bool INTERLEAVED, int G, bool NORM>
-__global__ void __launch_bounds__(kThreads, kAskedCtas<T, NORM>) kv_write_kernel(const WriteArgs a) {
+__global__ void __launch_bounds__(kThreads, kAskedCtas<T, KV, NORM>) kv_write_kernel(const WriteArgs a) {
     constexpr int kLanes = D / 16, kTeams = 32 / kLanes / G, kMake = 8 / G;
     constexpr int kBatch = sizeof(T) == 4 ? 2 : 3;            // (steps in flight, as above)
-    constexpr bool kAhead = NORM;                             // the next batch is asked for before this one is used
+    constexpr bool kAhead = NORM || kIsFp4<KV>;                             // the next batch is asked for before this one is used
     const int lane = threadIdx.x % 32;
     const int64_t job = static_cast<int64_t>(blockIdx.x) * kWarps + threadIdx.x / 32;
     const int64_t t0 = a.parts == 1 ? job : job / a.parts;
