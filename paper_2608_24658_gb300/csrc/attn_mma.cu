@@ -1459,7 +1459,18 @@ constexpr int kTcCvStages = 4;
 constexpr int kTcWantBlocks = 8;
 constexpr int kTcCvOffset = kTcF8Stages * kTcF8StageBytes;    // 64 KB
 constexpr int kTcF4OpBytes = kTcBlockPages * fp4_page_bytes(128);   // 4-bit: K (or V) of a block, as stored
-static_assert(2 * kTcF4OpBytes <= kTcF8StageBytes, "a 4-bit block fits a raw stage");
+// 4-bit KV.  With two S/P buffers the tile's chain was its period: S seen by the softmax
+// 470 cycles after its issue, softmax 790, P seen by the issuer 250, PV complete 330 + 760,
+// S issued 280, 2850 in all, 1430 a block, the softmax and the converters (760 a block) idle
+// for half of it.  So four S/P buffers take the columns of a second O (the next item's first
+// PV waits until the epilogue has stored this one's), and the smaller raw stages leave room for
+// a fifth converted block: XXX.
+constexpr int kTcF4Stages = 3, kTcF4CvStages = 5, kTcF4SBufs = 4;
+constexpr uint32_t kTmemSFp4 = 128;
+constexpr int kTcF4CvOffset = kTcF4Stages * 2 * kTcF4OpBytes;       // 27 KB
+static_assert(kTcF4Stages < kTcF8Stages && kTcF4CvOffset % 1024 == 0 &&
+                  kTcF4CvOffset + kTcF4CvStages * kTcStageBytes <= kTcRingBytes,
+              "4-bit rings fit");
 static_assert(kTcF8Stages < kTcStages, "raw e4m3 stages and kBarWant use the ring's barriers");
 static_assert(kTcCvOffset + kTcCvStages * kTcStageBytes <= kTcRingBytes, "e4m3 rings fit");
 constexpr int kTcTmemCols = 512;
@@ -1501,18 +1512,18 @@ __device__ __forceinline__ void stage_item_rows(TcMeta &m, const int32_t *src, i
 enum TcBar : int {
     kBarKvFull = 0,                          // [stages] producer -> MMA (TMA bytes)
     kBarKvEmpty = kBarKvFull + kTcStages,    // [stages] MMA commit -> producer
-    kBarSFull = kBarKvEmpty + kTcStages,     // [2] MMA commit -> softmax
-    kBarPFull = kBarSFull + 2,               // [2] softmax (128 arrivals) -> MMA
-    kBarPvDone = kBarPFull + 2,              // [2] MMA commit -> softmax (before a rescale)
-    kBarQReady = kBarPvDone + 2,             // [2] epilogue (128 arrivals) -> MMA
+    kBarSFull = kBarKvEmpty + kTcStages,     // [S buffers] MMA commit -> softmax
+    kBarPFull = kBarSFull + kTcF4SBufs,      // [S buffers] softmax (128 arrivals) -> MMA
+    kBarPvDone = kBarPFull + kTcF4SBufs,     // [S buffers] MMA commit -> softmax (before a rescale)
+    kBarQReady = kBarPvDone + kTcF4SBufs,    // [2] epilogue (128 arrivals) -> MMA
     kBarOFull = kBarQReady + 2,              // [2] MMA commit -> epilogue
     kBarOEmpty = kBarOFull + 2,              // [2] epilogue (4 arrivals) -> MMA
     kBarMetaFull = kBarOEmpty + 2,           // [kTcMeta] scheduler -> every role
     kBarMetaEmpty = kBarMetaFull + kTcMeta,  // [kTcMeta] epilogue (4 arrivals) -> scheduler
     kBarDrain = kBarMetaEmpty + kTcMeta,     // both issuers' commits -> issuers, before TMEM is freed
     kBarCvFull,                              // [kTcCvStages] converters (4 arrivals) -> MMA
-    kBarCvEmpty = kBarCvFull + kTcCvStages,  // [kTcCvStages] MMA commit -> converters
-    kTcBars = kBarCvEmpty + kTcCvStages,
+    kBarCvEmpty = kBarCvFull + kTcF4CvStages,  // [kTcCvStages] MMA commit -> converters
+    kTcBars = kBarCvEmpty + kTcF4CvStages,
     // producer -> scheduler: pull the next item (e4m3 tiles, which use
     // kTcF8Stages of the kTcStages staging barriers)
     kBarWant = kBarKvFull + kTcF8Stages
@@ -1521,13 +1532,13 @@ enum TcBar : int {
 // arrivals each barrier waits for; with e4m3 KV the 4 converter warps free
 // the staging stages
 __host__ __device__ constexpr int tc_bar_count(int i, bool f8) {
-    return (i == kBarPFull || i == kBarPFull + 1 || i == kBarQReady || i == kBarQReady + 1)
+    return ((i >= kBarPFull && i < kBarPFull + kTcF4SBufs) || i == kBarQReady || i == kBarQReady + 1)
                ? kTcRows
                : ((i == kBarOEmpty || i == kBarOEmpty + 1 ||
                    (i >= kBarMetaEmpty && i < kBarMetaEmpty + kTcMeta) ||
                    (f8 && i >= kBarKvEmpty && i < kBarKvEmpty + kTcStages))
                       ? 4
-                      : ((i >= kBarCvFull && i < kBarCvFull + kTcCvStages)
+                      : ((i >= kBarCvFull && i < kBarCvFull + kTcF4CvStages)
                              ? kTcRows
                              : (i == kBarDrain ? 2 : 1)));
 }
@@ -1579,57 +1590,55 @@ __device__ __forceinline__ void convert_block_e4m3(uint32_t src, uint32_t dst, i
 }
 
 // The same of a 4-bit block, 4 of its 512 16-byte chunks (32 elements, two scales) a
-// thread: pages as they are stored, K of 4 pages, then V.  A chunk fills four
-// 16-byte slots of a row; the quarter warp's two rows of four chunks take eight
-// bank groups when chunks 2 and 3, whose column block is the other one, take their
-// slots in another order.
-__device__ __forceinline__ void convert_block_e2m1(uint32_t src, uint32_t dst, int valid, int t) {
-    constexpr int kPage = fp4_page_bytes(128), kValues = fp4_value_bytes(128);
-    uint4 w[4];
-    uint32_t sc[4];
+// thread: pages as they are stored, K of 4 pages, then V.  A chunk fills four 16-byte
+// slots of a row; the quarter warp's two rows of four chunks take eight bank groups
+// when chunks 2 and 3, whose column block is the other one, are taken with their halves
+// in turn (`turned`; read so, as selects here took a third of the time).  Read and
+// written apart, so that the next block's reads go out before this one's writes are
+// waited for.
+struct Fp4Chunks {
+    uint2 w[4][2];                       // halves of 16 elements, in the order they are written
+    uint32_t scale[4];
+    __device__ __forceinline__ void read(uint32_t src, int t) {
+        constexpr int kPage = fp4_page_bytes(128), kValues = fp4_value_bytes(128);
+        const uint32_t turned = (t & 2) ? 8 : 0;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int idx = t + kTcRows * q;
-        const int op = idx >> 8;                 // 0: K, 1: V
-        const int r = (idx >> 2) & 63;           // token
-        const int c = idx & 3;                   // elements 32c .. 32c + 31
-        const uint32_t page = src + (op * kTcBlockPages + (r >> 4)) * kPage;
-        w[q] = lds128(page + (r & 15) * 64 + 16 * c);
-        sc[q] = lds16(page + kValues + (r & 15) * 8 + 2 * c);
-    }
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int idx = t + kTcRows * q;
-        const int op = idx >> 8, r = (idx >> 2) & 63, c = idx & 3;
-        if (r >= valid) w[q] = make_uint4(0u, 0u, 0u, 0u), sc[q] = 0u;
-        const bool turned = (c & 2) != 0;
-        const uint32_t both = e4m3x2_to_f16x2(sc[q]);
-        const uint32_t s0 = __byte_perm(both, 0u, turned ? 0x3232 : 0x1010);
-        const uint32_t s1 = __byte_perm(both, 0u, turned ? 0x1010 : 0x3232);
-        const uint32_t v[4] = {turned ? w[q].z : w[q].x, turned ? w[q].w : w[q].y, turned ? w[q].x : w[q].z,
-                               turned ? w[q].y : w[q].w};
-        const uint32_t row = dst + op * kTcKBytes + (c >> 1) * kTcColBlockBytes + r * 128;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint32_t p[4];
-            e2m1x8_to_f16(v[j], p);
-            const uint32_t s = j < 2 ? s0 : s1;
-            const int slot = 4 * (c & 1) + (turned ? j ^ 2 : j);
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + ((slot ^ (r & 7)) << 4)),
-                         "r"(mul_f16x2(p[0], s)), "r"(mul_f16x2(p[1], s)), "r"(mul_f16x2(p[2], s)),
-                         "r"(mul_f16x2(p[3], s))
-                         : "memory");
+        for (int q = 0; q < 4; ++q) {
+            // chunk t % 4 of row t / 4 + 32 (q % 2) of K, then of V
+            const int r = t >> 2, c = t & 3;
+            const uint32_t page = src + ((q >> 1) * kTcBlockPages + (r >> 4) + 2 * (q & 1)) * kPage;
+            const uint32_t at = page + (r & 15) * 64 + 16 * c;
+            w[q][0] = lds64(at + turned);
+            w[q][1] = lds64(at + (turned ^ 8));
+            scale[q] = lds16(page + kValues + (r & 15) * 8 + 2 * c);
         }
     }
-}
-
-template <class KV>
-__device__ __forceinline__ void convert_block(uint32_t src, uint32_t dst, int valid, int t) {
-    if constexpr (kFp4<KV>)
-        convert_block_e2m1(src, dst, valid, t);
-    else
-        convert_block_e4m3(src, dst, valid, t);
-}
+    // (MASKED: rows from `valid` on become zeros)
+    template <bool MASKED>
+    __device__ __forceinline__ void write(uint32_t dst, int valid, int t) const {
+        const int r = t >> 2, c = t & 3, turned = (t & 2) ? 2 : 0;
+        const uint32_t first = turned ? 0x3232 : 0x1010, second = turned ? 0x1010 : 0x3232;
+        const uint32_t row = dst + (c >> 1) * kTcColBlockBytes + r * 128;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const bool there = !MASKED || r + 32 * (q & 1) < valid;
+            const uint32_t both = e4m3x2_to_f16x2(there ? scale[q] : 0u);
+            const uint32_t s[2] = {__byte_perm(both, 0u, first), __byte_perm(both, 0u, second)};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t p[4];
+                const uint32_t word = (j & 1) ? w[q][j >> 1].y : w[q][j >> 1].x;
+                e2m1x8_to_f16(there ? word : 0u, p);
+                const int slot = 4 * (c & 1) + (j ^ turned);
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(
+                                 row + (q >> 1) * kTcKBytes + (q & 1) * 32 * 128 + ((slot ^ (r & 7)) << 4)),
+                             "r"(mul_f16x2(p[0], s[j >> 1])), "r"(mul_f16x2(p[1], s[j >> 1])),
+                             "r"(mul_f16x2(p[2], s[j >> 1])), "r"(mul_f16x2(p[3], s[j >> 1]))
+                             : "memory");
+            }
+        }
+    }
+};
 
 __device__ __forceinline__ int tc_blocks(int num_pages) {
     return (num_pages + kTcBlockPages - 1) / kTcBlockPages;
@@ -1645,6 +1654,12 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
     constexpr int kKBytes = kCols * kTcColBlockBytes;
     constexpr int kStageBytes = 2 * kKBytes;
     static_assert(kTcStages * kStageBytes <= Shape<D, KV>::kBodyBytes, "ring fits the CTA's memory");
+    constexpr int kRawStages = kFp4<KV> ? kTcF4Stages : kTcF8Stages;
+    constexpr int kRawStageBytes = kFp4<KV> ? 2 * kTcF4OpBytes : kTcF8StageBytes;
+    constexpr int kCvStages = kFp4<KV> ? kTcF4CvStages : kTcCvStages;
+    constexpr int kCvOffset = kFp4<KV> ? kTcF4CvOffset : kTcCvOffset;
+    constexpr int kSBufs = kFp4<KV> ? kTcF4SBufs : 2, kOBufs = kFp4<KV> ? 1 : 2;
+    constexpr uint32_t kS = kFp4<KV> ? kTmemSFp4 : kTmemS;
     const uint32_t ring = dev::smem_addr(smem);
     auto bar = [&](int i) { return bars + 8u * static_cast<uint32_t>(i); };
     const long long limit = a.wait_limit_ns;
@@ -1700,7 +1715,7 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
         // e4m3 blocks keep the default L2 policy (the per-page boxes use no hint)
         const uint64_t f8_pol = dev::l2_evict_normal_policy();
         const int kv_page_rows = a.num_kv_heads * kPageSize;   // TMA rows between consecutive pages
-        constexpr int NS = kF8 ? kTcF8Stages : kTcStages;
+        constexpr int NS = kF8 ? kRawStages : kTcStages;
         int last_issue[NS];
         for (int s = 0; s < NS; ++s) last_issue[s] = -1;
         int blk = 0;
@@ -1741,7 +1756,7 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
                         __syncwarp();
                         if (j < pages) {
                             const int64_t at = static_cast<int64_t>(m.rows[bi * kTcBlockPages + j] / kPageSize) * kBytes;
-                            dev::bulk_load_hint(ring + s * kTcF8StageBytes + (lane & 1) * kTcF4OpBytes + j * kBytes,
+                            dev::bulk_load_hint(ring + s * kRawStageBytes + (lane & 1) * kTcF4OpBytes + j * kBytes,
                                                 ((lane & 1) ? a.v_raw : a.k_raw) + at, kBytes, fb, f8_pol);
                         }
                         last_issue[s] = blk;
@@ -1818,7 +1833,7 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
                                           : tc::idesc_bf16_f32(kTcRows, kTcBlockTokens, false);
             constexpr uint32_t kIdPV = kF8 ? tc::idesc_f16_f32(kTcRows, D, true)
                                            : tc::idesc_bf16_f32(kTcRows, D, true);
-            constexpr int kMmaStages = kF8 ? kTcCvStages : kTcStages;
+            constexpr int kMmaStages = kF8 ? kCvStages : kTcStages;
             // A wait that runs out leaves its mark, and the warp goes on together
             // to the next point where it looks (lanes that part would leave the
             // others waiting in elect.sync; what is issued in between works on
@@ -1833,7 +1848,7 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
             auto failed = [&]() { return __any_sync(0xffffffffu, bad) != 0; };
             // descriptors of stage 0; a stage, a column block or a K step moves
             // the start address field (address / 16) by a constant
-            const uint32_t mma_ring = kF8 ? ring + kTcCvOffset : ring;
+            const uint32_t mma_ring = kF8 ? ring + kCvOffset : ring;
             const uint64_t desc_k = tc::smem_desc_sw128(mma_ring, 16, 1024);
             const uint64_t desc_v = tc::smem_desc_sw128(mma_ring + kKBytes, kTcColBlockBytes, 1024);
             constexpr uint32_t kStageStep = kStageBytes >> 4;
@@ -1851,9 +1866,9 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
                     for (int i = 0; i < nb; ++i, ++b) {
                         if (failed()) break;
                         wait((kF8 ? kBarCvFull : kBarKvFull) + st, ph);
-                        if (b >= 2) wait(kBarPvDone + (b & 1), (b - 2) >> 1);
+                        if (b >= kSBufs) wait(kBarPvDone + b % kSBufs, b / kSBufs - 1);
                         tc::fence_after_sync();
-                        const uint32_t tS = tmem + kTmemS + 64u * (b & 1);
+                        const uint32_t tS = tmem + kS + 64u * (b % kSBufs);
                         const uint64_t kd = desc_k + static_cast<uint64_t>(st * kStageStep);
                         if (tc::elect_one()) {
 #pragma unroll
@@ -1862,7 +1877,7 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
                                 const uint32_t off = ((ks >> 2) * kCb + (ks & 3) * 32) >> 4;
                                 tc::mma_bf16_tmem_a(tS, tQ + 8u * ks, kd + off, kIdS, ks > 0);
                             }
-                            tc::commit(bar(kBarSFull + (b & 1)));
+                            tc::commit(bar(kBarSFull + b % kSBufs));
                         }
                         if (++st == kMmaStages) {
                             st = 0;
@@ -1871,14 +1886,14 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
                     }
                 } else {
                     // PV of the item's blocks into O (buffer k & 1)
-                    const uint32_t tO = tmem + kTmemO + 128u * (k & 1);
+                    const uint32_t tO = tmem + kTmemO + 128u * (k % kOBufs);
                     for (int i = 0; i < nb; ++i, ++b) {
                         if (failed()) break;
-                        wait(kBarPFull + (b & 1), b >> 1);
-                        // the O buffer was last used by item k - 2: its epilogue must be done
-                        if (i == 0 && k >= 2) wait(kBarOEmpty + (k & 1), (k >> 1) - 1);
+                        wait(kBarPFull + b % kSBufs, b / kSBufs);
+                        // the O buffer was last used by item k - kOBufs: its epilogue must be done
+                        if (i == 0 && k >= kOBufs) wait(kBarOEmpty + k % kOBufs, k / kOBufs - 1);
                         tc::fence_after_sync();
-                        const uint32_t tP = tmem + kTmemS + 64u * (b & 1);
+                        const uint32_t tP = tmem + kS + 64u * (b % kSBufs);
                         const uint64_t vd = desc_v + static_cast<uint64_t>(st * kStageStep);
                         if (tc::elect_one()) {
 #pragma unroll
@@ -1889,8 +1904,8 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
                             // S(b) completed before P(b) was written: both
                             // products of the stage are done when these arrive
                             tc::commit(bar((kF8 ? kBarCvEmpty : kBarKvEmpty) + st));
-                            tc::commit(bar(kBarPvDone + (b & 1)));
-                            if (i == nb - 1) tc::commit(bar(kBarOFull + (k & 1)));
+                            tc::commit(bar(kBarPvDone + b % kSBufs));
+                            if (i == nb - 1) tc::commit(bar(kBarOFull + k % kOBufs));
                         }
                         if (++st == kMmaStages) st = 0;
                     }
@@ -1916,7 +1931,7 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
             const WorkItem it = meta[ms].it;
             const int nb = tc_blocks(it.num_pages);
             const int tokens = (it.num_pages - 1) * kPageSize + it.last_valid;
-            const uint32_t tO = lane_base + kTmemO + 128u * (k & 1);
+            const uint32_t tO = lane_base + kTmemO + 128u * (k % kOBufs);
             // e4m3 K: the kv head's scale goes into the logits
             const float sl = item_scales<KV>(a, it).x;
             const CapFactors cap(sl, a.cap_log2);      // (used under a cap)
@@ -1925,8 +1940,8 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
             for (int i = 0; i < nb; ++i) {
                 const int b = blk + i;
                 const int valid = tokens - i * kTcBlockTokens;   // of the block's keys (64 or more: all)
-                const uint32_t tS = lane_base + kTmemS + 64u * (b & 1);
-                if (!tc_warp_wait(bar(kBarSFull + (b & 1)), (b >> 1) & 1, limit, abort_flag, lane)) {
+                const uint32_t tS = lane_base + kS + 64u * (b % kSBufs);
+                if (!tc_warp_wait(bar(kBarSFull + b % kSBufs), (b / kSBufs) & 1, limit, abort_flag, lane)) {
                     ok = false;
                     break;
                 }
@@ -1937,7 +1952,7 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
                         m_use = mb;
                     } else if (__any_sync(0xffffffffu, mb > m_use + kTcRescaleLog2)) {
                         // O must hold PV(b - 1) before it is rescaled
-                        if (!tc_warp_wait(bar(kBarPvDone + ((b - 1) & 1)), ((b - 1) >> 1) & 1, limit,
+                        if (!tc_warp_wait(bar(kBarPvDone + (b - 1) % kSBufs), ((b - 1) / kSBufs) & 1, limit,
                                           abort_flag, lane)) {
                             return false;
                         }
@@ -2057,7 +2072,7 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
                     tc::fence_proxy_async_smem();
                 }
                 tc::fence_before_sync();
-                dev::mbar_arrive(bar(kBarPFull + (b & 1)));
+                dev::mbar_arrive(bar(kBarPFull + b % kSBufs));
             }
             if (!ok) {
                 if (lane == 0) tc_fail(a, abort_flag, kSiteConsumerFull);
@@ -2126,7 +2141,7 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
         // item j's O rows to its partials, times the kv head's V scale
         auto store_o = [&](int j, const WorkItem &it) {
             const float vs = a.v_scale[it.kv_head];
-            const uint32_t tO = lane_base + kTmemO + 128u * (j & 1);
+            const uint32_t tO = lane_base + kTmemO + 128u * (j % kOBufs);
             float *dst = a.part_o + (static_cast<int64_t>(it.slot_base) + r) * D;
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
@@ -2144,14 +2159,14 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
             // wait for the O is short (long-prefix step with e4m3 KV: 668 ->
             // 655 us).
             auto convert = [&](int gb, int valid) -> bool {
-                const int s = gb % kTcF8Stages, c = gb % kTcCvStages;
-                if (!tc_warp_wait(bar(kBarKvFull + s), (gb / kTcF8Stages) & 1, limit, abort_flag, lane))
+                const int s = gb % kRawStages, c = gb % kCvStages;
+                if (!tc_warp_wait(bar(kBarKvFull + s), (gb / kRawStages) & 1, limit, abort_flag, lane))
                     return false;
-                if (gb >= kTcCvStages &&
-                    !tc_warp_wait(bar(kBarCvEmpty + c), ((gb / kTcCvStages) - 1) & 1, limit, abort_flag,
+                if (gb >= kCvStages &&
+                    !tc_warp_wait(bar(kBarCvEmpty + c), ((gb / kCvStages) - 1) & 1, limit, abort_flag,
                                   lane))
                     return false;
-                convert_block<KV>(ring + s * kTcF8StageBytes, ring + kTcCvOffset + c * kStageBytes,
+                convert_block_e4m3(ring + s * kRawStageBytes, ring + kCvOffset + c * kStageBytes,
                                    valid, r);
                 tc::fence_proxy_async_smem();
                 dev::mbar_arrive(bar(kBarCvFull + c));
@@ -2162,17 +2177,42 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
             // store item j's O
             auto finish = [&](int j) -> bool {
                 const WorkItem it = meta[j % kTcMeta].it;
-                if (!tc_warp_wait(bar(kBarOFull + (j & 1)), (j >> 1) & 1, limit, abort_flag, lane))
+                if (!tc_warp_wait(bar(kBarOFull + j % kOBufs), (j / kOBufs) & 1, limit, abort_flag, lane))
                     return false;
                 tc::fence_after_sync();
                 store_o(j, it);
                 tc::fence_before_sync();
                 __syncwarp();
                 if (lane == 0) {
-                    dev::mbar_arrive(bar(kBarOEmpty + (j & 1)));
+                    dev::mbar_arrive(bar(kBarOEmpty + j % kOBufs));
                     dev::mbar_arrive(bar(kBarMetaEmpty + j % kTcMeta));
                 }
                 return true;
+            };
+            // 4-bit blocks: read block gb into registers (its stage is free then) ...
+            Fp4Chunks chunks;
+            auto read_fp4 = [&](int gb) -> bool {
+                const int s = gb % kRawStages;
+                if (!tc_wait(bar(kBarKvFull + s), (gb / kRawStages) & 1, limit, abort_flag)) return false;
+                chunks.read(ring + s * kRawStageBytes, r);
+                return true;
+            };
+            // ... and write it widened; with `more`, read the next one of the item meanwhile
+            auto write_fp4 = [&](int gb, int valid, bool more) -> bool {
+                const int c = gb % kCvStages;
+                bool fine = gb < kCvStages ||
+                            tc_wait(bar(kBarCvEmpty + c), ((gb / kCvStages) - 1) & 1, limit, abort_flag);
+                const uint32_t dst = ring + kCvOffset + c * kStageBytes;
+                if (fine && valid >= kTcBlockTokens)
+                    chunks.write<false>(dst, valid, r);
+                else if (fine)
+                    chunks.write<true>(dst, valid, r);
+                __syncwarp();
+                if (lane == 0) dev::mbar_arrive(bar(kBarKvEmpty + gb % kRawStages));
+                if (fine && more) fine = read_fp4(gb + 1);
+                tc::fence_proxy_async_smem();
+                dev::mbar_arrive(bar(kBarCvFull + c));
+                return __all_sync(0xffffffffu, fine) != 0;
             };
             bool have = has_item(0);
             for (int k = 0, gb = 0; ok && have; ++k) {
@@ -2184,7 +2224,13 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
                 const int nb = tc_blocks(it.num_pages);
                 const int tokens = (it.num_pages - 1) * kPageSize + it.last_valid;
                 for (int i = 0; i < nb && ok; ++i, ++gb) {
-                    ok = convert(gb, min(kTcBlockTokens, tokens - i * kTcBlockTokens));
+                    const int valid = min(kTcBlockTokens, tokens - i * kTcBlockTokens);
+                    if constexpr (kFp4<KV>) {
+                        if (i == 0) ok = __all_sync(0xffffffffu, read_fp4(gb)) != 0;
+                        if (ok) ok = write_fp4(gb, valid, i + 1 < nb);
+                    } else {
+                        ok = convert(gb, valid);
+                    }
                     if (ok && k > 0 && i == min(1, nb - 1)) ok = finish(k - 1);
                 }
                 if (!ok) break;

@@ -175,6 +175,10 @@ constexpr double kTcPageCost = 2.0;          // one page of a tcgen05 prefix til
 // of a 2k prefix over 16 branches 76.7, 76.7, 80.6; 2.6 and the start 184 and
 // 77.1; a 32k prefix over 128 branches of 4k to 16k 521, 521, 506)
 constexpr double kTcPageCostE4m3 = 2.6;
+// The same with 4-bit KV (44 trees, 2.2, 2.9, 3.2, 3.6 against 2.6: the geometric mean of
+// their steps 1.6% longer, level, level, 1.1% shorter).  The other constants of e4m3 KV hold
+// for it: at their neighbours that mean is level or longer, by 12% at most.
+constexpr double kTcPageCostFp4 = 3.6;
 // (a third of a short tile: with all 24 pages, tiles of 5 to 30 pages got more
 // CTAs than they fill and were cut for them, 16.7 -> 23.4 us and 21.3 -> 28.0)
 constexpr int64_t kTcStartPagesE4m3 = 24;
@@ -189,8 +193,9 @@ size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 // Time of one page of a prefix-pass tile (one 128-row MMA per 64 tokens,
 // whatever the rows) relative to one page of the suffix pass on the same SM,
 // measured.
-double wide_page_cost(int32_t head_dim, bool e4m3) {
-    return e4m3 ? kTcPageCostE4m3 : head_dim == 64 ? kTcPageCostD64 : kTcPageCost;
+double wide_page_cost(int32_t head_dim, int32_t mode) {
+    if (mode == PARASON_FP4_KV) return kTcPageCostFp4;
+    return mode == PARASON_FP8_E4M3_KV ? kTcPageCostE4m3 : head_dim == 64 ? kTcPageCostD64 : kTcPageCost;
 }
 
 // Pieces of a run of `pages` pages under the piece length `chunk`: equal
@@ -770,7 +775,7 @@ parason_status build_host(parason_plan_s *p, const parason_attn_config *cfg, int
                 run.leaf_lo = lo[n];
                 run.wide = wide;
                 if (wide)
-                    wide_cost += wide_page_cost(cfg->head_dim, parason::scaled_kv(mode)) *
+                    wide_cost += wide_page_cost(cfg->head_dim, mode) *
                                  static_cast<double>(P + (parason::scaled_kv(mode)
                                                               ? std::min<int64_t>(kTcStartPagesE4m3, P / 3)
                                                               : 0));
@@ -892,7 +897,7 @@ parason_status build_host(parason_plan_s *p, const parason_attn_config *cfg, int
                     longest = std::max(longest, std::min(per, r.pages));
                 }
             const double piece = static_cast<double>(longest * (p->tc_pairs ? 2 : 1)) *
-                                 wide_page_cost(cfg->head_dim, parason::scaled_kv(mode));
+                                 wide_page_cost(cfg->head_dim, mode);
             if (e <= n_wide && piece * S <= kLongestPiece * (wide_cost + static_cast<double>(narrow_pages))) {
                 wide_chunk = chunk;
                 n_wide = static_cast<int32_t>(e);
