@@ -704,10 +704,11 @@ def kv_scales(k: torch.Tensor, v: torch.Tensor, rotary: Optional[Rotary] = None,
     return k_scale, v_scale
 
 
-def _ints(name, t, shape, dev):
-    if t.dtype is not torch.int32 or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous int32 tensor of shape {tuple(shape)} on cuda:{dev}")
-    return t.data_ptr()
+_I32 = torch.int32
+
+
+def _not_ints(name, shape, dev):
+    raise ValueError(f"{name} must be a contiguous int32 tensor of shape {tuple(shape)} on cuda:{dev}")
 
 
 def kv_slots(page_table: torch.Tensor, held: torch.Tensor, added: Optional[torch.Tensor] = None,
@@ -729,23 +730,49 @@ def kv_slots(page_table: torch.Tensor, held: torch.Tensor, added: Optional[torch
     ``tokens``: rows of new outputs, as many as the sequences add or more (rows past
     the last token have slot -1); with neither it nor outputs there are R.  lens_out may
     be held, and used_out free_used.  Asynchronous."""
+    # (as small steps wait for this code, it checks each tensor in place)
     dev = page_table.get_device()
-    if page_table.dtype is not torch.int32 or page_table.dim() != 2 or dev < 0 or (
+    if page_table.dtype is not _I32 or page_table.dim() != 2 or dev < 0 or (
             page_table.stride(1) != 1 and page_table.numel() > 1):
         raise ValueError("page_table must be a cuda int32 tensor [sequences, pages] with contiguous rows")
     seqs, width = page_table.shape
+    stride = page_table.stride(0) if seqs > 1 else width
+    if stride < width:
+        raise ValueError("page_table's rows must not overlap")
     of_seq = (seqs,)
-    ha = _ints("held", held, of_seq, dev)
-    ad = 0 if added is None else _ints("added", added, of_seq, dev)
-    fi = 0 if first is None else _ints("first", first, of_seq, dev)
-    fp = fu = uo = free = 0
+    if (held.dtype is not _I32 or held.shape != of_seq or held.get_device() != dev
+            or not held.is_contiguous()):
+        _not_ints("held", of_seq, dev)
+    ha = held.data_ptr()
+    ad = fi = fp = fu = uo = free = tp = lo = 0
+    if added is not None:
+        if (added.dtype is not _I32 or added.shape != of_seq or added.get_device() != dev
+                or not added.is_contiguous()):
+            _not_ints("added", of_seq, dev)
+        ad = added.data_ptr()
+    if first is not None:
+        if (first.dtype is not _I32 or first.shape != of_seq or first.get_device() != dev
+                or not first.is_contiguous()):
+            _not_ints("first", of_seq, dev)
+        fi = first.data_ptr()
     if free_pages is not None:
         free = free_pages.numel()
-        fp = _ints("free_pages", free_pages, (free,), dev)
         if free == 0:
             raise ValueError("free_pages must have an entry")
-        fu = 0 if free_used is None else _ints("free_used", free_used, (1,), dev)
-        uo = 0 if used_out is None else _ints("used_out", used_out, (1,), dev)
+        if (free_pages.dtype is not _I32 or free_pages.shape != (free,) or free_pages.get_device() != dev
+                or not free_pages.is_contiguous()):
+            _not_ints("free_pages", (free,), dev)
+        fp = free_pages.data_ptr()
+        if free_used is not None:
+            if (free_used.dtype is not _I32 or free_used.shape != (1,) or free_used.get_device() != dev
+                    or not free_used.is_contiguous()):
+                _not_ints("free_used", (1,), dev)
+            fu = free_used.data_ptr()
+        if used_out is not None:
+            if (used_out.dtype is not _I32 or used_out.shape != (1,) or used_out.get_device() != dev
+                    or not used_out.is_contiguous()):
+                _not_ints("used_out", (1,), dev)
+            uo = used_out.data_ptr()
     elif free_used is not None or used_out is not None:
         raise ValueError("free_used and used_out need free_pages")
     if slots is not None:
@@ -754,20 +781,40 @@ def kv_slots(page_table: torch.Tensor, held: torch.Tensor, added: Optional[torch
             raise ValueError(f"slots must be [{tokens}]")
     elif positions is not None and positions.dim() == 1:
         rows = positions.shape[0]
+        if tokens is not None and tokens != rows:
+            raise ValueError(f"positions must be [{tokens}]")
     else:
         if tokens is None and added is not None:
             raise ValueError("added needs tokens, the rows of the outputs")
         rows = seqs if tokens is None else int(tokens)
     if rows < 0:
         raise ValueError("the outputs must be [rows]")
-    slots = _new(stream, (rows,), torch.int32, dev) if slots is None else slots
-    positions = _new(stream, (rows,), torch.int32, dev) if positions is None else positions
-    sl, po = _ints("slots", slots, (rows,), dev), _ints("positions", positions, (rows,), dev)
-    tp = 0 if token_ptr is None else _ints("token_ptr", token_ptr, (seqs + 1,), dev)
-    lo = 0 if lens_out is None else _ints("lens_out", lens_out, of_seq, dev)
+    of_row = (rows,)
+    if slots is None:
+        slots = _new(stream, of_row, _I32, dev)
+    if positions is None:
+        positions = _new(stream, of_row, _I32, dev)
+    if (slots.dtype is not _I32 or slots.shape != of_row or slots.get_device() != dev
+            or not slots.is_contiguous()):
+        _not_ints("slots", of_row, dev)
+    sl = slots.data_ptr()
+    if (positions.dtype is not _I32 or positions.shape != of_row or positions.get_device() != dev
+            or not positions.is_contiguous()):
+        _not_ints("positions", of_row, dev)
+    po = positions.data_ptr()
+    if token_ptr is not None:
+        if (token_ptr.dtype is not _I32 or token_ptr.shape != (seqs + 1,) or token_ptr.get_device() != dev
+                or not token_ptr.is_contiguous()):
+            _not_ints("token_ptr", (seqs + 1,), dev)
+        tp = token_ptr.data_ptr()
+    if lens_out is not None:
+        if (lens_out.dtype is not _I32 or lens_out.shape != of_seq or lens_out.get_device() != dev
+                or not lens_out.is_contiguous()):
+            _not_ints("lens_out", of_seq, dev)
+        lo = lens_out.data_ptr()
     st = _lib.load().parason_kv_slots(
-        _lib.SLOT_MAP.pack(seqs, rows, ha, ad, fi, page_table.data_ptr(), page_table.stride(0) if seqs > 1 else width,
-                           width, free, fp, fu, sl, po, tp, lo, uo), _stream_on(stream, dev))
+        _lib.SLOT_MAP.pack(seqs, rows, ha, ad, fi, page_table.data_ptr(), stride, width, free, fp, fu, sl, po, tp, lo,
+                           uo), _stream_on(stream, dev))
     if st:
         check(st, "parason_kv_slots")
     return slots, positions

@@ -257,9 +257,9 @@ extern "C" parason_status parason_kv_slots(const parason_slot_map *m, parason_st
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = a.in_place ? static_cast<unsigned>(ctas) : 1;
+    attr[1].val.clusterDim.x = static_cast<unsigned>(ctas);
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 2;
+    cfg.numAttrs = a.in_place ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kv_slots_kernel, a) == cudaSuccess ? PARASON_OK : PARASON_ECUDA;
 }
