@@ -1248,6 +1248,12 @@ __device__ void suffix_warp(const KvMaps &maps, const AttnArgs &a, uint32_t ring
 // stage of the ring is two pages, with one wait, one turn of the loop and one softmax
 // update, the whole warp copies (288 chunks of 16 bytes are nine a lane), and tiles of up
 // to 8 rows all take the transposed step.
+//
+// 64 branches of 8192 tokens, 8 kv heads: 117 us of 89 us of bytes.  Bound by issue and
+// latency of three warps a scheduler: 320 instructions a page, the conversions and their
+// bit work at 35 to 40% of the ALU pipe.  Page by page through suffix_warp: 173 us.  A page a
+// step with the rest as here: 129.  16 warps of 128 registers spill (an earlier form 135 -> 235);
+// q asked for ahead: 3 to 4% longer; pages by cp.async.bulk: level.
 template <int D, class KV>
 __device__ void suffix_warp_fp4(const AttnArgs &a, uint32_t ring, uint32_t bars, int warp, int lane, WorkItem *grab) {
     using S = Shape<D, KV>;
@@ -1464,7 +1470,10 @@ constexpr int kTcF4OpBytes = kTcBlockPages * fp4_page_bytes(128);   // 4-bit: K 
 // S issued 280, 2850 in all, 1430 a block, the softmax and the converters (760 a block) idle
 // for half of it.  So four S/P buffers take the columns of a second O (the next item's first
 // PV waits until the epilogue has stored this one's), and the smaller raw stages leave room for
-// a fifth converted block: XXX.
+// a fifth converted block.  The converters' own turn is the period then, 1300 cycles: 460 to
+// write a block, the rest its waits and the latency of its reads beside the writes (four row
+// tiles over a 32k prefix 106 -> 100 us).  Pairs of tiles in the prefill kernel, which widens a
+// block once for both, beside a launch for the suffix pass: 12% longer in the mean of 40 trees.
 constexpr int kTcF4Stages = 3, kTcF4CvStages = 5, kTcF4SBufs = 4;
 constexpr uint32_t kTmemSFp4 = 128;
 constexpr int kTcF4CvOffset = kTcF4Stages * 2 * kTcF4OpBytes;       // 27 KB

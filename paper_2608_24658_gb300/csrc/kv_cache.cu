@@ -178,8 +178,9 @@ constexpr int kThreads = 128;            // 4 warps, each of them on its own
 constexpr int kWarps = kThreads / 32;
 
 // CTAs of kv_write to ask an SM's registers for: bf16 and e4m3 rows fit 5 without
-// spills (e4m3 took 105 registers unasked, and 300 tokens of 64 / 8 heads 4.5 us for
-// 3.5); fp32 rows do not everywhere, and are left to themselves (96 to 104).
+// spills, 4 with a second batch in flight (e4m3 took 105 registers unasked, and 300
+// tokens of 64 / 8 heads 4.5 us for 3.5); fp32 rows do not everywhere, and are left to
+// themselves (96 to 104).
 template <class T, class KV, bool NORM>
 constexpr int kAskedCtas = sizeof(T) == 2 ? (NORM || kIsFp4<KV> ? 4 : 5) : 0;
 
@@ -287,8 +288,8 @@ __device__ __forceinline__ uint32_t e2m1_codes(const float (&x)[8], float y) {
 // division a block does (g, and s g, are between 2^-109 and 2^109).  A block of zeros, or
 // too small for a scale, has s = 0 and codes of 0; a NaN makes s NaN.  `row`: the token's
 // values; scales are `to_scales` bytes further.  pairs: the lane's chunks are of two
-// blocks, whose other halves other lanes have (38803 tokens of 8 heads without that: 42.5
-// -> XXX us).
+// blocks, whose other halves other lanes have (38803 tokens of 8 heads, unrotated, 42.5 us
+// with that, 37.5 without; 30.6 with the next batch asked for ahead, of 30.0 us of bytes).
 __device__ __forceinline__ void store_fp4(Fp4 *row, int to_scales, const float (&x0)[8], const float (&x1)[8], int e0,
                                           int e1, bool pairs, const BlockMates &mates, uint32_t group, float g) {
     const float r = __frcp_rn(6.f * g);
@@ -353,7 +354,9 @@ __device__ __forceinline__ float &pair_of(float (&x0)[8], float (&x1)[8], bool i
     return (i < 2 ? x0 : x1)[4 * (i & 1) + 2 * j + (q ? 1 : 0)];
 }
 
-// The norm's weights times cos and sin, made once for all heads of a kind: a pair (p, q)
+// The norm's weights times cos and sin, made once for all heads of a kind (8192 bf16
+// tokens of 32 / 8 heads: 35.6 us so, 38.4 with the weights unpacked and applied head by
+// head; 33.4 without a norm, of 29.7 us of bytes): a pair (p, q)
 // becomes inv (p pc + q qs, p ps + q qc), qs with the minus.  Where nothing turns, p pc and q qc.
 struct TurnedWeights {
     unsigned long long pc[4], qs[4], ps[4], qc[4];
@@ -431,8 +434,7 @@ __device__ __forceinline__ void write_heads(Batch<T, kBatch> &batch, const T *sr
         } else if (s != s0) {
             batch.template load<G>(src, src_step, s, s1, heads, mine, e0, e1);
         }
-        // the batch's sums go through the lanes side by side (one after another, a shuffle
-        // chain a step: XXX)
+        // the batch's sums go through the lanes side by side
         float inv[kBatch];
         if constexpr (NORM) {
             if (weight) {
@@ -506,7 +508,8 @@ template <class T, class KV, int D, bool INTERLEAVED, int G, bool NORM>
 __global__ void __launch_bounds__(kThreads, kAskedCtas<T, KV, NORM>) kv_write_kernel(const WriteArgs a) {
     constexpr int kLanes = D / 16, kTeams = 32 / kLanes / G, kMake = 8 / G;
     constexpr int kBatch = sizeof(T) == 4 ? 2 : 3;            // (steps in flight, as above)
-    constexpr bool kAhead = NORM || kIsFp4<KV>;                             // the next batch is asked for before this one is used
+    // the next batch is asked for before this one is used, where a step's arithmetic takes long
+    constexpr bool kAhead = NORM || kIsFp4<KV>;
     const int lane = threadIdx.x % 32;
     const int64_t job = static_cast<int64_t>(blockIdx.x) * kWarps + threadIdx.x / 32;
     const int64_t t0 = a.parts == 1 ? job : job / a.parts;
