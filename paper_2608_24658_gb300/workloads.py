@@ -46,7 +46,7 @@ class ForkTree:
     num_q_heads: int
     num_kv_heads: int
     head_dim: int
-    mode: str                      # "bf16" | "fp32" | "fp8"
+    mode: str                      # "bf16" | "fp32" | "fp8" | "fp4"
     parent: np.ndarray
     node_len: np.ndarray
     node_page_ptr: np.ndarray
@@ -56,7 +56,7 @@ class ForkTree:
     q: torch.Tensor                # [L, H_q, d]
     k_pages: torch.Tensor          # [P, H_kv, page_size, d]
     v_pages: torch.Tensor
-    k_scale: Optional[torch.Tensor] = None   # [H_kv] fp32, fp8 mode
+    k_scale: Optional[torch.Tensor] = None   # [H_kv] fp32, fp8 and fp4 mode
     v_scale: Optional[torch.Tensor] = None
     sm_scale: float = 0.0          # 0 => 1/sqrt(head_dim)
     page_size: int = PAGE_SIZE
@@ -100,7 +100,7 @@ class ForkTree:
         return int(sum(int(self.node_len[self.path(b)].sum()) for b in range(self.num_leaves)))
 
     def kv_elem_bytes(self) -> int:
-        return {"bf16": 2, "fp32": 4, "fp8": 1}[self.mode]
+        return {"bf16": 2, "fp32": 4, "fp8": 1, "fp4": 9 / 16}[self.mode]
 
     def q_elem_bytes(self) -> int:
         return 4 if self.mode == "fp32" else 2
@@ -196,8 +196,11 @@ def build_tree(name: str, parent, node_len, leaf_node, *, num_q_heads: int,
     """Assemble a workload from a tree shape; draws pages, then q, K, V.
 
     ``values=False`` stops after the page table (tensors are left empty): the
-    tree shape of a multi-GB workload without its q/K/V.
+    tree shape of a multi-GB workload without its q/K/V, and of one in fp4 mode, whose
+    pools ``kv_write`` fills.
     """
+    if mode == "fp4" and values:
+        raise ValueError("fp4 pools are filled by kv_write: build the shape with values=False")
     if rng is None:
         rng = np.random.default_rng(seed)
     meta = dict(meta or {})

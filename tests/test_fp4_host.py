@@ -7,6 +7,7 @@ import pytest
 from paper_2608_24658_gb300 import _lib, build
 from paper_2608_24658_gb300 import workloads as W
 from paper_2608_24658_gb300.api import ParasonError, Plan
+from tests.test_plan import verify_plan
 
 A = 1 << 20          # an address that nothing reads
 
@@ -119,3 +120,24 @@ def test_plans(lib):
         with pytest.raises(ParasonError) as e:
             Plan(head_dim=64, prefill=prefill, **kw)
         assert e.value.status == _lib.EUNSUPPORTED
+
+
+@pytest.mark.parametrize("prefix, branches, tokens, h_q, sms", [
+    (0, 1, 1, 8, 152), (17, 3, 33, 8, 152), (256, 4, 64, 64, 152), (512, 16, 1500, 32, 152), (16384, 32, 700, 64, 152),
+    (4096, 128, 100, 64, 8), (0, 64, 6000, 8, 152), (2048, 40, 15, 24, 3)])
+def test_plans_cover_their_trees(prefix, branches, tokens, h_q, sms):
+    """Every (branch, page) once: pieces of two pages where the pass is small, longer ones elsewhere."""
+    parent = [-1] * branches if prefix == 0 else [-1] + [0] * branches
+    lens = [tokens + i % 3 for i in range(branches)]
+    first = 0 if prefix == 0 else 1
+    tree = W.build_tree("cover", parent, ([prefix] if prefix else []) + lens, list(range(first, first + branches)),
+                        num_q_heads=h_q, num_kv_heads=8, head_dim=128, mode="fp4", values=False)
+    with Plan.for_tree(tree, host_only=True, num_sms=sms) as plan:
+        verify_plan(tree, plan)
+
+
+def test_workloads_of_the_shape():
+    with pytest.raises(ValueError):
+        W.figure3_tree(d=128, mode="fp4")
+    tree = W.figure3_tree(d=128, mode="fp4", values=False)
+    assert tree.kv_elem_bytes() * 128 == 72
