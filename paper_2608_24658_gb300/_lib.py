@@ -6,8 +6,12 @@ the import raises, so a GPU run cannot silently use anything else.
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 import struct
+import sysconfig
+
+import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "_build", "libparason.so")
@@ -145,6 +149,30 @@ SIGNATURES = {
 _lib = None
 
 
+def _unknown(*_):
+    return None
+
+
+# A tensor's properties in one call (csrc/python/tensors.cpp), from the first load on:
+#   flat(tensor, dtype, dev, *sizes)                 its address
+#   rows(tensor, dtype, dev, tokens, heads, dim)     the bytes of a Rows
+#   alike(a, b)                                      (dtype, dev, addresses, shape) of a pair
+# None where it is not plainly that (and always, where the module was not built).
+flat = rows = alike = _unknown
+
+
+def _load_tensors() -> None:
+    global flat, rows, alike
+    path = os.path.join(os.path.dirname(LIB_PATH),
+                        f"_tensors-{torch.__version__}{sysconfig.get_config_var('EXT_SUFFIX')}")
+    if not os.path.exists(path):
+        return
+    spec = importlib.util.spec_from_file_location("_tensors", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    flat, rows, alike = module.flat, module.rows, module.alike
+
+
 def load() -> ctypes.CDLL:
     """Load the in-tree libparason.so; raise if it has not been built."""
     global _lib
@@ -158,6 +186,7 @@ def load() -> ctypes.CDLL:
             fn = getattr(lib, name)
             fn.restype = res
             fn.argtypes = args
+        _load_tensors()
         _lib = lib
     return _lib
 

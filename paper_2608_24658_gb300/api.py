@@ -40,10 +40,13 @@ def _stream_handle(stream) -> ctypes.c_void_p:
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _stream_int(stream) -> int:
     if stream is None:
         if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device())
+            return _raw_stream(_current_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream if isinstance(stream, torch.cuda.Stream) else int(stream)
 
@@ -217,25 +220,34 @@ class Plan:
         """One decode step; returns (out, lse).  Asynchronous on ``stream``.
         ``q``, ``out`` and ``lse`` may be pinned host tensors: the kernels
         then read q from, and write the result to, host memory directly."""
-        # (small steps wait for this code: tensors are looked at once, and
-        # pointers go to the library as integers)
+        # (small steps wait for this code: tensors are looked at once, by _lib.alike and
+        # _lib.flat where they are plainly right, and pointers go to the library as integers)
         L, Hq, Hkv, d = self.num_leaves, self.num_q_heads, self.num_kv_heads, self.head_dim
         qd, kvd = _Q_DTYPES[self.mode], _KV_DTYPES[self.mode]
-        q_cuda = q.is_cuda
-        if (q.dtype != qd or q.shape != (L, Hq, d) or not q.is_contiguous()
-                or not (q_cuda or q.is_pinned())):
-            raise ValueError(f"q must be a contiguous cuda (or pinned host) {qd} tensor of "
-                             f"shape {(L, Hq, d)}")
-        dev = k_pages.device
         page = (Hkv, 9 * d) if kvd is torch.uint8 else (Hkv, 16, d)
-        for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
-            shape = t.shape
-            if (t.dtype != kvd or shape[1:] != page or shape[0] < self.num_physical_pages
-                    or not t.is_contiguous() or not t.is_cuda or t.device != dev):
-                raise ValueError(f"{name} must be a contiguous cuda {kvd} tensor "
-                                 f"[>= {self.num_physical_pages}, {', '.join(map(str, page))}] on one device")
-        if q_cuda and q.device != dev:
-            raise ValueError(f"q must be on {dev}")
+        dev = k_pages.device
+        pair = _lib.alike(k_pages, v_pages)
+        qa = None
+        if pair is not None:
+            dtype, on, ka, va, shape = pair
+            if dtype is kvd and shape[1:] == page and shape[0] >= self.num_physical_pages:
+                qa = _lib.flat(q, qd, on, L, Hq, d)
+        q_cuda = True
+        if qa is None:
+            q_cuda = q.is_cuda
+            if (q.dtype != qd or q.shape != (L, Hq, d) or not q.is_contiguous()
+                    or not (q_cuda or q.is_pinned())):
+                raise ValueError(f"q must be a contiguous cuda (or pinned host) {qd} tensor of "
+                                 f"shape {(L, Hq, d)}")
+            for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
+                shape = t.shape
+                if (t.dtype != kvd or shape[1:] != page or shape[0] < self.num_physical_pages
+                        or not t.is_contiguous() or not t.is_cuda or t.device != dev):
+                    raise ValueError(f"{name} must be a contiguous cuda {kvd} tensor "
+                                     f"[>= {self.num_physical_pages}, {', '.join(map(str, page))}] on one device")
+            if q_cuda and q.device != dev:
+                raise ValueError(f"q must be on {dev}")
+            qa, ka, va = q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr()
         if out is None:
             out = torch.empty_like(q) if q_cuda else torch.empty(q.shape, dtype=q.dtype).pin_memory()
         if lse is None and want_lse:
@@ -247,15 +259,18 @@ class Plan:
         if self.mode in ("fp8", "fp4"):
             if k_scale is None or v_scale is None:
                 raise ValueError(f"{self.mode} mode needs k_scale and v_scale")
-            for s in (k_scale, v_scale):
-                if s.dtype != torch.float32 or s.numel() != Hkv or not s.is_cuda:
-                    raise ValueError(f"scales must be cuda float32 [{Hkv}]")
-        if k_scale is not None:
+            ks = _lib.flat(k_scale, torch.float32, dev.index, Hkv)
+            vs = _lib.flat(v_scale, torch.float32, dev.index, Hkv)
+            if ks is None or vs is None:
+                for s in (k_scale, v_scale):
+                    if s.dtype != torch.float32 or s.numel() != Hkv or not s.is_cuda:
+                        raise ValueError(f"scales must be cuda float32 [{Hkv}]")
+        if ks is None and k_scale is not None:
             ks = k_scale.data_ptr()
-        if v_scale is not None:
+        if vs is None and v_scale is not None:
             vs = v_scale.data_ptr()
         st = _lib.load().parason_attn_decode(
-            self.handle, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), ks, vs,
+            self.handle, qa, ka, va, ks, vs,
             out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(),
             workspace.numel() * workspace.element_size(), _stream_int(stream))
         if st:
@@ -421,11 +436,9 @@ class Rotary:
         self._head = (self.rotary_dim, int(self.interleaved), self.num_axes,
                       0 if self._axes is None else self._axes.ctypes.data, self._turns.data_ptr())
 
-    def _desc(self, positions) -> bytes:
-        if positions is None:
-            return _lib.ROTARY.pack(*self._head, 0, 0)
-        return _lib.ROTARY.pack(*self._head, positions.data_ptr(),
-                                positions.stride(0) if self.num_axes > 1 else 0)
+    def _desc(self, positions, at=0) -> bytes:
+        """(at: the positions' address)"""
+        return _lib.ROTARY.pack(*self._head, at, positions.stride(0) if at and self.num_axes > 1 else 0)
 
 
 class HeadNorm:
@@ -462,11 +475,18 @@ class HeadNorm:
 
 # (small steps wait for this code: tensors are looked at once, devices as
 # numbers; records go to the library as bytes, pointers as integers)
-_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _token_rows(name, t, shape, dtype, dev, out=False) -> bytes:
     """The C view of rows [tokens, heads, dim] with any strides of 16 bytes."""
+    if not out:
+        rows = _lib.rows(t, dtype, dev, *shape)
+        if rows is not None:
+            return rows
+    else:
+        at = _lib.flat(t, dtype, dev, *shape)
+        if at and at & 15 == 0:
+            return _lib.ROWS.pack(at, shape[1] * shape[2], shape[2])
     if t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
         raise ValueError(f"{name} must be a {dtype} tensor of shape {tuple(shape)} on cuda:{dev}")
     ts, hs, es = t.stride()
@@ -490,6 +510,9 @@ def _token_rows(name, t, shape, dtype, dev, out=False) -> bytes:
 
 
 def _token_ints(name, t, shape, dev) -> int:
+    at = _lib.flat(t, torch.int32, dev, *shape)
+    if at is not None:
+        return at
     if t.dtype is not torch.int32 or t.shape != shape or t.get_device() != dev or (
             t.stride(-1) != 1 and t.numel() > 1):
         raise ValueError(f"{name} must be an int32 tensor of shape {shape} on cuda:{dev}, contiguous "
@@ -510,20 +533,28 @@ def _config(mode, q_heads, kv_heads, dim):
 
 
 def _pools(k_pages, v_pages):
-    """(mode, device number, pages, kv heads, head_dim) of a pair of pools."""
-    dtype, shape, dev = k_pages.dtype, k_pages.shape, k_pages.get_device()
+    """(mode, device number, pages, kv heads, head_dim, k's and v's address) of a pair of
+    pools."""
+    pair = _lib.alike(k_pages, v_pages)
+    if pair is not None:
+        dtype, dev, ka, va, shape = pair
+    else:
+        dtype, shape, dev = k_pages.dtype, k_pages.shape, k_pages.get_device()
     mode = _POOL_MODES.get(dtype)
     if (mode is None or (mode != "fp4" and (len(shape) != 4 or shape[2] != 16)) or dev < 0
-            or not k_pages.is_contiguous() or (mode == "fp4" and (len(shape) != 3 or shape[2] % 9))):
+            or (pair is None and not k_pages.is_contiguous())
+            or (mode == "fp4" and (len(shape) != 3 or shape[2] % 9))):
         raise ValueError("k_pages must be a contiguous cuda tensor [pages, kv heads, 16, head_dim] "
                          "in bf16, fp32 or float8_e4m3fn, or uint8 [pages, kv heads, 9 head_dim]")
-    if (v_pages.dtype is not dtype or v_pages.shape != shape or v_pages.get_device() != dev
-            or not v_pages.is_contiguous()):
-        raise ValueError("v_pages must be like k_pages")
+    if pair is None:
+        if (v_pages.dtype is not dtype or v_pages.shape != shape or v_pages.get_device() != dev
+                or not v_pages.is_contiguous()):
+            raise ValueError("v_pages must be like k_pages")
+        ka, va = k_pages.data_ptr(), v_pages.data_ptr()
     if mode == "fp4":
-        return mode, dev, shape[0], shape[1], shape[2] // 9
+        return mode, dev, shape[0], shape[1], shape[2] // 9, ka, va
     pages, heads, _, d = shape
-    return mode, dev, pages, heads, d
+    return mode, dev, pages, heads, d, ka, va
 
 
 def _stream_on(stream, dev) -> int:
@@ -536,6 +567,10 @@ def _stream_on(stream, dev) -> int:
 
 
 def _head_scales(k_scale, v_scale, heads, dev):
+    ks = _lib.flat(k_scale, torch.float32, dev, heads)
+    vs = _lib.flat(v_scale, torch.float32, dev, heads)
+    if ks is not None and vs is not None:
+        return ks, vs
     for s in (k_scale, v_scale):
         if (s is None or s.dtype is not torch.float32 or s.shape != (heads,) or s.get_device() != dev
                 or not s.is_contiguous()):
@@ -573,7 +608,7 @@ def kv_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: t
     whose slot is outside the pool (-1, say) is not written.  positions: cuda
     int32 [T], or [axes, T] as ``rotary`` has axes.  ``q_out`` may be ``q``
     itself where that is contiguous."""
-    mode, dev, pages, heads, d = _pools(k_pages, v_pages)
+    mode, dev, pages, heads, d, kp, vp = _pools(k_pages, v_pages)
     dtype = _Q_DTYPES[mode]
     shape = k.shape
     if shape[1:] != (heads, d):
@@ -592,9 +627,8 @@ def kv_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: t
         if rotary.device != dev or rotary.rotary_dim > d:
             raise ValueError(f"rotary must be on cuda:{dev} and turn at most {d} elements")
         axes = rotary.num_axes
-        _token_ints("positions", positions, (tokens,) if axes == 1 and positions.dim() == 1
-                    else (axes, tokens), dev)
-        rot = rotary._desc(positions)
+        rot = rotary._desc(positions, _token_ints(
+            "positions", positions, (tokens,) if axes == 1 and positions.dim() == 1 else (axes, tokens), dev))
     elif positions is not None:
         raise ValueError("positions need a rotary")
     cq = qo = None
@@ -609,11 +643,13 @@ def kv_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: t
             q_out = _new(stream, q_shape, dtype, dev)
             qo = q_out.data_ptr()
         else:
-            qo = q_out.data_ptr()
-            if (q_out.dtype is not dtype or q_out.shape != q_shape or q_out.get_device() != dev
-                    or not q_out.is_contiguous() or qo & 15):
-                raise ValueError(f"q_out must be a contiguous {dtype} tensor of q's shape on cuda:{dev}, "
-                                 "16-byte aligned")
+            qo = _lib.flat(q_out, dtype, dev, *q_shape)
+            if qo is None or qo & 15:
+                qo = q_out.data_ptr()
+                if (q_out.dtype is not dtype or q_out.shape != q_shape or q_out.get_device() != dev
+                        or not q_out.is_contiguous() or qo & 15):
+                    raise ValueError(f"q_out must be a contiguous {dtype} tensor of q's shape on cuda:{dev}, "
+                                     "16-byte aligned")
             if qo == q.data_ptr() and not q.is_contiguous():
                 raise ValueError("q_out may be q itself only where q is contiguous")
     elif q_out is not None:
@@ -627,13 +663,13 @@ def kv_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: t
             raise ValueError("a norm of q alone needs q")
         st = _lib.load().parason_kv_write_norm(
             _config(mode, q_heads, heads, d), tokens, cq, ck, cv, norm._desc, rot, at, ks, vs, qo,
-            k_pages.data_ptr(), v_pages.data_ptr(), pages, _stream_on(stream, dev))
+            kp, vp, pages, _stream_on(stream, dev))
         if st:
             check(st, "parason_kv_write_norm")
         return q_out
     st = _lib.load().parason_kv_write(
         _config(mode, q_heads, heads, d), tokens, cq, ck, cv, rot, at, ks, vs, qo,
-        k_pages.data_ptr(), v_pages.data_ptr(), pages, _stream_on(stream, dev))
+        kp, vp, pages, _stream_on(stream, dev))
     if st:
         check(st, "parason_kv_write")
     return q_out
@@ -646,7 +682,7 @@ def kv_read(k_pages: torch.Tensor, v_pages: torch.Tensor, slots: torch.Tensor,
     [T, H_kv, d] in bf16 (fp32 from an fp32 cache), e4m3 and 4 bits times their
     scales (``parason_kv_read``).  A slot outside the pool gives zeros.  Given ``k`` and
     ``v`` may be views with strides of 16 bytes.  Asynchronous."""
-    mode, dev, pages, heads, d = _pools(k_pages, v_pages)
+    mode, dev, pages, heads, d, kp, vp = _pools(k_pages, v_pages)
     dtype = _Q_DTYPES[mode]
     tokens = slots.shape
     if len(tokens) != 1:
@@ -661,8 +697,8 @@ def kv_read(k_pages: torch.Tensor, v_pages: torch.Tensor, slots: torch.Tensor,
     ck = _token_rows("k", k, shape, dtype, dev, out=True)
     cv = _token_rows("v", v, shape, dtype, dev, out=True)
     st = _lib.load().parason_kv_read(
-        _config(mode, heads, heads, d), shape[0], at, k_pages.data_ptr(), v_pages.data_ptr(),
-        pages, ks, vs, ck, cv, _stream_on(stream, dev))
+        _config(mode, heads, heads, d), shape[0], at, kp, vp, pages, ks, vs, ck, cv,
+        _stream_on(stream, dev))
     if st:
         check(st, "parason_kv_read")
     return k, v
@@ -707,8 +743,14 @@ def kv_scales(k: torch.Tensor, v: torch.Tensor, rotary: Optional[Rotary] = None,
 _I32 = torch.int32
 
 
-def _not_ints(name, shape, dev):
-    raise ValueError(f"{name} must be a contiguous int32 tensor of shape {tuple(shape)} on cuda:{dev}")
+def _ints(name, t, n, dev) -> int:
+    """The address of a contiguous int32 tensor [n]."""
+    at = _lib.flat(t, _I32, dev, n)
+    if at is None:
+        if t.dtype is not _I32 or t.shape != (n,) or t.get_device() != dev or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous int32 tensor of shape {(n,)} on cuda:{dev}")
+        at = t.data_ptr()
+    return at
 
 
 def kv_slots(page_table: torch.Tensor, held: torch.Tensor, added: Optional[torch.Tensor] = None,
@@ -730,53 +772,40 @@ def kv_slots(page_table: torch.Tensor, held: torch.Tensor, added: Optional[torch
     ``tokens``: rows of new outputs, as many as the sequences add or more (rows past
     the last token have slot -1); with neither it nor outputs there are R.  lens_out may
     be held, and used_out free_used.  Asynchronous."""
-    # (as small steps wait for this code, it checks each tensor in place)
-    dev = page_table.get_device()
-    if page_table.dtype is not _I32 or page_table.dim() != 2 or dev < 0 or (
-            page_table.stride(1) != 1 and page_table.numel() > 1):
-        raise ValueError("page_table must be a cuda int32 tensor [sequences, pages] with contiguous rows")
-    seqs, width = page_table.shape
-    stride = page_table.stride(0) if seqs > 1 else width
-    if stride < width:
-        raise ValueError("page_table's rows must not overlap")
-    of_seq = (seqs,)
-    if (held.dtype is not _I32 or held.shape != of_seq or held.get_device() != dev
-            or not held.is_contiguous()):
-        _not_ints("held", of_seq, dev)
-    ha = held.data_ptr()
+    dev, shape = page_table.get_device(), page_table.shape
+    table = _lib.flat(page_table, _I32, dev, *shape) if len(shape) == 2 else None
+    if table is not None:
+        seqs, stride = shape
+        width = stride
+    else:
+        if page_table.dtype is not _I32 or len(shape) != 2 or dev < 0 or (
+                page_table.stride(1) != 1 and page_table.numel() > 1):
+            raise ValueError("page_table must be a cuda int32 tensor [sequences, pages] with contiguous rows")
+        seqs, width = shape
+        stride = page_table.stride(0) if seqs > 1 else width
+        if stride < width:
+            raise ValueError("page_table's rows must not overlap")
+        table = page_table.data_ptr()
+    ha = _ints("held", held, seqs, dev)
     ad = fi = fp = fu = uo = free = tp = lo = 0
     if added is not None:
-        if (added.dtype is not _I32 or added.shape != of_seq or added.get_device() != dev
-                or not added.is_contiguous()):
-            _not_ints("added", of_seq, dev)
-        ad = added.data_ptr()
+        ad = _ints("added", added, seqs, dev)
     if first is not None:
-        if (first.dtype is not _I32 or first.shape != of_seq or first.get_device() != dev
-                or not first.is_contiguous()):
-            _not_ints("first", of_seq, dev)
-        fi = first.data_ptr()
+        fi = _ints("first", first, seqs, dev)
     if free_pages is not None:
         free = free_pages.numel()
         if free == 0:
             raise ValueError("free_pages must have an entry")
-        if (free_pages.dtype is not _I32 or free_pages.shape != (free,) or free_pages.get_device() != dev
-                or not free_pages.is_contiguous()):
-            _not_ints("free_pages", (free,), dev)
-        fp = free_pages.data_ptr()
+        fp = _ints("free_pages", free_pages, free, dev)
         if free_used is not None:
-            if (free_used.dtype is not _I32 or free_used.shape != (1,) or free_used.get_device() != dev
-                    or not free_used.is_contiguous()):
-                _not_ints("free_used", (1,), dev)
-            fu = free_used.data_ptr()
+            fu = _ints("free_used", free_used, 1, dev)
         if used_out is not None:
-            if (used_out.dtype is not _I32 or used_out.shape != (1,) or used_out.get_device() != dev
-                    or not used_out.is_contiguous()):
-                _not_ints("used_out", (1,), dev)
-            uo = used_out.data_ptr()
+            uo = _ints("used_out", used_out, 1, dev)
     elif free_used is not None or used_out is not None:
         raise ValueError("free_used and used_out need free_pages")
     if slots is not None:
-        rows = slots.shape[0] if slots.dim() == 1 else -1
+        shape = slots.shape
+        rows = shape[0] if len(shape) == 1 else -1
         if tokens is not None and tokens != rows:
             raise ValueError(f"slots must be [{tokens}]")
     elif positions is not None and positions.dim() == 1:
@@ -789,32 +818,19 @@ def kv_slots(page_table: torch.Tensor, held: torch.Tensor, added: Optional[torch
         rows = seqs if tokens is None else int(tokens)
     if rows < 0:
         raise ValueError("the outputs must be [rows]")
-    of_row = (rows,)
     if slots is None:
-        slots = _new(stream, of_row, _I32, dev)
+        slots = _new(stream, (rows,), _I32, dev)
     if positions is None:
-        positions = _new(stream, of_row, _I32, dev)
-    if (slots.dtype is not _I32 or slots.shape != of_row or slots.get_device() != dev
-            or not slots.is_contiguous()):
-        _not_ints("slots", of_row, dev)
-    sl = slots.data_ptr()
-    if (positions.dtype is not _I32 or positions.shape != of_row or positions.get_device() != dev
-            or not positions.is_contiguous()):
-        _not_ints("positions", of_row, dev)
-    po = positions.data_ptr()
+        positions = _new(stream, (rows,), _I32, dev)
+    sl = _ints("slots", slots, rows, dev)
+    po = _ints("positions", positions, rows, dev)
     if token_ptr is not None:
-        if (token_ptr.dtype is not _I32 or token_ptr.shape != (seqs + 1,) or token_ptr.get_device() != dev
-                or not token_ptr.is_contiguous()):
-            _not_ints("token_ptr", (seqs + 1,), dev)
-        tp = token_ptr.data_ptr()
+        tp = _ints("token_ptr", token_ptr, seqs + 1, dev)
     if lens_out is not None:
-        if (lens_out.dtype is not _I32 or lens_out.shape != of_seq or lens_out.get_device() != dev
-                or not lens_out.is_contiguous()):
-            _not_ints("lens_out", of_seq, dev)
-        lo = lens_out.data_ptr()
+        lo = _ints("lens_out", lens_out, seqs, dev)
     st = _lib.load().parason_kv_slots(
-        _lib.SLOT_MAP.pack(seqs, rows, ha, ad, fi, page_table.data_ptr(), stride, width, free, fp, fu, sl, po, tp, lo,
-                           uo), _stream_on(stream, dev))
+        _lib.SLOT_MAP.pack(seqs, rows, ha, ad, fi, table, stride, width, free, fp, fu, sl, po, tp, lo, uo),
+        _stream_on(stream, dev))
     if st:
         check(st, "parason_kv_slots")
     return slots, positions
