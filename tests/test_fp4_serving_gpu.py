@@ -142,3 +142,37 @@ def test_long_pieces():
                       leaf_node=np.array([0], np.int32), num_physical_pages=len(ids), q=q[b:b + 1],
                       k_pages=pools[0][ids.tolist()], v_pages=pools[1][ids.tolist()])
         F.check(one, out[b:b + 1], lse[b:b + 1])
+
+
+def test_pages_past_4_gb():
+    """Pages whose bytes lie more than 2^32 into a pool: written, read, decoded and prefilled as
+    in a small pool."""
+    pages, heads = 480_000, 8                            # 4.4 GB each
+    gen = R.generator(11)
+    small = [torch.zeros((40, heads, 9 * D), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    large = [torch.empty((pages, heads, 9 * D), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    last = torch.arange(pages - 40, pages, device="cuda")
+    for x in large:
+        x[last] = 0
+    tokens = 600
+    k, v = (torch.randn((tokens, heads, D), generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2))
+    scales = dict(k_scale=torch.full((heads,), 1e-3, device="cuda"), v_scale=torch.full((heads,), 1e-3, device="cuda"))
+    slots = torch.randperm(640, generator=gen, device="cuda")[:tokens].int()
+    far = slots + 16 * (pages - 40)
+    kv_write(k, v, *small, slots, **scales)
+    kv_write(k, v, *large, far, **scales)
+    assert all(torch.equal(x[last], y) for x, y in zip(large, small))
+    assert all(torch.equal(x, y) for x, y in zip(kv_read(*large, far, **scales), kv_read(*small, slots, **scales)))
+    kw = dict(num_q_heads=32, num_kv_heads=heads, head_dim=D, mode="fp4", parent=[-1, 0, 0, 0, 0, 0], sm_scale=0.1,
+              node_len=[330, 40, 64, 17, 50, 9], node_page_ptr=[0, 21, 24, 28, 30, 34, 35])
+    for prefill in (False, True):
+        out = []
+        for pools, first in ((small, 0), (large, pages - 40)):
+            ids = (torch.arange(35) * 11 % 40 + first).tolist()
+            with Plan(page_ids=ids, leaf_node=[1, 2, 3, 4, 5], num_physical_pages=pools[0].shape[0], prefill=prefill,
+                      **kw) as plan:
+                q = torch.randn((plan.num_leaves, 32, D), generator=R.generator(2), device="cuda").to(torch.bfloat16)
+                out.append(plan.decode(q, *pools, **scales))
+                plan.check()
+        assert out[0][0].isfinite().all() and out[0][0].abs().max() > 0.01
+        assert all(torch.equal(x, y) for x, y in zip(*out))
