@@ -135,6 +135,13 @@ __device__ __forceinline__ void hide_from(float &x, int q, int seen) {
     x = __uint_as_float(u);
 }
 
+// 8 consecutive fp32 values, 32-byte aligned: a whole sector in one store.
+__device__ __forceinline__ void store_f32x8(float *dst, const float (&y)[8]) {
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "f"(y[0]), "f"(y[1]),
+                 "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7])
+                 : "memory");
+}
+
 // 32 consecutive fp32 values of one partial row (128 bytes, 32-byte
 // aligned), scaled, as four 32-byte stores: every store fills whole sectors
 // (16-byte stores from the 32 rows of a warp left each sector to be filled
