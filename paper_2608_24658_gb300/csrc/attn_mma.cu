@@ -1272,7 +1272,7 @@ __device__ void suffix_warp(const KvMaps &maps, const AttnArgs &a, uint32_t ring
 // latency of three warps a scheduler: 320 instructions a page, the conversions and their
 // bit work at 35 to 40% of the ALU pipe.  Page by page through suffix_warp: 173 us.  A page a
 // step with the rest as here: 129.  16 warps of 128 registers spill (an earlier form 135 -> 235);
-// q asked for ahead: 3 to 4% longer; pages by cp.async.bulk: level.
+// q asked for ahead, into L1 or shared memory: 3 to 8% longer; pages by cp.async.bulk: level.
 template <int D, class KV>
 __device__ void suffix_warp_fp4(const AttnArgs &a, uint32_t ring, uint32_t bars, int warp, int lane, WorkItem *grab) {
     using S = Shape<D, KV>;
