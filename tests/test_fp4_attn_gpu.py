@@ -229,3 +229,20 @@ def test_wrong_pools():
                 plan.decode(t.q, k, t.v_pages, k_scale=t.k_scale, v_scale=t.v_scale)
         with pytest.raises(ValueError):
             plan.decode(t.q, t.k_pages, t.v_pages, k_scale=t.k_scale)
+
+
+def test_pinned_q_and_results():
+    """q read from, and out and lse written to, pinned host memory; then through the binding's own checks."""
+    t = F.tree_of(*NESTED, 24, 2, seed=17)
+    with Plan.for_tree(t) as plan:
+        out, lse = plan.decode_tree(t)
+        there, lse_there = plan.decode(t.q.cpu().pin_memory(), t.k_pages, t.v_pages, k_scale=t.k_scale, v_scale=t.v_scale)
+        torch.cuda.synchronize()
+        plan.check()
+        assert there.is_pinned() and torch.equal(there, out.cpu()) and torch.equal(lse_there, lse.cpu())
+        for bad in (t.q.float(), t.q[:-1], t.q.cpu(), t.q.transpose(1, 2).contiguous().transpose(1, 2)):
+            with pytest.raises(ValueError):
+                plan.decode(bad, t.k_pages, t.v_pages, k_scale=t.k_scale, v_scale=t.v_scale)
+        for bad in (t.k_scale[:1], t.k_scale.double(), t.k_scale.cpu()):
+            with pytest.raises(ValueError):
+                plan.decode(t.q, t.k_pages, t.v_pages, k_scale=bad, v_scale=t.v_scale)
