@@ -1268,10 +1268,10 @@ __device__ void suffix_warp(const KvMaps &maps, const AttnArgs &a, uint32_t ring
 // update, the whole warp copies (288 chunks of 16 bytes are nine a lane), and tiles of up
 // to 8 rows all take the transposed step.
 //
-// 64 branches of 8192 tokens, 8 kv heads: 117 us of 89 us of bytes.  Bound by issue and
+// 64 branches of 8192 tokens, 8 kv heads: 112 us of 89 us of bytes.  Bound by issue and
 // latency of three warps a scheduler: 320 instructions a page, the conversions and their
 // bit work at 35 to 40% of the ALU pipe.  Page by page through suffix_warp: 173 us.  A page a
-// step with the rest as here: 129.  16 warps of 128 registers spill (an earlier form 135 -> 235);
+// step with the rest as here: 129 for 117.  16 warps of 128 registers spill (an earlier form 135 -> 235);
 // q asked for ahead, into L1 or shared memory: 3 to 8% longer; pages by cp.async.bulk: level.
 template <int D, class KV>
 __device__ void suffix_warp_fp4(const AttnArgs &a, uint32_t ring, uint32_t bars, int warp, int lane, WorkItem *grab) {
