@@ -1,4 +1,4 @@
-// attn_mma.cu -- fork-tree decode attention for bf16 or e4m3 KV on sm_103a.
+// attn_mma.cu -- fork-tree decode attention for bf16, e4m3 or 4-bit KV on sm_103a.
 //
 // One persistent launch, one CTA per SM, two roles (the planner decides how
 // many SMs each gets so that both finish together):
@@ -19,7 +19,8 @@
 //        from shared memory; 4 softmax warps own one row per thread (TMEM
 //        lane) and write P over S; 4 epilogue warps store an item's O and
 //        load Q two items ahead (with e4m3 KV they also convert each staged
-//        block to f16, and load an item's Q before its first block).
+//        block to f16, and load an item's Q before its first block; 4-bit KV
+//        the same, with bulk copies of pages, 3 raw stages, 5 converted ones).
 //      - bf16 at head_dim 128, when the planner pairs row tiles: two
 //        128-row tiles of a piece against each staged block
 //        (prefix_cta_tc_pair), Q in shared memory, each tile's S/P and O in
@@ -32,7 +33,8 @@
 //    softmax; tiles of 5 to 8 rows (at head_dim 64 of up to 8) run the
 //    transposed step (S^T = K Q^T), with e4m3 KV or at head_dim 64 two pages
 //    per softmax update.  A bf16 page at head_dim 128
-//    comes in one TMA box per tensor (the 4-D page maps).
+//    comes in one TMA box per tensor (the 4-D page maps).  4-bit KV has a
+//    loop of its own (suffix_warp_fp4).
 //
 // Every item writes a partial (o, m, l) per row.  The merge kernel (merge.cu)
 // folds the partials of every branch's path; it is launched as a
@@ -50,6 +52,9 @@
 //    the 16-row step's QK^T takes d = 16ks + 4t + {0..3} for thread t of a
 //    quad, the transposed step's two 16-byte runs per token row, and PV
 //    gives each thread one 16-byte chunk of V's columns.
+//  * 4 bits (e2m1, an e4m3 scale for 16 elements, one fp32 scale per kv head; a page
+//    is 16 rows of values, then 16 of scales): code times block scale is exact in
+//    f16 (cvt.rn.f16x2.e2m1x2, one product), the rest is as with e4m3.
 //
 // Scores are kept in the log2 domain: x = scale*log2(e)*<q,k>, so a partial
 // is m = max x, l = sum 2^(x-m), o = sum 2^(x-m) v (unnormalised).  Under a logit

@@ -1,7 +1,8 @@
 // kv_cache.cu -- filling and reading the paged KV cache: rows of tokens rotated
 // to their positions, rounded to the cache's type and written into their slots
-// (parason_kv_write), taken out again (parason_kv_read), and the e4m3 scales
-// that hold them (parason_kv_scales).
+// (parason_kv_write; parason_kv_write_norm with q and k normed by the head first),
+// taken out again (parason_kv_read), and the e4m3 or 4-bit scales that hold them
+// (parason_kv_scales).
 //
 // All three move bytes: HBM bounds them on long inputs, launches and one chain
 // of dependent loads (slot or position, then rows) on short ones.

@@ -1,5 +1,5 @@
-// prefill_mma.cu -- tree-masked prefill attention on tcgen05 (bf16 or e4m3 KV,
-// head_dim 128).
+// prefill_mma.cu -- tree-masked prefill attention on tcgen05 (bf16, e4m3 or 4-bit
+// KV, head_dim 128).
 //
 // Every token of every chunk is a query (paper Sec. 3.1: after a join the new
 // text is prefilled against the whole tree), so the pass is a dense
@@ -18,13 +18,13 @@
 //               per page and column block took permuted pages from 495 to 595
 //               us on the join; one 32 KB box for consecutive pages is level).
 //               e4m3: one 16 KB box when the block's 8 pages are consecutive,
-//               else a box per 4 pages or per page
+//               else a box per 4 pages or per page.  4 bits: a bulk copy a page
 //   warp 9      MMA issuer: S_t = Q_t K^T (M 128, N 128, both operands in
 //               shared memory) and O_t += P_t V (P in TMEM) for t = A, B in
 //               turn (two issuers let the tiles fall into step, both in their
 //               softmax or both waiting: join prefill 555 -> 727 us)
 //   warp 10     scheduler: pulls pairs and stages their records
-//   warps 12-15 with e4m3 KV: widen each staged block to f16
+//   warps 12-15 with e4m3 and 4-bit KV: widen each staged block to f16
 //
 // TMEM, 512 columns: O_A, O_B at 0 and 128, S_A, S_B at 256 and 384.  P (bf16,
 // f16 with e4m3 KV) goes over the first 64 columns of its S in two halves,
@@ -56,7 +56,9 @@
 // (705 us).  With e4m3 KV the chain is about 4500 cycles, as the widening warps
 // share the schedulers and the shared memory with the softmax; 8 widening
 // warps (832 us), or widening over the raw bytes in a ring of 5 slots (932
-// us), are slower than a ring of 4 raw and 3 widened slots.
+// us), are slower than a ring of 4 raw and 3 widened slots.  4-bit KV: the join 585 us,
+// the fork 47 (3 raw and 4 widened slots); with the next block's codes read before this
+// one's stores, in 8-byte pieces whose order needs no selects, 650.
 //
 // Logit caps (logit_cap.cuh) have instantiations of their own.  Without a
 // reference (kCapFree) a half of a block has nothing to wait for but its own S:
