@@ -247,7 +247,8 @@ size_t parason_plan_workspace_bytes(parason_plan plan);
  *            e4m3 bytes by mode (4-bit: the bytes of pages), 16-byte aligned
  *   v_pages  device, same layout and dtype as k_pages
  *   k_scale, v_scale  device fp32 [H_kv] in FP8 mode (k = e4m3 * k_scale) and
- *            FP4 mode (k = e2m1 * e4m3 * k_scale), ignored otherwise (may be NULL)
+ *            FP4 mode (k = e2m1 * e4m3 * k_scale), ignored otherwise (may be NULL).
+ *            k_scale is not negative, and finite (NaN makes the head's rows NaN)
  *   out      device, [num_leaves, H_q, head_dim], dtype of q, 16-byte
  *            aligned; or page-locked host memory the device can address
  *            (cudaHostAlloc / cudaHostRegister): the plan's last kernel

@@ -998,7 +998,7 @@ __device__ __forceinline__ float2 item_scales(const AttnArgs &a, const WorkItem 
     if constexpr (KV::kElemBytes == 2)
         return make_float2(scale, 1.f);
     else
-        return make_float2(scale * a.k_scale[it.kv_head], a.v_scale[it.kv_head]);
+        return make_float2(score_factor(scale, a.k_scale[it.kv_head]), a.v_scale[it.kv_head]);
 }
 
 // A warp writes the partials of its item's up to 16 rows straight from registers.

@@ -399,7 +399,7 @@ __global__ void __launch_bounds__(Cfg<KV>::kThreads, 1)
                 // the row's last visible key, relative to the item's first
                 const int t_rel = key0 == kNoKey0 ? (1 << 30) : (it.row0 + r) / a.group - key0;
                 const float scale = CAP ? a.to_cap : a.scale_log2;
-                const float sl = F8 ? scale * a.k_scale[it.kv_head] : scale;
+                const float sl = F8 ? score_factor(scale, a.k_scale[it.kv_head]) : scale;
                 const CapFactors cap(sl, a.cap_log2);                 // (used under a cap)
                 const unsigned long long slp = dev::f32x2(sl, sl);
                 float m_use = CAP == kCapFree ? 0.f : -INFINITY, l = 0.f;

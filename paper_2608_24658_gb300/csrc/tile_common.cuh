@@ -68,6 +68,14 @@ __device__ __forceinline__ uint32_t mul_f16x2_by(uint32_t a, uint32_t b) {
     return c;
 }
 
+// The factor of a kv head's scores.  Hidden ones are -inf before it multiplies them, and
+// -inf * 0 is NaN: a factor of 0 (a K scale of 0, or one so small that the product is)
+// becomes 2^-126, by which every score is still 0 to within 2^-90.  NaN stays.
+__device__ __forceinline__ float score_factor(float scale, float k_scale) {
+    const float s = scale * k_scale;
+    return s == 0.f ? 0x1p-126f : s;
+}
+
 // A bf16 pair of q narrowed to an f16 pair for the e4m3 MMAs.  The f16
 // values are exact for |q| < 65504 (tiny values lose low bits); an element
 // of magnitude 65520 or more (including inf) would round to inf, so `big` is
