@@ -445,12 +445,18 @@ class HeadNorm:
     """The norm of each head of q and k before its rotation (C type
     ``parason_head_norm``): x / sqrt(mean x^2 + eps) * w in fp32.  ``q_weight`` and
     ``k_weight``: cuda [head_dim] for all heads or [heads, head_dim], in the rows' dtype;
-    None leaves q (or k) as it is.  ``unit_offset``: the weights are kept less 1.  The
-    weights are read at every write (a captured one's replays too)."""
+    None leaves q (or k) as it is.  ``unit_offset``: the weights are kept less 1.  A write
+    reads the weights that the tensors hold then (a captured one's replays: what is in the
+    memory that they had at the capture)."""
 
     def __init__(self, q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
                  eps: float = 1e-6, unit_offset: bool = False):
-        given = [w for w in (q_weight, k_weight) if w is not None]
+        self.q_weight, self.k_weight = q_weight, k_weight
+        self.eps, self.unit_offset = float(eps), bool(unit_offset)
+        self._look()
+
+    def _look(self) -> None:
+        given = [w for w in (self.q_weight, self.k_weight) if w is not None]
         if not given:
             raise ValueError("a norm needs q_weight or k_weight")
         for w in given:
@@ -459,18 +465,27 @@ class HeadNorm:
                     or w.shape[-1] != given[0].shape[-1]):
                 raise ValueError("weights must be cuda [head_dim] or [heads, head_dim] tensors, bf16 or "
                                  "fp32, alike in dtype, device and head_dim")
-            if (w.stride(-1) != 1 or w.data_ptr() % 16
+            if (w.stride(-1) != 1 or w.data_ptr() % 16 or not w.data_ptr()
                     or (w.dim() == 2 and (w.stride(0) * w.element_size() % 16 or w.stride(0) < 0))):
-                raise ValueError("weights must have contiguous elements and start and rows of 16 bytes")
-        self.q_weight, self.k_weight = q_weight, k_weight
-        self.eps, self.unit_offset = float(eps), bool(unit_offset)
+                raise ValueError("weights must have memory, contiguous elements, and start and rows of 16 bytes")
+        both = self.q_weight, self.k_weight
         self.dtype, self.device, self.head_dim = given[0].dtype, given[0].get_device(), given[0].shape[-1]
         # heads a weight is for; None: any number
         self.q_heads, self.k_heads = (None if w is None or w.dim() == 1 or w.stride(0) == 0 and w.shape[0] == 1
-                                      else w.shape[0] for w in (q_weight, k_weight))
-        at = [0 if w is None else w.data_ptr() for w in (q_weight, k_weight)]
-        step = [0 if w is None or w.dim() == 1 else w.stride(0) for w in (q_weight, k_weight)]
+                                      else w.shape[0] for w in both)
+        at = [0 if w is None else w.data_ptr() for w in both]
+        step = [0 if w is None or w.dim() == 1 else w.stride(0) for w in both]
         self._desc = _lib.HEAD_NORM.pack(*at, *step, self.eps, 1.0 if self.unit_offset else 0.0)
+        self._seen = [(w, a, w.shape) for w, a in zip(both, at) if w is not None]
+
+    def _record(self) -> bytes:
+        """The C record of the weights as they are: a tensor's memory may have been replaced
+        (Tensor.data) since they were looked at."""
+        for w, at, shape in self._seen:
+            if _lib.flat(w, self.dtype, self.device, *shape) != at:
+                self._look()
+                break
+        return self._desc
 
 
 # (small steps wait for this code: tensors are looked at once, devices as
@@ -655,6 +670,7 @@ def kv_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: t
     elif q_out is not None:
         raise ValueError("q_out needs q")
     if norm is not None:
+        norm_desc = norm._record()
         if (norm.dtype is not dtype or norm.device != dev or norm.head_dim != d
                 or norm.k_heads not in (None, heads) or (q is not None and norm.q_heads not in (None, q_heads))):
             raise ValueError(f"norm must have {dtype} weights of {d} elements on cuda:{dev}, for all heads "
@@ -662,7 +678,7 @@ def kv_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: t
         if norm.k_weight is None and q is None:
             raise ValueError("a norm of q alone needs q")
         st = _lib.load().parason_kv_write_norm(
-            _config(mode, q_heads, heads, d), tokens, cq, ck, cv, norm._desc, rot, at, ks, vs, qo,
+            _config(mode, q_heads, heads, d), tokens, cq, ck, cv, norm_desc, rot, at, ks, vs, qo,
             kp, vp, pages, _stream_on(stream, dev))
         if st:
             check(st, "parason_kv_write_norm")
