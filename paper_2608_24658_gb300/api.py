@@ -441,9 +441,12 @@ class Rotary:
         return _lib.ROTARY.pack(*self._head, at, positions.stride(0) if at and self.num_axes > 1 else 0)
 
 
+_FP32_MAX = float(np.finfo(np.float32).max)
+
+
 class HeadNorm:
     """The norm of each head of q and k before its rotation (C type
-    ``parason_head_norm``): x / sqrt(mean x^2 + eps) * w in fp32.  ``q_weight`` and
+    ``parason_head_norm``): x / sqrt(mean x^2 + eps) * w in fp32, eps at least 2^-126.  ``q_weight`` and
     ``k_weight``: cuda [head_dim] for all heads or [heads, head_dim], in the rows' dtype;
     None leaves q (or k) as it is.  ``unit_offset``: the weights are kept less 1.  A write
     reads the weights that the tensors hold then (a captured one's replays: what is in the
@@ -453,6 +456,8 @@ class HeadNorm:
                  eps: float = 1e-6, unit_offset: bool = False):
         self.q_weight, self.k_weight = q_weight, k_weight
         self.eps, self.unit_offset = float(eps), bool(unit_offset)
+        if not 2.0 ** -126 <= self.eps <= _FP32_MAX:
+            raise ValueError("eps must be at least 2^-126, and finite in float32")
         self._look()
 
     def _look(self) -> None:
