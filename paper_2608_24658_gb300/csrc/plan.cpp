@@ -222,6 +222,9 @@ void piece_split(int64_t pages, int64_t chunk, int64_t align, int64_t &per, int6
     n = (pages + per - 1) / per;
 }
 
+// What suffix-pass pieces are multiples of, in pages.
+int64_t narrow_align(int32_t mode) { return mode == PARASON_FP4_KV ? kNarrowAlignFp4 : 1; }
+
 // The suffix pass of `lens` (pages of a run, runs of that length) in pieces of at
 // most `chunk` (<= kMaxPiecePages) pages, multiples of `align`, in pages of one warp: `early` warps from
 // time 0, `late` more from t_late on; below `full` busy warps time runs at
@@ -636,7 +639,6 @@ parason_status build_host(parason_plan_s *p, const parason_attn_config *cfg, int
     // partial slots.  Row tiles start at multiples of g, so each branch's g
     // rows of a node sit in one tile.
     const int32_t mode = cfg->mode;
-    const int64_t narrow_align = mode == PARASON_FP4_KV ? kNarrowAlignFp4 : 1;
     struct Run {
         int32_t node, head, row0, nrows;
         int64_t pages;              // pages the run covers (from the node's first)
@@ -1079,7 +1081,7 @@ parason_status build_host(parason_plan_s *p, const parason_attn_config *cfg, int
                 const int64_t length = length_at(pieces);
                 if (length == tried) continue;
                 tried = length;
-                const double t = narrow_time(lens, length, narrow_align, start, full, early, late, t_late);
+                const double t = narrow_time(lens, length, narrow_align(mode), start, full, early, late, t_late);
                 if (t < 0.0) break;
                 if (best == 0.0 || t < best) {
                     best = t;
@@ -1112,7 +1114,7 @@ parason_status build_host(parason_plan_s *p, const parason_attn_config *cfg, int
             const size_t j = group_end(i);
             const Run &r = runs[i];
             const bool pairs = r.wide && p->tc_pairs;
-            const int64_t align = r.wide ? kWideBlockPages : narrow_align;
+            const int64_t align = r.wide ? kWideBlockPages : narrow_align(mode);
             int64_t per = 0, n = 0;
             if (prefill)
                 per = wide_chunk;
@@ -2212,12 +2214,12 @@ parason_status parason_plan_fork(parason_plan p, int32_t branch, int32_t num_chi
         items.push_back(it);
         return static_cast<int32_t>(item0 + items.size() - 1);
     };
-    // equal pieces of at most the plan's suffix piece length
+    // equal pieces of at most the plan's suffix piece length, cut as the plan's own
     auto pieces = [&](int32_t P, auto &&fn) {
-        const int64_t chunk = std::max<int64_t>(1, p->narrow_chunk);
-        const int64_t n = (P + chunk - 1) / chunk;
-        const int32_t per = static_cast<int32_t>((P + n - 1) / std::max<int64_t>(1, n));
-        for (int32_t pg = 0; pg < P; pg += per) fn(pg, std::min(per, P - pg));
+        int64_t per = 0, n = 0;
+        piece_split(P, std::max<int64_t>(1, p->narrow_chunk), narrow_align(p->cfg.mode), per, n);
+        for (int64_t pg = 0; pg < P; pg += per)
+            fn(static_cast<int32_t>(pg), static_cast<int32_t>(std::min<int64_t>(per, P - pg)));
     };
     // (a) the new branches on every node of the path, in tiles of whole
     // branches of at most 16 rows
