@@ -617,9 +617,9 @@ typedef struct {
 /* One kernel on `stream`, no allocation, capturable: it reads lengths, table and list
  * on the device.  Other than held_out and used_out, outputs overlap nothing here.
  * PARASON_EINVAL for a negative count, a missing or misaligned (4 bytes) array, a
- * table_stride below table_pages, slots = positions, or what belongs to a free list
- * without one; PARASON_EUNSUPPORTED for more than 16384 sequences or 2^31 - 1 rows;
- * PARASON_ECUDA if the launch fails. */
+ * table_stride below table_pages, an output that lies over another array (but for those
+ * two), or what belongs to a free list without one; PARASON_EUNSUPPORTED for more than
+ * 16384 sequences or 2^31 - 1 rows; PARASON_ECUDA if the launch fails. */
 parason_status parason_kv_slots(const parason_slot_map *map, parason_stream_t stream);
 
 /*

@@ -792,7 +792,8 @@ def kv_slots(page_table: torch.Tensor, held: torch.Tensor, added: Optional[torch
     first and ``lens_out`` [R], ``free_used`` and ``used_out`` [1], ``token_ptr`` [R + 1].
     ``tokens``: rows of new outputs, as many as the sequences add or more (rows past
     the last token have slot -1); with neither it nor outputs there are R.  lens_out may
-    be held, and used_out free_used.  Asynchronous."""
+    be held, and used_out free_used; outputs that lie over anything else are refused.
+    Asynchronous."""
     dev, shape = page_table.get_device(), page_table.shape
     table = _lib.flat(page_table, _I32, dev, *shape) if len(shape) == 2 else None
     if table is not None:

@@ -14,6 +14,7 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <iterator>
 
 #include "device_common.cuh"
 #include "internal.h"
@@ -191,6 +192,46 @@ __global__ void __launch_bounds__(kMaxThreads) kv_slots_kernel(const SlotArgs a)
     }
 }
 
+// Whether outputs lie over what is read, or over one another: CTAs read while others write.
+// held_out may be held, and used_out free_used (their writes wait for every read).
+bool overlaps(const parason_slot_map &m) {
+    struct Array {
+        const int32_t *at;
+        int64_t n;
+    };
+    const int64_t seqs = m.num_seqs;
+    const Array in[] = {{m.held, seqs}, {m.added, seqs}, {m.first, seqs}, {m.free_pages, m.num_free}, {m.free_used, 1}};
+    const Array out[] = {{m.held_out, seqs}, {m.used_out, 1}, {m.slots, m.num_rows}, {m.positions, m.num_rows},
+                         {m.token_ptr, seqs + 1}};
+    auto meet = [](const Array &a, const Array &b) {
+        const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+        return a.at && b.at && a.n > 0 && b.n > 0 && (x <= y ? (y - x) / 4 < static_cast<uintptr_t>(a.n)
+                                                              : (x - y) / 4 < static_cast<uintptr_t>(b.n));
+    };
+    // an array and the table's rows, which may lie apart: its first element's row, or the next one
+    auto meets_table = [&](const Array &a) {
+        if (!a.at || a.n <= 0 || seqs == 0 || m.table_pages == 0) return false;
+        const intptr_t off = static_cast<intptr_t>(reinterpret_cast<uintptr_t>(a.at) - reinterpret_cast<uintptr_t>(m.page_table));
+        const int64_t from = off >> 2, to = from + a.n;       // (both 4-byte aligned)
+        if (seqs == 1 || from < 0) return to > 0 && from < m.table_pages;
+        const int64_t r = from / m.table_stride, at = from % m.table_stride;
+        return r < seqs && (at < m.table_pages || (r + 1 < seqs && at + a.n > m.table_stride));
+    };
+    for (const Array &o : out) {
+        for (const Array &i : in)
+            if (meet(o, i) && !(o.at == i.at && ((&o == &out[0] && &i == &in[0]) || (&o == &out[1] && &i == &in[4]))))
+                return true;
+        for (const Array *p = &o + 1; p != std::end(out); ++p)
+            if (meet(o, *p)) return true;
+        if (meets_table(o)) return true;
+    }
+    // (the table is written where there is a free list)
+    if (m.free_pages)
+        for (const Array &i : in)
+            if (meets_table(i)) return true;
+    return false;
+}
+
 bool misaligned4(const void *p) { return reinterpret_cast<uintptr_t>(p) % 4 != 0; }
 
 }  // namespace
@@ -213,7 +254,7 @@ extern "C" parason_status parason_kv_slots(const parason_slot_map *m, parason_st
     if (m->num_seqs > 1 && m->table_stride < m->table_pages) return PARASON_EINVAL;
     if (m->num_rows > 0 && !m->slots) return PARASON_EINVAL;
     if (!m->free_pages && (m->free_used || m->used_out || m->num_free > 0)) return PARASON_EINVAL;
-    if (m->slots && m->slots == m->positions) return PARASON_EINVAL;
+    if (overlaps(*m)) return PARASON_EINVAL;
     SlotArgs a{};
     a.held = m->held;
     a.added = m->added;
