@@ -10,8 +10,7 @@ import importlib.util
 import os
 import struct
 import sysconfig
-
-import torch
+import warnings
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "_build", "libparason.so")
@@ -157,20 +156,31 @@ def _unknown(*_):
 #   flat(tensor, dtype, dev, *sizes)                 its address
 #   rows(tensor, dtype, dev, tokens, heads, dim)     the bytes of a Rows
 #   alike(a, b)                                      (dtype, dev, addresses, shape) of a pair
-# None where it is not plainly that (and always, where the module was not built).
+# None where it is not plainly that (and always, where the module was not built or does
+# not load).
 flat = rows = alike = _unknown
 
 
 def _load_tensors() -> None:
+    """The binding's module, where there is one that loads."""
     global flat, rows, alike
+    try:
+        import torch
+    except ImportError:
+        return
     path = os.path.join(os.path.dirname(LIB_PATH),
                         f"_tensors-{torch.__version__}{sysconfig.get_config_var('EXT_SUFFIX')}")
     if not os.path.exists(path):
         return
-    spec = importlib.util.spec_from_file_location("_tensors", path)
-    module = importlib.util.module_from_spec(spec)
-    spec.loader.exec_module(module)
-    flat, rows, alike = module.flat, module.rows, module.alike
+    try:
+        spec = importlib.util.spec_from_file_location("_tensors", path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        found = module.flat, module.rows, module.alike
+    except (ImportError, OSError, AttributeError) as e:
+        warnings.warn(f"{path} does not load ({e}): tensors are looked at without it, which takes longer")
+        return
+    flat, rows, alike = found
 
 
 def load() -> ctypes.CDLL:
