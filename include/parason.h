@@ -27,10 +27,10 @@
  * Layouts (row-major, innermost last):
  *   q         [num_leaves, H_q, head_dim]                 (branch b = row b)
  *   k_pages   [num_physical_pages, H_kv, page_size, head_dim]
- *   v_pages   same as k_pages
- *   out       [num_leaves, H_q, head_dim]   same dtype as q
  *             (PARASON_FP4_KV: [num_physical_pages, H_kv, 9 head_dim] bytes, see
  *             "Filling and reading the paged cache")
+ *   v_pages   same as k_pages
+ *   out       [num_leaves, H_q, head_dim]   same dtype as q
  *   lse       [num_leaves, H_q] fp32, natural log of sum_t exp(s_t); a row
  *             without keys has out 0 and lse -inf, one with a NaN score NaN in both
  *   q head h reads kv head h / (H_q / H_kv)  (grouped-query attention)

@@ -1554,8 +1554,8 @@ enum TcBar : int {
     kBarMetaFull = kBarOEmpty + 2,           // [kTcMeta] scheduler -> every role
     kBarMetaEmpty = kBarMetaFull + kTcMeta,  // [kTcMeta] epilogue (4 arrivals) -> scheduler
     kBarDrain = kBarMetaEmpty + kTcMeta,     // both issuers' commits -> issuers, before TMEM is freed
-    kBarCvFull,                              // [kTcCvStages] converters (4 arrivals) -> MMA
-    kBarCvEmpty = kBarCvFull + kTcF4CvStages,  // [kTcCvStages] MMA commit -> converters
+    kBarCvFull,                              // [kTcF4CvStages] converters (4 arrivals) -> MMA
+    kBarCvEmpty = kBarCvFull + kTcF4CvStages,  // [kTcF4CvStages] MMA commit -> converters
     kTcBars = kBarCvEmpty + kTcF4CvStages,
     // producer -> scheduler: pull the next item (e4m3 tiles, which use
     // kTcF8Stages of the kTcStages staging barriers)
@@ -2056,7 +2056,7 @@ __device__ void prefix_cta_tc(const KvMaps *maps, const AttnArgs &a, uint8_t *sm
 #pragma unroll
                         for (int j = 0; j < 64; ++j) hide_from(x[j], j, valid);
                     }
-                    // the block's max in the log2 domain (sl > 0)
+                    // the block's max in the log2 domain (sl > 0: score_factor)
                     float mr = x[0];
 #pragma unroll
                     for (int j = 1; j + 1 < 64; j += 2) mr = dev::max3(mr, x[j], x[j + 1]);

@@ -179,9 +179,10 @@ constexpr int kThreads = 128;            // 4 warps, each of them on its own
 constexpr int kWarps = kThreads / 32;
 
 // CTAs of kv_write to ask an SM's registers for: bf16 and e4m3 rows fit 5 without
-// spills, 4 with a second batch in flight (e4m3 took 105 registers unasked, and 300
-// tokens of 64 / 8 heads 4.5 us for 3.5); fp32 rows do not everywhere, and are left to
-// themselves (96 to 104).
+// spills (e4m3 took 105 registers unasked, and 300 tokens of 64 / 8 heads 4.5 us for 3.5),
+// 4 with a second batch in flight, at 128 registers but for 4 to 12 bytes where normed
+// tokens go four to a warp; fp32 rows do not everywhere, and are left to themselves (96 to
+// 104, normed 156 to 164).
 template <class T, class KV, bool NORM>
 constexpr int kAskedCtas = sizeof(T) == 2 ? (NORM || kIsFp4<KV> ? 4 : 5) : 0;
 
@@ -291,6 +292,10 @@ __device__ __forceinline__ uint32_t e2m1_codes(const float (&x)[8], float y) {
 // values; scales are `to_scales` bytes further.  pairs: the lane's chunks are of two
 // blocks, whose other halves other lanes have (38803 tokens of 8 heads, unrotated, 42.5 us
 // with that, 37.5 without; 30.6 with the next batch asked for ahead, of 30.0 us of bytes).
+// Prompts rotated by halves: 8192 tokens of 32 / 8 heads 31.8 us, normed 36.6, of 26.1 of
+// bytes; 32768 of 8 / 2 heads 35.6 and 40.2.  Few heads as they are: 38803 tokens of 2 heads
+// 12.1 us of 7.5, of one 8.2 of 3.8: tokens share a warp, whose life is one chain of slot,
+// rows and stores, at 16 warps an SM.
 __device__ __forceinline__ void store_fp4(Fp4 *row, int to_scales, const float (&x0)[8], const float (&x1)[8], int e0,
                                           int e1, bool pairs, const BlockMates &mates, uint32_t group, float g) {
     const float r = __frcp_rn(6.f * g);

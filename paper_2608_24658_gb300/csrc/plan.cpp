@@ -172,7 +172,8 @@ constexpr int64_t kEarlyKvBytes = int64_t{2} << 30, kEarlyKvBytesE4m3 = int64_t{
 constexpr int64_t kEarlyPrefillPages = 256;    // a CTA's share
 // 4-bit KV: from this many bytes on, where more than a fifth of the CTAs start on the
 // prefix pass, early steps of 15 trees were 5% longer in the mean (level to 13%); of 29
-// others 1% shorter.
+// others 1% shorter.  A rule of those trees: it fits prefix CTAs that are spread unevenly,
+// as above, but no count of where they ran stands behind it.
 constexpr int64_t kEarlyKvBytesFp4 = int64_t{90} << 20;
 constexpr int kFp32MinPages = 4;
 constexpr int64_t kFp32Slots = 3;
