@@ -63,6 +63,12 @@ def _ptr(x) -> Optional[ctypes.c_void_p]:
     return ctypes.c_void_p(x.data_ptr())
 
 
+def _check_scales(k_scale, v_scale, heads, dev) -> None:
+    for s in (k_scale, v_scale):
+        if s.dtype != torch.float32 or s.numel() != heads or s.device != dev or not s.is_contiguous():
+            raise ValueError(f"scales must be contiguous float32 [{heads}] on {dev}")
+
+
 class Plan:
     """Decode plan of one fork tree (C type ``parason_plan``).
 
@@ -262,9 +268,7 @@ class Plan:
             ks = _lib.flat(k_scale, torch.float32, dev.index, Hkv)
             vs = _lib.flat(v_scale, torch.float32, dev.index, Hkv)
             if ks is None or vs is None:
-                for s in (k_scale, v_scale):
-                    if s.dtype != torch.float32 or s.numel() != Hkv or not s.is_cuda:
-                        raise ValueError(f"scales must be cuda float32 [{Hkv}]")
+                _check_scales(k_scale, v_scale, Hkv, dev)
         if ks is None and k_scale is not None:
             ks = k_scale.data_ptr()
         if vs is None and v_scale is not None:
@@ -301,9 +305,7 @@ class Plan:
         if self.mode in ("fp8", "fp4"):
             if k_scale is None or v_scale is None:
                 raise ValueError(f"{self.mode} mode needs k_scale and v_scale")
-            for s in (k_scale, v_scale):
-                if s.dtype != torch.float32 or s.numel() != Hkv or not s.is_cuda:
-                    raise ValueError(f"scales must be cuda float32 [{Hkv}]")
+            _check_scales(k_scale, v_scale, Hkv, q.device)
         st = _lib.load().parason_attn_decode_no_alloc(
             self.handle, _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(k_scale), _ptr(v_scale),
             _ptr(out), _ptr(lse), _stream_handle(stream))
