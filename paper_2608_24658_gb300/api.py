@@ -69,6 +69,15 @@ def _check_scales(k_scale, v_scale, heads, dev) -> None:
             raise ValueError(f"scales must be contiguous float32 [{heads}] on {dev}")
 
 
+def _result(name, t, dtype, size, dev) -> int:
+    """The address of what a decode writes its result to."""
+    if (t.dtype != dtype or t.numel() < size or not t.is_contiguous()
+            or not (t.device == dev if t.is_cuda else t.is_pinned())):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {size} elements or more, on {dev} "
+                         "or pinned")
+    return t.data_ptr()
+
+
 class Plan:
     """Decode plan of one fork tree (C type ``parason_plan``).
 
@@ -225,7 +234,8 @@ class Plan:
                stream=None, want_lse: bool = True):
         """One decode step; returns (out, lse).  Asynchronous on ``stream``.
         ``q``, ``out`` and ``lse`` may be pinned host tensors: the kernels
-        then read q from, and write the result to, host memory directly."""
+        then read q from, and write the result to, host memory directly.
+        Given ``out`` and ``lse`` may be larger: their first rows are written."""
         # (small steps wait for this code: tensors are looked at once, by _lib.alike and
         # _lib.flat where they are plainly right, and pointers go to the library as integers)
         L, Hq, Hkv, d = self.num_leaves, self.num_q_heads, self.num_kv_heads, self.head_dim
@@ -254,29 +264,43 @@ class Plan:
             if q_cuda and q.device != dev:
                 raise ValueError(f"q must be on {dev}")
             qa, ka, va = q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr()
+        on, la = dev.index, None
         if out is None:
             out = torch.empty_like(q) if q_cuda else torch.empty(q.shape, dtype=q.dtype).pin_memory()
-        if lse is None and want_lse:
+            oa = out.data_ptr()
+        else:
+            oa = _lib.flat(out, qd, on, L, Hq, d)
+            if oa is None:
+                oa = _result("out", out, qd, L * Hq * d, dev)
+        if lse is not None:
+            la = _lib.flat(lse, torch.float32, on, L, Hq)
+            if la is None:
+                la = _result("lse", lse, torch.float32, L * Hq, dev)
+        elif want_lse:
             lse = (torch.empty((L, Hq), dtype=torch.float32, device=dev) if q_cuda else
                    torch.empty((L, Hq), dtype=torch.float32).pin_memory())
+            la = lse.data_ptr()
         if workspace is None:
             workspace = self.workspace(dev)
+        size = workspace.numel()
+        wa = _lib.flat(workspace, torch.uint8, on, size)
+        if wa is None:
+            if not workspace.is_contiguous() or workspace.device != dev:
+                raise ValueError(f"workspace must be contiguous memory on {dev}")
+            wa, size = workspace.data_ptr(), size * workspace.element_size()
         ks = vs = None
         if self.mode in ("fp8", "fp4"):
             if k_scale is None or v_scale is None:
                 raise ValueError(f"{self.mode} mode needs k_scale and v_scale")
-            ks = _lib.flat(k_scale, torch.float32, dev.index, Hkv)
-            vs = _lib.flat(v_scale, torch.float32, dev.index, Hkv)
+            ks = _lib.flat(k_scale, torch.float32, on, Hkv)
+            vs = _lib.flat(v_scale, torch.float32, on, Hkv)
             if ks is None or vs is None:
                 _check_scales(k_scale, v_scale, Hkv, dev)
         if ks is None and k_scale is not None:
             ks = k_scale.data_ptr()
         if vs is None and v_scale is not None:
             vs = v_scale.data_ptr()
-        st = _lib.load().parason_attn_decode(
-            self.handle, qa, ka, va, ks, vs,
-            out.data_ptr(), None if lse is None else lse.data_ptr(), workspace.data_ptr(),
-            workspace.numel() * workspace.element_size(), _stream_int(stream))
+        st = _lib.load().parason_attn_decode(self.handle, qa, ka, va, ks, vs, oa, la, wa, size, _stream_int(stream))
         if st:
             check(st, "parason_attn_decode")
         return out, lse
