@@ -51,6 +51,18 @@ def _stream_int(stream) -> int:
     return stream.cuda_stream if isinstance(stream, torch.cuda.Stream) else int(stream)
 
 
+def _new(stream, shape, dtype, dev):
+    """A new tensor whose memory belongs to the stream that will write it."""
+    here = stream is None or (_raw_stream is not None and _stream_int(stream) == _raw_stream(dev))
+    dev = torch.device("cuda", dev)
+    if here:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=dev)
+
+
 def _i32(a) -> np.ndarray:
     return np.ascontiguousarray(np.asarray(a, dtype=np.int32))
 
@@ -221,11 +233,13 @@ class Plan:
         return int(_lib.load().parason_plan_launches_per_decode(self.handle))
 
     # ---------------------------------------------------------------- decode
-    def workspace(self, device="cuda") -> torch.Tensor:
-        """A cached device workspace of the size the plan needs."""
+    def workspace(self, device="cuda", stream=None) -> torch.Tensor:
+        """A cached device workspace of the size the plan needs (``stream``: where it will be
+        used first, if that is not the current one)."""
         n = max(self.workspace_bytes, 256)
         if self._ws is None or self._ws.numel() < n or self._ws.device != torch.device(device):
-            self._ws = torch.empty(n, dtype=torch.uint8, device=device)
+            device = torch.device(device)
+            self._ws = _new(stream, n, torch.uint8, torch.cuda.current_device() if device.index is None else device.index)
         return self._ws
 
     def decode(self, q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
@@ -266,7 +280,10 @@ class Plan:
             qa, ka, va = q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr()
         on, la = dev.index, None
         if out is None:
-            out = torch.empty_like(q) if q_cuda else torch.empty(q.shape, dtype=q.dtype).pin_memory()
+            if not q_cuda:
+                out = torch.empty(q.shape, dtype=q.dtype).pin_memory()
+            else:
+                out = torch.empty_like(q) if stream is None else _new(stream, q.shape, qd, on)
             oa = out.data_ptr()
         else:
             oa = _lib.flat(out, qd, on, L, Hq, d)
@@ -277,11 +294,14 @@ class Plan:
             if la is None:
                 la = _result("lse", lse, torch.float32, L * Hq, dev)
         elif want_lse:
-            lse = (torch.empty((L, Hq), dtype=torch.float32, device=dev) if q_cuda else
-                   torch.empty((L, Hq), dtype=torch.float32).pin_memory())
+            if not q_cuda:
+                lse = torch.empty((L, Hq), dtype=torch.float32).pin_memory()
+            else:
+                lse = (torch.empty((L, Hq), dtype=torch.float32, device=dev) if stream is None else
+                       _new(stream, (L, Hq), torch.float32, on))
             la = lse.data_ptr()
         if workspace is None:
-            workspace = self.workspace(dev)
+            workspace = self.workspace(dev, stream)
         size = workspace.numel()
         wa = _lib.flat(workspace, torch.uint8, on, size)
         if wa is None:
@@ -411,8 +431,11 @@ def lse_merge(o_a: torch.Tensor, lse_a: torch.Tensor, o_b: torch.Tensor, lse_b: 
             raise ValueError("inputs must be contiguous cuda tensors")
     if lse_a.dtype != torch.float32 or lse_a.numel() != rows or lse_b.numel() != rows:
         raise ValueError("lse must be float32 with one value per row")
-    o_out = torch.empty_like(o_a) if o_out is None else o_out
-    lse_out = torch.empty_like(lse_a) if lse_out is None else lse_out
+    if o_out is None:
+        o_out = torch.empty_like(o_a) if stream is None else _new(stream, o_a.shape, o_a.dtype, o_a.get_device())
+    if lse_out is None:
+        lse_out = (torch.empty_like(lse_a) if stream is None else
+                   _new(stream, lse_a.shape, lse_a.dtype, lse_a.get_device()))
     mode = _lib.MODES["fp32" if o_a.dtype == torch.float32 else "bf16"]
     st = _lib.load().parason_lse_merge(o_a.data_ptr(), lse_a.data_ptr(), o_b.data_ptr(),
                                        lse_b.data_ptr(), o_out.data_ptr(), lse_out.data_ptr(),
@@ -623,17 +646,6 @@ def _head_scales(k_scale, v_scale, heads, dev):
             raise ValueError(f"an e4m3 or 4-bit cache needs k_scale and v_scale: contiguous float32 [{heads}] "
                              f"on cuda:{dev}")
     return k_scale.data_ptr(), v_scale.data_ptr()
-
-
-def _new(stream, shape, dtype, dev):
-    """A new tensor whose memory belongs to the stream that will write it."""
-    dev = torch.device("cuda", dev)
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=dev)
-    if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(int(stream), device=dev)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=dev)
 
 
 def kv_write(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
