@@ -1182,11 +1182,13 @@ __device__ void suffix_warp(const KvMaps &maps, const AttnArgs &a, uint32_t ring
 
     // consume side: the pulled items in order
     int consumed = 0;
-    bool ok = true, cap_large = false;           // (cap_free)
+    bool ok = true;
     for (int k = 0; consumed < issued && ok; ++k) {
         __syncwarp();
         const WorkItem it = grab[k % kGrabSlots];
         const float2 scl = item_scales<KV>(a, it);
+        // (an item's own: which items a warp had before it differs from call to call)
+        bool cap_large = false;
         if ((it.nrows > 4 || D == 64) && it.nrows <= 8) {
             // 5 to 8 rows, of one branch or several: the transposed step.  Up to 4
             // rows take it at head_dim 64, where it runs two pages per update
@@ -1355,7 +1357,7 @@ __device__ void suffix_warp_fp4(const AttnArgs &a, uint32_t ring, uint32_t bars,
     for (int i = 0; i < NS; ++i) issue_next();
 
     int consumed = 0, con_s = 0, con_ph = 0;             // stages
-    bool ok = true, cap_large = false;                   // (cap_free)
+    bool ok = true;
     auto next_stage = [&]() {
         __syncwarp();
         issue_next();
@@ -1369,6 +1371,8 @@ __device__ void suffix_warp_fp4(const AttnArgs &a, uint32_t ring, uint32_t bars,
         __syncwarp();
         const WorkItem it = grab[k % kGrabSlots];
         const float2 scl = item_scales<KV>(a, it);
+        // (an item's own: which items a warp had before it differs from call to call)
+        bool cap_large = false;
         if (it.nrows <= 8) {
             uint32_t qb[D / 16][2];
             load_q_fragments_t<D, KV>(a, it, lane, qb);

@@ -166,8 +166,8 @@ __device__ __forceinline__ void cap_exp_quad(float (&x)[4], const CapFactors &f)
 
 // ---------------------------------------------------------------- mma.sync steps
 // A lane's M accumulators of scores to logits in place; the whole warp calls.
-// Scores that do not count are finite.  large: whether the warp's last scores had one
-// at kCapSeries or past it.  The series runs on trust, and the scores are done again
+// Scores that do not count are finite.  large: whether the warp's last scores of the same
+// item had one at kCapSeries or past it.  The series runs on trust, and the scores are done again
 // if one turns up.
 template <int APART, int M>
 __device__ __forceinline__ void cap_scores(float (&x)[M][4], bool &large, const CapFactors &f) {
@@ -251,7 +251,7 @@ struct PackedRow {
 // P = 2^x (caps up to kCapFreeLog2) of N scores, the first `seen` of which count
 // (hidden: for some lane of the warp not all), handed pair by pair to `put` (again from
 // `start()` on where a block is done twice); the whole warp calls.  large: whether the
-// warp's last block had a score at kCapSeries or past it.  The series runs on trust,
+// warp's last block of the same item had a score at kCapSeries or past it.  The series runs on trust,
 // and the block is done again if one turns up; the exponential form then serves all of
 // its scores: its absolute error, 2e-7 cap, is 1e-5 at most there.  K pairs go
 // through the series side by side: 8 in the prefill, whose registers hold them (calls
