@@ -523,7 +523,8 @@ parason_status parason_rotary_turns(const float *inv_freq, int32_t n, uint64_t *
  *           pool (negative, or 16 * num_physical_pages and up) is not written;
  *           its query is rotated all the same.  Every other slot of the pool
  *           keeps what it holds.  Slots are distinct: of two tokens with one
- *           slot, it is unspecified which one's elements it holds.
+ *           slot, it is unspecified which one's elements it holds (4 bits: a block's
+ *           codes and scale may come from different ones).
  *   q_out   device [num_tokens, H_q, head_dim], contiguous, 16-byte aligned,
  *           the layout parason_attn_decode takes; may be q's own memory if q
  *           has that layout, and overlaps nothing else here
